@@ -482,6 +482,146 @@ typedef struct pace_gather_tensor {
 PACE_API pace_status_t pace_gather_multi(const pace_gather_tensor* tensors, int n_tensors, const int32_t* idx,
                                          int64_t n_idx, pace_stream_t stream);
 
+/* ==============================================================================
+ * Serve — the paged 8-bit KV cache that the pruned prompt goes into (Sec. 3.3: the kept tokens
+ * "formulate the final LLM context sequence"), its append and the attention over it.
+ * ============================================================================== */
+
+/* Slots that share a scale: slots 16 i .. 16 i + 15 of a sequence, per KV head. */
+#define PACE_KV_BLOCK 16
+
+/*
+ * A paged cache.  Slot s of a sequence is row s % page_size of the page that its block table
+ * names for s / page_size; the value there is code * scale, the codes e4m3 (8-bit floats of 4
+ * significant bits up to 448), the scales powers of two, one per PACE_KV_BLOCK slots and KV head.
+ *
+ *  k, v              device  e4m3 [n_pages][n_kv_heads][page_size][head_dim], 16-byte aligned
+ *  k_scale, v_scale  device  float [n_pages][n_kv_heads][page_size / 16]
+ *  page_stride       codes from one page to the next in k and in v, a multiple of 16, at least
+ *                    n_kv_heads * page_size * head_dim (pages may lie apart: several layers in
+ *                    one allocation)
+ *  scale_stride      floats from one page's scales to the next page's, at least
+ *                    n_kv_heads * page_size / 16
+ *  page_size         16, 32, 64, 128 or 256
+ *  n_kv_heads        1 .. 256;  head_dim 64 or 128;  n_pages 1 .. 2^31 - 1
+ *
+ * Codes and scales of slots that no call has written may hold anything, NaN included.
+ */
+typedef struct pace_kv_cache {
+  void* k;
+  void* v;
+  float* k_scale;
+  float* v_scale;
+  int64_t n_pages;
+  int64_t page_stride;
+  int64_t scale_stride;
+  int32_t page_size;
+  int32_t n_kv_heads;
+  int32_t head_dim;
+} pace_kv_cache;
+
+/*
+ * Position rotation (RoPE; with three id rows M-RoPE, as Qwen2.5-VL numbers visual tokens):
+ * pair (x[i], x[i + D/2]) is turned by the angle of table entry [positions[c(i)][token]][i],
+ * where c(i) = 0 for i < sections[0], 1 for the next sections[1] pairs, 2 for the last
+ * sections[2]; sections sum to D / 2 (D/2, 0, 0: one row of ids).
+ *
+ *  table            device  float [n_positions][D / 2][2]: (cos, sin), 16-byte aligned
+ *  positions        device  int32, row c starting at positions + c * positions_stride;
+ *                           each 0 .. n_positions - 1
+ */
+typedef struct pace_rope {
+  const float* table;
+  const int32_t* positions;
+  int64_t n_positions;
+  int64_t positions_stride;
+  int32_t sections[3];
+} pace_rope;
+
+/* Fills a rotation table: angle of (position p, pair i) = p * base^(-2 i / head_dim), worked out in
+ * 64 bits and rounded once.  table device float [n_positions][head_dim / 2][2]; head_dim 64 or
+ * 128; base > 0. */
+PACE_API pace_status_t pace_rope_table(float* table, int64_t n_positions, int head_dim, double base,
+                                       pace_stream_t stream);
+
+/*
+ * Appends the new tokens' keys and values to the cache, the keys (and the queries) rotated on the
+ * way.  The n_b = cu_new[b+1] - cu_new[b] new tokens of sequence b take its last slots,
+ * seq_lens[b] - n_b .. seq_lens[b] - 1, so seq_lens counts them already (the same array then goes
+ * to pace_kv_attention).  Token r (0 .. cu_new[B] - 1) is row rows[r] of K, V, Q and of the
+ * position ids (row r if rows is NULL): with pace_prune_index's list a pruned prompt goes from
+ * the prefill's tensors straight into the cache.
+ *
+ * A block's scale is the smallest power of two that covers every value of it (amax <= 448 s;
+ * between 2^-64 and 2^120).  A block that already holds earlier tokens keeps a scale that covers
+ * those too: where new tokens raise it, the earlier codes are multiplied by the (exact) ratio and
+ * rounded again.  Values are rotated in fp32, each product and sum rounded, and rounded once more
+ * to e4m3 (ties to even).  Calling again with the same arguments gives the same cache.
+ *
+ * K, V and Q must be finite: a NaN or infinite value is stored as 0 (in q_out as it comes out of
+ * the rotation) and records PACE_ERR_INVALID_ARG (kernel id 14) in the device status word.  So do
+ * a source row, position id or page number out of range and a sequence shorter than its new
+ * tokens; the tokens concerned are not stored and their rotated queries are not meaningful.
+ *
+ *  K, V          device  bf16 [n_src_rows, n_kv_heads, D]; consecutive rows k_row_stride,
+ *                        v_row_stride elements apart (a fused projection's output will do); the
+ *                        strides multiples of 8, the pointers 16-byte aligned
+ *  cu_new        host    int32 [B+1] prefix of the new tokens per sequence (0 allowed)
+ *  seq_lens      device  int32 [B]
+ *  block_table   device  int32 [B][table_stride]: page of slots page_size * i ..; entries behind
+ *                        a sequence's last page are not read
+ *  rows          device  int32 [cu_new[B]] or NULL
+ *  rope          host    NULL for no rotation
+ *  Q, q_out      device  bf16 [n_src_rows, n_q_heads, D] with rows q_row_stride apart, and
+ *                        [cu_new[B], n_q_heads, D] contiguous; both NULL: keys and values only.
+ *                        q_out may be Q itself where that is contiguous and rows is NULL
+ *  No two sequences may share a page that the call writes.
+ */
+PACE_API pace_status_t pace_kv_append(const pace_kv_cache* cache, const void* K, const void* V, int64_t k_row_stride,
+                                      int64_t v_row_stride, int64_t n_src_rows, const int32_t* cu_new, int B,
+                                      const int32_t* seq_lens, const int32_t* block_table, int64_t table_stride,
+                                      const int32_t* rows, const pace_rope* rope, const void* Q, int64_t q_row_stride,
+                                      int n_q_heads, void* q_out, pace_stream_t stream);
+
+/* Scratch bytes for pace_kv_attention (host cu_q [B+1]); 0 if the arguments are invalid. */
+PACE_API size_t pace_kv_attention_workspace_size(const pace_kv_cache* cache, const int32_t* cu_q, int B, int n_q_heads,
+                                                 int max_len);
+
+/*
+ * Causal attention of the newest tokens of each sequence over its cache, with grouped-query heads
+ * (query head h reads KV head h / (n_q_heads / n_kv_heads)): decode steps (one query per
+ * sequence), drafted tokens, and whole or chunked prefill, in any mix.  Query t of sequence b sits
+ * at slot p = seq_lens[b] - n_b + t and sees slot j iff j <= p and (window <= 0 or
+ * j > p - window or j < sinks):
+ *   out = sum_j softmax_j(scale q . k_j) v_j over the slots it sees,
+ *   lse = ln sum_j exp(scale q . k_j).
+ * A query that sees nothing (a sequence shorter than its new tokens, or empty) gives out = 0 and
+ * lse = -inf.  What slots hold that a query does not see has no influence on it, be it NaN; a
+ * query that sees a NaN code or scale has no meaningful result.  Products are formed in e4m3 with
+ * q and the softmax weights as sums of two e4m3 terms (q exactly, weights to 8 bits), sums and
+ * softmax statistics in fp32; results do not depend on anything but the arguments (no atomics on
+ * values).
+ *
+ *  Q            device  bf16 [cu_q[B], n_q_heads, D], rows q_row_stride elements apart (a multiple
+ *                       of 8), 16-byte aligned
+ *  cu_q         host    int32 [B+1] prefix of the queries per sequence (0 allowed)
+ *  seq_lens     device  int32 [B], the queries' own tokens included; each 0 .. max_len
+ *  block_table  device  int32 [B][table_stride], as for pace_kv_append
+ *  max_len      host    bound on seq_lens, at most table_stride * page_size; the workspace and the
+ *                       launch depend on it and on cu_q alone, so that a captured call can be
+ *                       replayed while the sequences grow
+ *  window       <= 0: every earlier slot;  sinks >= 0: the first slots that stay visible
+ *  out          device  bf16 [cu_q[B], n_q_heads, D] contiguous, 16-byte aligned
+ *  lse          device  float [cu_q[B], n_q_heads] or NULL
+ *  A page number out of range or a length above max_len records PACE_ERR_INVALID_ARG (kernel id
+ *  15) in the device status word; that sequence's results are then not meaningful.
+ *  n_q_heads % n_kv_heads == 0, n_q_heads / n_kv_heads <= 64.
+ */
+PACE_API pace_status_t pace_kv_attention(const pace_kv_cache* cache, const void* Q, int64_t q_row_stride, const int32_t* cu_q,
+                                         int B, int n_q_heads, const int32_t* seq_lens, const int32_t* block_table,
+                                         int64_t table_stride, int max_len, float scale, int window, int sinks, void* out,
+                                         float* lse, void* ws, size_t ws_bytes, pace_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -427,3 +427,107 @@ def prune_rows(n_pre: int, vis_start: int, n_vis: int, kept_local: Sequence[int]
     keep[vis_start:vis_start + n_vis] = False
     keep[vis_start + np.asarray(kept_local, dtype=np.int64)] = True
     return np.nonzero(keep)[0]
+
+
+# ----------------------------------------------------------------------------------------------
+# Serve: the paged 8-bit cache of the pruned context (Sec. 3.3 "the final LLM context sequence").
+# The paper has no counterpart; the definitions are the library's own.
+# ----------------------------------------------------------------------------------------------
+KV_BLOCK = 16     # slots that share a scale
+KV_EXP = (-64, 120)
+
+
+def e4m3_values() -> np.ndarray:
+    """The value of each of the 256 codes: sign, 4 exponent bits (bias 7), 3 mantissa bits, no infinities."""
+    c = np.arange(256)
+    e, m = (c >> 3) & 15, c & 7
+    v = np.where(e == 0, m * 2.0 ** -9, (8 + m) * 2.0 ** (e - 10.0))
+    v = np.where((c & 127) == 127, np.nan, v)
+    return np.where(c >= 128, -v, v)
+
+
+def e4m3_round(x: np.ndarray) -> np.ndarray:
+    """Nearest e4m3 value (ties to even), saturating at 448."""
+    x = np.asarray(x, dtype=np.float64)
+    _, e = np.frexp(x)
+    step = np.ldexp(1.0, np.maximum(e - 1, -6) - 3)
+    return np.clip(np.round(x / step) * step, -448.0, 448.0)
+
+
+def kv_scale(amax: np.ndarray) -> np.ndarray:
+    """The smallest power of two s, between 2^-64 and 2^120, with amax <= 448 s."""
+    f, e = np.frexp(np.asarray(amax, dtype=np.float64) / 448.0)
+    e = np.where(f > 0.5, e, e - 1)
+    return np.ldexp(1.0, np.clip(np.where(np.asarray(amax) > 0, e, KV_EXP[0]), *KV_EXP))
+
+
+def rope_rotate(x: np.ndarray, cos: np.ndarray, sin: np.ndarray) -> np.ndarray:
+    """x [tokens, heads, D]; cos, sin [tokens, D / 2]: pair (i, i + D / 2) turned by its angle."""
+    a, b = np.split(np.asarray(x, dtype=np.float64), 2, axis=2)
+    c, s = cos[:, None, :], sin[:, None, :]
+    return np.concatenate([a * c - b * s, b * c + a * s], axis=2)
+
+
+def rope_angles(table: np.ndarray, positions: np.ndarray, sections: Sequence[int]) -> np.ndarray:
+    """(cos, sin) [tokens, D / 2, 2] out of a table [positions, D / 2, 2], each pair by its section's id row."""
+    comp = np.repeat(np.arange(len(sections)), sections)
+    return np.stack([table[positions[c], i] for i, c in enumerate(comp)], axis=1).astype(np.float64)
+
+
+def kv_append(values: np.ndarray, scales: np.ndarray, x: np.ndarray, first: int, pages: Sequence[int]) -> None:
+    """Writes one sequence's new tokens x [n, heads, D] to slots first .. of its pages, in place.
+
+    values [n_pages, heads, page, D]: what the codes stand for before the scale; scales [n_pages, heads,
+    page / 16].  A block that already holds earlier tokens keeps a scale that covers those too."""
+    page, n = values.shape[2], len(x)
+    for blk in range(first // KV_BLOCK, -(-(first + n) // KV_BLOCK)):
+        lo, hi = max(first, blk * KV_BLOCK), min(first + n, (blk + 1) * KV_BLOCK)
+        pg, at = pages[blk * KV_BLOCK // page], blk * KV_BLOCK % page
+        rows = slice(at + lo - blk * KV_BLOCK, at + hi - blk * KV_BLOCK)
+        new = np.asarray(x[lo - first:hi - first], dtype=np.float64).transpose(1, 0, 2)
+        s = kv_scale(np.abs(new).max(axis=(1, 2)))
+        if lo % KV_BLOCK:
+            old = scales[pg, :, at // KV_BLOCK]
+            s = np.maximum(s, old)
+            early = slice(at, rows.start)
+            values[pg, :, early] = e4m3_round(values[pg, :, early] * (old / s)[:, None, None])
+        values[pg, :, rows] = e4m3_round(new / s[:, None, None])
+        scales[pg, :, at // KV_BLOCK] = s
+
+
+def kv_read(values: np.ndarray, scales: np.ndarray, pages: Sequence[int], length: int) -> np.ndarray:
+    """[length, heads, D]: the cached tokens of one sequence."""
+    x = values[list(pages)] * np.repeat(scales[list(pages)], KV_BLOCK, axis=2)[..., None]
+    return x.transpose(0, 2, 1, 3).reshape(-1, values.shape[1], values.shape[3])[:length]
+
+
+def kv_visible(length: int, n: int, window: int = 0, sinks: int = 0) -> np.ndarray:
+    """[n, length]: the slots that each of the last n queries of a sequence sees."""
+    p = np.arange(length - n, length)[:, None]
+    j = np.arange(length)[None, :]
+    return (j <= p) & ((window <= 0) | (j > p - window) | (j < sinks))
+
+
+def kv_attention(Q: np.ndarray, K: np.ndarray, V: np.ndarray, visible: np.ndarray, scale: float) -> Dict[str, np.ndarray]:
+    """One sequence: Q [n, Hq, D], K and V [length, Hkv, D], visible [n, length].
+
+    out; lse; and for error bounds abs_out = sum_j p_j |v_j|, abs_score = max_j scale sum_d |q_d k_jd| and
+    peak = sqrt(slots seen) max_j p_j max_d |v_jd|."""
+    n, hq, d = Q.shape
+    hkv = K.shape[1]
+    out, absout = np.zeros((n, hq, d)), np.zeros((n, hq, d))
+    lse, score, peak = np.full((n, hq), -np.inf), np.zeros((n, hq)), np.zeros((n, hq))
+    for t in range(n):
+        j = np.nonzero(visible[t])[0]
+        if j.size == 0:
+            continue
+        for h in range(hq):
+            g = h // (hq // hkv)
+            s = scale * (K[j, g] @ Q[t, h])
+            w = np.exp(s - s.max())
+            lse[t, h] = s.max() + np.log(w.sum())
+            w /= w.sum()
+            out[t, h], absout[t, h] = w @ V[j, g], w @ np.abs(V[j, g])
+            score[t, h] = scale * (np.abs(K[j, g]) @ np.abs(Q[t, h])).max()
+            peak[t, h] = np.sqrt(j.size) * (w * np.abs(V[j, g]).max(axis=1)).max()
+    return dict(out=out, lse=lse, abs_out=absout, abs_score=score, peak=peak)

@@ -1,0 +1,329 @@
+// Serve: new keys and values into the paged 8-bit cache, rotated on the way, and the rotation table.
+//
+// A pair (x1, x2) = (x[i], x[i + D/2]) of a key turns by its position's angle,
+//   y1 = x1 c - x2 s,  y2 = x2 c + x1 s,
+// and a block of 16 slots and one head is stored as e4m3 codes round(y / s) with the smallest power
+// of two s that covers the block.  The power costs e4m3 nothing (it is a floating format) and makes
+// the growth of a block's scale, when a later token needs more, an exact factor on its older codes.
+//
+// One CTA per touched block: it stages the tokens' (cos, sin) once for all heads, then a warp takes
+// a head's 16 rows at a time, 16 bytes per lane and load, both halves of a pair in one lane.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "pace_kv.cuh"
+#include "pace_ptx.cuh"
+
+namespace pace {
+namespace {
+
+constexpr int kAppendThreads = 256;
+
+struct AppendArgs {
+  KvView c;
+  const uint16_t* K;
+  const uint16_t* V;
+  const uint16_t* Q;
+  uint16_t* q_out;
+  int64_t k_stride, v_stride, q_stride, n_src, table_stride;
+  const int32_t* lens;
+  const int32_t* table;
+  const int32_t* rows;
+  const float2* rope;
+  const int32_t* pos;
+  int64_t n_pos, pos_stride;
+  int sec0, sec01, q_heads;
+  int b0, nb;                      // the launch's sequences
+  int cu[kKvMaxB + 1];             // first token of each
+  int block_prefix[kKvMaxB + 1];   // blocks that a sequence's tokens may touch, at most
+};
+
+struct Eight {
+  float v[8];
+};
+__device__ __forceinline__ Eight load8(const uint16_t* p) {
+  const uint4 u = *reinterpret_cast<const uint4*>(p);
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+  Eight e;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    e.v[2 * i] = __uint_as_float(w[i] << 16);
+    e.v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+  }
+  return e;
+}
+__device__ __forceinline__ uint32_t bf16x2(float lo, float hi) {
+  return static_cast<uint32_t>(__bfloat16_as_ushort(__float2bfloat16_rn(lo))) |
+         (static_cast<uint32_t>(__bfloat16_as_ushort(__float2bfloat16_rn(hi))) << 16);
+}
+
+// Products and sums rounded one by one, so that a result does not hang on the contraction into FMAs.
+__device__ __forceinline__ void turn(Eight& a, Eight& b, const float2* cs) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float2 t = cs[i];
+    const float x = a.v[i], y = b.v[i];
+    a.v[i] = __fsub_rn(__fmul_rn(x, t.x), __fmul_rn(y, t.y));
+    b.v[i] = __fadd_rn(__fmul_rn(y, t.x), __fmul_rn(x, t.y));
+  }
+}
+
+template <int D>
+__global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(const __grid_constant__ AppendArgs a, int* status) {
+  constexpr int H = D / 2, LPR = D / 16, RPP = 32 / LPR, PASS = kKvBlock / RPP;   // lanes per row, rows per pass
+  __shared__ __align__(16) float2 cs[kKvBlock][H];
+  __shared__ int64_t src[kKvBlock];   // source row of each slot; -1: no (valid) new token there
+  ptx::begin_call();
+  int lo = 0, hi = a.nb - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (a.block_prefix[mid] <= static_cast<int>(blockIdx.x)) lo = mid;
+    else hi = mid - 1;
+  }
+  const int b = lo, n = a.cu[b + 1] - a.cu[b];
+  const int len = a.lens[a.b0 + b], first = len - n;
+  if (first < 0) {
+    if (threadIdx.x == 0) record_error(status, PACE_ERR_INVALID_ARG, K_KV_APPEND);
+  }
+  // (of a sequence shorter than its new tokens those before its first slot are dropped)
+  const int blk = (first < 0 ? 0 : first / kKvBlock) + static_cast<int>(blockIdx.x) - a.block_prefix[b];
+  const int slot0 = blk * kKvBlock;
+  if (slot0 >= len) return;
+  const int r_lo = max(first - slot0, 0), r_hi = min(len - slot0, kKvBlock);
+  const int64_t pi = slot0 >> a.c.page_shift;
+  int page = -1;
+  if (pi < a.table_stride) page = a.table[(a.b0 + b) * a.table_stride + pi];
+  if (page < 0 || page >= a.c.n_pages) {
+    if (threadIdx.x == 0) record_error(status, PACE_ERR_INVALID_ARG, K_KV_APPEND);
+    page = -1;
+  }
+  const int token0 = a.cu[b] + slot0 - first;   // of row 0, where that is a new token
+  if (threadIdx.x < kKvBlock) {
+    const int r = threadIdx.x;
+    int64_t s = -1;
+    if (r >= r_lo && r < r_hi) {
+      s = a.rows != nullptr ? a.rows[token0 + r] : token0 + r;
+      bool ok = s >= 0 && s < a.n_src;
+      if (ok && a.rope != nullptr) {
+        const int n_rows = a.sec01 < H ? 3 : a.sec0 < a.sec01 ? 2 : 1;
+        for (int c = 0; c < n_rows; ++c) {
+          const int p = a.pos[c * a.pos_stride + s];
+          ok = ok && p >= 0 && p < a.n_pos;
+        }
+      }
+      if (!ok) {
+        record_error(status, PACE_ERR_INVALID_ARG, K_KV_APPEND);
+        s = -1;
+      }
+    }
+    src[r] = s;
+  }
+  __syncthreads();
+  if (a.rope != nullptr) {
+    for (int i = threadIdx.x; i < kKvBlock * H; i += kAppendThreads) {
+      const int r = i / H, p = i % H;
+      if (src[r] < 0) continue;
+      const int c = p < a.sec0 ? 0 : p < a.sec01 ? 1 : 2;
+      cs[r][p] = a.rope[static_cast<int64_t>(a.pos[c * a.pos_stride + src[r]]) * H + p];
+    }
+    __syncthreads();
+  }
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int col = (lane % LPR) * 8, row0 = lane / LPR;
+  const int tasks = 2 * a.c.heads + a.q_heads;
+  for (int task = warp; task < tasks; task += kAppendThreads / 32) {
+    const bool is_q = task >= 2 * a.c.heads, is_v = !is_q && task >= a.c.heads;
+    const int head = is_q ? task - 2 * a.c.heads : is_v ? task - a.c.heads : task;
+    const uint16_t* base = (is_q ? a.Q : is_v ? a.V : a.K) + static_cast<int64_t>(head) * D + col;
+    const int64_t stride = is_q ? a.q_stride : is_v ? a.v_stride : a.k_stride;
+    if (!is_q && page < 0) continue;
+    Eight x[PASS][2];
+#pragma unroll
+    for (int p = 0; p < PASS; ++p) {
+      const int64_t s = src[p * RPP + row0];
+      x[p][0] = x[p][1] = Eight{};
+      if (s >= 0) {
+        x[p][0] = load8(base + s * stride);
+        x[p][1] = load8(base + s * stride + H);
+      }
+    }
+    if (!is_v && a.rope != nullptr) {
+#pragma unroll
+      for (int p = 0; p < PASS; ++p)
+        if (src[p * RPP + row0] >= 0) turn(x[p][0], x[p][1], &cs[p * RPP + row0][col]);
+    }
+    bool bad = false;
+    float amax = 0.f;
+#pragma unroll
+    for (int p = 0; p < PASS; ++p)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float v = fabsf(x[p][h].v[i]);
+          const bool fin = v < INFINITY;
+          bad |= !fin;
+          amax = fmaxf(amax, fin ? v : 0.f);
+        }
+    if (bad) record_error(status, PACE_ERR_INVALID_ARG, K_KV_APPEND);
+    if (is_q) {
+#pragma unroll
+      for (int p = 0; p < PASS; ++p) {
+        const int r = p * RPP + row0;
+        if (r < r_lo || r >= r_hi) continue;
+        uint16_t* o = a.q_out + (static_cast<int64_t>(token0 + r) * a.q_heads + head) * D + col;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float* v = x[p][h].v;
+          *reinterpret_cast<uint4*>(o + h * H) =
+              make_uint4(bf16x2(v[0], v[1]), bf16x2(v[2], v[3]), bf16x2(v[4], v[5]), bf16x2(v[6], v[7]));
+        }
+      }
+      continue;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+    const int slot = slot0 & ((1 << a.c.page_shift) - 1), blocks = 1 << (a.c.page_shift - 4);
+    float* scale = (is_v ? a.c.vs : a.c.ks) + page * a.c.scale_stride + head * blocks + slot / kKvBlock;
+    uint8_t* codes = (is_v ? a.c.v : a.c.k) + page * a.c.page_stride +
+                     ((static_cast<int64_t>(head) << a.c.page_shift) + slot) * D + col;
+    float s = scale_for(amax), ratio = 1.f;
+    if (r_lo > 0) {
+      const float old = *scale;
+      if (old > 0.f && old < INFINITY) {
+        s = fmaxf(s, old);
+        ratio = __fdiv_rn(old, s);
+      }
+      __syncwarp();   // every lane has read the scale
+    }
+    if (lane == 0) *scale = s;
+    const float inv = __frcp_rn(s);   // exact: a power of two from 2^-120 to 2^64
+#pragma unroll
+    for (int p = 0; p < PASS; ++p) {
+      const int r = p * RPP + row0;
+      uint8_t* o = codes + r * D;
+      if (src[r] >= 0) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float y[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) y[i] = fabsf(x[p][h].v[i]) < INFINITY ? __fmul_rn(x[p][h].v[i], inv) : 0.f;
+          *reinterpret_cast<uint2*>(o + h * H) = make_uint2(e4m3x4(y[0], y[1], y[2], y[3]), e4m3x4(y[4], y[5], y[6], y[7]));
+        }
+      } else if (r < r_lo && ratio != 1.f) {   // an older token under the grown scale
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint2 w = *reinterpret_cast<const uint2*>(o + h * H);
+          uint32_t z[2];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const uint32_t u = i == 0 ? w.x : w.y;
+            const uint32_t f0 = e4m3x2_to_f16x2(u & 0xFFFFu), f1 = e4m3x2_to_f16x2(u >> 16);
+            const float2 g0 = __half22float2(*reinterpret_cast<const __half2*>(&f0));
+            const float2 g1 = __half22float2(*reinterpret_cast<const __half2*>(&f1));
+            z[i] = e4m3x4(g0.x * ratio, g0.y * ratio, g1.x * ratio, g1.y * ratio);
+          }
+          *reinterpret_cast<uint2*>(o + h * H) = make_uint2(z[0], z[1]);
+        }
+      }
+    }
+  }
+}
+
+__global__ void __launch_bounds__(256) rope_table_kernel(float2* table, int64_t n_positions, int half, double step) {
+  ptx::begin_call();
+  const int64_t total = n_positions * half;
+  for (int64_t i = blockIdx.x * static_cast<int64_t>(blockDim.x) + threadIdx.x; i < total; i += static_cast<int64_t>(gridDim.x) * blockDim.x) {
+    double s, c;
+    sincos(static_cast<double>(i / half) * exp(step * static_cast<double>(i % half)), &s, &c);
+    table[i] = make_float2(static_cast<float>(c), static_cast<float>(s));
+  }
+}
+
+}  // namespace
+}  // namespace pace
+
+using namespace pace;
+
+extern "C" pace_status_t pace_rope_table(float* table, int64_t n_positions, int head_dim, double base, pace_stream_t stream) {
+  if (n_positions < 0 || n_positions > INT32_MAX || (head_dim != 64 && head_dim != 128) || !(base > 0.0) || !std::isfinite(base))
+    return PACE_ERR_INVALID_ARG;
+  if (n_positions == 0) return PACE_OK;
+  if (table == nullptr || reinterpret_cast<uintptr_t>(table) % 16 != 0) return PACE_ERR_INVALID_ARG;
+  PACE_CHECK(check_device());
+  const int half = head_dim / 2;
+  const unsigned grid = static_cast<unsigned>(std::min<int64_t>((n_positions * half + 255) / 256, 4096));
+  return launch_dependent(rope_table_kernel, grid, 256, 0, 1, stream, reinterpret_cast<float2*>(table), n_positions, half,
+                          -2.0 * std::log(base) / head_dim);
+}
+
+extern "C" pace_status_t pace_kv_append(const pace_kv_cache* cache, const void* K, const void* V, int64_t k_row_stride,
+                                        int64_t v_row_stride, int64_t n_src_rows, const int32_t* cu_new, int B,
+                                        const int32_t* seq_lens, const int32_t* block_table, int64_t table_stride,
+                                        const int32_t* rows, const pace_rope* rope, const void* Q, int64_t q_row_stride,
+                                        int n_q_heads, void* q_out, pace_stream_t stream) {
+  if (B < 0) return PACE_ERR_INVALID_ARG;
+  if (B == 0) return PACE_OK;
+  PACE_CHECK(check_cache(cache));
+  PACE_CHECK(check_prefix(cu_new, B));
+  if (cu_new[B] == 0) return PACE_OK;
+  const int D = cache->head_dim;
+  if (!rows_ok(K, k_row_stride, cache->n_kv_heads, D) || !rows_ok(V, v_row_stride, cache->n_kv_heads, D)) return PACE_ERR_INVALID_ARG;
+  if (seq_lens == nullptr || block_table == nullptr || table_stride < 1 || n_src_rows < 1 || n_src_rows > INT32_MAX)
+    return PACE_ERR_INVALID_ARG;
+  if (rows == nullptr && n_src_rows < cu_new[B]) return PACE_ERR_INVALID_ARG;
+  if ((Q == nullptr) != (q_out == nullptr)) return PACE_ERR_INVALID_ARG;
+  if (Q != nullptr && (n_q_heads < 1 || n_q_heads > 256 || !rows_ok(Q, q_row_stride, n_q_heads, D) ||
+                       reinterpret_cast<uintptr_t>(q_out) % 16 != 0))
+    return PACE_ERR_INVALID_ARG;
+  AppendArgs a{};
+  if (rope != nullptr) {
+    const int32_t* s = rope->sections;
+    if (rope->table == nullptr || rope->positions == nullptr || reinterpret_cast<uintptr_t>(rope->table) % 16 != 0 ||
+        rope->n_positions < 1 || rope->positions_stride < 0 || s[0] < 0 || s[1] < 0 || s[2] < 0 ||
+        static_cast<int64_t>(s[0]) + s[1] + s[2] != D / 2)
+      return PACE_ERR_INVALID_ARG;
+    a.rope = reinterpret_cast<const float2*>(rope->table);
+    a.pos = rope->positions;
+    a.n_pos = rope->n_positions;
+    a.pos_stride = rope->positions_stride;
+    a.sec0 = s[0];
+    a.sec01 = s[0] + s[1];
+  }
+  PACE_CHECK(check_device());
+  a.c = kv_view(cache);
+  a.K = static_cast<const uint16_t*>(K);
+  a.V = static_cast<const uint16_t*>(V);
+  a.Q = static_cast<const uint16_t*>(Q);
+  a.q_out = static_cast<uint16_t*>(q_out);
+  a.k_stride = k_row_stride;
+  a.v_stride = v_row_stride;
+  a.q_stride = q_row_stride;
+  a.n_src = n_src_rows;
+  a.table_stride = table_stride;
+  a.lens = seq_lens;
+  a.table = block_table;
+  a.rows = rows;
+  a.q_heads = Q != nullptr ? n_q_heads : 0;
+  int* status = device_status_word();
+  for (int b0 = 0; b0 < B; b0 += kKvMaxB) {
+    a.b0 = b0;
+    a.nb = std::min(kKvMaxB, B - b0);
+    int64_t blocks = 0;
+    for (int i = 0; i <= a.nb; ++i) {
+      a.cu[i] = cu_new[b0 + i];
+      a.block_prefix[i] = static_cast<int>(blocks);
+      if (i < a.nb) {
+        const int n = cu_new[b0 + i + 1] - cu_new[b0 + i];
+        if (n > 0) blocks += (n + 2 * (kKvBlock - 1)) / kKvBlock;   // wherever in a block the first one lands
+      }
+    }
+    if (blocks == 0) continue;
+    auto* kernel = D == 128 ? kv_append_kernel<128> : kv_append_kernel<64>;
+    PACE_CHECK(launch_dependent(kernel, static_cast<unsigned>(blocks), kAppendThreads, 0, 1, stream, a, status));
+  }
+  return PACE_OK;
+}

@@ -25,6 +25,8 @@ enum KernelId : int {
   K_SELFTEST = 11,
   K_PRUNE_INDEX = 12,
   K_GATHER_MULTI = 13,
+  K_KV_APPEND = 14,
+  K_KV_ATTN = 15,
 };
 
 // Device status word layout: [0] = code (pace_status_t), [1] = kernel id.

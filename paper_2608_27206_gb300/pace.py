@@ -58,6 +58,17 @@ class GatherTensor(ctypes.Structure):
 GATHER_MAX_TENSORS = 16
 
 
+class KvCacheView(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("n_pages", ctypes.c_int64), ("page_stride", ctypes.c_int64), ("scale_stride", ctypes.c_int64),
+                ("page_size", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
+
+
+class Rope(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("n_positions", ctypes.c_int64),
+                ("positions_stride", ctypes.c_int64), ("sections", ctypes.c_int32 * 3)]
+
+
 _P = ctypes.c_void_p   # device addresses and host index arrays alike
 _SIGS = {
     "pace_status_string": (ctypes.c_char_p, [ctypes.c_int]),
@@ -105,6 +116,13 @@ _SIGS = {
     "pace_ddae_select": (ctypes.c_int, [_P, _P, _P, _P, ctypes.c_int, ctypes.POINTER(DdaeParams), _P, _P,
                                         _P, _P]),
     "pace_gather": (ctypes.c_int, [_P, ctypes.c_int64, ctypes.c_int64, _P, ctypes.c_int64, _P, _P]),
+    "pace_rope_table": (ctypes.c_int, [_P, ctypes.c_int64, ctypes.c_int, ctypes.c_double, _P]),
+    "pace_kv_append": (ctypes.c_int, [_P, _P, _P, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, _P, ctypes.c_int, _P, _P,
+                                      ctypes.c_int64, _P, _P, _P, ctypes.c_int64, ctypes.c_int, _P, _P]),
+    "pace_kv_attention_workspace_size": (ctypes.c_size_t, [_P, _P, ctypes.c_int, ctypes.c_int, ctypes.c_int]),
+    "pace_kv_attention": (ctypes.c_int, [_P, _P, ctypes.c_int64, _P, ctypes.c_int, ctypes.c_int, _P, _P, ctypes.c_int64,
+                                         ctypes.c_int, ctypes.c_float, ctypes.c_int, ctypes.c_int, _P, _P, _P,
+                                         ctypes.c_size_t, _P]),
 }
 
 _lib = None
@@ -593,3 +611,162 @@ def pace_gather(src: torch.Tensor, idx: torch.Tensor, dst: Optional[torch.Tensor
     st = lib().pace_gather(_dev(src), n_src, row_bytes, _dev(idx), n, _dev(dst), _stream(stream))
     _check("pace_gather", st)
     return _first(dst, n)
+
+
+# ----------------------------------------------------------------------------------------------
+# Serve
+# ----------------------------------------------------------------------------------------------
+KV_BLOCK = 16   # slots that share a scale
+
+
+class KvCache:
+    """Handle of a paged 8-bit cache: e4m3 codes k, v [n_pages, n_kv_heads, page_size, head_dim] (float8_e4m3fn or
+    uint8) and their float32 scales [n_pages, n_kv_heads, page_size / 16].  Pages may lie apart (k and v alike);
+    within a page everything is contiguous."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor):
+        for t, s in ((k, k_scale), (v, v_scale)):
+            if t.dim() != 4 or t.element_size() != 1 or s.dtype != torch.float32:
+                raise ValueError("codes are 4-dimensional of one byte each, scales float32")
+            if t.shape != k.shape or tuple(s.shape) != (t.shape[0], t.shape[1], t.shape[2] // KV_BLOCK):
+                raise ValueError("k, v and their scales do not fit together")
+            if not (t.is_cuda and s.is_cuda):
+                raise ValueError("expected CUDA tensors")
+            if not (t[0].is_contiguous() and s[0].is_contiguous()):
+                raise ValueError("expected contiguous pages")
+            if t.stride(0) != k.stride(0) or s.stride(0) != k_scale.stride(0):
+                raise ValueError("k and v differ in the distance between their pages")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        n, self.n_kv_heads, self.page_size, self.head_dim = k.shape
+        self.n_pages = n
+        self.view = KvCacheView(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), n,
+                                max(k.stride(0), k[0].numel()), max(k_scale.stride(0), k_scale[0].numel()), self.page_size,
+                                self.n_kv_heads, self.head_dim)
+        self._address = ctypes.addressof(self.view)
+
+    @classmethod
+    def empty(cls, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, device="cuda") -> "KvCache":
+        """A cache of uninitialised pages."""
+        codes = [torch.empty((n_pages, n_kv_heads, page_size, head_dim), dtype=torch.float8_e4m3fn, device=device) for _ in "kv"]
+        scales = [torch.empty((n_pages, n_kv_heads, page_size // KV_BLOCK), dtype=torch.float32, device=device) for _ in "kv"]
+        return cls(*codes, *scales)
+
+
+def pace_rope_table(n_positions: int, head_dim: int, base: float = 1e6, out: Optional[torch.Tensor] = None, device="cuda",
+                    stream=None) -> torch.Tensor:
+    """Rotation table float32 [n_positions, head_dim / 2, 2] of (cos, sin)."""
+    if out is None:
+        out = torch.empty((n_positions, head_dim // 2, 2), dtype=torch.float32, device=device)
+    _check("pace_rope_table", lib().pace_rope_table(_dev(out), n_positions, head_dim, float(base), _stream(stream)))
+    return out
+
+
+def _rows_of(t: torch.Tensor, heads: int, dim: int):
+    """(address, elements between rows) of bf16 [rows, heads, dim] whose rows may lie apart."""
+    if not t.is_cuda or t.dtype != torch.bfloat16:
+        raise ValueError("expected a CUDA tensor of bfloat16")
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim:
+        raise ValueError(f"expected [rows, {heads}, {dim}], got {tuple(t.shape)}")
+    stride = t.stride()
+    if stride[2] != 1 or (heads > 1 and stride[1] != dim):
+        raise ValueError("expected contiguous rows")
+    return t.data_ptr(), stride[0] if t.shape[0] > 1 else max(stride[0], heads * dim)
+
+
+def _int32(t: torch.Tensor, n: int, what: str) -> int:
+    if t.dtype != torch.int32 or not t.is_cuda or not t.is_contiguous() or t.numel() < n:
+        raise ValueError(f"{what}: expected at least {n} contiguous int32 on the device")
+    return t.data_ptr()
+
+
+def _table(block_table: torch.Tensor, B: int):
+    if block_table.dim() != 2:
+        raise ValueError("block_table: expected [sequences, pages]")
+    return _int32(block_table, B * block_table.shape[1], "block_table"), block_table.shape[1]
+
+
+def pace_kv_append(cache: KvCache, K: torch.Tensor, V: torch.Tensor, cu_new, seq_lens: torch.Tensor,
+                   block_table: torch.Tensor, rows: Optional[torch.Tensor] = None, rope: Optional[torch.Tensor] = None,
+                   positions: Optional[torch.Tensor] = None, sections=None, q: Optional[torch.Tensor] = None,
+                   q_out: Optional[torch.Tensor] = None, stream=None) -> Optional[torch.Tensor]:
+    """Appends the new tokens' K, V (bf16 [source rows, heads, D], rows may lie apart) to the cache, K and q rotated.
+
+    seq_lens (device int32 [B]) counts the new tokens already; rows (device int32) picks source rows, by
+    default all in order.  rope is a table as pace_rope_table gives it, positions int32 [rows of ids, source
+    rows] or [source rows], sections the pairs that each row of ids turns (default: all the first).
+    Returns the rotated queries [cu_new[-1], heads, D], or None without q."""
+    cu, cp, B = _i32(cu_new)
+    B -= 1
+    n, hk, D = int(cu[-1]), cache.n_kv_heads, cache.head_dim
+    kp, ks = _rows_of(K, hk, D)
+    vp, vs = _rows_of(V, hk, D)
+    src = K.shape[0]
+    if V.shape[0] != src:
+        raise ValueError("K and V differ in rows")
+    tp, ts = _table(block_table, B)
+    turn = None
+    if rope is not None:
+        if rope.dtype != torch.float32 or rope.dim() != 3 or rope.shape[1] * 2 != D or rope.shape[2] != 2:
+            raise ValueError("rope: expected float32 [positions, D / 2, 2]")
+        if positions is None or positions.shape[-1] != src:
+            raise ValueError("positions: expected ids of every source row")
+        sec = list(sections) if sections is not None else [D // 2]
+        sec += [0] * (3 - len(sec))
+        ids = positions.shape[0] if positions.dim() == 2 else 1
+        if len(sec) != 3 or any(s > 0 for s in sec[ids:]):
+            raise ValueError("sections: more than rows of ids")
+        turn = Rope(_dev(rope), _int32(positions, ids * src, "positions"), rope.shape[0], src, (ctypes.c_int32 * 3)(*sec))
+    qp, qs, hq, op = None, 0, 0, None
+    if q is not None:
+        hq = q.shape[1]
+        qp, qs = _rows_of(q, hq, D)
+        if q.shape[0] != src:
+            raise ValueError("K and q differ in rows")
+        if q_out is None:
+            q_out = torch.empty((n, hq, D), dtype=torch.bfloat16, device=q.device)
+        elif q_out.dtype != torch.bfloat16 or q_out.numel() < n * hq * D:
+            raise ValueError("q_out: expected bfloat16 [new tokens, heads, D]")
+        op = _dev(q_out)
+    _check("pace_kv_append",
+           lib().pace_kv_append(cache._address, kp, vp, ks, vs, src, cp, B, _int32(seq_lens, B, "seq_lens"), tp, ts,
+                                None if rows is None else _int32(rows, n, "rows"), None if turn is None else ctypes.addressof(turn),
+                                qp, qs, hq, op, _stream(stream)))
+    return q_out if q is not None else None
+
+
+def pace_kv_attention_workspace_size(cache: KvCache, cu_q, n_q_heads: int, max_len: int) -> int:
+    _c, cp, n = _i32(cu_q)
+    return int(lib().pace_kv_attention_workspace_size(cache._address, cp, n - 1, int(n_q_heads), int(max_len)))
+
+
+def pace_kv_attention(cache: KvCache, Q: torch.Tensor, cu_q, seq_lens: torch.Tensor, block_table: torch.Tensor, max_len: int,
+                      scale: Optional[float] = None, window: int = 0, sinks: int = 0, out: Optional[torch.Tensor] = None,
+                      lse: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Causal attention of Q (bf16 [new tokens, heads, D]) over the cache: bf16 [new tokens, heads, D].
+
+    The queries are the last of their sequences' seq_lens (device int32, none above max_len) slots; with
+    window > 0 one sees the last `window` slots up to its own and the first `sinks`.  lse (float32 [new
+    tokens, heads]) receives the log-sum-exp of the scores."""
+    cu, cp, B = _i32(cu_q)
+    B -= 1
+    n, D = int(cu[-1]), cache.head_dim
+    hq = Q.shape[1]
+    qp, qs = _rows_of(Q, hq, D)
+    if Q.shape[0] < n:
+        raise ValueError("fewer queries than cu_q says")
+    if scale is None:
+        scale = float(D) ** -0.5
+    if out is None:
+        out = torch.empty((n, hq, D), dtype=torch.bfloat16, device=Q.device)
+    elif out.dtype != torch.bfloat16 or out.numel() < n * hq * D:
+        raise ValueError("out: expected bfloat16 [new tokens, heads, D]")
+    if lse is not None and (lse.dtype != torch.float32 or lse.numel() < n * hq):
+        raise ValueError("lse: expected float32 [new tokens, heads]")
+    tp, ts = _table(block_table, B)
+    L = lib()
+    buf, nbytes = _workspace(L.pace_kv_attention_workspace_size, (cache._address, cp, B, hq, int(max_len)), ws, Q.device)
+    _check_ws("pace_kv_attention",
+              L.pace_kv_attention(cache._address, qp, qs, cp, B, hq, _int32(seq_lens, B, "seq_lens"), tp, ts, int(max_len),
+                                  float(scale), int(window), int(sinks), _dev(out), _dev(lse), _dev(buf), nbytes,
+                                  _stream(stream)), ws)
+    return out
