@@ -995,24 +995,10 @@ __global__ void __launch_bounds__(256) attn_reduce(const float* __restrict__ par
 // ------------------------------------------------------------------------------------------------
 // host side
 // ------------------------------------------------------------------------------------------------
-PFN_cuTensorMapEncodeTiled_v12000 tensor_map_encoder() {
-  static std::once_flag once;
-  static PFN_cuTensorMapEncodeTiled_v12000 fn = nullptr;
-  std::call_once(once, [] {
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) ==
-            cudaSuccess &&
-        q == cudaDriverEntryPointSuccess)
-      fn = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(p);
-  });
-  return fn;
-}
-
 // 2-D map over a row-major bf16 matrix [rows, cols]; box = 64 columns (128-byte swizzle) or
 // 16 columns (32-byte swizzle) x 128 rows.
 pace_status_t make_map(CUtensorMap* m, const void* ptr, int64_t rows, int64_t cols, bool wide) {
-  auto enc = tensor_map_encoder();
+  auto enc = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(tensor_map_encoder());
   if (enc == nullptr) return set_cuda_error(cudaErrorNotSupported);
   cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)};
   cuuint64_t strides[1] = {static_cast<cuuint64_t>(cols * 2)};

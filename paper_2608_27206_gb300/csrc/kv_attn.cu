@@ -13,7 +13,9 @@
 #include <algorithm>
 #include <cmath>
 
-#include "pace_kv.cuh"
+#include <cudaTypedefs.h>
+
+#include "kv_attn.cuh"
 #include "pace_ptx.cuh"
 
 namespace pace {
@@ -21,44 +23,25 @@ namespace {
 
 constexpr int kRows = 16, kAttnThreads = 128;
 
-struct KvAttnArgs {
-  KvView c;
-  const uint16_t* Q;
-  uint16_t* out;
-  float* lse;
-  int64_t q_stride, table_stride;
-  const int32_t* lens;
-  const int32_t* table;
-  float scale2;                   // scale * log2(e)
-  int q_heads, group, window, sinks, max_len;
-  int b0, nb;
-  int cu[kKvMaxB + 1];
-  int tile_prefix[kKvMaxB + 1];   // tiles of kRows rows
-};
-
-__device__ __forceinline__ bool sees(int j, int p, int window, int sinks) {
-  return j <= p && (window <= 0 || j > p - window || j < sinks);
-}
-
 template <int D>
 __global__ void __launch_bounds__(kAttnThreads) kv_attn_rows(const __grid_constant__ KvAttnArgs a, int* status) {
   __shared__ float q[kRows][D + 1], kv[kKvBlock][D + 1], p[kRows][kKvBlock], m[kRows], l[kRows], f[kRows];
   ptx::begin_call();
-  int lo = 0, hi = a.nb - 1;
+  int lo = 0, hi = a.s.nb - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
-    if (a.tile_prefix[mid] <= static_cast<int>(blockIdx.x)) lo = mid;
+    if (a.s.tile0[mid] <= static_cast<int>(blockIdx.x)) lo = mid;
     else hi = mid - 1;
   }
-  const int b = lo, n = a.cu[b + 1] - a.cu[b], head = blockIdx.y, tid = threadIdx.x;
-  const int row0 = (static_cast<int>(blockIdx.x) - a.tile_prefix[b]) * kRows, rows = min(n * a.group - row0, kRows);
-  int len = max(a.lens[a.b0 + b], 0);
+  const int b = lo, n = a.s.nq[b], head = blockIdx.y, tid = threadIdx.x;
+  const int row0 = (static_cast<int>(blockIdx.x) - a.s.tile0[b]) * kRows, rows = min(n * a.group - row0, kRows);
+  int len = max(a.lens[a.s.seq[b]], 0);
   if (len > a.max_len) {
     if (tid == 0) record_error(status, PACE_ERR_INVALID_ARG, K_KV_ATTN);
     len = a.max_len;
   }
   const int p0 = len - n;   // slot of query 0
-  auto token = [&](int r) { return a.cu[b] + (row0 + r) / a.group; };
+  auto token = [&](int r) { return a.s.q0[b] + (row0 + r) / a.group; };
   auto qhead = [&](int r) { return head * a.group + (row0 + r) % a.group; };
   for (int i = tid; i < kRows * D; i += kAttnThreads) {
     const int r = i / D, d = i % D;
@@ -77,7 +60,7 @@ __global__ void __launch_bounds__(kAttnThreads) kv_attn_rows(const __grid_consta
   for (int blk = 0; blk * kKvBlock <= p_last; ++blk) {
     if (blk < from && blk * kKvBlock >= a.sinks) blk = from;
     const int slot = blk * kKvBlock;
-    const int page = a.table[(a.b0 + b) * a.table_stride + (slot >> a.c.page_shift)];
+    const int page = a.table[a.s.seq[b] * a.table_stride + (slot >> a.c.page_shift)];
     const bool ok = page >= 0 && page < a.c.n_pages;
     if (!ok && tid == 0) record_error(status, PACE_ERR_INVALID_ARG, K_KV_ATTN);
     const int at = slot & ((1 << a.c.page_shift) - 1);
@@ -88,7 +71,7 @@ __global__ void __launch_bounds__(kAttnThreads) kv_attn_rows(const __grid_consta
       for (int i = tid; i < kKvBlock * D / 2; i += kAttnThreads) {
         const int j = 2 * i / D, d = 2 * i % D;
         float2 x = make_float2(0.f, 0.f);
-        if (ok && sees(slot + j, p_last, 0, 0) && (a.window <= 0 || slot + j < a.sinks || slot + j > p_first - a.window)) {
+        if (ok && kv_sees(slot + j, p_last, 0, 0) && (a.window <= 0 || slot + j < a.sinks || slot + j > p_first - a.window)) {
           const uint32_t h = e4m3x2_to_f16x2(*reinterpret_cast<const uint16_t*>(codes + co + 2 * i));
           x = __half22float2(*reinterpret_cast<const __half2*>(&h));
           x.x *= s;
@@ -105,7 +88,7 @@ __global__ void __launch_bounds__(kAttnThreads) kv_attn_rows(const __grid_consta
       const int r = i / kKvBlock, j = i % kKvBlock;
       float s = 0.f;
       for (int d = 0; d < D; ++d) s = fmaf(q[r][d], kv[j][d], s);
-      const bool see = r < rows && sees(slot + j, p0 + (row0 + r) / a.group, a.window, a.sinks);
+      const bool see = r < rows && kv_sees(slot + j, p0 + (row0 + r) / a.group, a.window, a.sinks);
       p[r][j] = see ? s * a.scale2 : -INFINITY;
     }
     __syncthreads();
@@ -149,12 +132,52 @@ __global__ void __launch_bounds__(kAttnThreads) kv_attn_rows(const __grid_consta
   }
 }
 
+// 3-D map over the codes: D bytes x the rows of all heads of a page x pages; a box is 16 to 128 rows of one page.
+pace_status_t make_map(CUtensorMap* m, const pace_kv_cache* c, void* codes) {
+  auto enc = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(tensor_map_encoder());
+  if (enc == nullptr) return set_cuda_error(cudaErrorNotSupported);
+  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(c->head_dim), static_cast<cuuint64_t>(c->n_kv_heads) * c->page_size,
+                              static_cast<cuuint64_t>(c->n_pages)};
+  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(c->head_dim), static_cast<cuuint64_t>(c->page_stride)};
+  const cuuint32_t box[3] = {static_cast<cuuint32_t>(c->head_dim), static_cast<cuuint32_t>(std::min(c->page_size, kKvTile)), 1};
+  const cuuint32_t step[3] = {1, 1, 1};
+  const CUresult r = enc(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, codes, dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                         c->head_dim == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                         CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? PACE_OK : PACE_ERR_INVALID_ARG;
+}
+
 pace_status_t check_attention(const pace_kv_cache* cache, const int32_t* cu_q, int B, int n_q_heads, int max_len) {
   PACE_CHECK(check_cache(cache));
   PACE_CHECK(check_prefix(cu_q, B));
   if (n_q_heads < 1 || n_q_heads % cache->n_kv_heads != 0 || n_q_heads / cache->n_kv_heads > 64) return PACE_ERR_INVALID_ARG;
   if (max_len < 0 || max_len > (1 << 30)) return PACE_ERR_INVALID_ARG;
+  if (cu_q[B] > (1 << 30) / (n_q_heads / cache->n_kv_heads)) return PACE_ERR_INVALID_ARG;
   return PACE_OK;
+}
+
+// Sequences of at most kFewRows query rows per KV head take the transposed products of kv_decode.cu.
+constexpr int kFewRows = 32;
+
+// Rows of a tile for few-row sequences: 8, 16 or 32, what the largest needs (0: there are none).
+int few_rows(const int32_t* cu_q, int B, int group) {
+  int most = 0;
+  for (int b = 0; b < B; ++b) {
+    const int64_t rows = static_cast<int64_t>(cu_q[b + 1] - cu_q[b]) * group;
+    if (rows <= kFewRows) most = std::max(most, static_cast<int>(rows));
+  }
+  return most == 0 ? 0 : most <= 8 ? 8 : most <= 16 ? 16 : 32;
+}
+
+struct Workspace {
+  size_t lse, part, total;
+};
+Workspace workspace(int rows, int D) {
+  Workspace w{};
+  w.lse = align_up(kPlanCtas * sizeof(KvSplit), 256);
+  w.part = w.lse + align_up(static_cast<size_t>(2) * kPlanCtas * rows * sizeof(float), 256);
+  w.total = w.part + static_cast<size_t>(2) * kPlanCtas * rows * D * sizeof(float);
+  return w;
 }
 
 }  // namespace
@@ -165,7 +188,7 @@ using namespace pace;
 extern "C" size_t pace_kv_attention_workspace_size(const pace_kv_cache* cache, const int32_t* cu_q, int B, int n_q_heads,
                                                    int max_len) {
   if (B <= 0 || check_attention(cache, cu_q, B, n_q_heads, max_len) != PACE_OK) return 0;
-  return 16;
+  return workspace(few_rows(cu_q, B, n_q_heads / cache->n_kv_heads), cache->head_dim).total;
 }
 
 extern "C" pace_status_t pace_kv_attention(const pace_kv_cache* cache, const void* Q, int64_t q_row_stride, const int32_t* cu_q,
@@ -176,16 +199,19 @@ extern "C" pace_status_t pace_kv_attention(const pace_kv_cache* cache, const voi
   if (B == 0) return PACE_OK;
   PACE_CHECK(check_attention(cache, cu_q, B, n_q_heads, max_len));
   if (cu_q[B] == 0) return PACE_OK;
-  const int D = cache->head_dim;
+  const int D = cache->head_dim, group = n_q_heads / cache->n_kv_heads;
   if (!rows_ok(Q, q_row_stride, n_q_heads, D) || out == nullptr || reinterpret_cast<uintptr_t>(out) % 16 != 0)
     return PACE_ERR_INVALID_ARG;
-  if (seq_lens == nullptr || block_table == nullptr || table_stride < 1 || sinks < 0) return PACE_ERR_INVALID_ARG;
+  if (seq_lens == nullptr || block_table == nullptr || table_stride < 1 || table_stride > INT32_MAX || sinks < 0) return PACE_ERR_INVALID_ARG;
   if (max_len > table_stride * cache->page_size) return PACE_ERR_INVALID_ARG;
   if (!(scale > 0.f) || !std::isfinite(scale)) return PACE_ERR_INVALID_ARG;
-  if (ws == nullptr || reinterpret_cast<uintptr_t>(ws) % 16 != 0 ||
-      ws_bytes < pace_kv_attention_workspace_size(cache, cu_q, B, n_q_heads, max_len))
-    return PACE_ERR_WORKSPACE;
+  const int few = few_rows(cu_q, B, group);
+  const Workspace w = workspace(few, D);
+  if (ws == nullptr || reinterpret_cast<uintptr_t>(ws) % 16 != 0 || ws_bytes < w.total) return PACE_ERR_WORKSPACE;
   PACE_CHECK(check_device());
+  KvMaps maps;
+  PACE_CHECK(make_map(&maps.k, cache, cache->k));
+  PACE_CHECK(make_map(&maps.v, cache, cache->v));
   KvAttnArgs a{};
   a.c = kv_view(cache);
   a.Q = static_cast<const uint16_t*>(Q);
@@ -195,27 +221,48 @@ extern "C" pace_status_t pace_kv_attention(const pace_kv_cache* cache, const voi
   a.table_stride = table_stride;
   a.lens = seq_lens;
   a.table = block_table;
+  a.split = static_cast<KvSplit*>(ws);
+  a.part_lse = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + w.lse);
+  a.part = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + w.part);
   a.scale2 = static_cast<float>(static_cast<double>(scale) * 1.4426950408889634);
   a.q_heads = n_q_heads;
-  a.group = n_q_heads / cache->n_kv_heads;
+  a.group = group;
   a.window = window;
   a.sinks = sinks;
   a.max_len = max_len;
   int* status = device_status_word();
-  for (int b0 = 0; b0 < B; b0 += kKvMaxB) {
-    a.b0 = b0;
-    a.nb = std::min(kKvMaxB, B - b0);
-    int64_t tiles = 0;
-    for (int i = 0; i <= a.nb; ++i) {
-      a.cu[i] = cu_q[b0 + i];
-      a.tile_prefix[i] = static_cast<int>(tiles);
-      if (i < a.nb) tiles += (static_cast<int64_t>(cu_q[b0 + i + 1] - cu_q[b0 + i]) * a.group + kRows - 1) / kRows;
+  int sms = 0;
+  PACE_CHECK(sm_count(&sms));
+  const int64_t slot_tiles = std::max(1, (max_len + kKvTile - 1) / kKvTile);
+  for (const bool is_few : {true, false}) {
+    const int rows = is_few ? few : kRows;
+    for (int b = 0; b < B;) {
+      a.s.nb = 0;
+      a.s.tile0[0] = 0;
+      int64_t tiles = 0;
+      for (; b < B && a.s.nb < kKvMaxB; ++b) {
+        const int n = cu_q[b + 1] - cu_q[b];
+        const int64_t r = static_cast<int64_t>(n) * group;
+        if (n == 0 || (r <= kFewRows) != is_few) continue;
+        const int i = a.s.nb++;
+        a.s.seq[i] = b;
+        a.s.q0[i] = cu_q[b];
+        a.s.nq[i] = n;
+        tiles += (r + rows - 1) / rows;
+        a.s.tile0[i + 1] = static_cast<int>(tiles);
+      }
+      if (a.s.nb == 0) break;
+      if (is_few) {
+        const int64_t most = tiles * cache->n_kv_heads * slot_tiles;
+        const unsigned grid = static_cast<unsigned>(std::min<int64_t>({most, sms, kPlanCtas}));
+        PACE_CHECK(launch_kv_decode(maps, a, D, rows, grid, status, stream));
+        if (slot_tiles > 1) PACE_CHECK(launch_kv_combine(a, D, rows, grid, stream));
+      } else {
+        auto* kernel = D == 128 ? kv_attn_rows<128> : kv_attn_rows<64>;
+        PACE_CHECK(launch_dependent(kernel, dim3(static_cast<unsigned>(tiles), static_cast<unsigned>(cache->n_kv_heads)), kAttnThreads,
+                                    0, 1, stream, a, status));
+      }
     }
-    if (tiles == 0) continue;
-    if (tiles > INT32_MAX) return PACE_ERR_INVALID_ARG;
-    auto* kernel = D == 128 ? kv_attn_rows<128> : kv_attn_rows<64>;
-    PACE_CHECK(launch_dependent(kernel, dim3(static_cast<unsigned>(tiles), static_cast<unsigned>(cache->n_kv_heads)), kAttnThreads, 0,
-                                1, stream, a, status));
   }
   return PACE_OK;
 }

@@ -1,0 +1,237 @@
+// What the kernels of the attention over the paged cache share: arguments, the slots that a row tile looks
+// at, and how the work is cut into equal shares.
+//
+// The query rows of a sequence that share a KV head (row r = query r / G, head r % G of the group) are cut
+// into row tiles, and the slots that a row tile sees into tiles of 128.  Row tile by row tile, KV head by KV
+// head, slot tile by slot tile, the tiles of a launch form one line; CTA c of g walks tiles T c / g ..
+// T (c + 1) / g - 1 of it.  So every CTA has the same work to a tile, whatever the lengths are, and at most
+// its first and its last (row tile, head) are shared with others: those leave a normalised partial output
+// and its log-sum-exp per row (slot 2 c: it begins inside, 2 c + 1: it begins there and goes on elsewhere),
+// which kv_attn_combine weighs together.
+#pragma once
+#include <cuda.h>
+
+#include "pace_kv.cuh"
+#include "pace_ptx.cuh"
+
+namespace pace {
+
+constexpr int kKvTile = 128;      // slots of one tile
+constexpr int kPlanCtas = 152;    // CTAs of a launch at most: an SM each (the size queries need no device)
+
+// The launch's sequences, those without queries left out.
+struct KvSeqs {
+  int nb;
+  int seq[kKvMaxB];        // number in the call
+  int q0[kKvMaxB];         // first query
+  int nq[kKvMaxB];
+  int tile0[kKvMaxB + 1];  // row tiles before it
+};
+
+// Written by CTA c where its last (row tile, head) goes on in CTAs c + 1 .. c + followers.
+struct KvSplit {
+  int i, row_tile, head, followers;
+};
+
+struct KvAttnArgs {
+  KvView c;
+  const uint16_t* Q;
+  uint16_t* out;
+  float* lse;
+  int64_t q_stride, table_stride;
+  const int32_t* lens;
+  const int32_t* table;
+  KvSplit* split;       // [CTAs]
+  float* part_lse;      // [2 CTAs][rows of a tile], base 2
+  float* part;          // [2 CTAs][rows of a tile][D]
+  float scale2;         // scale * log2(e)
+  int q_heads, group, window, sinks, max_len;
+  KvSeqs s;
+};
+
+__device__ __forceinline__ bool kv_sees(int j, int p, int window, int sinks) {
+  return j <= p && (window <= 0 || j > p - window || j < sinks);
+}
+
+// The slot tiles that queries at slots p_first .. p_last look at: n of them, the i-th being i for i < head, else i + skip.
+struct KvSpan {
+  int n, head, skip;
+  __device__ __forceinline__ int tile(int i) const { return i < head ? i : i + skip; }
+};
+__device__ __forceinline__ KvSpan kv_span(int p_first, int p_last, int window, int sinks) {
+  KvSpan s{0, 0, 0};
+  if (p_last < 0) return s;
+  const int end = p_last / kKvTile + 1;
+  s.n = s.head = end;
+  if (window > 0) {
+    const int from = max(p_first - window + 1, 0) / kKvTile;             // first tile of the window
+    const int few = min((min(sinks, p_last + 1) + kKvTile - 1) / kKvTile, end);   // tiles that hold the first slots
+    if (few < from) s = KvSpan{few + end - from, few, from - few};
+  }
+  return s;
+}
+
+// One (row tile, KV head) of the line, of which this CTA walks slot tiles t0 .. t1 - 1.
+struct KvItem {
+  int i, row_tile, head, t0, t1;
+  int row0, rows;           // its query rows
+  int len, p0;              // slots of the sequence; slot of its query 0
+  int p_first, p_last;      // slots of the tile's first and last query
+  KvSpan span;
+};
+
+template <int ROWS>
+__device__ __forceinline__ void kv_item_rows(const KvAttnArgs& a, int i, int row_tile, KvItem& it) {
+  it.i = i;
+  it.row_tile = row_tile;
+  it.len = min(max(a.lens[a.s.seq[i]], 0), a.max_len);
+  it.p0 = it.len - a.s.nq[i];
+  it.row0 = row_tile * ROWS;
+  it.rows = min(a.s.nq[i] * a.group - it.row0, ROWS);
+  it.p_first = it.p0 + it.row0 / a.group;
+  it.p_last = it.p0 + (it.row0 + it.rows - 1) / a.group;
+  it.span = kv_span(it.p_first, it.p_last, a.window, a.sinks);
+}
+
+// Where a CTA's share lies; the same for all its threads.
+struct KvShare {
+  int64_t pos, end;         // its tiles of the line
+  int64_t total;
+  int64_t base;             // first tile of (i, row_tile)
+  int i, row_tile;
+  int ctas;                 // that have a share
+};
+
+// Walks a share (item) by item.
+template <int ROWS>
+struct KvWalk {
+  const KvAttnArgs& a;
+  KvShare s;
+  KvItem it;
+  bool have = false;
+  __device__ __forceinline__ KvWalk(const KvAttnArgs& args, const KvShare& share) : a(args), s(share) {}
+  __device__ __forceinline__ bool next() {
+    if (s.pos >= s.end) return false;
+    while (true) {
+      if (!have) {
+        kv_item_rows<ROWS>(a, s.i, s.row_tile, it);
+        have = true;
+      }
+      const uint32_t off = static_cast<uint32_t>(s.pos - s.base), n = it.span.n;
+      if (off < n * static_cast<uint32_t>(a.c.heads)) {
+        it.head = off / n;
+        it.t0 = off - it.head * n;
+        it.t1 = static_cast<int>(min(static_cast<int64_t>(n), it.t0 + (s.end - s.pos)));
+        s.pos += it.t1 - it.t0;
+        return true;
+      }
+      s.base += static_cast<int64_t>(n) * a.c.heads;
+      have = false;
+      if (++s.row_tile >= a.s.tile0[s.i + 1] - a.s.tile0[s.i]) {
+        s.row_tile = 0;
+        ++s.i;
+      }
+    }
+  }
+};
+
+// Every thread of the block (a multiple of 32, at most 1024) calls this once; `buf` holds blockDim.x 64-bit words.  Row
+// tiles that see nothing get their zeros here.
+template <int ROWS, int D>
+__device__ __forceinline__ KvShare kv_share(const KvAttnArgs& a, int64_t* buf, KvShare* found, int* status) {
+  const int threads = blockDim.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int tiles = a.s.tile0[a.s.nb], per = (tiles + threads - 1) / threads;
+  const int first = min(tid * per, tiles), last = min(first + per, tiles);
+  int i0 = 0, hi = a.s.nb - 1;      // the sequence of row tile `first`
+  while (i0 < hi) {
+    const int mid = (i0 + hi + 1) >> 1;
+    if (a.s.tile0[mid] <= first) i0 = mid;
+    else hi = mid - 1;
+  }
+  auto each = [&](auto&& f) {
+    int i = i0;
+    for (int t = first; t < last; ++t) {
+      while (t >= a.s.tile0[i + 1]) ++i;
+      KvItem it;
+      kv_item_rows<ROWS>(a, i, t - a.s.tile0[i], it);
+      if (!f(it, static_cast<int64_t>(it.span.n) * a.c.heads)) break;
+    }
+  };
+  int64_t mine = 0;
+  each([&](const KvItem& it, int64_t n) {
+    mine += n;
+    if (it.row_tile == 0 && a.lens[a.s.seq[it.i]] > a.max_len && blockIdx.x == 0) record_error(status, PACE_ERR_INVALID_ARG, K_KV_ATTN);
+    if (n == 0 && (a.s.tile0[it.i] + it.row_tile) % gridDim.x == blockIdx.x) {
+      for (int r = 0; r < it.rows * a.c.heads; ++r) {
+        const int row = it.row0 + r / a.c.heads, h = (r % a.c.heads) * a.group + row % a.group;
+        const int64_t at = static_cast<int64_t>(a.s.q0[it.i] + row / a.group) * a.q_heads + h;
+        for (int d = 0; d < D; d += 8) *reinterpret_cast<uint4*>(a.out + at * D + d) = make_uint4(0, 0, 0, 0);
+        if (a.lse != nullptr) a.lse[at] = -INFINITY;
+      }
+    }
+    return true;
+  });
+  int64_t incl = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t x = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += x;
+  }
+  if (lane == 31) buf[warp] = incl;
+  __syncthreads();
+  if (warp == 0) {
+    int64_t x = lane < threads / 32 ? buf[lane] : 0;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
+      if (lane >= o) x += y;
+    }
+    if (lane < threads / 32) buf[lane] = x;
+  }
+  __syncthreads();
+  const int64_t total = buf[threads / 32 - 1];
+  const int64_t before = incl - mine + (warp > 0 ? buf[warp - 1] : 0);
+  const int ctas = static_cast<int>(min(static_cast<int64_t>(gridDim.x), total));
+  KvShare s{};
+  s.total = total;
+  s.ctas = ctas;
+  if (static_cast<int>(blockIdx.x) >= ctas) return s;      // nothing to do (uniform)
+  s.pos = total * blockIdx.x / ctas;
+  s.end = total * (blockIdx.x + 1) / ctas;
+  if (s.pos >= before && s.pos < before + mine) {
+    int64_t base = before;
+    each([&](const KvItem& it, int64_t n) {
+      if (s.pos < base + n) {
+        s.base = base;
+        s.i = it.i;
+        s.row_tile = it.row_tile;
+        return false;
+      }
+      base += n;
+      return true;
+    });
+    *found = s;
+  }
+  __syncthreads();
+  return *found;
+}
+
+// What CTA c tells the combine kernel: how many later CTAs its last item goes on in.
+__device__ __forceinline__ void kv_write_split(const KvAttnArgs& a, const KvShare& s, const KvItem& it) {
+  KvSplit sp{it.i, it.row_tile, it.head, 0};
+  if (it.t0 == 0 && it.t1 < it.span.n) {   // CTA j takes part iff total j / ctas < the item's end
+    const int64_t end = s.end + (it.span.n - it.t1);
+    sp.followers = static_cast<int>((end * s.ctas + s.total - 1) / s.total) - 1 - static_cast<int>(blockIdx.x);
+  }
+  a.split[blockIdx.x] = sp;
+}
+
+struct KvMaps {
+  CUtensorMap k, v;
+};
+
+// Launches of the two forms (rows of a tile at most 32, and 256); `grid` CTAs, then the combine kernel.
+pace_status_t launch_kv_decode(const KvMaps& maps, const KvAttnArgs& a, int D, int rows, unsigned grid, int* status, cudaStream_t stream);
+pace_status_t launch_kv_combine(const KvAttnArgs& a, int D, int rows, unsigned grid, cudaStream_t stream);
+
+}  // namespace pace

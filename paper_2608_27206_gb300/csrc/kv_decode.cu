@@ -1,0 +1,582 @@
+// Serve: attention over the paged cache for few query rows per KV head (decode steps, drafted tokens).
+//
+// K and V cross HBM once and go to the tensor cores as the 8-bit codes they are.  With so few rows the
+// codes are the large operand of both products, so both are formed transposed:
+//   S^T [128 slots x rows] = K [slots x D] q^T         O^T [D x rows] += V^T [D x slots] P^T
+// A 16-bit factor enters as two e4m3 terms side by side, x = hi + lo / 16: exactly for bf16 q (8 significant
+// bits are two times 4; each row of q is first brought under 256 by a power of two), to 8 bits for the
+// weights P.  The two terms are two columns of the same product, so they cost nothing while N is small.
+//
+// A TMEM lane of S^T is a slot.  Its thread applies the block's K scale and the mask, and turns the score x
+// (base 2) of row q into the weight 2^(x - m_q), which it sums, and into P = 16 * 2^(x - m_q) vs 2^(m_q - w_q),
+// vs being the block's V scale.  m_q and w_q stand for the largest x and the largest x + log2(vs) so far, but lag
+// behind: they move only when a weight would pass 2^60 or P 256 (e4m3 ends at 448).  So the usual tile has no maximum and no
+// exchange between threads but one barrier's vote, and O^T stays in TMEM untouched.
+//
+// What bounds it is HBM: per slot and head 2 D bytes.  Roles of a CTA (one per SM): warp 0 fetches tiles of 128 slots
+// (TMA boxes of a page each, scales by 4-byte copies) through a ring of stages, warp 1 issues the MMAs, warps 2-5 own the
+// 128 lanes.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include <algorithm>
+
+#include "kv_attn.cuh"
+
+namespace pace {
+namespace {
+
+using namespace ptx;
+
+constexpr int kWarps = 6, kThreads = 32 * kWarps;
+constexpr float kFar = 60.f;         // how far a score may pass m_q
+constexpr float kOver = 4.f;         // ... and x + log2(vs) may pass w_q
+constexpr float kUnit = 4.f;         // log2 of P at w_q
+constexpr float kNone = -1e30f;      // m_q and w_q before the first slot (finite: x - m_q is never NaN)
+
+template <int D, int NQ>
+struct DecodeCfg {
+  static constexpr int TILE = kKvTile * D;              // bytes of a K or V tile
+  static constexpr int STAGES = D == 128 ? 6 : 12;
+  static constexpr int QBYTES = 2 * NQ * D;             // hi rows, then lo rows
+  static constexpr int PBYTES = 2 * NQ * kKvTile;       // 16 columns of every slot, then the next 16
+  static constexpr uint32_t SWIZZLE = D == 128 ? 2 : 4;
+  static constexpr uint32_t GROUP = 8 * D;              // bytes of 8 rows
+  static constexpr int COLS = 2 * NQ;                   // TMEM: S twice, then O
+  static constexpr uint32_t TMEM = 6 * NQ <= 64 ? 64 : 6 * NQ <= 128 ? 128 : 256;
+  static constexpr uint32_t IDESC_S = idesc_e4m3_f32(128, COLS, false, false);
+  static constexpr uint32_t IDESC_O = idesc_e4m3_f32(128, COLS, true, true);
+};
+
+struct Stat {
+  float m, w, far, g;     // m_q, w_q, m_q + kFar, 2^(kUnit + m_q - w_q)
+};
+
+template <int D, int NQ>
+struct alignas(16) DecodeCtl {
+  uint64_t full[DecodeCfg<D, NQ>::STAGES], empty[DecodeCfg<D, NQ>::STAGES], s_full[2], p_full[2], q_full, pv_done;
+  Stat stat[NQ];
+  float qc[NQ];             // scale2 * the row's power of two
+  int slot_of[NQ];          // slot of the row's query
+  float2 fac[NQ];
+  float2 red[4][NQ];
+  float scales[DecodeCfg<D, NQ>::STAGES][16];   // a tile's K scales, then its V scales
+  int64_t scan[kWarps];
+  KvShare share;
+  uint32_t tmem;
+  int abort;
+};
+
+__device__ __forceinline__ bool stopped(const int* abort) { return *reinterpret_cast<const volatile int*>(abort) != 0; }
+__device__ __forceinline__ void stop(int* abort, int* status) {
+  *reinterpret_cast<volatile int*>(abort) = 1;
+  record_error(status, PACE_ERR_TIMEOUT, K_KV_ATTN);
+}
+
+template <int N>
+__device__ __forceinline__ void load_cols(uint32_t addr, uint32_t (&v)[N]) {
+  if constexpr (N == 64) {
+    tmem_ld_32x32b_x64(addr, v);
+    tmem_wait_ld();
+    reg_fence64(v);
+  } else {
+    tmem_ld_32x32b(addr, v);
+    tmem_wait_ld();
+    reg_fence(v);
+  }
+}
+
+template <int D, int NQ>
+__global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_constant__ KvMaps maps, const __grid_constant__ KvAttnArgs a,
+                                                                int* status) {
+  using C = DecodeCfg<D, NQ>;
+  constexpr int ST = C::STAGES;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* sKV = smem;                         // stages of a K tile and a V tile
+  uint8_t* sQ = sKV + ST * 2 * C::TILE;
+  uint8_t* sP = sQ + C::QBYTES;                // two
+  auto* ctl = reinterpret_cast<DecodeCtl<D, NQ>*>(sP + 2 * C::PBYTES);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  auto full = [&](int s) { return smem_u32(&ctl->full[s]); };
+  auto empty = [&](int s) { return smem_u32(&ctl->empty[s]); };
+  auto s_full = [&](int p) { return smem_u32(&ctl->s_full[p]); };
+  auto p_full = [&](int p) { return smem_u32(&ctl->p_full[p]); };
+  const uint32_t q_full = smem_u32(&ctl->q_full), pv_done = smem_u32(&ctl->pv_done);
+
+  begin_call();
+  const KvShare share = kv_share<NQ, D>(a, ctl->scan, &ctl->share, status);
+  if (static_cast<int>(blockIdx.x) >= share.ctas) {
+    if (threadIdx.x == 0) a.split[blockIdx.x] = KvSplit{0, 0, 0, 0};
+    return;
+  }
+  if (warp == 0 && lane == 0) {
+    prefetch_tensormap(&maps.k);
+    prefetch_tensormap(&maps.v);
+    for (int s = 0; s < ST; ++s) {
+      mbar_init(full(s), 33);      // the byte count's arrival and 32 lanes' scales
+      mbar_init(empty(s), 1);
+    }
+    for (int p = 0; p < 2; ++p) {
+      mbar_init(s_full(p), 1);
+      mbar_init(p_full(p), 4);
+    }
+    mbar_init(q_full, 4);
+    mbar_init(pv_done, 1);
+    fence_mbar_init();
+    ctl->abort = 0;
+  }
+  if (warp == 1) {
+    tmem_alloc(smem_u32(&ctl->tmem), C::TMEM);
+    tmem_relinquish();
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem = ctl->tmem;
+  KvWalk<NQ> walk(a, share);
+
+  if (warp == 0) {
+    // ---- fetch -------------------------------------------------------------------------------
+    const int shift = min(a.c.page_shift, 7), box_rows = 1 << shift, boxes = kKvTile >> shift;
+    const int tiles_per_load = 32 / boxes;     // a lane holds the page of one box
+    int t = 0;                                 // tiles so far
+    while (!stopped(&ctl->abort) && walk.next()) {
+      const KvItem& it = walk.it;
+      const int32_t* table = a.table + static_cast<int64_t>(a.s.seq[it.i]) * a.table_stride;
+      const int last = it.p_last;
+      auto page_of = [&](int tile_i) {         // of box lane % boxes of tile tile_i + lane / boxes
+        const int i = tile_i + lane / boxes;
+        if (i >= it.t1) return -2;
+        const int slot = it.span.tile(i) * kKvTile + (lane % boxes) * box_rows;
+        if (slot > last) return -2;            // nothing there
+        const int page = table[slot >> a.c.page_shift];
+        return page >= 0 && page < a.c.n_pages ? page : -1;
+      };
+      int mine = page_of(it.t0), next = -2;
+      for (int i = it.t0; i < it.t1; ++i, ++t) {
+        const int k = (i - it.t0) % tiles_per_load;
+        if (k == 0) {
+          if (i > it.t0) mine = next;
+          next = page_of(i + tiles_per_load);
+        }
+        int page = __shfl_sync(0xffffffffu, mine, k * boxes + lane % boxes);
+        const bool there = page != -2;
+        if (page == -1) {
+          if (lane < boxes) record_error(status, PACE_ERR_INVALID_ARG, K_KV_ATTN);
+          page = 0;      // (the sequence's results mean nothing then; the copy stays inside the cache)
+        }
+        const int s = t % ST, round = t / ST;
+        if (round > 0) {
+          const bool ok = __all_sync(0xffffffffu, mbar_wait(empty(s), (round - 1) & 1, kWaitLimitNs));
+          if (!ok) {
+            if (lane == 0) stop(&ctl->abort, status);
+            break;
+          }
+        }
+        const int slot0 = it.span.tile(i) * kKvTile;
+        uint8_t* dst = sKV + s * 2 * C::TILE;
+        const int n_there = __popc(__ballot_sync(0xffffffffu, there && lane < boxes));
+        if (lane == 0) mbar_arrive_expect_tx(full(s), 2 * n_there * box_rows * D);
+        // scale j (K: 0-7, V: 8-15) of the tile: block j % 8, in box (j % 8) * 16 / box_rows
+        const int blk = lane & 7;
+        const int bpage = __shfl_sync(0xffffffffu, page, blk * kKvBlock >> shift);
+        const int row = (slot0 + blk * kKvBlock) & ((1 << a.c.page_shift) - 1);
+        if (lane < 16 && slot0 + blk * kKvBlock <= last)
+          cp_async4(smem_u32(&ctl->scales[s][lane]),
+                    (lane < 8 ? a.c.ks : a.c.vs) + bpage * a.c.scale_stride + (static_cast<int64_t>(it.head) << (a.c.page_shift - 4)) + row / kKvBlock);
+        cp_async_arrive(full(s));
+        __syncwarp();
+        if (lane < boxes && there) {
+          const int y = (it.head << a.c.page_shift) + ((slot0 + lane * box_rows) & ((1 << a.c.page_shift) - 1));
+          tma_load_3d(smem_u32(dst + lane * box_rows * D), &maps.k, 0, y, page, full(s));
+          tma_load_3d(smem_u32(dst + C::TILE + lane * box_rows * D), &maps.v, 0, y, page, full(s));
+        }
+      }
+    }
+  } else if (warp == 1) {
+    // ---- products ----------------------------------------------------------------------------
+    if (lane == 0) {
+      const uint64_t dq = smem_desc(smem_u32(sQ), 16, C::GROUP, C::SWIZZLE);
+      // V^T: 8 slots of D contiguous codes per repeat.  (D = 64 fills lanes 0-63; the other half of the 128 rows reads
+      // the same codes again and is not used.)
+      uint64_t dk[2], dp[2];
+      dk[0] = smem_desc(smem_u32(sKV), 16, C::GROUP, C::SWIZZLE);
+      dk[1] = smem_desc(smem_u32(sKV), 0, C::GROUP, C::SWIZZLE);
+      for (int p = 0; p < 2; ++p) dp[p] = smem_desc(smem_u32(sP + p * C::PBYTES), 8 * 16, NQ == 8 ? 8 * 16 : 16 * kKvTile, 0);
+      int t = 0, items = 0;
+      bool ok = true;
+      auto weigh = [&](int u, bool first) {     // O += V^T P of tile u
+        if (!mbar_wait(p_full(u & 1), (u >> 1) & 1, kWaitLimitNs)) return false;
+        tc_fence_after_sync();
+        const uint64_t v = dk[1] + static_cast<uint64_t>(((u % ST) * 2 + 1) * (C::TILE >> 4));
+#pragma unroll
+        for (int k = 0; k < kKvTile / 32; ++k)
+          mma_f8_ss(tmem + 2 * C::COLS, v + static_cast<uint64_t>(k * (32 * D >> 4)), dp[u & 1] + static_cast<uint64_t>(k * (32 * 16 >> 4)), C::IDESC_O,
+                    !first || k > 0);
+        mma_commit(empty(u % ST));
+        mma_commit(pv_done);
+        return true;
+      };
+      while (ok && walk.next()) {
+        ok = mbar_wait(q_full, items & 1, kWaitLimitNs);
+        ++items;
+        const int n = walk.it.t1 - walk.it.t0;
+        for (int i = 0; ok && i < n; ++i, ++t) {
+          ok = mbar_wait(full(t % ST), (t / ST) & 1, kWaitLimitNs);
+          if (!ok) break;
+          tc_fence_after_sync();
+          const uint64_t k0 = dk[0] + static_cast<uint64_t>((t % ST) * 2 * (C::TILE >> 4));
+#pragma unroll
+          for (int k = 0; k < D / 32; ++k)
+            mma_f8_ss(tmem + (t & 1) * C::COLS, k0 + static_cast<uint64_t>(2 * k), dq + static_cast<uint64_t>(2 * k), C::IDESC_S, k > 0);
+          mma_commit(s_full(t & 1));
+          if (i > 0) ok = weigh(t - 1, i == 1);
+        }
+        if (ok) ok = weigh(t - 1, n == 1);
+      }
+      if (!ok) stop(&ctl->abort, status);
+    }
+    __syncwarp();
+  } else {
+    // ---- weights -----------------------------------------------------------------------------
+    const int quad = warp & 3, me = quad * 32 + lane;    // TMEM lane: slot of the tile, then column of the output
+    const uint32_t lanes = tmem + (static_cast<uint32_t>(quad * 32) << 16);
+    int t = 0;
+    bool bad = false;
+    while (!bad && walk.next()) {
+      const KvItem& it = walk.it;
+      named_barrier_sync(1, 128);      // the last item's shared statistics have been read
+      // q: rows of this item as hi and lo codes (rows past it are zero), the power of two of each
+      for (int q = quad; q < NQ; q += 4) {
+        constexpr int E = D / 32;      // elements of a lane
+        float x[E];
+        const int r = it.row0 + q, h = it.head * a.group + r % a.group;
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] = 0.f;
+        if (q < it.rows) {
+          const uint16_t* src = a.Q + (a.s.q0[it.i] + r / a.group) * a.q_stride + static_cast<int64_t>(h) * D + lane * E;
+          uint32_t w[E / 2];
+          if constexpr (E == 4) {
+            const uint2 u = *reinterpret_cast<const uint2*>(src);
+            w[0] = u.x;
+            w[1] = u.y;
+          } else {
+            w[0] = *reinterpret_cast<const uint32_t*>(src);
+          }
+#pragma unroll
+          for (int e = 0; e < E; ++e) x[e] = __uint_as_float(e & 1 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);
+        }
+        float top = 0.f;
+        bool fin = true;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          top = fmaxf(top, fabsf(x[e]));
+          fin = fin && fabsf(x[e]) < INFINITY;
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        fin = __all_sync(0xffffffffu, fin);
+        const int e2 = fin ? max(static_cast<int>(__float_as_uint(top) >> 23) - 127 - 7, -110) : 0;   // top 2^-e2 in [128, 256)
+        const float inv = __uint_as_float(static_cast<uint32_t>(127 - e2) << 23);
+        uint32_t hi = 0x7F7F7F7Fu, lo = 0;      // a row that is not finite: NaN throughout
+        if (fin) {
+          float y[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int e = 0; e < E; ++e) y[e] = x[e] * inv;
+          hi = e4m3x4(y[0], y[1], y[2], y[3]);
+          const uint32_t f0 = e4m3x2_to_f16x2(hi & 0xFFFFu), f1 = e4m3x2_to_f16x2(hi >> 16);
+          const float2 g0 = __half22float2(*reinterpret_cast<const __half2*>(&f0)), g1 = __half22float2(*reinterpret_cast<const __half2*>(&f1));
+          lo = e4m3x4((y[0] - g0.x) * 16.f, (y[1] - g0.y) * 16.f, (y[2] - g1.x) * 16.f, (y[3] - g1.y) * 16.f);
+        }
+#pragma unroll
+        for (int part = 0; part < 2; ++part) {
+          const int row = part * NQ + q, byte = lane * E, chunk = byte / 16 ^ (D == 128 ? row & 7 : (row >> 1) & 3);
+          uint8_t* dst = sQ + row * D + chunk * 16 + byte % 16;
+          if constexpr (E == 4) *reinterpret_cast<uint32_t*>(dst) = part ? lo : hi;
+          else *reinterpret_cast<uint16_t*>(dst) = static_cast<uint16_t>(part ? lo : hi);
+        }
+        if (lane == 0) {
+          const bool real = q < it.rows;
+          ctl->qc[q] = real ? a.scale2 * __uint_as_float(static_cast<uint32_t>(127 + e2) << 23) : 0.f;
+          ctl->slot_of[q] = real ? it.p0 + r / a.group : -1;
+          // (rows past the item score 0 and must not ask for anything)
+          ctl->stat[q] = real ? Stat{kNone, kNone, kNone, 0.f} : Stat{-kNone, -kNone, -kNone, 0.f};
+        }
+      }
+      fence_proxy_async_shared();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(q_full);
+      named_barrier_sync(1, 128);
+      float l[NQ];
+#pragma unroll
+      for (int q = 0; q < NQ; ++q) l[q] = 0.f;
+      for (int i = it.t0; i < it.t1; ++i, ++t) {
+        const int s = t % ST, p = t & 1;
+        const int slot0 = it.span.tile(i) * kKvTile, slot = slot0 + me;
+        bool ok = mbar_wait(full(s), (t / ST) & 1, kWaitLimitNs);        // the tile's scales (and V, below)
+        ok = __all_sync(0xffffffffu, ok && mbar_wait(s_full(p), (t >> 1) & 1, kWaitLimitNs));
+        if (!ok) {
+          if (lane == 0) stop(&ctl->abort, status);
+          bad = true;
+        }
+        tc_fence_after_sync();
+        // every row sees the whole tile?
+        const bool whole = slot0 + kKvTile - 1 <= it.p_first &&
+                           (a.window <= 0 || slot0 > it.p_last - a.window || slot0 + kKvTile <= a.sinks);
+        float ks = ctl->scales[s][me >> 4], vs = ctl->scales[s][8 + (me >> 4)];
+        float x[NQ];
+        {
+          uint32_t sv[C::COLS];
+          load_cols(lanes + p * C::COLS, sv);
+          bool any = whole;
+          if (!whole) {
+#pragma unroll
+            for (int q = 0; q < NQ; ++q) any = any || kv_sees(slot, ctl->slot_of[q], a.window, a.sinks);
+            if (!any) ks = vs = 0.f;     // (what is there may be NaN)
+          }
+#pragma unroll
+          for (int q = 0; q < NQ; ++q) {
+            x[q] = fmaf(__uint_as_float(sv[NQ + q]), 0.0625f, __uint_as_float(sv[q])) * (ks * ctl->qc[q]);
+            if (!whole && !kv_sees(slot, ctl->slot_of[q], a.window, a.sinks)) x[q] = -INFINITY;
+          }
+          if (!whole) {
+            // 0 * NaN is NaN: a slot of V that some row does not see must not hold one.  Slots that nobody sees are
+            // cleared; where rows differ, a slot with a NaN code is cleared and those that see it get a NaN weight.
+            uint4* v = reinterpret_cast<uint4*>(sKV + (2 * s + 1) * C::TILE + me * D);
+            bool nan = false;
+            if (any) {
+#pragma unroll
+              for (int e = 0; e < D / 16; ++e) {
+                const uint4 u = v[e];
+                const uint32_t w = (((u.x & 0x7F7F7F7Fu) + 0x01010101u) | ((u.y & 0x7F7F7F7Fu) + 0x01010101u) | ((u.z & 0x7F7F7F7Fu) + 0x01010101u) |
+                                    ((u.w & 0x7F7F7F7Fu) + 0x01010101u)) & 0x80808080u;
+                nan = nan || w != 0;
+              }
+            }
+            if (!any || nan) {
+#pragma unroll
+              for (int e = 0; e < D / 16; ++e) v[e] = make_uint4(0, 0, 0, 0);
+            }
+            if (nan) vs = NAN;
+          }
+        }
+        const float lv = static_cast<float>(static_cast<int>(__float_as_uint(vs) >> 23) - 127);   // log2(vs), far down for 0
+        bool ask = bad;
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) ask = ask || x[q] > fminf(ctl->stat[q].far, ctl->stat[q].w + (kOver - lv));
+        if (named_barrier_any(1, 128, ask)) {
+          // some row's m or w has to move: the tile's maxima over all slots, new values, factors for l and O
+#pragma unroll
+          for (int q = 0; q < NQ; ++q) {
+            float mx = x[q], mw = x[q] + lv;
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) {
+              mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+              mw = fmaxf(mw, __shfl_xor_sync(0xffffffffu, mw, o));
+            }
+            if (lane == 0) ctl->red[quad][q] = make_float2(mx, mw);
+          }
+          named_barrier_sync(1, 128);
+          if (me < NQ) {
+            Stat st = ctl->stat[me];
+            float mx = kNone, mw = kNone;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+              mx = fmaxf(mx, ctl->red[w][me].x);
+              mw = fmaxf(mw, ctl->red[w][me].y);
+            }
+            const bool move = mx > st.far || mw > st.w + kOver;     // (each row by itself)
+            const float m = move ? fmaxf(st.m, mx) : st.m, w = move ? fmaxf(st.w, mw) : st.w;
+            ctl->fac[me] = make_float2(exp2f(st.m - m), exp2f(st.w - w));
+            ctl->stat[me] = Stat{m, w, m + kFar, exp2f(kUnit + m - w)};
+          }
+          if (i > it.t0 && !mbar_wait(pv_done, (t - 1) & 1, kWaitLimitNs)) stop(&ctl->abort, status);
+          named_barrier_sync(1, 128);
+          bad = named_barrier_any(1, 128, stopped(&ctl->abort));
+          if (bad) break;
+#pragma unroll
+          for (int q = 0; q < NQ; ++q) l[q] *= ctl->fac[q].x;
+          if (i > it.t0) {
+            tc_fence_after_sync();
+            uint32_t o[C::COLS];
+            load_cols(lanes + 2 * C::COLS, o);
+#pragma unroll
+            for (int q = 0; q < NQ; ++q) {
+              const float f = ctl->fac[q].y;
+              o[q] = __float_as_uint(__uint_as_float(o[q]) * f);
+              o[NQ + q] = __float_as_uint(__uint_as_float(o[NQ + q]) * f);
+            }
+            if constexpr (C::COLS == 64) {
+              uint32_t lo[32], hi[32];
+#pragma unroll
+              for (int e = 0; e < 32; ++e) {
+                lo[e] = o[e];
+                hi[e] = o[32 + e];
+              }
+              tmem_st_32x32b(lanes + 2 * C::COLS, lo);
+              tmem_st_32x32b(lanes + 2 * C::COLS + 32, hi);
+            } else {
+              tmem_st_32x32b(lanes + 2 * C::COLS, o);
+            }
+            tmem_wait_st();
+          }
+        }
+        // weights, and P as hi and lo codes: 16 columns of this slot at a time
+        uint32_t w[2 * NQ / 4];
+#pragma unroll
+        for (int q = 0; q < NQ; q += 4) {
+          float y[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float pr = ex2_approx(x[q + e] - ctl->stat[q + e].m);
+            l[q + e] += pr;
+            y[e] = pr * fminf(vs * ctl->stat[q + e].g, 0x1p100f);      // (a bound only where pr is 0: no infinity)
+            if (vs != vs && x[q + e] > -INFINITY) y[e] = vs;           // (fminf drops a NaN)
+          }
+          const uint32_t hi = e4m3x4(y[0], y[1], y[2], y[3]);
+          const uint32_t f0 = e4m3x2_to_f16x2(hi & 0xFFFFu), f1 = e4m3x2_to_f16x2(hi >> 16);
+          const float2 g0 = __half22float2(*reinterpret_cast<const __half2*>(&f0)), g1 = __half22float2(*reinterpret_cast<const __half2*>(&f1));
+          w[q / 4] = hi;
+          w[NQ / 4 + q / 4] = e4m3x4((y[0] - g0.x) * 16.f, (y[1] - g0.y) * 16.f, (y[2] - g1.x) * 16.f, (y[3] - g1.y) * 16.f);
+        }
+        uint8_t* dst = sP + p * C::PBYTES + me * 16;
+#pragma unroll
+        for (int c = 0; c < C::COLS / 16; ++c)
+          *reinterpret_cast<uint4*>(dst + c * 16 * kKvTile) = make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
+        fence_proxy_async_shared();
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_full(p));
+      }
+      if (bad) break;
+      // ---- the item's (part of the) output --------------------------------------------------
+      if (!mbar_wait(pv_done, (t - 1) & 1, kWaitLimitNs)) stop(&ctl->abort, status);
+#pragma unroll
+      for (int q = 0; q < NQ; ++q) {
+        float v = l[q];
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        if (lane == 0) ctl->red[quad][q].x = v;
+      }
+      named_barrier_sync(1, 128);
+      bad = named_barrier_any(1, 128, stopped(&ctl->abort));
+      if (bad) break;
+      tc_fence_after_sync();
+      uint32_t o[C::COLS];
+      load_cols(lanes + 2 * C::COLS, o);
+      tc_fence_before_sync();
+      const bool complete = it.t0 == 0 && it.t1 == it.span.n;
+      const int64_t slot = 2 * blockIdx.x + (it.t0 == 0 ? 1 : 0);
+#pragma unroll
+      for (int q = 0; q < NQ; ++q) {
+        if (q >= it.rows) continue;
+        const float sum = (ctl->red[0][q].x + ctl->red[1][q].x) + (ctl->red[2][q].x + ctl->red[3][q].x);
+        const Stat st = ctl->stat[q];
+        // O / (g l); a row that saw nothing here is zero
+        const float v = sum == 0.f ? 0.f : fmaf(__uint_as_float(o[NQ + q]), 0.0625f, __uint_as_float(o[q])) / (st.g * sum);
+        const float lse2 = sum == 0.f ? -INFINITY : st.m + log2f(sum);
+        const int r = it.row0 + q, h = it.head * a.group + r % a.group;
+        if (complete) {
+          const int64_t at = static_cast<int64_t>(a.s.q0[it.i] + r / a.group) * a.q_heads + h;
+          if (me < D) a.out[at * D + me] = __bfloat16_as_ushort(__float2bfloat16_rn(v));
+          if (me == 0 && a.lse != nullptr) a.lse[at] = lse2 * 0.69314718055994531f;
+        } else {
+          if (me < D) a.part[(slot * NQ + q) * D + me] = v;
+          if (me == 0) a.part_lse[slot * NQ + q] = lse2;
+        }
+      }
+    }
+    if (me == 0) kv_write_split(a, share, walk.it);
+  }
+  // everything issued has completed: the last tile's commit has been waited for, unless the CTA gave up
+  tc_fence_before_sync();
+  __syncthreads();
+  if (stopped(&ctl->abort)) {
+    const uint64_t t0 = globaltimer_ns();
+    while (globaltimer_ns() - t0 < 100000ull) {
+    }
+    __syncthreads();
+  }
+  tc_fence_after_sync();
+  if (warp == 1) tmem_dealloc(tmem, C::TMEM);
+}
+
+// Rows of 16 of the items that several CTAs walked: out = sum_c 2^(lse_c - max) o_c / sum_c 2^(lse_c - max), in the CTAs'
+// order.  Sixteen threads per row.
+template <int D>
+__global__ void __launch_bounds__(256) kv_attn_combine(const __grid_constant__ KvAttnArgs a, int tile_rows) {
+  launch_dependents();
+  grid_dependency_wait();
+  const int c = blockIdx.x;
+  const int4 raw = __ldcg(reinterpret_cast<const int4*>(a.split + c));
+  const KvSplit sp{raw.x, raw.y, raw.z, raw.w};
+  if (sp.followers == 0) return;
+  const int q = blockIdx.y * 16 + threadIdx.x / 16, col = threadIdx.x % 16 * (D / 16);
+  const int row = sp.row_tile * tile_rows + q;
+  if (q >= tile_rows || row >= a.s.nq[sp.i] * a.group) return;
+  auto at = [&](int j) { return static_cast<int64_t>(j == 0 ? 2 * c + 1 : 2 * (c + j)) * tile_rows + q; };
+  float top = -INFINITY;
+  for (int j = 0; j <= sp.followers; ++j) top = fmaxf(top, __ldcg(a.part_lse + at(j)));
+  const float base = top == -INFINITY ? 0.f : top;
+  float sum = 0.f, o[D / 16];
+#pragma unroll
+  for (int e = 0; e < D / 16; ++e) o[e] = 0.f;
+#pragma unroll 4
+  for (int j = 0; j <= sp.followers; ++j) {
+    const float lse = __ldcg(a.part_lse + at(j));
+    const float w = exp2f(lse - base);
+    const float4* p = reinterpret_cast<const float4*>(a.part + at(j) * D + col);
+    sum += w;
+#pragma unroll
+    for (int e = 0; e < D / 64; ++e) {
+      const float4 v = __ldcg(p + e);
+      o[4 * e] = fmaf(w, v.x, o[4 * e]);
+      o[4 * e + 1] = fmaf(w, v.y, o[4 * e + 1]);
+      o[4 * e + 2] = fmaf(w, v.z, o[4 * e + 2]);
+      o[4 * e + 3] = fmaf(w, v.w, o[4 * e + 3]);
+    }
+  }
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  const int64_t dst = static_cast<int64_t>(a.s.q0[sp.i] + row / a.group) * a.q_heads + sp.head * a.group + row % a.group;
+  uint32_t w[D / 32];
+#pragma unroll
+  for (int e = 0; e < D / 32; ++e)
+    w[e] = static_cast<uint32_t>(__bfloat16_as_ushort(__float2bfloat16_rn(o[2 * e] * inv))) |
+           static_cast<uint32_t>(__bfloat16_as_ushort(__float2bfloat16_rn(o[2 * e + 1] * inv))) << 16;
+  if constexpr (D == 128) *reinterpret_cast<uint4*>(a.out + dst * D + col) = make_uint4(w[0], w[1], w[2], w[3]);
+  else *reinterpret_cast<uint2*>(a.out + dst * D + col) = make_uint2(w[0], w[1]);
+  if (col == 0 && a.lse != nullptr) a.lse[dst] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.69314718055994531f;
+}
+
+template <int D, int NQ>
+pace_status_t run_decode(const KvMaps& maps, const KvAttnArgs& a, unsigned grid, int* status, cudaStream_t stream) {
+  using C = DecodeCfg<D, NQ>;
+  constexpr size_t smem = 1024 + C::STAGES * 2 * C::TILE + C::QBYTES + 2 * C::PBYTES + sizeof(DecodeCtl<D, NQ>);
+  static_assert(smem <= 227 * 1024, "shared memory");
+  static DeviceOnce once;
+  int dev = 0;
+  PACE_CUDA(cudaGetDevice(&dev));
+  if (!once.done(dev)) {
+    PACE_CUDA(cudaFuncSetAttribute(kv_decode_kernel<D, NQ>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
+    once.mark(dev);
+  }
+  return launch_dependent(kv_decode_kernel<D, NQ>, grid, kThreads, smem, 1, stream, maps, a, status);
+}
+
+}  // namespace
+
+pace_status_t launch_kv_decode(const KvMaps& maps, const KvAttnArgs& a, int D, int rows, unsigned grid, int* status, cudaStream_t stream) {
+  if (D == 128)
+    return rows == 8 ? run_decode<128, 8>(maps, a, grid, status, stream) : rows == 16 ? run_decode<128, 16>(maps, a, grid, status, stream)
+                                                                                   : run_decode<128, 32>(maps, a, grid, status, stream);
+  return rows == 8 ? run_decode<64, 8>(maps, a, grid, status, stream) : rows == 16 ? run_decode<64, 16>(maps, a, grid, status, stream)
+                                                                                 : run_decode<64, 32>(maps, a, grid, status, stream);
+}
+
+pace_status_t launch_kv_combine(const KvAttnArgs& a, int D, int rows, unsigned grid, cudaStream_t stream) {
+  auto* kernel = D == 128 ? kv_attn_combine<128> : kv_attn_combine<64>;
+  return launch_dependent(kernel, dim3(grid, static_cast<unsigned>((rows + 15) / 16)), 256, 0, 1, stream, a, rows);
+}
+
+}  // namespace pace

@@ -93,6 +93,19 @@ pace_status_t sm_count(int* sms) {
   return PACE_OK;
 }
 
+void* tensor_map_encoder() {
+  static std::once_flag once;
+  static void* fn = nullptr;
+  std::call_once(once, [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) == cudaSuccess &&
+        q == cudaDriverEntryPointSuccess)
+      fn = p;
+  });
+  return fn;
+}
+
 // One CTA waits on an mbarrier that nothing ever arrives at: the bounded wait must give up
 // after limit_ns and record PACE_ERR_TIMEOUT, leaving the context usable.
 __global__ void selftest_wait_kernel(uint64_t limit_ns, int* status) {
