@@ -17,6 +17,8 @@
 namespace pace {
 
 constexpr int kKvTile = 128;      // slots of one tile
+constexpr float kNone = -1e30f;   // a row's maximum before its first slot (finite: x - kNone is never NaN)
+constexpr int kManyRows = 256;    // rows of a tile of the form for many
 constexpr int kPlanCtas = 152;    // CTAs of a launch at most: an SM each (the size queries need no device)
 
 // The launch's sequences, those without queries left out.
@@ -105,12 +107,14 @@ struct KvShare {
 // Walks a share (item) by item.
 template <int ROWS>
 struct KvWalk {
-  const KvAttnArgs& a;
   KvShare s;
   KvItem it;
-  bool have = false;
-  __device__ __forceinline__ KvWalk(const KvAttnArgs& args, const KvShare& share) : a(args), s(share) {}
-  __device__ __forceinline__ bool next() {
+  bool have;
+  __device__ __forceinline__ void begin(const KvShare& share) {
+    s = share;
+    have = false;
+  }
+  __device__ __forceinline__ bool next(const KvAttnArgs& a) {
     if (s.pos >= s.end) return false;
     while (true) {
       if (!have) {
@@ -230,8 +234,99 @@ struct KvMaps {
   CUtensorMap k, v;
 };
 
-// Launches of the two forms (rows of a tile at most 32, and 256); `grid` CTAs, then the combine kernel.
+// A role that gives up on a wait says so here; the others leave as their own waits run out.
+__device__ __forceinline__ bool stopped(const int* abort) { return *reinterpret_cast<const volatile int*>(abort) != 0; }
+__device__ __forceinline__ void stop(int* abort, int* status) {
+  *reinterpret_cast<volatile int*>(abort) = 1;
+  record_error(status, PACE_ERR_TIMEOUT, K_KV_ATTN);
+}
+
+// N columns of this warp's 32 lanes, ready to use.
+template <int N>
+__device__ __forceinline__ void load_cols(uint32_t addr, uint32_t (&v)[N]) {
+  if constexpr (N == 64) {
+    ptx::tmem_ld_32x32b_x64(addr, v);
+    ptx::tmem_wait_ld();
+    ptx::reg_fence64(v);
+  } else {
+    ptx::tmem_ld_32x32b(addr, v);
+    ptx::tmem_wait_ld();
+    ptx::reg_fence(v);
+  }
+}
+
+// Warp 0 of a CTA: fetches the slot tiles of its share, a K and a V tile per stage (boxes of a page, at most 128 rows, each by
+// TMA; the tile's 8 K and 8 V scales by 4-byte copies).  full[s] counts the bytes, their announcement and 32 lanes' copies;
+// empty[s] one arrival.
+// `also()` runs after each tile's copies have been issued.
+template <int D, int ST, int ROWS, typename F>
+__device__ __forceinline__ void kv_fetch(const KvMaps& maps, const KvAttnArgs& a, KvWalk<ROWS>& walk, uint8_t* stages, uint64_t* full,
+                                         uint64_t* empty, float (*scales)[16], int* abort, int* status, F&& also) {
+  using namespace ptx;
+  constexpr int TILE = kKvTile * D;
+  const int lane = threadIdx.x & 31;
+  const int shift = min(a.c.page_shift, 7), box_rows = 1 << shift, boxes = kKvTile >> shift;
+  const int tiles_per_load = 32 / boxes;     // a lane holds the page of one box
+  int t = 0;                                 // tiles so far
+  while (!stopped(abort) && walk.next(a)) {
+    const KvItem& it = walk.it;
+    const int32_t* table = a.table + static_cast<int64_t>(a.s.seq[it.i]) * a.table_stride;
+    const int last = it.p_last;
+    auto page_of = [&](int tile_i) {         // of box lane % boxes of tile tile_i + lane / boxes
+      const int i = tile_i + lane / boxes;
+      if (i >= it.t1) return -2;
+      const int slot = it.span.tile(i) * kKvTile + (lane % boxes) * box_rows;
+      if (slot > last) return -2;            // nothing there
+      const int page = table[slot >> a.c.page_shift];
+      return page >= 0 && page < a.c.n_pages ? page : -1;
+    };
+    int mine = page_of(it.t0), next = -2;
+    for (int i = it.t0; i < it.t1; ++i, ++t) {
+      const int k = (i - it.t0) % tiles_per_load;
+      if (k == 0) {
+        if (i > it.t0) mine = next;
+        next = page_of(i + tiles_per_load);
+      }
+      int page = __shfl_sync(0xffffffffu, mine, k * boxes + lane % boxes);
+      const bool there = page != -2;
+      if (page == -1) {
+        if (lane < boxes) record_error(status, PACE_ERR_INVALID_ARG, K_KV_ATTN);
+        page = 0;      // (the sequence's results mean nothing then; the copy stays inside the cache)
+      }
+      const int s = t % ST, round = t / ST;
+      if (round > 0) {
+        const bool ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&empty[s]), (round - 1) & 1, kWaitLimitNs));
+        if (!ok) {
+          if (lane == 0) stop(abort, status);
+          break;
+        }
+      }
+      const int slot0 = it.span.tile(i) * kKvTile;
+      uint8_t* dst = stages + s * 2 * TILE;
+      const int n_there = __popc(__ballot_sync(0xffffffffu, there && lane < boxes));
+      if (lane == 0) mbar_arrive_expect_tx(smem_u32(&full[s]), 2 * n_there * box_rows * D);
+      // scale j (K: 0-7, V: 8-15) of the tile: block j % 8, in box (j % 8) * 16 / box_rows
+      const int blk = lane & 7;
+      const int bpage = __shfl_sync(0xffffffffu, page, blk * kKvBlock >> shift);
+      const int row = (slot0 + blk * kKvBlock) & ((1 << a.c.page_shift) - 1);
+      if (lane < 16 && slot0 + blk * kKvBlock <= last)
+        cp_async4(smem_u32(&scales[s][lane]),
+                  (lane < 8 ? a.c.ks : a.c.vs) + bpage * a.c.scale_stride + (static_cast<int64_t>(it.head) << (a.c.page_shift - 4)) + row / kKvBlock);
+      cp_async_arrive(smem_u32(&full[s]));
+      __syncwarp();
+      if (lane < boxes && there) {
+        const int y = (it.head << a.c.page_shift) + ((slot0 + lane * box_rows) & ((1 << a.c.page_shift) - 1));
+        tma_load_3d(smem_u32(dst + lane * box_rows * D), &maps.k, 0, y, page, smem_u32(&full[s]));
+        tma_load_3d(smem_u32(dst + TILE + lane * box_rows * D), &maps.v, 0, y, page, smem_u32(&full[s]));
+      }
+      also();
+    }
+  }
+}
+
+// Launches of the two forms (rows of a tile: 8, 16 or 32, and kManyRows); `grid` CTAs, then the combine kernel.
 pace_status_t launch_kv_decode(const KvMaps& maps, const KvAttnArgs& a, int D, int rows, unsigned grid, int* status, cudaStream_t stream);
+pace_status_t launch_kv_prefill(const KvMaps& maps, const KvAttnArgs& a, int D, unsigned grid, int* status, cudaStream_t stream);
 pace_status_t launch_kv_combine(const KvAttnArgs& a, int D, int rows, unsigned grid, cudaStream_t stream);
 
 }  // namespace pace

@@ -32,7 +32,6 @@ constexpr int kWarps = 6, kThreads = 32 * kWarps;
 constexpr float kFar = 60.f;         // how far a score may pass m_q
 constexpr float kOver = 4.f;         // ... and x + log2(vs) may pass w_q
 constexpr float kUnit = 4.f;         // log2 of P at w_q
-constexpr float kNone = -1e30f;      // m_q and w_q before the first slot (finite: x - m_q is never NaN)
 
 template <int D, int NQ>
 struct DecodeCfg {
@@ -66,25 +65,6 @@ struct alignas(16) DecodeCtl {
   uint32_t tmem;
   int abort;
 };
-
-__device__ __forceinline__ bool stopped(const int* abort) { return *reinterpret_cast<const volatile int*>(abort) != 0; }
-__device__ __forceinline__ void stop(int* abort, int* status) {
-  *reinterpret_cast<volatile int*>(abort) = 1;
-  record_error(status, PACE_ERR_TIMEOUT, K_KV_ATTN);
-}
-
-template <int N>
-__device__ __forceinline__ void load_cols(uint32_t addr, uint32_t (&v)[N]) {
-  if constexpr (N == 64) {
-    tmem_ld_32x32b_x64(addr, v);
-    tmem_wait_ld();
-    reg_fence64(v);
-  } else {
-    tmem_ld_32x32b(addr, v);
-    tmem_wait_ld();
-    reg_fence(v);
-  }
-}
 
 template <int D, int NQ>
 __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_constant__ KvMaps maps, const __grid_constant__ KvAttnArgs a,
@@ -134,66 +114,11 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
   __syncthreads();
   tc_fence_after_sync();
   const uint32_t tmem = ctl->tmem;
-  KvWalk<NQ> walk(a, share);
+  KvWalk<NQ> walk;
+  walk.begin(share);
 
   if (warp == 0) {
-    // ---- fetch -------------------------------------------------------------------------------
-    const int shift = min(a.c.page_shift, 7), box_rows = 1 << shift, boxes = kKvTile >> shift;
-    const int tiles_per_load = 32 / boxes;     // a lane holds the page of one box
-    int t = 0;                                 // tiles so far
-    while (!stopped(&ctl->abort) && walk.next()) {
-      const KvItem& it = walk.it;
-      const int32_t* table = a.table + static_cast<int64_t>(a.s.seq[it.i]) * a.table_stride;
-      const int last = it.p_last;
-      auto page_of = [&](int tile_i) {         // of box lane % boxes of tile tile_i + lane / boxes
-        const int i = tile_i + lane / boxes;
-        if (i >= it.t1) return -2;
-        const int slot = it.span.tile(i) * kKvTile + (lane % boxes) * box_rows;
-        if (slot > last) return -2;            // nothing there
-        const int page = table[slot >> a.c.page_shift];
-        return page >= 0 && page < a.c.n_pages ? page : -1;
-      };
-      int mine = page_of(it.t0), next = -2;
-      for (int i = it.t0; i < it.t1; ++i, ++t) {
-        const int k = (i - it.t0) % tiles_per_load;
-        if (k == 0) {
-          if (i > it.t0) mine = next;
-          next = page_of(i + tiles_per_load);
-        }
-        int page = __shfl_sync(0xffffffffu, mine, k * boxes + lane % boxes);
-        const bool there = page != -2;
-        if (page == -1) {
-          if (lane < boxes) record_error(status, PACE_ERR_INVALID_ARG, K_KV_ATTN);
-          page = 0;      // (the sequence's results mean nothing then; the copy stays inside the cache)
-        }
-        const int s = t % ST, round = t / ST;
-        if (round > 0) {
-          const bool ok = __all_sync(0xffffffffu, mbar_wait(empty(s), (round - 1) & 1, kWaitLimitNs));
-          if (!ok) {
-            if (lane == 0) stop(&ctl->abort, status);
-            break;
-          }
-        }
-        const int slot0 = it.span.tile(i) * kKvTile;
-        uint8_t* dst = sKV + s * 2 * C::TILE;
-        const int n_there = __popc(__ballot_sync(0xffffffffu, there && lane < boxes));
-        if (lane == 0) mbar_arrive_expect_tx(full(s), 2 * n_there * box_rows * D);
-        // scale j (K: 0-7, V: 8-15) of the tile: block j % 8, in box (j % 8) * 16 / box_rows
-        const int blk = lane & 7;
-        const int bpage = __shfl_sync(0xffffffffu, page, blk * kKvBlock >> shift);
-        const int row = (slot0 + blk * kKvBlock) & ((1 << a.c.page_shift) - 1);
-        if (lane < 16 && slot0 + blk * kKvBlock <= last)
-          cp_async4(smem_u32(&ctl->scales[s][lane]),
-                    (lane < 8 ? a.c.ks : a.c.vs) + bpage * a.c.scale_stride + (static_cast<int64_t>(it.head) << (a.c.page_shift - 4)) + row / kKvBlock);
-        cp_async_arrive(full(s));
-        __syncwarp();
-        if (lane < boxes && there) {
-          const int y = (it.head << a.c.page_shift) + ((slot0 + lane * box_rows) & ((1 << a.c.page_shift) - 1));
-          tma_load_3d(smem_u32(dst + lane * box_rows * D), &maps.k, 0, y, page, full(s));
-          tma_load_3d(smem_u32(dst + C::TILE + lane * box_rows * D), &maps.v, 0, y, page, full(s));
-        }
-      }
-    }
+    kv_fetch<D, ST>(maps, a, walk, sKV, ctl->full, ctl->empty, ctl->scales, &ctl->abort, status, [] {});
   } else if (warp == 1) {
     // ---- products ----------------------------------------------------------------------------
     if (lane == 0) {
@@ -218,7 +143,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
         mma_commit(pv_done);
         return true;
       };
-      while (ok && walk.next()) {
+      while (ok && walk.next(a)) {
         ok = mbar_wait(q_full, items & 1, kWaitLimitNs);
         ++items;
         const int n = walk.it.t1 - walk.it.t0;
@@ -244,7 +169,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
     const uint32_t lanes = tmem + (static_cast<uint32_t>(quad * 32) << 16);
     int t = 0;
     bool bad = false;
-    while (!bad && walk.next()) {
+    while (!bad && walk.next(a)) {
       const KvItem& it = walk.it;
       named_barrier_sync(1, 128);      // the last item's shared statistics have been read
       // q: rows of this item as hi and lo codes (rows past it are zero), the power of two of each

@@ -1,0 +1,510 @@
+// Serve: attention over the paged cache for many query rows per KV head (prefill, whole or in chunks).
+//
+//   S [128 rows x 128 slots] = q K^T        O [128 rows x D] += P V
+// S is formed in 8 bits: K as the codes it is stored as, bf16 q as two e4m3 terms, which is exact (8 significant bits are two
+// times 4; each row is first brought under 256 by a power of two).  Two e4m3 products cost what one of 16 bits would, at half the
+// shared memory and with no work on K.  P V is formed in f16, which holds every e4m3 number, and a weight to 11 bits.
+//
+// A TMEM lane of S is a query row and one thread's.  With x the score in base 2 and vs the V scale of a slot's block, the row's
+// weights are P = 2^(x + log2(vs) - w) and l = sum P / vs; both scales are constants of 16 columns, so a weight costs
+// one multiply-add, one exponential, one addition and half a conversion.  w is a whole number, the maximum of the row's first
+// 64 slots rounded up, and then stays: f16 has room for weights up to 2^15 above it, and below it 14 binary orders keep all their bits
+// and what is lost is under 2^-24.  Only when the weights of 64 columns sum up to more does w move, and O, l and the tile's weights so
+// far with it.  There is no maximum in the common path.  (Weights of blocks whose V scale is below 2^-110 of the largest are
+// lost to l.)
+//
+// What bounds it is the tensor pipe: 1092 clocks per 128 x 128 tile at D = 128, against 512 clocks of exponentials.  Two row
+// tiles A and B share every K and V tile and take turns: while one's weights are worked out, the other's products run.  P overwrites
+// its S in TMEM.  Roles of a CTA (one per SM): warp 0 fetches, warp 1 issues the MMAs, warps 2-3 turn V into f16 (they also
+// see to NaN that must not reach rows that do not look at it), warps 4-7 and 8-11 own the rows of A and B.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include <algorithm>
+
+#include "kv_attn.cuh"
+
+namespace pace {
+namespace {
+
+using namespace ptx;
+
+constexpr int kThreads = 384;
+constexpr float kMost = 32768.f;   // sum of 64 weights at which w moves
+constexpr uint32_t kTmem = 512;    // S of A and B, then O of A and B, 128 columns each
+
+template <int D>
+struct PrefillCfg {
+  static constexpr int TILE = kKvTile * D;
+  static constexpr int STAGES = D == 128 ? 3 : 6;
+  static constexpr int QTILE = 128 * D;                 // hi or lo codes of a row tile
+  static constexpr int VCHUNK = kKvTile * 128;          // f16 V: 64 columns of every slot, 128 bytes each
+  static constexpr int VTILE = VCHUNK * D / 64;
+  static constexpr uint32_t SWIZZLE = D == 128 ? 2 : 4;
+  static constexpr uint32_t GROUP = 8 * D;
+  static constexpr uint32_t IDESC_S = idesc_e4m3_f32(128, 128, false, false);
+  static constexpr uint32_t IDESC_O = idesc_f16_mn_f32(128, D);
+};
+
+template <int D>
+struct alignas(16) PrefillCtl {
+  static constexpr int ST = PrefillCfg<D>::STAGES;
+  uint64_t full[ST], empty[ST], ready[2], vfree[2], s_full[2], p_full[2], q_full[2], o_full[2];
+  float scales[ST][16];
+  float4 block[2][8];           // per block of 16 slots: K scale, log2(V scale), 1 / V scale
+  uint32_t nan[2][4];           // slots of which some row sees a NaN value
+  int64_t scan[kThreads / 32];
+  KvShare share;
+  uint32_t tmem;
+  int abort;
+};
+
+// A tile that rows at slots p_first .. p_last all see whole.
+__device__ __forceinline__ bool kv_whole(int slot0, int p_first, int p_last, int window, int sinks) {
+  return slot0 + kKvTile - 1 <= p_first && (window <= 0 || slot0 > p_last - window || slot0 + kKvTile <= sinks);
+}
+
+__device__ __forceinline__ uint32_t f16x2(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_constant__ KvMaps maps, const __grid_constant__ KvAttnArgs a,
+                                                                 int* status) {
+  using C = PrefillCfg<D>;
+  constexpr int ST = C::STAGES;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* sKV = smem;                             // stages of a K tile and a V tile, as codes
+  uint8_t* sV = sKV + ST * 2 * C::TILE;            // two V tiles in f16
+  uint8_t* sQ = sV + 2 * C::VTILE;                 // A hi, A lo, B hi, B lo
+  auto* ctl = reinterpret_cast<PrefillCtl<D>*>(sQ + 4 * C::QTILE);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  auto full = [&](int s) { return smem_u32(&ctl->full[s]); };
+  auto empty = [&](int s) { return smem_u32(&ctl->empty[s]); };
+  auto ready = [&](int b) { return smem_u32(&ctl->ready[b]); };
+  auto vfree = [&](int b) { return smem_u32(&ctl->vfree[b]); };
+  auto s_full = [&](int i) { return smem_u32(&ctl->s_full[i]); };
+  auto p_full = [&](int i) { return smem_u32(&ctl->p_full[i]); };
+  auto q_full = [&](int i) { return smem_u32(&ctl->q_full[i]); };
+  auto o_full = [&](int i) { return smem_u32(&ctl->o_full[i]); };
+
+  begin_call();
+  const KvShare share = kv_share<kManyRows, D>(a, ctl->scan, &ctl->share, status);
+  if (static_cast<int>(blockIdx.x) >= share.ctas) {
+    if (threadIdx.x == 0) a.split[blockIdx.x] = KvSplit{0, 0, 0, 0};
+    return;
+  }
+  if (warp == 0 && lane == 0) {
+    prefetch_tensormap(&maps.k);
+    prefetch_tensormap(&maps.v);
+    for (int s = 0; s < ST; ++s) {
+      mbar_init(full(s), 33);
+      mbar_init(empty(s), 3);       // S has been formed, two warps have read V
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(ready(i), 2);
+      mbar_init(vfree(i), 1);
+      mbar_init(s_full(i), 1);
+      mbar_init(p_full(i), 4);
+      mbar_init(q_full(i), 4);
+      mbar_init(o_full(i), 1);
+    }
+    fence_mbar_init();
+    ctl->abort = 0;
+  }
+  if (warp == 1) {
+    tmem_alloc(smem_u32(&ctl->tmem), kTmem);
+    tmem_relinquish();
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem = ctl->tmem;
+  KvWalk<kManyRows> walk;
+  walk.begin(share);
+  const KvItem& it = walk.it;
+
+  if (warp == 0) {
+    kv_fetch<D, ST>(maps, a, walk, sKV, ctl->full, ctl->empty, ctl->scales, &ctl->abort, status, [] {});
+  } else if (warp == 1) {
+    // ---- products: of A and B in turn, so that those of one run while the weights of the other are worked out --------------
+    const uint32_t issue = elect_one();
+    const uint64_t dq = smem_desc(smem_u32(sQ), 16, C::GROUP, C::SWIZZLE);
+    const uint64_t dk = smem_desc(smem_u32(sKV), 16, C::GROUP, C::SWIZZLE);
+    const uint64_t dv = smem_desc(smem_u32(sV), C::VCHUNK, 1024, 2);
+    int t = 0, rounds[2] = {0, 0}, items[2] = {0, 0};      // slot tiles; weights taken and items, of a row tile
+    bool ok = true;
+    auto wait = [&](uint32_t bar, int round) {
+      ok = __all_sync(0xffffffffu, mbar_wait(bar, round & 1, kWaitLimitNs));
+      return ok;
+    };
+    while (ok && walk.next(a)) {
+      const int n = it.t1 - it.t0;
+      const bool two = it.rows > 128;
+      for (int j = 0; ok && j <= n; ++j) {      // P V of slot tile j - 1, then S of slot tile j
+        const int u = t + j - 1, s = (t + j) % ST;
+        if (j < n && !wait(full(s), (t + j) / ST)) break;
+        if (j > 0 && !wait(ready(u & 1), u >> 1)) break;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          if (i == 1 && !two) break;
+          if (!(j > 0 ? wait(p_full(i), rounds[i]++) : wait(q_full(i), items[i]++))) break;
+          tc_fence_after_sync();
+          if (j > 0) {
+            const uint64_t v = dv + static_cast<uint64_t>((u & 1) * (C::VTILE >> 4));
+#pragma unroll
+            for (int k = 0; k < kKvTile / 16; ++k)
+              mma_f16_ts(tmem + 256 + i * 128, tmem + i * 128 + k * 8, v + static_cast<uint64_t>(k * (2048 >> 4)), C::IDESC_O, j > 1 || k > 0, issue);
+            if (issue && j == n) mma_commit(o_full(i));
+          }
+          if (j < n) {
+            const uint64_t q = dq + static_cast<uint64_t>(i * 2 * (C::QTILE >> 4)), k0 = dk + static_cast<uint64_t>(s * 2 * (C::TILE >> 4));
+#pragma unroll
+            for (int part = 0; part < 2; ++part)
+#pragma unroll
+              for (int k = 0; k < D / 32; ++k)
+                mma_f8_ss(tmem + i * 128, q + static_cast<uint64_t>(part * (C::QTILE >> 4) + 2 * k), k0 + static_cast<uint64_t>(2 * k), C::IDESC_S,
+                          part > 0 || k > 0, issue);
+            if (issue) mma_commit(s_full(i));
+          }
+        }
+        if (ok && issue) {
+          if (j > 0) mma_commit(vfree(u & 1));
+          if (j < n) mma_commit(empty(s));
+        }
+      }
+      t += n;
+    }
+    if (!ok && lane == 0) stop(&ctl->abort, status);
+    __syncwarp();
+  } else if (warp < 4) {
+    // ---- V of a slot tile as f16, and the tile's constants ---------------------------------------
+    int t = 0;
+    bool ok = true;
+    while (ok && walk.next(a)) {
+      for (int j = it.t0; ok && j < it.t1; ++j, ++t) {
+        const int s = t % ST, b = t & 1, slot0 = it.span.tile(j) * kKvTile;
+        ok = mbar_wait(full(s), (t / ST) & 1, kWaitLimitNs) && (t < 2 || mbar_wait(vfree(b), ((t >> 1) - 1) & 1, kWaitLimitNs));
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        // 0 * NaN is NaN: no slot of V that some row does not see may hold one.  Slots that nobody sees become zero; where rows
+        // differ, so does a slot with a NaN, and rows that see it take a NaN weight for it.
+        const bool whole = kv_whole(slot0, it.p_first, it.p_last, a.window, a.sinks);
+        auto usable = [](float x) { return x > 0.f && x < INFINITY; };
+        if (warp == 2 && lane < 8) {      // (where the slots are not there, or rows differ, no scale may be NaN either)
+          float ks = ctl->scales[s][lane], vs = ctl->scales[s][8 + lane];
+          if (!whole && (slot0 + lane * kKvBlock > it.p_last || !usable(ks) || !usable(vs))) ks = vs = 1.f;
+          ctl->block[b][lane] = make_float4(ks, log2f(vs), 1.f / vs, 0.f);
+        }
+#pragma unroll 1
+        for (int part = warp - 2; part < 4; part += 2) {
+          const int row = part * 32 + lane, slot = slot0 + row;      // a slot of the tile
+          const bool any = slot <= it.p_last && (a.window <= 0 || slot > it.p_first - a.window || slot < a.sinks);
+          const uint8_t* src = sKV + (2 * s + 1) * C::TILE + row * D;
+          uint4 u[D / 16];
+#pragma unroll
+          for (int e = 0; e < D / 16; ++e) u[e] = *reinterpret_cast<const uint4*>(src + (e ^ (D == 128 ? row & 7 : (row >> 1) & 3)) * 16);
+          if (!whole) {
+            bool nan = false;
+            if (any) {
+#pragma unroll
+              for (int e = 0; e < D / 16; ++e)
+                nan = nan || ((((u[e].x & 0x7F7F7F7Fu) + 0x01010101u) | ((u[e].y & 0x7F7F7F7Fu) + 0x01010101u) |
+                               ((u[e].z & 0x7F7F7F7Fu) + 0x01010101u) | ((u[e].w & 0x7F7F7F7Fu) + 0x01010101u)) & 0x80808080u) != 0;
+              nan = nan || !usable(ctl->scales[s][row >> 4]) || !usable(ctl->scales[s][8 + (row >> 4)]);
+            }
+            if (!any || nan) {
+#pragma unroll
+              for (int e = 0; e < D / 16; ++e) u[e] = make_uint4(0, 0, 0, 0);
+            }
+            const uint32_t bits = __ballot_sync(0xffffffffu, nan);
+            if (lane == 0) ctl->nan[b][part] = bits;
+          }
+          uint8_t* dst = sV + b * C::VTILE + row * 128;
+#pragma unroll
+          for (int e = 0; e < D / 16; ++e) {
+            uint8_t* d = dst + (e >> 2) * C::VCHUNK;
+            const int c = (e & 3) * 2;
+            *reinterpret_cast<uint4*>(d + ((c ^ (row & 7)) * 16)) =
+                make_uint4(e4m3x2_to_f16x2(u[e].x), e4m3x2_to_f16x2(u[e].x >> 16), e4m3x2_to_f16x2(u[e].y), e4m3x2_to_f16x2(u[e].y >> 16));
+            *reinterpret_cast<uint4*>(d + (((c + 1) ^ (row & 7)) * 16)) =
+                make_uint4(e4m3x2_to_f16x2(u[e].z), e4m3x2_to_f16x2(u[e].z >> 16), e4m3x2_to_f16x2(u[e].w), e4m3x2_to_f16x2(u[e].w >> 16));
+          }
+        }
+        fence_proxy_async_shared();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(ready(b));
+          mbar_arrive(empty(s));
+        }
+      }
+    }
+    if (!ok && lane == 0) stop(&ctl->abort, status);
+  } else {
+    // ---- weights -----------------------------------------------------------------------------
+    const int i = (warp - 4) >> 2, quad = warp & 3, me = quad * 32 + lane;
+    const uint32_t lanes = static_cast<uint32_t>(quad * 32) << 16;
+    const uint32_t sS = tmem + lanes + i * 128, sO = tmem + lanes + 256 + i * 128;
+    int t = 0, s_rounds = 0, o_rounds = 0;
+    bool ok = true;
+    while (ok && walk.next(a)) {
+      if (i == 1 && it.rows <= 128) {
+        t += it.t1 - it.t0;
+        continue;
+      }
+      const int row = i * 128 + me, r = it.row0 + row;          // of the item, of the sequence
+      const bool real = row < it.rows;
+      const int token = r / a.group, h = it.head * a.group + r % a.group;
+      const int p = real ? it.p0 + token : it.p_last;
+      // slots of this tile's first and last row
+      const int p_lo = it.p0 + (it.row0 + i * 128) / a.group, p_hi = it.p0 + (it.row0 + min(i * 128 + 127, it.rows - 1)) / a.group;
+      float c = 0.f;            // scale2 * the row's power of two
+      {
+        // q as hi and lo codes.  D / 8 lanes read a row, 16 bytes each; it takes the places of its codes (128 or 64 bytes in the
+        // hi tile, the rest in the lo tile) until its owner turns it into them
+        constexpr int LANES = D / 8, STEP = 32 / LANES;
+        const int sub = lane / LANES, part = lane % LANES;
+        uint8_t* tile = sQ + i * 2 * C::QTILE;
+        auto place = [&](int row, int chunk) {      // of a row's 16-byte chunk: the swizzle of the operand tiles
+          constexpr int PER = D / 16;
+          return tile + (chunk >= PER ? C::QTILE : 0) + row * D + ((chunk % PER) ^ (D == 128 ? row & 7 : (row >> 1) & 3)) * 16;
+        };
+        {
+          uint4 u[32 / STEP];
+#pragma unroll
+          for (int k = 0; k < 32 / STEP; ++k) {
+            const int rk = it.row0 + i * 128 + quad * 32 + k * STEP + sub;
+            u[k] = make_uint4(0, 0, 0, 0);
+            if (rk < it.row0 + it.rows)
+              u[k] = *reinterpret_cast<const uint4*>(a.Q + (a.s.q0[it.i] + rk / a.group) * a.q_stride +
+                                                     static_cast<int64_t>(it.head * a.group + rk % a.group) * D + part * 8);
+          }
+#pragma unroll
+          for (int k = 0; k < 32 / STEP; ++k) *reinterpret_cast<uint4*>(place(quad * 32 + k * STEP + sub, part)) = u[k];
+        }
+        __syncwarp();
+        uint4 u[D / 8];
+        uint32_t most = 0;      // largest magnitude, as the bits of two bf16 without their signs
+#pragma unroll
+        for (int e = 0; e < D / 8; ++e) {
+          u[e] = *reinterpret_cast<const uint4*>(place(me, e));
+          most = __vmaxu2(__vmaxu2(most, __vmaxu2(u[e].x & 0x7FFF7FFFu, u[e].y & 0x7FFF7FFFu)), __vmaxu2(u[e].z & 0x7FFF7FFFu, u[e].w & 0x7FFF7FFFu));
+        }
+        const uint32_t top = max(most & 0xFFFFu, most >> 16);
+        const bool fin = top < 0x7F80u;
+        const int e2 = fin ? max(static_cast<int>(top >> 7) - 127 - 7, -110) : 0;      // top 2^-e2 in [128, 256)
+        const float inv = __uint_as_float(static_cast<uint32_t>(127 - e2) << 23);
+        c = a.scale2 * __uint_as_float(static_cast<uint32_t>(127 + e2) << 23);
+#pragma unroll
+        for (int e = 0; e < D / 16; ++e) {      // 16 elements at a time
+          const uint32_t w[8] = {u[2 * e].x, u[2 * e].y, u[2 * e].z, u[2 * e].w, u[2 * e + 1].x, u[2 * e + 1].y, u[2 * e + 1].z, u[2 * e + 1].w};
+          uint32_t hi[4], lo[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float y[4] = {__uint_as_float(w[2 * k] << 16) * inv, __uint_as_float(w[2 * k] & 0xFFFF0000u) * inv,
+                                __uint_as_float(w[2 * k + 1] << 16) * inv, __uint_as_float(w[2 * k + 1] & 0xFFFF0000u) * inv};
+            hi[k] = fin ? e4m3x4(y[0], y[1], y[2], y[3]) : 0x7F7F7F7Fu;      // a row that is not finite: NaN throughout
+            const uint32_t f0 = e4m3x2_to_f16x2(hi[k] & 0xFFFFu), f1 = e4m3x2_to_f16x2(hi[k] >> 16);
+            const float2 g0 = __half22float2(*reinterpret_cast<const __half2*>(&f0)), g1 = __half22float2(*reinterpret_cast<const __half2*>(&f1));
+            lo[k] = fin ? e4m3x4(y[0] - g0.x, y[1] - g0.y, y[2] - g1.x, y[3] - g1.y) : 0u;
+          }
+          *reinterpret_cast<uint4*>(place(me, e)) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+          *reinterpret_cast<uint4*>(place(me, e + D / 16)) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+        }
+        fence_proxy_async_shared();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(q_full(i));
+      }
+      float w = kNone, l = 0.f;
+      for (int j = it.t0; j < it.t1; ++j, ++t, ++s_rounds) {
+        const int b = t & 1, slot0 = it.span.tile(j) * kKvTile;
+        // (S first: a row tile that left items out may be rounds ahead of the others until its products run)
+        ok = mbar_wait(s_full(i), s_rounds & 1, kWaitLimitNs) && mbar_wait(ready(b), (t >> 1) & 1, kWaitLimitNs);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        tc_fence_after_sync();
+        const bool whole = kv_whole(slot0, p_lo, p_hi, a.window, a.sinks);
+        if (!whole) {      // what the row does not see becomes -inf: all but columns up to `to` that are past `from` or before `few`
+          const int to = p - slot0, from = a.window > 0 ? p - a.window - slot0 : -1, few = a.window > 0 ? a.sinks - slot0 : kKvTile;
+#pragma unroll 1
+          for (int q = 0; q < 4; ++q) {
+            uint32_t x[32];
+            load_cols(sS + 32 * q, x);
+            const uint32_t nan = ctl->nan[b][q];
+#pragma unroll
+            for (int e = 0; e < 32; ++e) {
+              const int col = 32 * q + e;
+              if (nan >> e & 1) x[e] = 0x7FC00000u;
+              if (col > to || (col <= from && col >= few)) x[e] = 0xFF800000u;
+            }
+            tmem_st_32x32b(sS + 32 * q, x);
+          }
+          tmem_wait_st();
+        }
+#pragma unroll 1
+        for (int q = 0; q < 2; ++q) {      // 64 columns
+          const float4* block = &ctl->block[b][4 * q];
+          uint32_t words[32];
+          while (true) {
+            uint32_t x[64];
+            load_cols(sS + 64 * q, x);
+            float sum = 0.f, dl = 0.f;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {      // a block's columns
+              const float4 k = block[g];
+              const float mul = fmaxf(k.x * c, 1e-37f), add = k.y - w;      // (not 0: -inf stays what it is)
+              const float2 mul2 = make_float2(mul, mul), add2 = make_float2(add, add);
+              float2 s0 = make_float2(0.f, 0.f), s1 = s0;
+#pragma unroll
+              for (int e = 0; e < 16; e += 4) {
+                const uint32_t* v = x + 16 * g + e;
+                float2 y0 = ffma2(make_float2(__uint_as_float(v[0]), __uint_as_float(v[1])), mul2, add2);
+                float2 y1 = ffma2(make_float2(__uint_as_float(v[2]), __uint_as_float(v[3])), mul2, add2);
+                y0 = make_float2(ex2_approx(y0.x), ex2_approx(y0.y));
+                y1 = make_float2(ex2_approx(y1.x), ex2_approx(y1.y));
+                s0 = fadd2(s0, y0);
+                s1 = fadd2(s1, y1);
+                words[8 * g + e / 2] = f16x2(y0.x, y0.y);
+                words[8 * g + e / 2 + 1] = f16x2(y1.x, y1.y);
+              }
+              s0 = fadd2(s0, s1);
+              const float part = s0.x + s0.y;
+              sum += part;
+              dl = fmaf(part, k.z, dl);
+            }
+            if (!__any_sync(0xffffffffu, sum >= kMost)) {
+              l += dl;
+              break;
+            }
+            // w moves to the maximum, in the rows that need it; the tile's weights so far, O (whose products so far have
+            // completed: S came after them) and l follow, and these columns start again
+            float top = kNone;
+#pragma unroll 1
+            for (int g = 0; g < 4; ++g) {
+              uint32_t y[16];
+              load_cols(sS + 64 * q + 16 * g, y);
+#pragma unroll
+              for (int e = 0; e < 16; ++e) top = fmaxf(top, fmaf(__uint_as_float(y[e]), fmaxf(block[g].x * c, 1e-37f), block[g].y));
+            }
+            const float now = sum >= kMost ? ceilf(top) : w, f = ex2_approx(w - now);
+            w = now;
+            l *= f;
+            tmem_wait_st();
+            if (q == 1) {
+              load_cols(sS, words);
+#pragma unroll
+              for (int k = 0; k < 32; ++k) {
+                const float2 z = __half22float2(*reinterpret_cast<const __half2*>(&words[k]));      // (f itself may be below f16)
+                words[k] = f16x2(z.x * f, z.y * f);
+              }
+              tmem_st_32x32b(sS, words);
+            }
+            if (j > it.t0) {
+#pragma unroll 1
+              for (int e = 0; e < D / 32; ++e) {
+                load_cols(sO + 32 * e, words);
+#pragma unroll
+                for (int k = 0; k < 32; ++k) words[k] = __float_as_uint(__uint_as_float(words[k]) * f);
+                tmem_st_32x32b(sO + 32 * e, words);
+              }
+            }
+            tmem_wait_st();
+          }
+          tmem_st_32x32b(sS + 32 * q, words);
+        }
+        tmem_wait_st();
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_full(i));
+      }
+      if (!ok) break;
+      // ---- the item's (part of the) output -----------------------------------------------------
+      ok = __all_sync(0xffffffffu, mbar_wait(o_full(i), o_rounds & 1, kWaitLimitNs));
+      ++o_rounds;
+      if (!ok) break;
+      tc_fence_after_sync();
+      const float inv = l == 0.f ? 0.f : 1.f / l, lse2 = l == 0.f ? -INFINITY : w + log2f(l);
+      const bool complete = it.t0 == 0 && it.t1 == it.span.n;
+      const int64_t at = static_cast<int64_t>(a.s.q0[it.i] + token) * a.q_heads + h;
+      const int64_t slot = (2 * static_cast<int64_t>(blockIdx.x) + (it.t0 == 0 ? 1 : 0)) * kManyRows + row;
+      // complete rows go out by way of the q tile, which is done with (this warp's rows only), so that lanes write side by side
+      uint8_t* stage = sQ + i * 2 * C::QTILE + quad * 32 * 2 * D;
+#pragma unroll
+      for (int q = 0; q < D / 32; ++q) {
+        uint32_t o[32];
+        load_cols(sO + 32 * q, o);
+        // (a row that saw nothing here is zero, whatever its accumulator holds)
+        auto v = [&](int e) { return l == 0.f ? 0.f : __uint_as_float(o[e]) * inv; };
+        if (complete) {
+#pragma unroll
+          for (int e = 0; e < 32; e += 8) {
+            uint32_t x[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              x[k] = static_cast<uint32_t>(__bfloat16_as_ushort(__float2bfloat16_rn(v(e + 2 * k)))) |
+                     static_cast<uint32_t>(__bfloat16_as_ushort(__float2bfloat16_rn(v(e + 2 * k + 1)))) << 16;
+            *reinterpret_cast<uint4*>(stage + lane * 2 * D + ((4 * q + e / 8) ^ (lane & 7)) * 16) = make_uint4(x[0], x[1], x[2], x[3]);
+          }
+        } else if (real) {
+#pragma unroll
+          for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(a.part + slot * D + 32 * q + e) = make_float4(v(e), v(e + 1), v(e + 2), v(e + 3));
+        }
+      }
+      if (complete) {
+        constexpr int LANES = D / 8, STEP = 32 / LANES;
+        __syncwarp();
+#pragma unroll 8
+        for (int k = 0; k < 32; k += STEP) {
+          const int rw = k + lane / LANES, part = lane % LANES, rk = it.row0 + i * 128 + quad * 32 + rw;
+          if (rk < it.row0 + it.rows)
+            *reinterpret_cast<uint4*>(a.out + (static_cast<int64_t>(a.s.q0[it.i] + rk / a.group) * a.q_heads + it.head * a.group + rk % a.group) * D +
+                                      part * 8) = *reinterpret_cast<const uint4*>(stage + rw * 2 * D + (part ^ (rw & 7)) * 16);
+        }
+        __syncwarp();
+      }
+      tc_fence_before_sync();
+      if (real) {
+        if (!complete) a.part_lse[slot] = lse2;
+        else if (a.lse != nullptr) a.lse[at] = lse2 * 0.69314718055994531f;
+      }
+    }
+    if (!ok && lane == 0) stop(&ctl->abort, status);
+    if (threadIdx.x == 4 * 32) kv_write_split(a, share, it);
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  if (stopped(&ctl->abort)) {
+    const uint64_t t0 = globaltimer_ns();
+    while (globaltimer_ns() - t0 < 100000ull) {
+    }
+    __syncthreads();
+  }
+  tc_fence_after_sync();
+  if (warp == 1) tmem_dealloc(tmem, kTmem);
+}
+
+template <int D>
+pace_status_t run_prefill(const KvMaps& maps, const KvAttnArgs& a, unsigned grid, int* status, cudaStream_t stream) {
+  using C = PrefillCfg<D>;
+  constexpr size_t smem = 1024 + C::STAGES * 2 * C::TILE + 2 * C::VTILE + 4 * C::QTILE + sizeof(PrefillCtl<D>);
+  static_assert(smem <= 227 * 1024, "shared memory");
+  static DeviceOnce once;
+  int dev = 0;
+  PACE_CUDA(cudaGetDevice(&dev));
+  if (!once.done(dev)) {
+    PACE_CUDA(cudaFuncSetAttribute(kv_prefill_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
+    once.mark(dev);
+  }
+  return launch_dependent(kv_prefill_kernel<D>, grid, kThreads, smem, 1, stream, maps, a, status);
+}
+
+}  // namespace
+
+pace_status_t launch_kv_prefill(const KvMaps& maps, const KvAttnArgs& a, int D, unsigned grid, int* status, cudaStream_t stream) {
+  return D == 128 ? run_prefill<128>(maps, a, grid, status, stream) : run_prefill<64>(maps, a, grid, status, stream);
+}
+
+}  // namespace pace
