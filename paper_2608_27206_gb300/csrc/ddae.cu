@@ -635,16 +635,6 @@ __global__ void __launch_bounds__(256) prune_index_kernel(const __grid_constant_
 constexpr int kGmThreads = 256, kGmU = 4, kGmBlock = kGmThreads * kGmU;
 constexpr int kGmShort = 4, kGmRow = 64, kGmLong = 256;   // elements of a row
 constexpr int kGmMost = 2048, kGmLeast = 384;             // rows: at most for short ones, at least for long ones
-// Division of n < 2^31 by d >= 1 as a multiplication (Granlund and Montgomery): with 2^(l-1) < d <= 2^l and
-// m = floor(2^(31+l) / d) + 1, m d exceeds 2^(31+l) by at most 2^l, so floor(n m / 2^(31+l)) is the quotient.
-struct FastDiv {
-  uint32_t m, shift;
-};
-FastDiv fast_div(uint32_t d) {
-  uint32_t l = 0;
-  while ((uint64_t{1} << l) < d) ++l;
-  return {static_cast<uint32_t>((uint64_t{1} << (31 + l)) / d + 1), 31 + l};
-}
 struct GatherMultiTable {
   pace_gather_tensor g[PACE_GATHER_MAX_TENSORS];
   int64_t block_prefix[PACE_GATHER_MAX_TENSORS + 1];   // blocks of kGmBlock elements, or of a row per warp

@@ -115,6 +115,7 @@ extern "C" pace_status_t pace_kv_attention(const pace_kv_cache* cache, const voi
   a.scale2 = static_cast<float>(static_cast<double>(scale) * 1.4426950408889634);
   a.q_heads = n_q_heads;
   a.group = group;
+  a.by_group = fast_div(static_cast<uint32_t>(group));
   a.window = window;
   a.sinks = sinks;
   a.max_len = max_len;
@@ -141,6 +142,7 @@ extern "C" pace_status_t pace_kv_attention(const pace_kv_cache* cache, const voi
       }
       if (a.s.nb == 0) break;
       const int64_t most = tiles * cache->n_kv_heads * slot_tiles;
+      if (most > INT32_MAX) return PACE_ERR_INVALID_ARG;
       const unsigned grid = static_cast<unsigned>(std::min<int64_t>({most, sms, kPlanCtas}));
       if (is_few) PACE_CHECK(launch_kv_decode(maps, a, D, rows, grid, status, stream));
       else PACE_CHECK(launch_kv_prefill(maps, a, D, grid, status, stream));

@@ -48,6 +48,7 @@ struct KvAttnArgs {
   float* part;          // [2 CTAs][rows of a tile][D]
   float scale2;         // scale * log2(e)
   int q_heads, group, window, sinks, max_len;
+  FastDiv by_group;
   KvSeqs s;
 };
 
@@ -77,7 +78,7 @@ __device__ __forceinline__ KvSpan kv_span(int p_first, int p_last, int window, i
 struct KvItem {
   int i, row_tile, head, t0, t1;
   int row0, rows;           // its query rows
-  int len, p0;              // slots of the sequence; slot of its query 0
+  int p0;                   // slot of the sequence's query 0
   int p_first, p_last;      // slots of the tile's first and last query
   KvSpan span;
 };
@@ -86,22 +87,32 @@ template <int ROWS>
 __device__ __forceinline__ void kv_item_rows(const KvAttnArgs& a, int i, int row_tile, KvItem& it) {
   it.i = i;
   it.row_tile = row_tile;
-  it.len = min(max(a.lens[a.s.seq[i]], 0), a.max_len);
-  it.p0 = it.len - a.s.nq[i];
+  it.p0 = min(max(a.lens[a.s.seq[i]], 0), a.max_len) - a.s.nq[i];
   it.row0 = row_tile * ROWS;
   it.rows = min(a.s.nq[i] * a.group - it.row0, ROWS);
-  it.p_first = it.p0 + it.row0 / a.group;
-  it.p_last = it.p0 + (it.row0 + it.rows - 1) / a.group;
+  it.p_first = it.p0 + static_cast<int>(a.by_group(it.row0));
+  it.p_last = it.p0 + static_cast<int>(a.by_group(it.row0 + it.rows - 1));
   it.span = kv_span(it.p_first, it.p_last, a.window, a.sinks);
 }
 
-// Where a CTA's share lies; the same for all its threads.
+// Output row of the item's row r, (query, head) flattened.
+__device__ __forceinline__ int64_t kv_out_row(const KvAttnArgs& a, const KvItem& it, int r) {
+  const int row = it.row0 + r, token = static_cast<int>(a.by_group(row));
+  return static_cast<int64_t>(a.s.q0[it.i] + token) * a.q_heads + it.head * a.group + row - token * a.group;
+}
+// Its query.
+__device__ __forceinline__ const uint16_t* kv_query(const KvAttnArgs& a, const KvItem& it, int r, int D) {
+  const int row = it.row0 + r, token = static_cast<int>(a.by_group(row));
+  return a.Q + (a.s.q0[it.i] + token) * a.q_stride + static_cast<int64_t>(it.head * a.group + row - token * a.group) * D;
+}
+
+// Where a CTA's share lies; the same for all its threads.  CTA c of a line of total = each * ctas + more tiles begins at
+// c * each + min(c, more).  (The call keeps a launch below 2^31 tiles.)
 struct KvShare {
-  int64_t pos, end;         // its tiles of the line
-  int64_t total;
-  int64_t base;             // first tile of (i, row_tile)
+  int pos, end;             // its tiles of the line
+  int each, more, ctas;
+  int base;                 // first tile of (i, row_tile)
   int i, row_tile;
-  int ctas;                 // that have a share
 };
 
 // Walks a share (item) by item.
@@ -116,20 +127,21 @@ struct KvWalk {
   }
   __device__ __forceinline__ bool next(const KvAttnArgs& a) {
     if (s.pos >= s.end) return false;
+#pragma unroll 1
     while (true) {
       if (!have) {
         kv_item_rows<ROWS>(a, s.i, s.row_tile, it);
         have = true;
       }
-      const uint32_t off = static_cast<uint32_t>(s.pos - s.base), n = it.span.n;
-      if (off < n * static_cast<uint32_t>(a.c.heads)) {
+      const uint32_t off = s.pos - s.base, n = it.span.n;
+      if (off < n * a.c.heads) {
         it.head = off / n;
         it.t0 = off - it.head * n;
-        it.t1 = static_cast<int>(min(static_cast<int64_t>(n), it.t0 + (s.end - s.pos)));
+        it.t1 = min(static_cast<int>(n), it.t0 + (s.end - s.pos));
         s.pos += it.t1 - it.t0;
         return true;
       }
-      s.base += static_cast<int64_t>(n) * a.c.heads;
+      s.base += n * a.c.heads;
       have = false;
       if (++s.row_tile >= a.s.tile0[s.i + 1] - a.s.tile0[s.i]) {
         s.row_tile = 0;
@@ -139,82 +151,82 @@ struct KvWalk {
   }
 };
 
-// Every thread of the block (a multiple of 32, at most 1024) calls this once; `buf` holds blockDim.x 64-bit words.  Row
-// tiles that see nothing get their zeros here.
+// Every thread of the block (whole warps, at most 32) calls this once; `buf` holds an int per warp.  Row tiles that see
+// nothing get their zeros here.
 template <int ROWS, int D>
-__device__ __forceinline__ KvShare kv_share(const KvAttnArgs& a, int64_t* buf, KvShare* found, int* status) {
+__device__ __forceinline__ KvShare kv_share(const KvAttnArgs& a, int* buf, KvShare* found, int* status) {
   const int threads = blockDim.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int tiles = a.s.tile0[a.s.nb], per = (tiles + threads - 1) / threads;
   const int first = min(tid * per, tiles), last = min(first + per, tiles);
   int i0 = 0, hi = a.s.nb - 1;      // the sequence of row tile `first`
+#pragma unroll 1
   while (i0 < hi) {
     const int mid = (i0 + hi + 1) >> 1;
     if (a.s.tile0[mid] <= first) i0 = mid;
     else hi = mid - 1;
   }
-  auto each = [&](auto&& f) {
+  KvShare s{};
+  int mine = 0, before = 0;
+#pragma unroll 1
+  for (int round = 0; round < 2; ++round) {      // how many tiles there are; where this CTA's begin
+    if (round == 1) {
+      int incl = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int x = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += x;
+      }
+      if (lane == 31) buf[warp] = incl;
+      __syncthreads();
+      int total = 0;
+#pragma unroll 1
+      for (int w = 0; w < threads / 32; ++w) {
+        if (w == warp) before = total;
+        total += buf[w];
+      }
+      before += incl - mine;
+      s.ctas = min(static_cast<int>(gridDim.x), total);
+      const int c = blockIdx.x;
+      if (c >= s.ctas) return s;      // nothing to do (the whole block)
+      s.each = total / s.ctas;
+      s.more = total - s.each * s.ctas;
+      s.pos = c * s.each + min(c, s.more);
+      s.end = s.pos + s.each + (c < s.more ? 1 : 0);
+      if (s.pos < before || s.pos >= before + mine) break;
+    }
     int i = i0;
+#pragma unroll 1
     for (int t = first; t < last; ++t) {
+#pragma unroll 1
       while (t >= a.s.tile0[i + 1]) ++i;
       KvItem it;
       kv_item_rows<ROWS>(a, i, t - a.s.tile0[i], it);
-      if (!f(it, static_cast<int64_t>(it.span.n) * a.c.heads)) break;
-    }
-  };
-  int64_t mine = 0;
-  each([&](const KvItem& it, int64_t n) {
-    mine += n;
-    if (it.row_tile == 0 && a.lens[a.s.seq[it.i]] > a.max_len && blockIdx.x == 0) record_error(status, PACE_ERR_INVALID_ARG, K_KV_ATTN);
-    if (n == 0 && (a.s.tile0[it.i] + it.row_tile) % gridDim.x == blockIdx.x) {
-      for (int r = 0; r < it.rows * a.c.heads; ++r) {
-        const int row = it.row0 + r / a.c.heads, h = (r % a.c.heads) * a.group + row % a.group;
-        const int64_t at = static_cast<int64_t>(a.s.q0[it.i] + row / a.group) * a.q_heads + h;
-        for (int d = 0; d < D; d += 8) *reinterpret_cast<uint4*>(a.out + at * D + d) = make_uint4(0, 0, 0, 0);
-        if (a.lse != nullptr) a.lse[at] = -INFINITY;
+      const int n = it.span.n * a.c.heads;
+      if (round == 1) {
+        if (s.pos < before + n) {
+          s.base = before;
+          s.i = i;
+          s.row_tile = it.row_tile;
+          *found = s;
+          break;
+        }
+        before += n;
+        continue;
+      }
+      mine += n;
+      if (blockIdx.x == 0 && it.row_tile == 0 && a.lens[a.s.seq[i]] > a.max_len) record_error(status, PACE_ERR_INVALID_ARG, K_KV_ATTN);
+      if (n == 0 && t % gridDim.x == blockIdx.x) {
+#pragma unroll 1
+        for (it.head = 0; it.head < a.c.heads; ++it.head)
+#pragma unroll 1
+          for (int r = 0; r < it.rows; ++r) {
+            const int64_t at = kv_out_row(a, it, r);
+#pragma unroll 1
+            for (int d = 0; d < D; d += 8) *reinterpret_cast<uint4*>(a.out + at * D + d) = make_uint4(0, 0, 0, 0);
+            if (a.lse != nullptr) a.lse[at] = -INFINITY;
+          }
       }
     }
-    return true;
-  });
-  int64_t incl = mine;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int64_t x = __shfl_up_sync(0xffffffffu, incl, o);
-    if (lane >= o) incl += x;
-  }
-  if (lane == 31) buf[warp] = incl;
-  __syncthreads();
-  if (warp == 0) {
-    int64_t x = lane < threads / 32 ? buf[lane] : 0;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
-      if (lane >= o) x += y;
-    }
-    if (lane < threads / 32) buf[lane] = x;
-  }
-  __syncthreads();
-  const int64_t total = buf[threads / 32 - 1];
-  const int64_t before = incl - mine + (warp > 0 ? buf[warp - 1] : 0);
-  const int ctas = static_cast<int>(min(static_cast<int64_t>(gridDim.x), total));
-  KvShare s{};
-  s.total = total;
-  s.ctas = ctas;
-  if (static_cast<int>(blockIdx.x) >= ctas) return s;      // nothing to do (uniform)
-  s.pos = total * blockIdx.x / ctas;
-  s.end = total * (blockIdx.x + 1) / ctas;
-  if (s.pos >= before && s.pos < before + mine) {
-    int64_t base = before;
-    each([&](const KvItem& it, int64_t n) {
-      if (s.pos < base + n) {
-        s.base = base;
-        s.i = it.i;
-        s.row_tile = it.row_tile;
-        return false;
-      }
-      base += n;
-      return true;
-    });
-    *found = s;
   }
   __syncthreads();
   return *found;
@@ -223,9 +235,10 @@ __device__ __forceinline__ KvShare kv_share(const KvAttnArgs& a, int64_t* buf, K
 // What CTA c tells the combine kernel: how many later CTAs its last item goes on in.
 __device__ __forceinline__ void kv_write_split(const KvAttnArgs& a, const KvShare& s, const KvItem& it) {
   KvSplit sp{it.i, it.row_tile, it.head, 0};
-  if (it.t0 == 0 && it.t1 < it.span.n) {   // CTA j takes part iff total j / ctas < the item's end
-    const int64_t end = s.end + (it.span.n - it.t1);
-    sp.followers = static_cast<int>((end * s.ctas + s.total - 1) / s.total) - 1 - static_cast<int>(blockIdx.x);
+  if (it.t0 == 0 && it.t1 < it.span.n) {   // CTA j takes part iff it begins before the item's end
+    const int c = blockIdx.x, end = (c + 1) * s.each + min(c + 1, s.more) + it.span.n - it.t1, wide = s.more * (s.each + 1);
+    const int last = end <= wide ? (end + s.each) / (s.each + 1) : s.more + (end - wide + s.each - 1) / s.each;
+    sp.followers = last - 1 - c;
   }
   a.split[blockIdx.x] = sp;
 }
@@ -233,6 +246,13 @@ __device__ __forceinline__ void kv_write_split(const KvAttnArgs& a, const KvShar
 struct KvMaps {
   CUtensorMap k, v;
 };
+
+// mbar_wait with its loop out of line: the kernels here wait in many places, and instructions that are not run push those that
+// are out of the instruction cache.
+static __device__ __noinline__ bool kv_wait_loop(uint32_t bar, uint32_t parity) { return ptx::mbar_wait(bar, parity, kWaitLimitNs); }
+__device__ __forceinline__ bool kv_wait(uint32_t bar, uint32_t parity) {
+  return ptx::mbar_try_wait(bar, parity) || kv_wait_loop(bar, parity);
+}
 
 // A role that gives up on a wait says so here; the others leave as their own waits run out.
 __device__ __forceinline__ bool stopped(const int* abort) { return *reinterpret_cast<const volatile int*>(abort) != 0; }
@@ -281,8 +301,9 @@ __device__ __forceinline__ void kv_fetch(const KvMaps& maps, const KvAttnArgs& a
       return page >= 0 && page < a.c.n_pages ? page : -1;
     };
     int mine = page_of(it.t0), next = -2;
+#pragma unroll 1
     for (int i = it.t0; i < it.t1; ++i, ++t) {
-      const int k = (i - it.t0) % tiles_per_load;
+      const int k = (i - it.t0) & (tiles_per_load - 1);
       if (k == 0) {
         if (i > it.t0) mine = next;
         next = page_of(i + tiles_per_load);
@@ -295,7 +316,7 @@ __device__ __forceinline__ void kv_fetch(const KvMaps& maps, const KvAttnArgs& a
       }
       const int s = t % ST, round = t / ST;
       if (round > 0) {
-        const bool ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&empty[s]), (round - 1) & 1, kWaitLimitNs));
+        const bool ok = __all_sync(0xffffffffu, kv_wait(smem_u32(&empty[s]), (round - 1) & 1));
         if (!ok) {
           if (lane == 0) stop(abort, status);
           break;

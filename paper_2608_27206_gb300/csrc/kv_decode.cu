@@ -58,13 +58,21 @@ struct alignas(16) DecodeCtl {
   float qc[NQ];             // scale2 * the row's power of two
   int slot_of[NQ];          // slot of the row's query
   float2 fac[NQ];
+  int64_t out_at[NQ];
   float2 red[4][NQ];
   float scales[DecodeCfg<D, NQ>::STAGES][16];   // a tile's K scales, then its V scales
-  int64_t scan[kWarps];
+  int scan[kWarps];
   KvShare share;
   uint32_t tmem;
   int abort;
 };
+
+// Largest of the warp's values (a NaN counts only where all are).
+__device__ __forceinline__ float warp_max(float x) {
+  float r;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
+  return r;
+}
 
 template <int D, int NQ>
 __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_constant__ KvMaps maps, const __grid_constant__ KvAttnArgs a,
@@ -132,7 +140,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
       int t = 0, items = 0;
       bool ok = true;
       auto weigh = [&](int u, bool first) {     // O += V^T P of tile u
-        if (!mbar_wait(p_full(u & 1), (u >> 1) & 1, kWaitLimitNs)) return false;
+        if (!kv_wait(p_full(u & 1), (u >> 1) & 1)) return false;
         tc_fence_after_sync();
         const uint64_t v = dk[1] + static_cast<uint64_t>(((u % ST) * 2 + 1) * (C::TILE >> 4));
 #pragma unroll
@@ -144,11 +152,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
         return true;
       };
       while (ok && walk.next(a)) {
-        ok = mbar_wait(q_full, items & 1, kWaitLimitNs);
+        ok = kv_wait(q_full, items & 1);
         ++items;
         const int n = walk.it.t1 - walk.it.t0;
+#pragma unroll 1
         for (int i = 0; ok && i < n; ++i, ++t) {
-          ok = mbar_wait(full(t % ST), (t / ST) & 1, kWaitLimitNs);
+          ok = kv_wait(full(t % ST), (t / ST) & 1);
           if (!ok) break;
           tc_fence_after_sync();
           const uint64_t k0 = dk[0] + static_cast<uint64_t>((t % ST) * 2 * (C::TILE >> 4));
@@ -173,14 +182,14 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
       const KvItem& it = walk.it;
       named_barrier_sync(1, 128);      // the last item's shared statistics have been read
       // q: rows of this item as hi and lo codes (rows past it are zero), the power of two of each
+#pragma unroll 1
       for (int q = quad; q < NQ; q += 4) {
         constexpr int E = D / 32;      // elements of a lane
         float x[E];
-        const int r = it.row0 + q, h = it.head * a.group + r % a.group;
 #pragma unroll
         for (int e = 0; e < E; ++e) x[e] = 0.f;
         if (q < it.rows) {
-          const uint16_t* src = a.Q + (a.s.q0[it.i] + r / a.group) * a.q_stride + static_cast<int64_t>(h) * D + lane * E;
+          const uint16_t* src = kv_query(a, it, q, D) + lane * E;
           uint32_t w[E / 2];
           if constexpr (E == 4) {
             const uint2 u = *reinterpret_cast<const uint2*>(src);
@@ -224,7 +233,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
         if (lane == 0) {
           const bool real = q < it.rows;
           ctl->qc[q] = real ? a.scale2 * __uint_as_float(static_cast<uint32_t>(127 + e2) << 23) : 0.f;
-          ctl->slot_of[q] = real ? it.p0 + r / a.group : -1;
+          ctl->slot_of[q] = real ? it.p0 + static_cast<int>(a.by_group(it.row0 + q)) : -1;
           // (rows past the item score 0 and must not ask for anything)
           ctl->stat[q] = real ? Stat{kNone, kNone, kNone, 0.f} : Stat{-kNone, -kNone, -kNone, 0.f};
         }
@@ -236,11 +245,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
       float l[NQ];
 #pragma unroll
       for (int q = 0; q < NQ; ++q) l[q] = 0.f;
+#pragma unroll 1
       for (int i = it.t0; i < it.t1; ++i, ++t) {
         const int s = t % ST, p = t & 1;
         const int slot0 = it.span.tile(i) * kKvTile, slot = slot0 + me;
-        bool ok = mbar_wait(full(s), (t / ST) & 1, kWaitLimitNs);        // the tile's scales (and V, below)
-        ok = __all_sync(0xffffffffu, ok && mbar_wait(s_full(p), (t >> 1) & 1, kWaitLimitNs));
+        bool ok = kv_wait(full(s), (t / ST) & 1);        // the tile's scales (and V, below)
+        ok = __all_sync(0xffffffffu, ok && kv_wait(s_full(p), (t >> 1) & 1));
         if (!ok) {
           if (lane == 0) stop(&ctl->abort, status);
           bad = true;
@@ -294,12 +304,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
           // some row's m or w has to move: the tile's maxima over all slots, new values, factors for l and O
 #pragma unroll
           for (int q = 0; q < NQ; ++q) {
-            float mx = x[q], mw = x[q] + lv;
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) {
-              mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-              mw = fmaxf(mw, __shfl_xor_sync(0xffffffffu, mw, o));
-            }
+            const float mx = warp_max(x[q]), mw = warp_max(x[q] + lv);
             if (lane == 0) ctl->red[quad][q] = make_float2(mx, mw);
           }
           named_barrier_sync(1, 128);
@@ -316,7 +321,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
             ctl->fac[me] = make_float2(exp2f(st.m - m), exp2f(st.w - w));
             ctl->stat[me] = Stat{m, w, m + kFar, exp2f(kUnit + m - w)};
           }
-          if (i > it.t0 && !mbar_wait(pv_done, (t - 1) & 1, kWaitLimitNs)) stop(&ctl->abort, status);
+          if (i > it.t0 && !kv_wait(pv_done, (t - 1) & 1)) stop(&ctl->abort, status);
           named_barrier_sync(1, 128);
           bad = named_barrier_any(1, 128, stopped(&ctl->abort));
           if (bad) break;
@@ -376,7 +381,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
       }
       if (bad) break;
       // ---- the item's (part of the) output --------------------------------------------------
-      if (!mbar_wait(pv_done, (t - 1) & 1, kWaitLimitNs)) stop(&ctl->abort, status);
+      if (!kv_wait(pv_done, (t - 1) & 1)) stop(&ctl->abort, status);
 #pragma unroll
       for (int q = 0; q < NQ; ++q) {
         float v = l[q];
@@ -384,31 +389,32 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
         for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
         if (lane == 0) ctl->red[quad][q].x = v;
       }
+      const bool complete = it.t0 == 0 && it.t1 == it.span.n;
+      const int64_t slot = (2 * static_cast<int64_t>(blockIdx.x) + (it.t0 == 0 ? 1 : 0)) * NQ;
       named_barrier_sync(1, 128);
+      if (me < it.rows) {
+        const float sum = (ctl->red[0][me].x + ctl->red[1][me].x) + (ctl->red[2][me].x + ctl->red[3][me].x);
+        const Stat st = ctl->stat[me];
+        const int64_t at = complete ? kv_out_row(a, it, me) : slot + me;
+        ctl->fac[me].x = sum == 0.f ? 0.f : 1.f / (st.g * sum);      // out = O / (g l); a row that saw nothing here is zero
+        ctl->out_at[me] = at * D;
+        float* lse = complete ? a.lse : a.part_lse;
+        if (lse != nullptr) lse[at] = sum == 0.f ? -INFINITY : (st.m + log2f(sum)) * (complete ? 0.69314718055994531f : 1.f);
+      }
       bad = named_barrier_any(1, 128, stopped(&ctl->abort));
       if (bad) break;
       tc_fence_after_sync();
       uint32_t o[C::COLS];
       load_cols(lanes + 2 * C::COLS, o);
       tc_fence_before_sync();
-      const bool complete = it.t0 == 0 && it.t1 == it.span.n;
-      const int64_t slot = 2 * blockIdx.x + (it.t0 == 0 ? 1 : 0);
+      if (me < D) {
 #pragma unroll
-      for (int q = 0; q < NQ; ++q) {
-        if (q >= it.rows) continue;
-        const float sum = (ctl->red[0][q].x + ctl->red[1][q].x) + (ctl->red[2][q].x + ctl->red[3][q].x);
-        const Stat st = ctl->stat[q];
-        // O / (g l); a row that saw nothing here is zero
-        const float v = sum == 0.f ? 0.f : fmaf(__uint_as_float(o[NQ + q]), 0.0625f, __uint_as_float(o[q])) / (st.g * sum);
-        const float lse2 = sum == 0.f ? -INFINITY : st.m + log2f(sum);
-        const int r = it.row0 + q, h = it.head * a.group + r % a.group;
-        if (complete) {
-          const int64_t at = static_cast<int64_t>(a.s.q0[it.i] + r / a.group) * a.q_heads + h;
-          if (me < D) a.out[at * D + me] = __bfloat16_as_ushort(__float2bfloat16_rn(v));
-          if (me == 0 && a.lse != nullptr) a.lse[at] = lse2 * 0.69314718055994531f;
-        } else {
-          if (me < D) a.part[(slot * NQ + q) * D + me] = v;
-          if (me == 0) a.part_lse[slot * NQ + q] = lse2;
+        for (int q = 0; q < NQ; ++q) {
+          if (q >= it.rows) break;
+          const float f = ctl->fac[q].x;
+          const float v = f == 0.f ? 0.f : fmaf(__uint_as_float(o[NQ + q]), 0.0625f, __uint_as_float(o[q])) * f;
+          if (complete) a.out[ctl->out_at[q] + me] = __bfloat16_as_ushort(__float2bfloat16_rn(v));
+          else a.part[ctl->out_at[q] + me] = v;
         }
       }
     }
@@ -463,7 +469,8 @@ __global__ void __launch_bounds__(256) kv_attn_combine(const __grid_constant__ K
     }
   }
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  const int64_t dst = static_cast<int64_t>(a.s.q0[sp.i] + row / a.group) * a.q_heads + sp.head * a.group + row % a.group;
+  const int token = static_cast<int>(a.by_group(row));
+  const int64_t dst = static_cast<int64_t>(a.s.q0[sp.i] + token) * a.q_heads + sp.head * a.group + row - token * a.group;
   uint32_t w[D / 32];
 #pragma unroll
   for (int e = 0; e < D / 32; ++e)

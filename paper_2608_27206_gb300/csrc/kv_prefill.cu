@@ -53,7 +53,7 @@ struct alignas(16) PrefillCtl {
   float scales[ST][16];
   float4 block[2][8];           // per block of 16 slots: K scale, log2(V scale), 1 / V scale
   uint32_t nan[2][4];           // slots of which some row sees a NaN value
-  int64_t scan[kThreads / 32];
+  int scan[kThreads / 32];
   KvShare share;
   uint32_t tmem;
   int abort;
@@ -68,6 +68,27 @@ __device__ __forceinline__ uint32_t f16x2(float lo, float hi) {
   uint32_t r;
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
+}
+
+// Two bf16 times a power of two, as f16.
+__device__ __forceinline__ uint32_t pair_f16(uint32_t two, float by) {
+  return f16x2(__uint_as_float(two << 16) * by, __uint_as_float(two & 0xFFFF0000u) * by);
+}
+// Four f16 as e4m3 terms: hi, and what is left of them.
+__device__ __forceinline__ void split_e4m3(uint32_t a, uint32_t b, uint32_t& hi, uint32_t& lo) {
+  auto code = [](uint32_t two) {
+    uint16_t r;
+    asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(r) : "r"(two));
+    return static_cast<uint32_t>(r);
+  };
+  auto rest = [](uint32_t two, uint32_t codes) {
+    uint32_t r;
+    asm("sub.f16x2 %0, %1, %2;" : "=r"(r) : "r"(two), "r"(e4m3x2_to_f16x2(codes)));
+    return r;
+  };
+  const uint32_t ca = code(a), cb = code(b);
+  hi = ca | cb << 16;
+  lo = code(rest(a, ca)) | code(rest(b, cb)) << 16;
 }
 
 template <int D>
@@ -135,23 +156,24 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
     const uint64_t dq = smem_desc(smem_u32(sQ), 16, C::GROUP, C::SWIZZLE);
     const uint64_t dk = smem_desc(smem_u32(sKV), 16, C::GROUP, C::SWIZZLE);
     const uint64_t dv = smem_desc(smem_u32(sV), C::VCHUNK, 1024, 2);
-    int t = 0, rounds[2] = {0, 0}, items[2] = {0, 0};      // slot tiles; weights taken and items, of a row tile
+    int t = 0, rounds_a = 0, rounds_b = 0, items_a = 0, items_b = 0;      // slot tiles; weights taken and items, of a row tile
     bool ok = true;
     auto wait = [&](uint32_t bar, int round) {
-      ok = __all_sync(0xffffffffu, mbar_wait(bar, round & 1, kWaitLimitNs));
+      ok = __all_sync(0xffffffffu, kv_wait(bar, round & 1));
       return ok;
     };
     while (ok && walk.next(a)) {
       const int n = it.t1 - it.t0;
       const bool two = it.rows > 128;
+#pragma unroll 1
       for (int j = 0; ok && j <= n; ++j) {      // P V of slot tile j - 1, then S of slot tile j
         const int u = t + j - 1, s = (t + j) % ST;
         if (j < n && !wait(full(s), (t + j) / ST)) break;
         if (j > 0 && !wait(ready(u & 1), u >> 1)) break;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          if (i == 1 && !two) break;
-          if (!(j > 0 ? wait(p_full(i), rounds[i]++) : wait(q_full(i), items[i]++))) break;
+#pragma unroll 1
+        for (int i = 0; i <= static_cast<int>(two); ++i) {
+          const int round = j > 0 ? (i == 0 ? rounds_a++ : rounds_b++) : i == 0 ? items_a++ : items_b++;
+          if (!wait(j > 0 ? p_full(i) : q_full(i), round)) break;
           tc_fence_after_sync();
           if (j > 0) {
             const uint64_t v = dv + static_cast<uint64_t>((u & 1) * (C::VTILE >> 4));
@@ -185,9 +207,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
     int t = 0;
     bool ok = true;
     while (ok && walk.next(a)) {
+#pragma unroll 1
       for (int j = it.t0; ok && j < it.t1; ++j, ++t) {
         const int s = t % ST, b = t & 1, slot0 = it.span.tile(j) * kKvTile;
-        ok = mbar_wait(full(s), (t / ST) & 1, kWaitLimitNs) && (t < 2 || mbar_wait(vfree(b), ((t >> 1) - 1) & 1, kWaitLimitNs));
+        ok = kv_wait(full(s), (t / ST) & 1) && (t < 2 || kv_wait(vfree(b), ((t >> 1) - 1) & 1));
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         // 0 * NaN is NaN: no slot of V that some row does not see may hold one.  Slots that nobody sees become zero; where rows
@@ -255,12 +278,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
         t += it.t1 - it.t0;
         continue;
       }
-      const int row = i * 128 + me, r = it.row0 + row;          // of the item, of the sequence
+      const int row = i * 128 + me;
       const bool real = row < it.rows;
-      const int token = r / a.group, h = it.head * a.group + r % a.group;
-      const int p = real ? it.p0 + token : it.p_last;
-      // slots of this tile's first and last row
-      const int p_lo = it.p0 + (it.row0 + i * 128) / a.group, p_hi = it.p0 + (it.row0 + min(i * 128 + 127, it.rows - 1)) / a.group;
+      auto slot_of = [&](int r) { return it.p0 + static_cast<int>(a.by_group(it.row0 + min(r, it.rows - 1))); };
+      const int p = slot_of(row), p_lo = slot_of(i * 128), p_hi = slot_of(i * 128 + 127);      // of the row, of the tile's first and last
       float c = 0.f;            // scale2 * the row's power of two
       {
         // q as hi and lo codes.  D / 8 lanes read a row, 16 bytes each; it takes the places of its codes (128 or 64 bytes in the
@@ -273,14 +294,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
           return tile + (chunk >= PER ? C::QTILE : 0) + row * D + ((chunk % PER) ^ (D == 128 ? row & 7 : (row >> 1) & 3)) * 16;
         };
         {
+          const unsigned long long from = real ? reinterpret_cast<unsigned long long>(kv_query(a, it, i * 128 + me, D)) : 0;
           uint4 u[32 / STEP];
 #pragma unroll
           for (int k = 0; k < 32 / STEP; ++k) {
-            const int rk = it.row0 + i * 128 + quad * 32 + k * STEP + sub;
-            u[k] = make_uint4(0, 0, 0, 0);
-            if (rk < it.row0 + it.rows)
-              u[k] = *reinterpret_cast<const uint4*>(a.Q + (a.s.q0[it.i] + rk / a.group) * a.q_stride +
-                                                     static_cast<int64_t>(it.head * a.group + rk % a.group) * D + part * 8);
+            const unsigned long long src = __shfl_sync(0xffffffffu, from, k * STEP + sub);
+            u[k] = src != 0 ? *(reinterpret_cast<const uint4*>(src) + part) : make_uint4(0, 0, 0, 0);
           }
 #pragma unroll
           for (int k = 0; k < 32 / STEP; ++k) *reinterpret_cast<uint4*>(place(quad * 32 + k * STEP + sub, part)) = u[k];
@@ -296,21 +315,14 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
         const uint32_t top = max(most & 0xFFFFu, most >> 16);
         const bool fin = top < 0x7F80u;
         const int e2 = fin ? max(static_cast<int>(top >> 7) - 127 - 7, -110) : 0;      // top 2^-e2 in [128, 256)
-        const float inv = __uint_as_float(static_cast<uint32_t>(127 - e2) << 23);
+        const float inv = fin ? __uint_as_float(static_cast<uint32_t>(127 - e2) << 23) : NAN;      // (a row that is not finite: NaN throughout)
         c = a.scale2 * __uint_as_float(static_cast<uint32_t>(127 + e2) << 23);
 #pragma unroll
-        for (int e = 0; e < D / 16; ++e) {      // 16 elements at a time
+        for (int e = 0; e < D / 16; ++e) {      // 16 elements at a time: by way of f16, which holds them (and 2^-24 where e4m3 ends at 2^-9)
           const uint32_t w[8] = {u[2 * e].x, u[2 * e].y, u[2 * e].z, u[2 * e].w, u[2 * e + 1].x, u[2 * e + 1].y, u[2 * e + 1].z, u[2 * e + 1].w};
           uint32_t hi[4], lo[4];
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const float y[4] = {__uint_as_float(w[2 * k] << 16) * inv, __uint_as_float(w[2 * k] & 0xFFFF0000u) * inv,
-                                __uint_as_float(w[2 * k + 1] << 16) * inv, __uint_as_float(w[2 * k + 1] & 0xFFFF0000u) * inv};
-            hi[k] = fin ? e4m3x4(y[0], y[1], y[2], y[3]) : 0x7F7F7F7Fu;      // a row that is not finite: NaN throughout
-            const uint32_t f0 = e4m3x2_to_f16x2(hi[k] & 0xFFFFu), f1 = e4m3x2_to_f16x2(hi[k] >> 16);
-            const float2 g0 = __half22float2(*reinterpret_cast<const __half2*>(&f0)), g1 = __half22float2(*reinterpret_cast<const __half2*>(&f1));
-            lo[k] = fin ? e4m3x4(y[0] - g0.x, y[1] - g0.y, y[2] - g1.x, y[3] - g1.y) : 0u;
-          }
+          for (int k = 0; k < 4; ++k) split_e4m3(pair_f16(w[2 * k], inv), pair_f16(w[2 * k + 1], inv), hi[k], lo[k]);
           *reinterpret_cast<uint4*>(place(me, e)) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
           *reinterpret_cast<uint4*>(place(me, e + D / 16)) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
         }
@@ -319,10 +331,11 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
         if (lane == 0) mbar_arrive(q_full(i));
       }
       float w = kNone, l = 0.f;
+#pragma unroll 1
       for (int j = it.t0; j < it.t1; ++j, ++t, ++s_rounds) {
         const int b = t & 1, slot0 = it.span.tile(j) * kKvTile;
         // (S first: a row tile that left items out may be rounds ahead of the others until its products run)
-        ok = mbar_wait(s_full(i), s_rounds & 1, kWaitLimitNs) && mbar_wait(ready(b), (t >> 1) & 1, kWaitLimitNs);
+        ok = kv_wait(s_full(i), s_rounds & 1) && kv_wait(ready(b), (t >> 1) & 1);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         tc_fence_after_sync();
@@ -348,6 +361,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
         for (int q = 0; q < 2; ++q) {      // 64 columns
           const float4* block = &ctl->block[b][4 * q];
           uint32_t words[32];
+#pragma unroll 1
           while (true) {
             uint32_t x[64];
             load_cols(sS + 64 * q, x);
@@ -422,17 +436,17 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
       }
       if (!ok) break;
       // ---- the item's (part of the) output -----------------------------------------------------
-      ok = __all_sync(0xffffffffu, mbar_wait(o_full(i), o_rounds & 1, kWaitLimitNs));
+      ok = __all_sync(0xffffffffu, kv_wait(o_full(i), o_rounds & 1));
       ++o_rounds;
       if (!ok) break;
       tc_fence_after_sync();
       const float inv = l == 0.f ? 0.f : 1.f / l, lse2 = l == 0.f ? -INFINITY : w + log2f(l);
       const bool complete = it.t0 == 0 && it.t1 == it.span.n;
-      const int64_t at = static_cast<int64_t>(a.s.q0[it.i] + token) * a.q_heads + h;
+      const int64_t at = kv_out_row(a, it, real ? row : 0);
       const int64_t slot = (2 * static_cast<int64_t>(blockIdx.x) + (it.t0 == 0 ? 1 : 0)) * kManyRows + row;
       // complete rows go out by way of the q tile, which is done with (this warp's rows only), so that lanes write side by side
       uint8_t* stage = sQ + i * 2 * C::QTILE + quad * 32 * 2 * D;
-#pragma unroll
+#pragma unroll 1
       for (int q = 0; q < D / 32; ++q) {
         uint32_t o[32];
         load_cols(sO + 32 * q, o);
@@ -456,12 +470,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
       if (complete) {
         constexpr int LANES = D / 8, STEP = 32 / LANES;
         __syncwarp();
-#pragma unroll 8
+        const unsigned long long to = real ? reinterpret_cast<unsigned long long>(a.out + at * D) : 0;
+#pragma unroll 4
         for (int k = 0; k < 32; k += STEP) {
-          const int rw = k + lane / LANES, part = lane % LANES, rk = it.row0 + i * 128 + quad * 32 + rw;
-          if (rk < it.row0 + it.rows)
-            *reinterpret_cast<uint4*>(a.out + (static_cast<int64_t>(a.s.q0[it.i] + rk / a.group) * a.q_heads + it.head * a.group + rk % a.group) * D +
-                                      part * 8) = *reinterpret_cast<const uint4*>(stage + rw * 2 * D + (part ^ (rw & 7)) * 16);
+          const int rw = k + lane / LANES, part = lane % LANES;
+          const unsigned long long dst = __shfl_sync(0xffffffffu, to, rw);
+          if (dst != 0) *(reinterpret_cast<uint4*>(dst) + part) = *reinterpret_cast<const uint4*>(stage + rw * 2 * D + (part ^ (rw & 7)) * 16);
         }
         __syncwarp();
       }

@@ -103,6 +103,18 @@ pace_status_t launch_dependent(void (*kernel)(Params...), dim3 grid, dim3 thread
   return launch_ex(true, kernel, grid, threads, smem, cluster, stream, args...);
 }
 
+// Division of n < 2^31 by d >= 1 as a multiplication (Granlund and Montgomery): with 2^(l-1) < d <= 2^l and
+// m = floor(2^(31+l) / d) + 1, m d exceeds 2^(31+l) by at most 2^l, so floor(n m / 2^(31+l)) is the quotient.
+struct FastDiv {
+  uint32_t m, shift;
+  __device__ __forceinline__ uint32_t operator()(uint32_t n) const { return static_cast<uint32_t>(static_cast<uint64_t>(n) * m >> shift); }
+};
+inline FastDiv fast_div(uint32_t d) {
+  uint32_t l = 0;
+  while ((uint64_t{1} << l) < d) ++l;
+  return {static_cast<uint32_t>((uint64_t{1} << (31 + l)) / d + 1), 31 + l};
+}
+
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 }  // namespace pace
