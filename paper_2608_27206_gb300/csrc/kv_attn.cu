@@ -141,9 +141,9 @@ extern "C" pace_status_t pace_kv_attention(const pace_kv_cache* cache, const voi
         a.s.tile0[i + 1] = static_cast<int>(tiles);
       }
       if (a.s.nb == 0) break;
-      const int64_t most = tiles * cache->n_kv_heads * slot_tiles;
+      const int64_t most = tiles * cache->n_kv_heads * (slot_tiles + kItemCost);
       if (most > INT32_MAX) return PACE_ERR_INVALID_ARG;
-      const unsigned grid = static_cast<unsigned>(std::min<int64_t>({most, sms, kPlanCtas}));
+      const unsigned grid = static_cast<unsigned>(std::min<int64_t>({tiles * cache->n_kv_heads * slot_tiles, sms, kPlanCtas}));
       if (is_few) PACE_CHECK(launch_kv_decode(maps, a, D, rows, grid, status, stream));
       else PACE_CHECK(launch_kv_prefill(maps, a, D, grid, status, stream));
       if (slot_tiles > 1) PACE_CHECK(launch_kv_combine(a, D, rows, grid, stream));

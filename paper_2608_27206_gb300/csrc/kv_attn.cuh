@@ -3,11 +3,12 @@
 //
 // The query rows of a sequence that share a KV head (row r = query r / G, head r % G of the group) are cut
 // into row tiles, and the slots that a row tile sees into tiles of 128.  Row tile by row tile, KV head by KV
-// head, slot tile by slot tile, the tiles of a launch form one line; CTA c of g walks tiles T c / g ..
-// T (c + 1) / g - 1 of it.  So every CTA has the same work to a tile, whatever the lengths are, and at most
-// its first and its last (row tile, head) are shared with others: those leave a normalised partial output
-// and its log-sum-exp per row (slot 2 c: it begins inside, 2 c + 1: it begins there and goes on elsewhere),
-// which kv_attn_combine weighs together.
+// head, slot tile by slot tile, the tiles of a launch form one line, in which every (row tile, head) also takes
+// kItemCost places for what it costs by itself; CTA c of g walks places T c / g .. T (c + 1) / g - 1.  So
+// every CTA has the same work to a tile, whatever the lengths are, and at most its first and its last (row
+// tile, head) are shared with others: those leave a normalised partial output and its log-sum-exp per row
+// (slot 2 c: it begins inside, 2 c + 1: it begins there and goes on elsewhere), which kv_attn_combine weighs
+// together.
 #pragma once
 #include <cuda.h>
 
@@ -19,6 +20,7 @@ namespace pace {
 constexpr int kKvTile = 128;      // slots of one tile
 constexpr float kNone = -1e30f;   // a row's maximum before its first slot (finite: x - kNone is never NaN)
 constexpr int kManyRows = 256;    // rows of a tile of the form for many
+constexpr int kItemCost = 3;      // slot tiles that the queries and the output of a (row tile, head) are worth
 constexpr int kPlanCtas = 152;    // CTAs of a launch at most: an SM each (the size queries need no device)
 
 // The launch's sequences, those without queries left out.
@@ -111,6 +113,7 @@ __device__ __forceinline__ const uint16_t* kv_query(const KvAttnArgs& a, const K
 struct KvShare {
   int pos, end;             // its tiles of the line
   int each, more, ctas;
+  int cost;                 // places of an item besides its tiles
   int base;                 // first tile of (i, row_tile)
   int i, row_tile;
 };
@@ -133,13 +136,16 @@ struct KvWalk {
         kv_item_rows<ROWS>(a, s.i, s.row_tile, it);
         have = true;
       }
-      const uint32_t off = s.pos - s.base, n = it.span.n;
+      const uint32_t off = s.pos - s.base, n = it.span.n > 0 ? it.span.n + s.cost : 0;
       if (off < n * a.c.heads) {
         it.head = off / n;
-        it.t0 = off - it.head * n;
-        it.t1 = min(static_cast<int>(n), it.t0 + (s.end - s.pos));
-        s.pos += it.t1 - it.t0;
-        return true;
+        const int from = off - it.head * n, to = min(static_cast<int>(n), from + (s.end - s.pos));
+        s.pos += to - from;
+        it.t0 = max(from - s.cost, 0);
+        it.t1 = max(to - s.cost, 0);
+        if (it.t0 < it.t1) return true;
+        if (s.pos >= s.end) return false;
+        continue;
       }
       s.base += n * a.c.heads;
       have = false;
@@ -151,7 +157,7 @@ struct KvWalk {
   }
 };
 
-// Every thread of the block (whole warps, at most 32) calls this once; `buf` holds an int per warp.  Row tiles that see
+// Every thread of the block (whole warps, at most 32) calls this once; `buf` holds two ints per warp.  Row tiles that see
 // nothing get their zeros here.
 template <int ROWS, int D>
 __device__ __forceinline__ KvShare kv_share(const KvAttnArgs& a, int* buf, KvShare* found, int* status) {
@@ -166,28 +172,41 @@ __device__ __forceinline__ KvShare kv_share(const KvAttnArgs& a, int* buf, KvSha
     else hi = mid - 1;
   }
   KvShare s{};
-  int mine = 0, before = 0;
+  int mine = 0, items = 0, before = 0;      // of this thread's row tiles: slot tiles, items; places before them
 #pragma unroll 1
-  for (int round = 0; round < 2; ++round) {      // how many tiles there are; where this CTA's begin
+  for (int round = 0; round < 2; ++round) {      // how many there are; where this CTA's begin
     if (round == 1) {
-      int incl = mine;
+      int sum = mine, num = items;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
-        const int x = __shfl_up_sync(0xffffffffu, incl, o);
-        if (lane >= o) incl += x;
+        const int x = __shfl_up_sync(0xffffffffu, sum, o), y = __shfl_up_sync(0xffffffffu, num, o);
+        if (lane >= o) {
+          sum += x;
+          num += y;
+        }
       }
-      if (lane == 31) buf[warp] = incl;
+      if (lane == 31) {
+        buf[2 * warp] = sum;
+        buf[2 * warp + 1] = num;
+      }
       __syncthreads();
-      int total = 0;
+      int total = 0, total_items = 0, before_items = 0;
 #pragma unroll 1
       for (int w = 0; w < threads / 32; ++w) {
-        if (w == warp) before = total;
-        total += buf[w];
+        if (w == warp) {
+          before = total;
+          before_items = total_items;
+        }
+        total += buf[2 * w];
+        total_items += buf[2 * w + 1];
       }
-      before += incl - mine;
       s.ctas = min(static_cast<int>(gridDim.x), total);
       const int c = blockIdx.x;
       if (c >= s.ctas) return s;      // nothing to do (the whole block)
+      s.cost = total >= kItemCost * s.ctas ? kItemCost : 0;      // (few tiles: one each, however dear the rest is)
+      total += s.cost * total_items;
+      before += sum - mine + s.cost * (before_items + num - items);
+      mine += s.cost * items;
       s.each = total / s.ctas;
       s.more = total - s.each * s.ctas;
       s.pos = c * s.each + min(c, s.more);
@@ -201,7 +220,7 @@ __device__ __forceinline__ KvShare kv_share(const KvAttnArgs& a, int* buf, KvSha
       while (t >= a.s.tile0[i + 1]) ++i;
       KvItem it;
       kv_item_rows<ROWS>(a, i, t - a.s.tile0[i], it);
-      const int n = it.span.n * a.c.heads;
+      const int n = it.span.n > 0 ? (it.span.n + s.cost) * a.c.heads : 0;
       if (round == 1) {
         if (s.pos < before + n) {
           s.base = before;
@@ -214,6 +233,7 @@ __device__ __forceinline__ KvShare kv_share(const KvAttnArgs& a, int* buf, KvSha
         continue;
       }
       mine += n;
+      items += n > 0 ? a.c.heads : 0;
       if (blockIdx.x == 0 && it.row_tile == 0 && a.lens[a.s.seq[i]] > a.max_len) record_error(status, PACE_ERR_INVALID_ARG, K_KV_ATTN);
       if (n == 0 && t % gridDim.x == blockIdx.x) {
 #pragma unroll 1
@@ -235,7 +255,7 @@ __device__ __forceinline__ KvShare kv_share(const KvAttnArgs& a, int* buf, KvSha
 // What CTA c tells the combine kernel: how many later CTAs its last item goes on in.
 __device__ __forceinline__ void kv_write_split(const KvAttnArgs& a, const KvShare& s, const KvItem& it) {
   KvSplit sp{it.i, it.row_tile, it.head, 0};
-  if (it.t0 == 0 && it.t1 < it.span.n) {   // CTA j takes part iff it begins before the item's end
+  if (it.t0 == 0 && it.t1 > 0 && it.t1 < it.span.n) {   // CTA j takes part iff it begins before the item's end
     const int c = blockIdx.x, end = (c + 1) * s.each + min(c + 1, s.more) + it.span.n - it.t1, wide = s.more * (s.each + 1);
     const int last = end <= wide ? (end + s.each) / (s.each + 1) : s.more + (end - wide + s.each - 1) / s.each;
     sp.followers = last - 1 - c;

@@ -61,7 +61,7 @@ struct alignas(16) DecodeCtl {
   int64_t out_at[NQ];
   float2 red[4][NQ];
   float scales[DecodeCfg<D, NQ>::STAGES][16];   // a tile's K scales, then its V scales
-  int scan[kWarps];
+  int scan[2 * kWarps];
   KvShare share;
   uint32_t tmem;
   int abort;

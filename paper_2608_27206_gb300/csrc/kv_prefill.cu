@@ -53,7 +53,7 @@ struct alignas(16) PrefillCtl {
   float scales[ST][16];
   float4 block[2][8];           // per block of 16 slots: K scale, log2(V scale), 1 / V scale
   uint32_t nan[2][4];           // slots of which some row sees a NaN value
-  int scan[kThreads / 32];
+  int scan[2 * kThreads / 32];
   KvShare share;
   uint32_t tmem;
   int abort;
