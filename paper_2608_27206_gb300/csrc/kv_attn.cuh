@@ -295,15 +295,23 @@ __device__ __forceinline__ void load_cols(uint32_t addr, uint32_t (&v)[N]) {
   }
 }
 
-// Warp 0 of a CTA: fetches the slot tiles of its share, a K and a V tile per stage (boxes of a page, at most 128 rows, each by
-// TMA; the tile's 8 K and 8 V scales by 4-byte copies).  full[s] counts the bytes, their announcement and 32 lanes' copies;
-// empty[s] one arrival.
-// `also()` runs after each tile's copies have been issued.
-template <int D, int ST, int ROWS, typename F>
-__device__ __forceinline__ void kv_fetch(const KvMaps& maps, const KvAttnArgs& a, KvWalk<ROWS>& walk, uint8_t* stages, uint64_t* full,
-                                         uint64_t* empty, float (*scales)[16], int* abort, int* status, F&& also) {
+// The rings that warp 0 fills: ST places of a K tile, SV of a V tile, `stride` bytes apart.
+struct KvRings {
+  uint8_t* k;
+  uint8_t* v;
+  int stride;
+  uint64_t* full;        // [ST] the tile's bytes, their announcement and 32 lanes' copies (33 arrivals)
+  uint64_t* empty;       // [ST]
+  uint64_t* v_empty;     // [SV] (null: as `empty`, SV = ST)
+  float (*scales)[16];   // [ST] a tile's K scales, then its V scales
+};
+
+// Warp 0 of a CTA: fetches the slot tiles of its share, K and V in boxes of a page, at most 128 rows, each by TMA; the tile's 8 K
+// and 8 V scales by 4-byte copies.
+template <int D, int ST, int SV, int ROWS>
+__device__ __forceinline__ void kv_fetch(const KvMaps& maps, const KvAttnArgs& a, KvWalk<ROWS>& walk, const KvRings& ring, int* abort,
+                                         int* status) {
   using namespace ptx;
-  constexpr int TILE = kKvTile * D;
   const int lane = threadIdx.x & 31;
   const int shift = min(a.c.page_shift, 7), box_rows = 1 << shift, boxes = kKvTile >> shift;
   const int tiles_per_load = 32 / boxes;     // a lane holds the page of one box
@@ -334,33 +342,31 @@ __device__ __forceinline__ void kv_fetch(const KvMaps& maps, const KvAttnArgs& a
         if (lane < boxes) record_error(status, PACE_ERR_INVALID_ARG, K_KV_ATTN);
         page = 0;      // (the sequence's results mean nothing then; the copy stays inside the cache)
       }
-      const int s = t % ST, round = t / ST;
-      if (round > 0) {
-        const bool ok = __all_sync(0xffffffffu, kv_wait(smem_u32(&empty[s]), (round - 1) & 1));
-        if (!ok) {
-          if (lane == 0) stop(abort, status);
-          break;
-        }
+      const int s = t % ST, v = t % SV;
+      bool ok = t < ST || kv_wait(smem_u32(&ring.empty[s]), (t / ST - 1) & 1);
+      if (ring.v_empty != nullptr) ok = ok && (t < SV || kv_wait(smem_u32(&ring.v_empty[v]), (t / SV - 1) & 1));
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) {
+        if (lane == 0) stop(abort, status);
+        break;
       }
       const int slot0 = it.span.tile(i) * kKvTile;
-      uint8_t* dst = stages + s * 2 * TILE;
       const int n_there = __popc(__ballot_sync(0xffffffffu, there && lane < boxes));
-      if (lane == 0) mbar_arrive_expect_tx(smem_u32(&full[s]), 2 * n_there * box_rows * D);
+      if (lane == 0) mbar_arrive_expect_tx(smem_u32(&ring.full[s]), 2 * n_there * box_rows * D);
       // scale j (K: 0-7, V: 8-15) of the tile: block j % 8, in box (j % 8) * 16 / box_rows
       const int blk = lane & 7;
       const int bpage = __shfl_sync(0xffffffffu, page, blk * kKvBlock >> shift);
       const int row = (slot0 + blk * kKvBlock) & ((1 << a.c.page_shift) - 1);
       if (lane < 16 && slot0 + blk * kKvBlock <= last)
-        cp_async4(smem_u32(&scales[s][lane]),
+        cp_async4(smem_u32(&ring.scales[s][lane]),
                   (lane < 8 ? a.c.ks : a.c.vs) + bpage * a.c.scale_stride + (static_cast<int64_t>(it.head) << (a.c.page_shift - 4)) + row / kKvBlock);
-      cp_async_arrive(smem_u32(&full[s]));
+      cp_async_arrive(smem_u32(&ring.full[s]));
       __syncwarp();
       if (lane < boxes && there) {
         const int y = (it.head << a.c.page_shift) + ((slot0 + lane * box_rows) & ((1 << a.c.page_shift) - 1));
-        tma_load_3d(smem_u32(dst + lane * box_rows * D), &maps.k, 0, y, page, smem_u32(&full[s]));
-        tma_load_3d(smem_u32(dst + TILE + lane * box_rows * D), &maps.v, 0, y, page, smem_u32(&full[s]));
+        tma_load_3d(smem_u32(ring.k + s * ring.stride + lane * box_rows * D), &maps.k, 0, y, page, smem_u32(&ring.full[s]));
+        tma_load_3d(smem_u32(ring.v + v * ring.stride + lane * box_rows * D), &maps.v, 0, y, page, smem_u32(&ring.full[s]));
       }
-      also();
     }
   }
 }

@@ -126,7 +126,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
   walk.begin(share);
 
   if (warp == 0) {
-    kv_fetch<D, ST>(maps, a, walk, sKV, ctl->full, ctl->empty, ctl->scales, &ctl->abort, status, [] {});
+    kv_fetch<D, ST, ST>(maps, a, walk, KvRings{sKV, sKV + C::TILE, 2 * C::TILE, ctl->full, ctl->empty, nullptr, ctl->scales}, &ctl->abort, status);
   } else if (warp == 1) {
     // ---- products ----------------------------------------------------------------------------
     if (lane == 0) {

@@ -5,7 +5,7 @@
 // times 4; each row is first brought under 256 by a power of two).  Two e4m3 products cost what one of 16 bits would, at half the
 // shared memory and with no work on K.  P V is formed in f16, which holds every e4m3 number, and a weight to 11 bits.
 //
-// A TMEM lane of S is a query row and one thread's.  With x the score in base 2 and vs the V scale of a slot's block, the row's
+// A TMEM lane of S is a query row; two threads own it, 64 columns each.  With x the score in base 2 and vs the V scale of a slot's block, the row's
 // weights are P = 2^(x + log2(vs) - w) and l = sum P / vs; both scales are constants of 16 columns, so a weight costs
 // one multiply-add, one exponential, one addition and half a conversion.  w is a whole number, the maximum of the row's first
 // 64 slots rounded up, and then stays: f16 has room for weights up to 2^15 above it, and below it 14 binary orders keep all their bits
@@ -16,7 +16,7 @@
 // What bounds it is the tensor pipe: 1092 clocks per 128 x 128 tile at D = 128, against 512 clocks of exponentials.  Two row
 // tiles A and B share every K and V tile and take turns: while one's weights are worked out, the other's products run.  P overwrites
 // its S in TMEM.  Roles of a CTA (one per SM): warp 0 fetches, warp 1 issues the MMAs, warps 2-3 turn V into f16 (they also
-// see to NaN that must not reach rows that do not look at it), warps 4-7 and 8-11 own the rows of A and B.
+// see to NaN that must not reach rows that do not look at it), warps 4-11 and 12-19 own the rows of A and B.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -29,14 +29,15 @@ namespace {
 
 using namespace ptx;
 
-constexpr int kThreads = 384;
+constexpr int kThreads = 640;
 constexpr float kMost = 32768.f;   // sum of 64 weights at which w moves
 constexpr uint32_t kTmem = 512;    // S of A and B, then O of A and B, 128 columns each
 
 template <int D>
 struct PrefillCfg {
   static constexpr int TILE = kKvTile * D;
-  static constexpr int STAGES = D == 128 ? 3 : 6;
+  static constexpr int STAGES = D == 128 ? 3 : 6;       // places of K tiles,
+  static constexpr int VSTAGES = D == 128 ? 2 : 4;      // of V tiles
   static constexpr int QTILE = 128 * D;                 // hi or lo codes of a row tile
   static constexpr int VCHUNK = kKvTile * 128;          // f16 V: 64 columns of every slot, 128 bytes each
   static constexpr int VTILE = VCHUNK * D / 64;
@@ -48,11 +49,13 @@ struct PrefillCfg {
 
 template <int D>
 struct alignas(16) PrefillCtl {
-  static constexpr int ST = PrefillCfg<D>::STAGES;
-  uint64_t full[ST], empty[ST], ready[2], vfree[2], s_full[2], p_full[2], q_full[2], o_full[2];
+  static constexpr int ST = PrefillCfg<D>::STAGES, SV = PrefillCfg<D>::VSTAGES;
+  uint64_t full[ST], empty[ST], v_empty[SV], ready[2], vfree[2], s_full[2], p_full[2], q_full[2], o_full[2];
   float scales[ST][16];
   float4 block[2][8];           // per block of 16 slots: K scale, log2(V scale), 1 / V scale
   uint32_t nan[2][4];           // slots of which some row sees a NaN value
+  float2 xchg[2][2][128];       // between a row's two owners
+  KvWalk<kManyRows> walk[16];   // of the rows' owners, a warp each: their registers are for scores
   int scan[2 * kThreads / 32];
   KvShare share;
   uint32_t tmem;
@@ -98,8 +101,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
   constexpr int ST = C::STAGES;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  uint8_t* sKV = smem;                             // stages of a K tile and a V tile, as codes
-  uint8_t* sV = sKV + ST * 2 * C::TILE;            // two V tiles in f16
+  uint8_t* sK = smem;                              // K tiles, as codes
+  uint8_t* sC = sK + ST * C::TILE;                 // V tiles, as codes
+  uint8_t* sV = sC + C::VSTAGES * C::TILE;         // two V tiles in f16
   uint8_t* sQ = sV + 2 * C::VTILE;                 // A hi, A lo, B hi, B lo
   auto* ctl = reinterpret_cast<PrefillCtl<D>*>(sQ + 4 * C::QTILE);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -123,14 +127,15 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
     prefetch_tensormap(&maps.v);
     for (int s = 0; s < ST; ++s) {
       mbar_init(full(s), 33);
-      mbar_init(empty(s), 3);       // S has been formed, two warps have read V
+      mbar_init(empty(s), 1);
     }
+    for (int s = 0; s < C::VSTAGES; ++s) mbar_init(smem_u32(&ctl->v_empty[s]), 2);
     for (int i = 0; i < 2; ++i) {
       mbar_init(ready(i), 2);
       mbar_init(vfree(i), 1);
       mbar_init(s_full(i), 1);
-      mbar_init(p_full(i), 4);
-      mbar_init(q_full(i), 4);
+      mbar_init(p_full(i), 8);
+      mbar_init(q_full(i), 8);
       mbar_init(o_full(i), 1);
     }
     fence_mbar_init();
@@ -144,17 +149,19 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
   __syncthreads();
   tc_fence_after_sync();
   const uint32_t tmem = ctl->tmem;
-  KvWalk<kManyRows> walk;
-  walk.begin(share);
-  const KvItem& it = walk.it;
 
   if (warp == 0) {
-    kv_fetch<D, ST>(maps, a, walk, sKV, ctl->full, ctl->empty, ctl->scales, &ctl->abort, status, [] {});
+    KvWalk<kManyRows> walk;
+    walk.begin(share);
+    kv_fetch<D, ST, C::VSTAGES>(maps, a, walk, KvRings{sK, sC, C::TILE, ctl->full, ctl->empty, ctl->v_empty, ctl->scales}, &ctl->abort, status);
   } else if (warp == 1) {
     // ---- products: of A and B in turn, so that those of one run while the weights of the other are worked out --------------
+    KvWalk<kManyRows> walk;
+    walk.begin(share);
+    const KvItem& it = walk.it;
     const uint32_t issue = elect_one();
     const uint64_t dq = smem_desc(smem_u32(sQ), 16, C::GROUP, C::SWIZZLE);
-    const uint64_t dk = smem_desc(smem_u32(sKV), 16, C::GROUP, C::SWIZZLE);
+    const uint64_t dk = smem_desc(smem_u32(sK), 16, C::GROUP, C::SWIZZLE);
     const uint64_t dv = smem_desc(smem_u32(sV), C::VCHUNK, 1024, 2);
     int t = 0, rounds_a = 0, rounds_b = 0, items_a = 0, items_b = 0;      // slot tiles; weights taken and items, of a row tile
     bool ok = true;
@@ -163,27 +170,28 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
       return ok;
     };
     while (ok && walk.next(a)) {
-      const int n = it.t1 - it.t0;
-      const bool two = it.rows > 128;
+      const int n = it.t1 - it.t0, two = it.rows > 128;
 #pragma unroll 1
       for (int j = 0; ok && j <= n; ++j) {      // P V of slot tile j - 1, then S of slot tile j
         const int u = t + j - 1, s = (t + j) % ST;
-        if (j < n && !wait(full(s), (t + j) / ST)) break;
-        if (j > 0 && !wait(ready(u & 1), u >> 1)) break;
 #pragma unroll 1
-        for (int i = 0; i <= static_cast<int>(two); ++i) {
+        for (int i = 0; i <= two; ++i) {
           const int round = j > 0 ? (i == 0 ? rounds_a++ : rounds_b++) : i == 0 ? items_a++ : items_b++;
+          if (j > 0 && i == 0 && !wait(ready(u & 1), u >> 1)) break;
           if (!wait(j > 0 ? p_full(i) : q_full(i), round)) break;
           tc_fence_after_sync();
-          if (j > 0) {
+          if (j > 0) {      // (the weights of the second 64 slots begin 64 columns on)
             const uint64_t v = dv + static_cast<uint64_t>((u & 1) * (C::VTILE >> 4));
 #pragma unroll
             for (int k = 0; k < kKvTile / 16; ++k)
-              mma_f16_ts(tmem + 256 + i * 128, tmem + i * 128 + k * 8, v + static_cast<uint64_t>(k * (2048 >> 4)), C::IDESC_O, j > 1 || k > 0, issue);
+              mma_f16_ts(tmem + 256 + i * 128, tmem + i * 128 + (k & 3) * 8 + (k >> 2) * 64, v + static_cast<uint64_t>(k * (2048 >> 4)), C::IDESC_O,
+                         j > 1 || k > 0, issue);
             if (issue && j == n) mma_commit(o_full(i));
           }
           if (j < n) {
-            const uint64_t q = dq + static_cast<uint64_t>(i * 2 * (C::QTILE >> 4)), k0 = dk + static_cast<uint64_t>(s * 2 * (C::TILE >> 4));
+            if (i == 0 && !wait(full(s), (t + j) / ST)) break;
+            tc_fence_after_sync();
+            const uint64_t q = dq + static_cast<uint64_t>(i * 2 * (C::QTILE >> 4)), k0 = dk + static_cast<uint64_t>(s * (C::TILE >> 4));
 #pragma unroll
             for (int part = 0; part < 2; ++part)
 #pragma unroll
@@ -204,6 +212,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
     __syncwarp();
   } else if (warp < 4) {
     // ---- V of a slot tile as f16, and the tile's constants ---------------------------------------
+    KvWalk<kManyRows> walk;
+    walk.begin(share);
+    const KvItem& it = walk.it;
     int t = 0;
     bool ok = true;
     while (ok && walk.next(a)) {
@@ -226,7 +237,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
         for (int part = warp - 2; part < 4; part += 2) {
           const int row = part * 32 + lane, slot = slot0 + row;      // a slot of the tile
           const bool any = slot <= it.p_last && (a.window <= 0 || slot > it.p_first - a.window || slot < a.sinks);
-          const uint8_t* src = sKV + (2 * s + 1) * C::TILE + row * D;
+          const uint8_t* src = sC + (t % C::VSTAGES) * C::TILE + row * D;
           uint4 u[D / 16];
 #pragma unroll
           for (int e = 0; e < D / 16; ++e) u[e] = *reinterpret_cast<const uint4*>(src + (e ^ (D == 128 ? row & 7 : (row >> 1) & 3)) * 16);
@@ -261,19 +272,31 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
         __syncwarp();
         if (lane == 0) {
           mbar_arrive(ready(b));
-          mbar_arrive(empty(s));
+          mbar_arrive(smem_u32(&ctl->v_empty[t % C::VSTAGES]));
         }
       }
     }
     if (!ok && lane == 0) stop(&ctl->abort, status);
   } else {
-    // ---- weights -----------------------------------------------------------------------------
-    const int i = (warp - 4) >> 2, quad = warp & 3, me = quad * 32 + lane;
+    // ---- weights: a row has two owners, 64 columns of S (and half of D) each ---------------------
+    const int rw = warp - 4, i = rw >> 3, half = rw >> 2 & 1, quad = warp & 3, me = quad * 32 + lane;
     const uint32_t lanes = static_cast<uint32_t>(quad * 32) << 16;
-    const uint32_t sS = tmem + lanes + i * 128, sO = tmem + lanes + 256 + i * 128;
+    const uint32_t sS = tmem + lanes + i * 128 + half * 64, sO = tmem + lanes + 256 + i * 128 + half * (D / 2);
+    const uint32_t pair = 1 + i * 4 + quad;      // barrier of the two warps that own the same rows
+    // Both come here; both leave when one has given up, so that neither waits for the other.
+    auto meet = [&](bool flag) { return named_barrier_any(pair, 64, flag); };
+    KvWalk<kManyRows>& walk = ctl->walk[rw];
+    const KvItem& it = walk.it;
+    if (lane == 0) walk.begin(share);
+    auto next = [&] {
+      __syncwarp();
+      const int more = lane == 0 && walk.next(a);
+      __syncwarp();
+      return __shfl_sync(0xffffffffu, more, 0) != 0;
+    };
     int t = 0, s_rounds = 0, o_rounds = 0;
     bool ok = true;
-    while (ok && walk.next(a)) {
+    while (ok && next()) {
       if (i == 1 && it.rows <= 128) {
         t += it.t1 - it.t0;
         continue;
@@ -282,19 +305,16 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
       const bool real = row < it.rows;
       auto slot_of = [&](int r) { return it.p0 + static_cast<int>(a.by_group(it.row0 + min(r, it.rows - 1))); };
       const int p = slot_of(row), p_lo = slot_of(i * 128), p_hi = slot_of(i * 128 + 127);      // of the row, of the tile's first and last
-      float c = 0.f;            // scale2 * the row's power of two
+      constexpr int LANES = D / 16, STEP = 32 / LANES;      // lanes that move this half of a row, rows at a time
+      const int sub = lane / LANES, part = lane % LANES;
+      float c;                  // scale2 * the row's power of two
       {
-        // q as hi and lo codes.  D / 8 lanes read a row, 16 bytes each; it takes the places of its codes (128 or 64 bytes in the
-        // hi tile, the rest in the lo tile) until its owner turns it into them
-        constexpr int LANES = D / 8, STEP = 32 / LANES;
-        const int sub = lane / LANES, part = lane % LANES;
-        uint8_t* tile = sQ + i * 2 * C::QTILE;
-        auto place = [&](int row, int chunk) {      // of a row's 16-byte chunk: the swizzle of the operand tiles
-          constexpr int PER = D / 16;
-          return tile + (chunk >= PER ? C::QTILE : 0) + row * D + ((chunk % PER) ^ (D == 128 ? row & 7 : (row >> 1) & 3)) * 16;
-        };
+        // q as hi and lo codes.  Half a row waits in the hi tile's place of the row, the other in the lo tile's, until its owners
+        // have read it and turn it into codes
+        uint8_t* tile = sQ + i * 2 * C::QTILE + quad * 32 * D;
+        auto place = [&](int r, int chunk) { return r * D + (chunk ^ (D == 128 ? r & 7 : (r >> 1) & 3)) * 16; };      // the operands' swizzle
         {
-          const unsigned long long from = real ? reinterpret_cast<unsigned long long>(kv_query(a, it, i * 128 + me, D)) : 0;
+          const unsigned long long from = real ? reinterpret_cast<unsigned long long>(kv_query(a, it, row, D) + half * (D / 2)) : 0;
           uint4 u[32 / STEP];
 #pragma unroll
           for (int k = 0; k < 32 / STEP; ++k) {
@@ -302,73 +322,81 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
             u[k] = src != 0 ? *(reinterpret_cast<const uint4*>(src) + part) : make_uint4(0, 0, 0, 0);
           }
 #pragma unroll
-          for (int k = 0; k < 32 / STEP; ++k) *reinterpret_cast<uint4*>(place(quad * 32 + k * STEP + sub, part)) = u[k];
+          for (int k = 0; k < 32 / STEP; ++k) *reinterpret_cast<uint4*>(tile + half * C::QTILE + place(k * STEP + sub, part)) = u[k];
         }
         __syncwarp();
-        uint4 u[D / 8];
+        uint4 u[D / 16];
         uint32_t most = 0;      // largest magnitude, as the bits of two bf16 without their signs
 #pragma unroll
-        for (int e = 0; e < D / 8; ++e) {
-          u[e] = *reinterpret_cast<const uint4*>(place(me, e));
+        for (int e = 0; e < D / 16; ++e) {
+          u[e] = *reinterpret_cast<const uint4*>(tile + half * C::QTILE + place(lane, e));
           most = __vmaxu2(__vmaxu2(most, __vmaxu2(u[e].x & 0x7FFF7FFFu, u[e].y & 0x7FFF7FFFu)), __vmaxu2(u[e].z & 0x7FFF7FFFu, u[e].w & 0x7FFF7FFFu));
         }
-        const uint32_t top = max(most & 0xFFFFu, most >> 16);
+        uint32_t top = max(most & 0xFFFFu, most >> 16);
+        ctl->xchg[i][half][me].x = __uint_as_float(top);
+        meet(false);
+        top = max(top, __float_as_uint(ctl->xchg[i][half ^ 1][me].x));
         const bool fin = top < 0x7F80u;
         const int e2 = fin ? max(static_cast<int>(top >> 7) - 127 - 7, -110) : 0;      // top 2^-e2 in [128, 256)
         const float inv = fin ? __uint_as_float(static_cast<uint32_t>(127 - e2) << 23) : NAN;      // (a row that is not finite: NaN throughout)
         c = a.scale2 * __uint_as_float(static_cast<uint32_t>(127 + e2) << 23);
 #pragma unroll
-        for (int e = 0; e < D / 16; ++e) {      // 16 elements at a time: by way of f16, which holds them (and 2^-24 where e4m3 ends at 2^-9)
+        for (int e = 0; e < D / 32; ++e) {      // 16 elements at a time: by way of f16, which holds them (and 2^-24 where e4m3 ends at 2^-9)
           const uint32_t w[8] = {u[2 * e].x, u[2 * e].y, u[2 * e].z, u[2 * e].w, u[2 * e + 1].x, u[2 * e + 1].y, u[2 * e + 1].z, u[2 * e + 1].w};
           uint32_t hi[4], lo[4];
 #pragma unroll
           for (int k = 0; k < 4; ++k) split_e4m3(pair_f16(w[2 * k], inv), pair_f16(w[2 * k + 1], inv), hi[k], lo[k]);
-          *reinterpret_cast<uint4*>(place(me, e)) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-          *reinterpret_cast<uint4*>(place(me, e + D / 16)) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+          uint8_t* dst = tile + place(lane, half * (D / 32) + e);
+          *reinterpret_cast<uint4*>(dst) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+          *reinterpret_cast<uint4*>(dst + C::QTILE) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
         }
         fence_proxy_async_shared();
         __syncwarp();
         if (lane == 0) mbar_arrive(q_full(i));
       }
       float w = kNone, l = 0.f;
+      const int n_tiles = it.t1 - it.t0;
 #pragma unroll 1
-      for (int j = it.t0; j < it.t1; ++j, ++t, ++s_rounds) {
-        const int b = t & 1, slot0 = it.span.tile(j) * kKvTile;
+      for (int j = 0; j < n_tiles; ++j, ++t, ++s_rounds) {
+        const int b = t & 1, slot0 = it.span.tile(it.t0 + j) * kKvTile;
         // (S first: a row tile that left items out may be rounds ahead of the others until its products run)
         ok = kv_wait(s_full(i), s_rounds & 1) && kv_wait(ready(b), (t >> 1) & 1);
         ok = __all_sync(0xffffffffu, ok);
-        if (!ok) break;
         tc_fence_after_sync();
-        const bool whole = kv_whole(slot0, p_lo, p_hi, a.window, a.sinks);
-        if (!whole) {      // what the row does not see becomes -inf: all but columns up to `to` that are past `from` or before `few`
-          const int to = p - slot0, from = a.window > 0 ? p - a.window - slot0 : -1, few = a.window > 0 ? a.sinks - slot0 : kKvTile;
+        const float4* block = &ctl->block[b][4 * half];
+        if (!kv_whole(slot0, p_lo, p_hi, a.window, a.sinks)) {      // what the row does not see becomes -inf
+          // (it sees slots up to p that are past `from` or before `few`)
+          const int base = slot0 + half * 64, from = a.window > 0 ? p - a.window : -1, few = a.window > 0 ? a.sinks : INT32_MAX;
+          auto below = [](int n) { return n >= 32 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << n) - 1u; };      // columns 0 .. n - 1
 #pragma unroll 1
-          for (int q = 0; q < 4; ++q) {
+          for (int q = 0; q < 2; ++q) {
+            const int at = base + 32 * q;
+            const uint32_t see = below(p + 1 - at) & (~below(from + 1 - at) | below(few - at)), nan = ctl->nan[b][2 * half + q] & see;
+            if (__all_sync(0xffffffffu, (see & ~nan) == 0xFFFFFFFFu)) continue;
             uint32_t x[32];
             load_cols(sS + 32 * q, x);
-            const uint32_t nan = ctl->nan[b][q];
 #pragma unroll
-            for (int e = 0; e < 32; ++e) {
-              const int col = 32 * q + e;
-              if (nan >> e & 1) x[e] = 0x7FC00000u;
-              if (col > to || (col <= from && col >= few)) x[e] = 0xFF800000u;
+            for (int e = 0; e < 32; ++e) x[e] = see >> e & 1 ? x[e] : 0xFF800000u;
+            if (__any_sync(0xffffffffu, nan != 0)) {
+#pragma unroll
+              for (int e = 0; e < 32; ++e) x[e] = nan >> e & 1 ? 0x7FC00000u : x[e];
             }
             tmem_st_32x32b(sS + 32 * q, x);
           }
           tmem_wait_st();
         }
+        uint32_t words[32];
+        bool again;
 #pragma unroll 1
-        for (int q = 0; q < 2; ++q) {      // 64 columns
-          const float4* block = &ctl->block[b][4 * q];
-          uint32_t words[32];
-#pragma unroll 1
-          while (true) {
-            uint32_t x[64];
-            load_cols(sS + 64 * q, x);
-            float sum = 0.f, dl = 0.f;
+        do {
+          float sum = 0.f, dl = 0.f;
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {      // a block's columns
-              const float4 k = block[g];
+          for (int q = 0; q < 2; ++q) {      // 32 columns
+            uint32_t x[32];
+            load_cols(sS + 32 * q, x);
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {      // a block's columns
+              const float4 k = block[2 * q + g];
               const float mul = fmaxf(k.x * c, 1e-37f), add = k.y - w;      // (not 0: -inf stays what it is)
               const float2 mul2 = make_float2(mul, mul), add2 = make_float2(add, add);
               float2 s0 = make_float2(0.f, 0.f), s1 = s0;
@@ -381,54 +409,55 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                 y1 = make_float2(ex2_approx(y1.x), ex2_approx(y1.y));
                 s0 = fadd2(s0, y0);
                 s1 = fadd2(s1, y1);
-                words[8 * g + e / 2] = f16x2(y0.x, y0.y);
-                words[8 * g + e / 2 + 1] = f16x2(y1.x, y1.y);
+                words[16 * q + 8 * g + e / 2] = f16x2(y0.x, y0.y);
+                words[16 * q + 8 * g + e / 2 + 1] = f16x2(y1.x, y1.y);
               }
               s0 = fadd2(s0, s1);
-              const float part = s0.x + s0.y;
-              sum += part;
-              dl = fmaf(part, k.z, dl);
+              const float all = s0.x + s0.y;
+              sum += all;
+              dl = fmaf(all, k.z, dl);
             }
-            if (!__any_sync(0xffffffffu, sum >= kMost)) {
-              l += dl;
-              break;
-            }
-            // w moves to the maximum, in the rows that need it; the tile's weights so far, O (whose products so far have
-            // completed: S came after them) and l follow, and these columns start again
-            float top = kNone;
+          }
+          again = meet(sum >= kMost || !ok);
+          if (!again) {
+            l += dl;
+            break;
+          }
+          // w moves to the maximum, in the rows that need it, and O (whose products so far have completed: S came after them)
+          // and l with it; the weights start again from S, which is still whole
+          float top = kNone;
 #pragma unroll 1
-            for (int g = 0; g < 4; ++g) {
-              uint32_t y[16];
-              load_cols(sS + 64 * q + 16 * g, y);
+          for (int g = 0; g < 4; ++g) {
+            uint32_t x[16];
+            load_cols(sS + 16 * g, x);
+            const float4 k = block[g];
 #pragma unroll
-              for (int e = 0; e < 16; ++e) top = fmaxf(top, fmaf(__uint_as_float(y[e]), fmaxf(block[g].x * c, 1e-37f), block[g].y));
-            }
-            const float now = sum >= kMost ? ceilf(top) : w, f = ex2_approx(w - now);
-            w = now;
-            l *= f;
-            tmem_wait_st();
-            if (q == 1) {
-              load_cols(sS, words);
-#pragma unroll
-              for (int k = 0; k < 32; ++k) {
-                const float2 z = __half22float2(*reinterpret_cast<const __half2*>(&words[k]));      // (f itself may be below f16)
-                words[k] = f16x2(z.x * f, z.y * f);
-              }
-              tmem_st_32x32b(sS, words);
-            }
-            if (j > it.t0) {
+            for (int e = 0; e < 16; ++e) top = fmaxf(top, fmaf(__uint_as_float(x[e]), fmaxf(k.x * c, 1e-37f), k.y));
+          }
+          ctl->xchg[i][half][me] = make_float2(top, sum >= kMost ? 1.f : 0.f);
+          if (meet(!ok)) break;
+          const float2 other = ctl->xchg[i][half ^ 1][me];
+          if (meet(false)) break;      // (both have read; the flag is never set)
+          const float now = sum >= kMost || other.y != 0.f ? ceilf(fmaxf(top, other.x)) : w, f = ex2_approx(w - now);
+          w = now;
+          l *= f;
+          if (j > 0) {
 #pragma unroll 1
-              for (int e = 0; e < D / 32; ++e) {
-                load_cols(sO + 32 * e, words);
+            for (int e = 0; e < D / 32; ++e) {
+              uint32_t x[16];
+              load_cols(sO + 16 * e, x);
 #pragma unroll
-                for (int k = 0; k < 32; ++k) words[k] = __float_as_uint(__uint_as_float(words[k]) * f);
-                tmem_st_32x32b(sO + 32 * e, words);
-              }
+              for (int k = 0; k < 16; ++k) x[k] = __float_as_uint(__uint_as_float(x[k]) * f);
+              tmem_st_32x32b(sO + 16 * e, x);
             }
             tmem_wait_st();
           }
-          tmem_st_32x32b(sS + 32 * q, words);
+        } while (true);
+        if (again) {      // given up, both
+          ok = false;
+          break;
         }
+        tmem_st_32x32b(sS, words);
         tmem_wait_st();
         tc_fence_before_sync();
         __syncwarp();
@@ -436,54 +465,60 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
       }
       if (!ok) break;
       // ---- the item's (part of the) output -----------------------------------------------------
-      ok = __all_sync(0xffffffffu, kv_wait(o_full(i), o_rounds & 1));
+      ctl->xchg[i][half][me].x = l;
+      const bool done = __all_sync(0xffffffffu, kv_wait(o_full(i), o_rounds & 1));
       ++o_rounds;
-      if (!ok) break;
+      if (meet(!done)) {
+        ok = false;
+        break;
+      }
+      l = half == 0 ? l + ctl->xchg[i][1][me].x : ctl->xchg[i][0][me].x + l;
       tc_fence_after_sync();
       const float inv = l == 0.f ? 0.f : 1.f / l, lse2 = l == 0.f ? -INFINITY : w + log2f(l);
       const bool complete = it.t0 == 0 && it.t1 == it.span.n;
-      const int64_t at = kv_out_row(a, it, real ? row : 0);
       const int64_t slot = (2 * static_cast<int64_t>(blockIdx.x) + (it.t0 == 0 ? 1 : 0)) * kManyRows + row;
-      // complete rows go out by way of the q tile, which is done with (this warp's rows only), so that lanes write side by side
-      uint8_t* stage = sQ + i * 2 * C::QTILE + quad * 32 * 2 * D;
+      const int64_t at = complete ? kv_out_row(a, it, real ? row : 0) : slot;
+      // complete rows go out by way of the q tile, which is done with (this half of this warp's rows, D bytes each), so that lanes write
+      // side by side
+      uint8_t* stage = sQ + i * 2 * C::QTILE + half * C::QTILE + quad * 32 * D;
+      auto place = [&](int r, int chunk) { return r * D + (chunk ^ (D == 128 ? r & 7 : (r >> 1) & 3)) * 16; };
 #pragma unroll 1
-      for (int q = 0; q < D / 32; ++q) {
+      for (int q = 0; q < D / 64; ++q) {
         uint32_t o[32];
         load_cols(sO + 32 * q, o);
         // (a row that saw nothing here is zero, whatever its accumulator holds)
-        auto v = [&](int e) { return l == 0.f ? 0.f : __uint_as_float(o[e]) * inv; };
+#pragma unroll
+        for (int e = 0; e < 32; ++e) o[e] = l == 0.f ? 0u : __float_as_uint(__uint_as_float(o[e]) * inv);
         if (complete) {
 #pragma unroll
           for (int e = 0; e < 32; e += 8) {
             uint32_t x[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-              x[k] = static_cast<uint32_t>(__bfloat16_as_ushort(__float2bfloat16_rn(v(e + 2 * k)))) |
-                     static_cast<uint32_t>(__bfloat16_as_ushort(__float2bfloat16_rn(v(e + 2 * k + 1)))) << 16;
-            *reinterpret_cast<uint4*>(stage + lane * 2 * D + ((4 * q + e / 8) ^ (lane & 7)) * 16) = make_uint4(x[0], x[1], x[2], x[3]);
+              asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(x[k]) : "f"(__uint_as_float(o[e + 2 * k + 1])), "f"(__uint_as_float(o[e + 2 * k])));
+            *reinterpret_cast<uint4*>(stage + place(lane, 4 * q + e / 8)) = make_uint4(x[0], x[1], x[2], x[3]);
           }
         } else if (real) {
 #pragma unroll
-          for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(a.part + slot * D + 32 * q + e) = make_float4(v(e), v(e + 1), v(e + 2), v(e + 3));
+          for (int e = 0; e < 32; e += 4)
+            *reinterpret_cast<uint4*>(a.part + slot * D + half * (D / 2) + 32 * q + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
         }
-      }
-      if (complete) {
-        constexpr int LANES = D / 8, STEP = 32 / LANES;
-        __syncwarp();
-        const unsigned long long to = real ? reinterpret_cast<unsigned long long>(a.out + at * D) : 0;
-#pragma unroll 4
-        for (int k = 0; k < 32; k += STEP) {
-          const int rw = k + lane / LANES, part = lane % LANES;
-          const unsigned long long dst = __shfl_sync(0xffffffffu, to, rw);
-          if (dst != 0) *(reinterpret_cast<uint4*>(dst) + part) = *reinterpret_cast<const uint4*>(stage + rw * 2 * D + (part ^ (rw & 7)) * 16);
-        }
-        __syncwarp();
       }
       tc_fence_before_sync();
-      if (real) {
+      if (complete) {
+        __syncwarp();
+        const unsigned long long to = real ? reinterpret_cast<unsigned long long>(a.out + at * D + half * (D / 2)) : 0;
+#pragma unroll 4
+        for (int k = 0; k < 32; k += STEP) {
+          const unsigned long long dst = __shfl_sync(0xffffffffu, to, k + sub);
+          if (dst != 0) *(reinterpret_cast<uint4*>(dst) + part) = *reinterpret_cast<const uint4*>(stage + place(k + sub, part));
+        }
+      }
+      if (real && half == 0) {
         if (!complete) a.part_lse[slot] = lse2;
         else if (a.lse != nullptr) a.lse[at] = lse2 * 0.69314718055994531f;
       }
+      meet(false);      // the exchange and the q tile have been read
     }
     if (!ok && lane == 0) stop(&ctl->abort, status);
     if (threadIdx.x == 4 * 32) kv_write_split(a, share, it);
@@ -503,7 +538,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
 template <int D>
 pace_status_t run_prefill(const KvMaps& maps, const KvAttnArgs& a, unsigned grid, int* status, cudaStream_t stream) {
   using C = PrefillCfg<D>;
-  constexpr size_t smem = 1024 + C::STAGES * 2 * C::TILE + 2 * C::VTILE + 4 * C::QTILE + sizeof(PrefillCtl<D>);
+  constexpr size_t smem = 1024 + (C::STAGES + C::VSTAGES) * C::TILE + 2 * C::VTILE + 4 * C::QTILE + sizeof(PrefillCtl<D>);
   static_assert(smem <= 227 * 1024, "shared memory");
   static DeviceOnce once;
   int dev = 0;
