@@ -267,11 +267,14 @@ struct KvMaps {
   CUtensorMap k, v;
 };
 
-// mbar_wait with its loop out of line: the kernels here wait in many places, and instructions that are not run push those that
-// are out of the instruction cache.
-static __device__ __noinline__ bool kv_wait_loop(uint32_t bar, uint32_t parity) { return ptx::mbar_wait(bar, parity, kWaitLimitNs); }
+// mbar_wait with its limit counted in tries (16 million, a quarter of a second at the very least): a few instructions, where the kernels
+// here wait in many places and instructions that are not run push those that are out of the instruction cache.
 __device__ __forceinline__ bool kv_wait(uint32_t bar, uint32_t parity) {
-  return ptx::mbar_try_wait(bar, parity) || kv_wait_loop(bar, parity);
+  int left = 1 << 24;
+#pragma unroll 1
+  while (!ptx::mbar_try_wait(bar, parity))
+    if (--left == 0) return false;
+  return true;
 }
 
 // A role that gives up on a wait says so here; the others leave as their own waits run out.

@@ -133,19 +133,18 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
       const uint64_t dq = smem_desc(smem_u32(sQ), 16, C::GROUP, C::SWIZZLE);
       // V^T: 8 slots of D contiguous codes per repeat.  (D = 64 fills lanes 0-63; the other half of the 128 rows reads
       // the same codes again and is not used.)
-      uint64_t dk[2], dp[2];
-      dk[0] = smem_desc(smem_u32(sKV), 16, C::GROUP, C::SWIZZLE);
-      dk[1] = smem_desc(smem_u32(sKV), 0, C::GROUP, C::SWIZZLE);
-      for (int p = 0; p < 2; ++p) dp[p] = smem_desc(smem_u32(sP + p * C::PBYTES), 8 * 16, NQ == 8 ? 8 * 16 : 16 * kKvTile, 0);
+      const uint64_t dk = smem_desc(smem_u32(sKV), 16, C::GROUP, C::SWIZZLE);
+      const uint64_t dv = smem_desc(smem_u32(sKV + C::TILE), 0, C::GROUP, C::SWIZZLE);
+      const uint64_t dp = smem_desc(smem_u32(sP), 8 * 16, NQ == 8 ? 8 * 16 : 16 * kKvTile, 0);
       int t = 0, items = 0;
       bool ok = true;
       auto weigh = [&](int u, bool first) {     // O += V^T P of tile u
         if (!kv_wait(p_full(u & 1), (u >> 1) & 1)) return false;
         tc_fence_after_sync();
-        const uint64_t v = dk[1] + static_cast<uint64_t>(((u % ST) * 2 + 1) * (C::TILE >> 4));
+        const uint64_t v = dv + static_cast<uint64_t>((u % ST) * 2 * (C::TILE >> 4)), p = dp + static_cast<uint64_t>((u & 1) * (C::PBYTES >> 4));
 #pragma unroll
         for (int k = 0; k < kKvTile / 32; ++k)
-          mma_f8_ss(tmem + 2 * C::COLS, v + static_cast<uint64_t>(k * (32 * D >> 4)), dp[u & 1] + static_cast<uint64_t>(k * (32 * 16 >> 4)), C::IDESC_O,
+          mma_f8_ss(tmem + 2 * C::COLS, v + static_cast<uint64_t>(k * (32 * D >> 4)), p + static_cast<uint64_t>(k * (32 * 16 >> 4)), C::IDESC_O,
                     !first || k > 0);
         mma_commit(empty(u % ST));
         mma_commit(pv_done);
@@ -160,7 +159,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
           ok = kv_wait(full(t % ST), (t / ST) & 1);
           if (!ok) break;
           tc_fence_after_sync();
-          const uint64_t k0 = dk[0] + static_cast<uint64_t>((t % ST) * 2 * (C::TILE >> 4));
+          const uint64_t k0 = dk + static_cast<uint64_t>((t % ST) * 2 * (C::TILE >> 4));
 #pragma unroll
           for (int k = 0; k < D / 32; ++k)
             mma_f8_ss(tmem + (t & 1) * C::COLS, k0 + static_cast<uint64_t>(2 * k), dq + static_cast<uint64_t>(2 * k), C::IDESC_S, k > 0);

@@ -56,6 +56,7 @@ struct alignas(16) PrefillCtl {
   uint32_t nan[2][4];           // slots of which some row sees a NaN value
   float2 xchg[2][2][128];       // between a row's two owners
   KvWalk<kManyRows> walk[16];   // of the rows' owners, a warp each: their registers are for scores
+  int2 span[16];                // slots of their tile's first and last row
   int scan[2 * kThreads / 32];
   KvShare share;
   uint32_t tmem;
@@ -281,7 +282,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
     // ---- weights: a row has two owners, 64 columns of S (and half of D) each ---------------------
     const int rw = warp - 4, i = rw >> 3, half = rw >> 2 & 1, quad = warp & 3, me = quad * 32 + lane;
     const uint32_t lanes = static_cast<uint32_t>(quad * 32) << 16;
-    const uint32_t sS = tmem + lanes + i * 128 + half * 64, sO = tmem + lanes + 256 + i * 128 + half * (D / 2);
+    const uint32_t sS = tmem + lanes + i * 128 + half * 64;
+    auto sO = [&] { return sS + 256 - half * (64 - D / 2); };      // this half of the row's O
     const uint32_t pair = 1 + i * 4 + quad;      // barrier of the two warps that own the same rows
     // Both come here; both leave when one has given up, so that neither waits for the other.
     auto meet = [&](bool flag) { return named_barrier_any(pair, 64, flag); };
@@ -304,7 +306,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
       const int row = i * 128 + me;
       const bool real = row < it.rows;
       auto slot_of = [&](int r) { return it.p0 + static_cast<int>(a.by_group(it.row0 + min(r, it.rows - 1))); };
-      const int p = slot_of(row), p_lo = slot_of(i * 128), p_hi = slot_of(i * 128 + 127);      // of the row, of the tile's first and last
+      if (lane == 0) ctl->span[rw] = make_int2(slot_of(i * 128), slot_of(i * 128 + 127));
       constexpr int LANES = D / 16, STEP = 32 / LANES;      // lanes that move this half of a row, rows at a time
       const int sub = lane / LANES, part = lane % LANES;
       float c;                  // scale2 * the row's power of two
@@ -364,7 +366,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
         ok = __all_sync(0xffffffffu, ok);
         tc_fence_after_sync();
         const float4* block = &ctl->block[b][4 * half];
-        if (!kv_whole(slot0, p_lo, p_hi, a.window, a.sinks)) {      // what the row does not see becomes -inf
+        if (!kv_whole(slot0, ctl->span[rw].x, ctl->span[rw].y, a.window, a.sinks)) {      // what the row does not see becomes -inf
+          const int p = slot_of(row);
           // (it sees slots up to p that are past `from` or before `few`)
           const int base = slot0 + half * 64, from = a.window > 0 ? p - a.window : -1, few = a.window > 0 ? a.sinks : INT32_MAX;
           auto below = [](int n) { return n >= 32 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << n) - 1u; };      // columns 0 .. n - 1
@@ -385,7 +388,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
           }
           tmem_wait_st();
         }
-        uint32_t words[32];
+        uint32_t words[2][16];
         bool again;
 #pragma unroll 1
         do {
@@ -409,14 +412,15 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                 y1 = make_float2(ex2_approx(y1.x), ex2_approx(y1.y));
                 s0 = fadd2(s0, y0);
                 s1 = fadd2(s1, y1);
-                words[16 * q + 8 * g + e / 2] = f16x2(y0.x, y0.y);
-                words[16 * q + 8 * g + e / 2 + 1] = f16x2(y1.x, y1.y);
+                words[q][8 * g + e / 2] = f16x2(y0.x, y0.y);
+                words[q][8 * g + e / 2 + 1] = f16x2(y1.x, y1.y);
               }
               s0 = fadd2(s0, s1);
               const float all = s0.x + s0.y;
               sum += all;
               dl = fmaf(all, k.z, dl);
             }
+            reg_fence(words[q]);      // (worked out before the next columns are loaded: there is no room for both)
           }
           again = meet(sum >= kMost || !ok);
           if (!again) {
@@ -445,10 +449,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
 #pragma unroll 1
             for (int e = 0; e < D / 32; ++e) {
               uint32_t x[16];
-              load_cols(sO + 16 * e, x);
+              load_cols(sO() + 16 * e, x);
 #pragma unroll
               for (int k = 0; k < 16; ++k) x[k] = __float_as_uint(__uint_as_float(x[k]) * f);
-              tmem_st_32x32b(sO + 16 * e, x);
+              tmem_st_32x32b(sO() + 16 * e, x);
             }
             tmem_wait_st();
           }
@@ -457,7 +461,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
           ok = false;
           break;
         }
-        tmem_st_32x32b(sS, words);
+        tmem_st_32x32b(sS, words[0]);
+        tmem_st_32x32b(sS + 16, words[1]);
         tmem_wait_st();
         tc_fence_before_sync();
         __syncwarp();
@@ -485,7 +490,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
 #pragma unroll 1
       for (int q = 0; q < D / 64; ++q) {
         uint32_t o[32];
-        load_cols(sO + 32 * q, o);
+        load_cols(sO() + 32 * q, o);
         // (a row that saw nothing here is zero, whatever its accumulator holds)
 #pragma unroll
         for (int e = 0; e < 32; ++e) o[e] = l == 0.f ? 0u : __float_as_uint(__uint_as_float(o[e]) * inv);
