@@ -5,7 +5,7 @@
 // times 4; each row is first brought under 256 by a power of two).  Two e4m3 products cost what one of 16 bits would, at half the
 // shared memory and with no work on K.  P V is formed in f16, which holds every e4m3 number, and a weight to 11 bits.
 //
-// A TMEM lane of S is a query row; two threads own it, 64 columns each.  With x the score in base 2 and vs the V scale of a slot's block, the row's
+// A TMEM lane of S is a query row and one thread's.  With x the score in base 2 and vs the V scale of a slot's block, the row's
 // weights are P = 2^(x + log2(vs) - w) and l = sum P / vs; both scales are constants of 16 columns, so a weight costs
 // one multiply-add, one exponential, one addition and half a conversion.  w is a whole number, the maximum of the row's first
 // 64 slots rounded up, and then stays: f16 has room for weights up to 2^15 above it, and below it 14 binary orders keep all their bits
@@ -16,7 +16,7 @@
 // What bounds it is the tensor pipe: 1092 clocks per 128 x 128 tile at D = 128, against 512 clocks of exponentials.  Two row
 // tiles A and B share every K and V tile and take turns: while one's weights are worked out, the other's products run.  P overwrites
 // its S in TMEM.  Roles of a CTA (one per SM): warp 0 fetches, warp 1 issues the MMAs, warps 2-3 turn V into f16 (they also
-// see to NaN that must not reach rows that do not look at it), warps 4-11 and 12-19 own the rows of A and B.
+// see to NaN that must not reach rows that do not look at it), warps 4-7 and 8-11 own the rows of A and B.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -29,7 +29,8 @@ namespace {
 
 using namespace ptx;
 
-constexpr int kThreads = 640;
+constexpr int kThreads = 384;
+constexpr int kHalf = 64;          // columns of S at a time
 constexpr float kMost = 32768.f;   // sum of 64 weights at which w moves
 constexpr uint32_t kTmem = 512;    // S of A and B, then O of A and B, 128 columns each
 
@@ -43,20 +44,17 @@ struct PrefillCfg {
   static constexpr int VTILE = VCHUNK * D / 64;
   static constexpr uint32_t SWIZZLE = D == 128 ? 2 : 4;
   static constexpr uint32_t GROUP = 8 * D;
-  static constexpr uint32_t IDESC_S = idesc_e4m3_f32(128, 128, false, false);
+  static constexpr uint32_t IDESC_S = idesc_e4m3_f32(128, kHalf, false, false);
   static constexpr uint32_t IDESC_O = idesc_f16_mn_f32(128, D);
 };
 
 template <int D>
 struct alignas(16) PrefillCtl {
   static constexpr int ST = PrefillCfg<D>::STAGES, SV = PrefillCfg<D>::VSTAGES;
-  uint64_t full[ST], empty[ST], v_empty[SV], ready[2], vfree[2], s_full[2], p_full[2], q_full[2], o_full[2];
+  uint64_t full[ST], empty[ST], v_empty[SV], ready[2], vfree[2], s_full[2][2], p_full[2][2], q_full[2], o_done[2][2];
   float scales[ST][16];
   float4 block[2][8];           // per block of 16 slots: K scale, log2(V scale), 1 / V scale
   uint32_t nan[2][4];           // slots of which some row sees a NaN value
-  float2 xchg[2][2][128];       // between a row's two owners
-  KvWalk<kManyRows> walk[16];   // of the rows' owners, a warp each: their registers are for scores
-  int2 span[16];                // slots of their tile's first and last row
   int scan[2 * kThreads / 32];
   KvShare share;
   uint32_t tmem;
@@ -112,10 +110,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
   auto empty = [&](int s) { return smem_u32(&ctl->empty[s]); };
   auto ready = [&](int b) { return smem_u32(&ctl->ready[b]); };
   auto vfree = [&](int b) { return smem_u32(&ctl->vfree[b]); };
-  auto s_full = [&](int i) { return smem_u32(&ctl->s_full[i]); };
-  auto p_full = [&](int i) { return smem_u32(&ctl->p_full[i]); };
+  auto s_full = [&](int i, int h) { return smem_u32(&ctl->s_full[i][h]); };
+  auto p_full = [&](int i, int h) { return smem_u32(&ctl->p_full[i][h]); };
   auto q_full = [&](int i) { return smem_u32(&ctl->q_full[i]); };
-  auto o_full = [&](int i) { return smem_u32(&ctl->o_full[i]); };
+  auto o_done = [&](int i, int h) { return smem_u32(&ctl->o_done[i][h]); };
 
   begin_call();
   const KvShare share = kv_share<kManyRows, D>(a, ctl->scan, &ctl->share, status);
@@ -134,10 +132,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
     for (int i = 0; i < 2; ++i) {
       mbar_init(ready(i), 2);
       mbar_init(vfree(i), 1);
-      mbar_init(s_full(i), 1);
-      mbar_init(p_full(i), 8);
-      mbar_init(q_full(i), 8);
-      mbar_init(o_full(i), 1);
+      for (int h = 0; h < 2; ++h) {
+        mbar_init(s_full(i, h), 1);
+        mbar_init(p_full(i, h), 4);
+        mbar_init(o_done(i, h), 1);
+      }
+      mbar_init(q_full(i), 4);
     }
     fence_mbar_init();
     ctl->abort = 0;
@@ -156,7 +156,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
     walk.begin(share);
     kv_fetch<D, ST, C::VSTAGES>(maps, a, walk, KvRings{sK, sC, C::TILE, ctl->full, ctl->empty, ctl->v_empty, ctl->scales}, &ctl->abort, status);
   } else if (warp == 1) {
-    // ---- products: of A and B in turn, so that those of one run while the weights of the other are worked out --------------
+    // ---- products: S of a half tile goes ahead of the P V before it, so that neither the tensor pipe nor the rows' owners
+    // wait for the other; A and B in turn -----------------------------------------------------------
     KvWalk<kManyRows> walk;
     walk.begin(share);
     const KvItem& it = walk.it;
@@ -164,50 +165,60 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
     const uint64_t dq = smem_desc(smem_u32(sQ), 16, C::GROUP, C::SWIZZLE);
     const uint64_t dk = smem_desc(smem_u32(sK), 16, C::GROUP, C::SWIZZLE);
     const uint64_t dv = smem_desc(smem_u32(sV), C::VCHUNK, 1024, 2);
-    int t = 0, rounds_a = 0, rounds_b = 0, items_a = 0, items_b = 0;      // slot tiles; weights taken and items, of a row tile
+    int t = 0, done_a = 0, done_b = 0, items_a = 0, items_b = 0;      // slot tiles; of a row tile: slot tiles, items
     bool ok = true;
     auto wait = [&](uint32_t bar, int round) {
       ok = __all_sync(0xffffffffu, kv_wait(bar, round & 1));
       return ok;
     };
+    auto scores = [&](int i, int u, int h) {      // S of half h of slot tile u
+      const uint64_t q = dq + static_cast<uint64_t>(i * 2 * (C::QTILE >> 4));
+      const uint64_t k0 = dk + static_cast<uint64_t>((u % ST) * (C::TILE >> 4) + h * (kHalf * D >> 4));
+#pragma unroll
+      for (int part = 0; part < 2; ++part)
+#pragma unroll
+        for (int k = 0; k < D / 32; ++k)
+          mma_f8_ss(tmem + i * 128 + h * kHalf, q + static_cast<uint64_t>(part * (C::QTILE >> 4) + 2 * k), k0 + static_cast<uint64_t>(2 * k), C::IDESC_S,
+                    part > 0 || k > 0, issue);
+      if (issue) mma_commit(s_full(i, h));
+    };
     while (ok && walk.next(a)) {
       const int n = it.t1 - it.t0, two = it.rows > 128;
+      if (!wait(full(t % ST), t / ST)) break;
 #pragma unroll 1
-      for (int j = 0; ok && j <= n; ++j) {      // P V of slot tile j - 1, then S of slot tile j
-        const int u = t + j - 1, s = (t + j) % ST;
+      for (int i = 0; i <= two; ++i) {
+        if (!wait(q_full(i), i == 0 ? items_a++ : items_b++)) break;
+        tc_fence_after_sync();
+        scores(i, t, 0);
+        scores(i, t, 1);
+      }
+      if (!ok) break;
+      if (issue) mma_commit(empty(t % ST));
+#pragma unroll 1
+      for (int g = 0; ok && g < 2 * n; ++g) {      // P V of half tile g, S of half tile g + 2
+        const int u = t + (g >> 1), h = g & 1;
+        const bool more = g + 2 < 2 * n;
+        if (h == 0 && !wait(ready(u & 1), u >> 1)) break;
+        if (h == 0 && more && !wait(full((u + 1) % ST), (u + 1) / ST)) break;
 #pragma unroll 1
         for (int i = 0; i <= two; ++i) {
-          const int round = j > 0 ? (i == 0 ? rounds_a++ : rounds_b++) : i == 0 ? items_a++ : items_b++;
-          if (j > 0 && i == 0 && !wait(ready(u & 1), u >> 1)) break;
-          if (!wait(j > 0 ? p_full(i) : q_full(i), round)) break;
+          if (!wait(p_full(i, h), (i == 0 ? done_a : done_b) + (g >> 1))) break;
           tc_fence_after_sync();
-          if (j > 0) {      // (the weights of the second 64 slots begin 64 columns on)
-            const uint64_t v = dv + static_cast<uint64_t>((u & 1) * (C::VTILE >> 4));
+          const uint64_t v = dv + static_cast<uint64_t>((u & 1) * (C::VTILE >> 4) + h * (kHalf * 128 >> 4));
 #pragma unroll
-            for (int k = 0; k < kKvTile / 16; ++k)
-              mma_f16_ts(tmem + 256 + i * 128, tmem + i * 128 + (k & 3) * 8 + (k >> 2) * 64, v + static_cast<uint64_t>(k * (2048 >> 4)), C::IDESC_O,
-                         j > 1 || k > 0, issue);
-            if (issue && j == n) mma_commit(o_full(i));
-          }
-          if (j < n) {
-            if (i == 0 && !wait(full(s), (t + j) / ST)) break;
-            tc_fence_after_sync();
-            const uint64_t q = dq + static_cast<uint64_t>(i * 2 * (C::QTILE >> 4)), k0 = dk + static_cast<uint64_t>(s * (C::TILE >> 4));
-#pragma unroll
-            for (int part = 0; part < 2; ++part)
-#pragma unroll
-              for (int k = 0; k < D / 32; ++k)
-                mma_f8_ss(tmem + i * 128, q + static_cast<uint64_t>(part * (C::QTILE >> 4) + 2 * k), k0 + static_cast<uint64_t>(2 * k), C::IDESC_S,
-                          part > 0 || k > 0, issue);
-            if (issue) mma_commit(s_full(i));
-          }
+          for (int k = 0; k < kHalf / 16; ++k)
+            mma_f16_ts(tmem + 256 + i * 128, tmem + i * 128 + h * kHalf + k * 8, v + static_cast<uint64_t>(k * (2048 >> 4)), C::IDESC_O, g > 0 || k > 0, issue);
+          if (issue) mma_commit(o_done(i, h));
+          if (more) scores(i, u + 1, h);
         }
-        if (ok && issue) {
-          if (j > 0) mma_commit(vfree(u & 1));
-          if (j < n) mma_commit(empty(s));
+        if (ok && issue && h == 1) {
+          mma_commit(vfree(u & 1));
+          if (more) mma_commit(empty((u + 1) % ST));
         }
       }
       t += n;
+      done_a += n;
+      if (two) done_b += n;
     }
     if (!ok && lane == 0) stop(&ctl->abort, status);
     __syncwarp();
@@ -279,26 +290,15 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
     }
     if (!ok && lane == 0) stop(&ctl->abort, status);
   } else {
-    // ---- weights: a row has two owners, 64 columns of S (and half of D) each ---------------------
-    const int rw = warp - 4, i = rw >> 3, half = rw >> 2 & 1, quad = warp & 3, me = quad * 32 + lane;
-    const uint32_t lanes = static_cast<uint32_t>(quad * 32) << 16;
-    const uint32_t sS = tmem + lanes + i * 128 + half * 64;
-    auto sO = [&] { return sS + 256 - half * (64 - D / 2); };      // this half of the row's O
-    const uint32_t pair = 1 + i * 4 + quad;      // barrier of the two warps that own the same rows
-    // Both come here; both leave when one has given up, so that neither waits for the other.
-    auto meet = [&](bool flag) { return named_barrier_any(pair, 64, flag); };
-    KvWalk<kManyRows>& walk = ctl->walk[rw];
+    // ---- weights: a thread owns a row -------------------------------------------------------------
+    const int i = (warp - 4) >> 2, quad = warp & 3, me = quad * 32 + lane;
+    const uint32_t sS = tmem + (static_cast<uint32_t>(quad * 32) << 16) + i * 128, sO = sS + 256;
+    KvWalk<kManyRows> walk;
+    walk.begin(share);
     const KvItem& it = walk.it;
-    if (lane == 0) walk.begin(share);
-    auto next = [&] {
-      __syncwarp();
-      const int more = lane == 0 && walk.next(a);
-      __syncwarp();
-      return __shfl_sync(0xffffffffu, more, 0) != 0;
-    };
-    int t = 0, s_rounds = 0, o_rounds = 0;
+    int t = 0, mine = 0;      // slot tiles of the CTA, of this row tile
     bool ok = true;
-    while (ok && next()) {
+    while (ok && walk.next(a)) {
       if (i == 1 && it.rows <= 128) {
         t += it.t1 - it.t0;
         continue;
@@ -306,17 +306,19 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
       const int row = i * 128 + me;
       const bool real = row < it.rows;
       auto slot_of = [&](int r) { return it.p0 + static_cast<int>(a.by_group(it.row0 + min(r, it.rows - 1))); };
-      if (lane == 0) ctl->span[rw] = make_int2(slot_of(i * 128), slot_of(i * 128 + 127));
-      constexpr int LANES = D / 16, STEP = 32 / LANES;      // lanes that move this half of a row, rows at a time
+      const int p = slot_of(row), p_lo = slot_of(i * 128), p_hi = slot_of(i * 128 + 127);      // of the row, of the tile's first and last
+      constexpr int LANES = D / 8, STEP = 32 / LANES;      // lanes that move a row, rows at a time
       const int sub = lane / LANES, part = lane % LANES;
+      uint8_t* tile = sQ + i * 2 * C::QTILE + quad * 32 * D;
+      auto place = [&](int r, int chunk) {      // of a row's 16-byte chunk: the swizzle of the operand tiles, the second half in the lo tile
+        constexpr int PER = D / 16;
+        return tile + (chunk >= PER ? C::QTILE : 0) + r * D + ((chunk % PER) ^ (D == 128 ? r & 7 : (r >> 1) & 3)) * 16;
+      };
       float c;                  // scale2 * the row's power of two
       {
-        // q as hi and lo codes.  Half a row waits in the hi tile's place of the row, the other in the lo tile's, until its owners
-        // have read it and turn it into codes
-        uint8_t* tile = sQ + i * 2 * C::QTILE + quad * 32 * D;
-        auto place = [&](int r, int chunk) { return r * D + (chunk ^ (D == 128 ? r & 7 : (r >> 1) & 3)) * 16; };      // the operands' swizzle
+        // q as hi and lo codes.  A row waits in its places in the hi and the lo tile until its owner turns it into them
         {
-          const unsigned long long from = real ? reinterpret_cast<unsigned long long>(kv_query(a, it, row, D) + half * (D / 2)) : 0;
+          const unsigned long long from = real ? reinterpret_cast<unsigned long long>(kv_query(a, it, row, D)) : 0;
           uint4 u[32 / STEP];
 #pragma unroll
           for (int k = 0; k < 32 / STEP; ++k) {
@@ -324,173 +326,152 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
             u[k] = src != 0 ? *(reinterpret_cast<const uint4*>(src) + part) : make_uint4(0, 0, 0, 0);
           }
 #pragma unroll
-          for (int k = 0; k < 32 / STEP; ++k) *reinterpret_cast<uint4*>(tile + half * C::QTILE + place(k * STEP + sub, part)) = u[k];
+          for (int k = 0; k < 32 / STEP; ++k) *reinterpret_cast<uint4*>(place(k * STEP + sub, part)) = u[k];
         }
         __syncwarp();
-        uint4 u[D / 16];
+        uint4 u[D / 8];
         uint32_t most = 0;      // largest magnitude, as the bits of two bf16 without their signs
 #pragma unroll
-        for (int e = 0; e < D / 16; ++e) {
-          u[e] = *reinterpret_cast<const uint4*>(tile + half * C::QTILE + place(lane, e));
+        for (int e = 0; e < D / 8; ++e) {
+          u[e] = *reinterpret_cast<const uint4*>(place(lane, e));
           most = __vmaxu2(__vmaxu2(most, __vmaxu2(u[e].x & 0x7FFF7FFFu, u[e].y & 0x7FFF7FFFu)), __vmaxu2(u[e].z & 0x7FFF7FFFu, u[e].w & 0x7FFF7FFFu));
         }
-        uint32_t top = max(most & 0xFFFFu, most >> 16);
-        ctl->xchg[i][half][me].x = __uint_as_float(top);
-        meet(false);
-        top = max(top, __float_as_uint(ctl->xchg[i][half ^ 1][me].x));
+        const uint32_t top = max(most & 0xFFFFu, most >> 16);
         const bool fin = top < 0x7F80u;
         const int e2 = fin ? max(static_cast<int>(top >> 7) - 127 - 7, -110) : 0;      // top 2^-e2 in [128, 256)
         const float inv = fin ? __uint_as_float(static_cast<uint32_t>(127 - e2) << 23) : NAN;      // (a row that is not finite: NaN throughout)
         c = a.scale2 * __uint_as_float(static_cast<uint32_t>(127 + e2) << 23);
 #pragma unroll
-        for (int e = 0; e < D / 32; ++e) {      // 16 elements at a time: by way of f16, which holds them (and 2^-24 where e4m3 ends at 2^-9)
+        for (int e = 0; e < D / 16; ++e) {      // 16 elements at a time: by way of f16, which holds them (and 2^-24 where e4m3 ends at 2^-9)
           const uint32_t w[8] = {u[2 * e].x, u[2 * e].y, u[2 * e].z, u[2 * e].w, u[2 * e + 1].x, u[2 * e + 1].y, u[2 * e + 1].z, u[2 * e + 1].w};
           uint32_t hi[4], lo[4];
 #pragma unroll
           for (int k = 0; k < 4; ++k) split_e4m3(pair_f16(w[2 * k], inv), pair_f16(w[2 * k + 1], inv), hi[k], lo[k]);
-          uint8_t* dst = tile + place(lane, half * (D / 32) + e);
-          *reinterpret_cast<uint4*>(dst) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-          *reinterpret_cast<uint4*>(dst + C::QTILE) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+          *reinterpret_cast<uint4*>(place(lane, e)) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+          *reinterpret_cast<uint4*>(place(lane, e + D / 16)) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
         }
         fence_proxy_async_shared();
         __syncwarp();
         if (lane == 0) mbar_arrive(q_full(i));
       }
       float w = kNone, l = 0.f;
-      const int n_tiles = it.t1 - it.t0;
+      const int n = it.t1 - it.t0;
 #pragma unroll 1
-      for (int j = 0; j < n_tiles; ++j, ++t, ++s_rounds) {
-        const int b = t & 1, slot0 = it.span.tile(it.t0 + j) * kKvTile;
+      for (int g = 0; g < 2 * n; ++g) {      // half tiles
+        const int h = g & 1, u = t + (g >> 1), b = u & 1, slot0 = it.span.tile(it.t0 + (g >> 1)) * kKvTile;
+        const uint32_t sX = sS + h * kHalf;
         // (S first: a row tile that left items out may be rounds ahead of the others until its products run)
-        ok = kv_wait(s_full(i), s_rounds & 1) && kv_wait(ready(b), (t >> 1) & 1);
+        ok = kv_wait(s_full(i, h), (mine + (g >> 1)) & 1) && (h == 1 || kv_wait(ready(b), (u >> 1) & 1));
         ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
         tc_fence_after_sync();
-        const float4* block = &ctl->block[b][4 * half];
-        if (!kv_whole(slot0, ctl->span[rw].x, ctl->span[rw].y, a.window, a.sinks)) {      // what the row does not see becomes -inf
-          const int p = slot_of(row);
+        const float4* block = &ctl->block[b][4 * h];
+        if (!kv_whole(slot0, p_lo, p_hi, a.window, a.sinks)) {      // what the row does not see becomes -inf
           // (it sees slots up to p that are past `from` or before `few`)
-          const int base = slot0 + half * 64, from = a.window > 0 ? p - a.window : -1, few = a.window > 0 ? a.sinks : INT32_MAX;
-          auto below = [](int n) { return n >= 32 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << n) - 1u; };      // columns 0 .. n - 1
+          const int from = a.window > 0 ? p - a.window : -1, few = a.window > 0 ? a.sinks : INT32_MAX;
+          auto below = [](int m) { return m >= 32 ? 0xFFFFFFFFu : m <= 0 ? 0u : (1u << m) - 1u; };      // columns 0 .. m - 1
 #pragma unroll 1
           for (int q = 0; q < 2; ++q) {
-            const int at = base + 32 * q;
-            const uint32_t see = below(p + 1 - at) & (~below(from + 1 - at) | below(few - at)), nan = ctl->nan[b][2 * half + q] & see;
+            const int at = slot0 + kHalf * h + 32 * q;
+            const uint32_t see = below(p + 1 - at) & (~below(from + 1 - at) | below(few - at)), nan = ctl->nan[b][2 * h + q] & see;
             if (__all_sync(0xffffffffu, (see & ~nan) == 0xFFFFFFFFu)) continue;
             uint32_t x[32];
-            load_cols(sS + 32 * q, x);
+            load_cols(sX + 32 * q, x);
 #pragma unroll
             for (int e = 0; e < 32; ++e) x[e] = see >> e & 1 ? x[e] : 0xFF800000u;
             if (__any_sync(0xffffffffu, nan != 0)) {
 #pragma unroll
               for (int e = 0; e < 32; ++e) x[e] = nan >> e & 1 ? 0x7FC00000u : x[e];
             }
-            tmem_st_32x32b(sS + 32 * q, x);
+            tmem_st_32x32b(sX + 32 * q, x);
           }
           tmem_wait_st();
         }
-        uint32_t words[2][16];
-        bool again;
+        uint32_t words[32];
 #pragma unroll 1
-        do {
+        while (true) {
+          uint32_t x[64];
+          load_cols(sX, x);
           float sum = 0.f, dl = 0.f;
 #pragma unroll
-          for (int q = 0; q < 2; ++q) {      // 32 columns
-            uint32_t x[32];
-            load_cols(sS + 32 * q, x);
+          for (int e0 = 0; e0 < 4; ++e0) {      // a block's columns
+            const float4 k = block[e0];
+            const float mul = fmaxf(k.x * c, 1e-37f), add = k.y - w;      // (not 0: -inf stays what it is)
+            const float2 mul2 = make_float2(mul, mul), add2 = make_float2(add, add);
+            float2 s0 = make_float2(0.f, 0.f), s1 = s0;
 #pragma unroll
-            for (int g = 0; g < 2; ++g) {      // a block's columns
-              const float4 k = block[2 * q + g];
-              const float mul = fmaxf(k.x * c, 1e-37f), add = k.y - w;      // (not 0: -inf stays what it is)
-              const float2 mul2 = make_float2(mul, mul), add2 = make_float2(add, add);
-              float2 s0 = make_float2(0.f, 0.f), s1 = s0;
-#pragma unroll
-              for (int e = 0; e < 16; e += 4) {
-                const uint32_t* v = x + 16 * g + e;
-                float2 y0 = ffma2(make_float2(__uint_as_float(v[0]), __uint_as_float(v[1])), mul2, add2);
-                float2 y1 = ffma2(make_float2(__uint_as_float(v[2]), __uint_as_float(v[3])), mul2, add2);
-                y0 = make_float2(ex2_approx(y0.x), ex2_approx(y0.y));
-                y1 = make_float2(ex2_approx(y1.x), ex2_approx(y1.y));
-                s0 = fadd2(s0, y0);
-                s1 = fadd2(s1, y1);
-                words[q][8 * g + e / 2] = f16x2(y0.x, y0.y);
-                words[q][8 * g + e / 2 + 1] = f16x2(y1.x, y1.y);
-              }
-              s0 = fadd2(s0, s1);
-              const float all = s0.x + s0.y;
-              sum += all;
-              dl = fmaf(all, k.z, dl);
+            for (int e = 0; e < 16; e += 4) {
+              const uint32_t* v = x + 16 * e0 + e;
+              float2 y0 = ffma2(make_float2(__uint_as_float(v[0]), __uint_as_float(v[1])), mul2, add2);
+              float2 y1 = ffma2(make_float2(__uint_as_float(v[2]), __uint_as_float(v[3])), mul2, add2);
+              y0 = make_float2(ex2_approx(y0.x), ex2_approx(y0.y));
+              y1 = make_float2(ex2_approx(y1.x), ex2_approx(y1.y));
+              s0 = fadd2(s0, y0);
+              s1 = fadd2(s1, y1);
+              words[8 * e0 + e / 2] = f16x2(y0.x, y0.y);
+              words[8 * e0 + e / 2 + 1] = f16x2(y1.x, y1.y);
             }
-            reg_fence(words[q]);      // (worked out before the next columns are loaded: there is no room for both)
+            s0 = fadd2(s0, s1);
+            const float all = s0.x + s0.y;
+            sum += all;
+            dl = fmaf(all, k.z, dl);
           }
-          again = meet(sum >= kMost || !ok);
-          if (!again) {
+          if (!__any_sync(0xffffffffu, sum >= kMost)) {
             l += dl;
             break;
           }
-          // w moves to the maximum, in the rows that need it, and O (whose products so far have completed: S came after them)
-          // and l with it; the weights start again from S, which is still whole
+          // w moves to the maximum, in the rows that need it, and O (once its products have completed) and l with it; the
+          // weights start again from S, which is still whole
           float top = kNone;
 #pragma unroll 1
-          for (int g = 0; g < 4; ++g) {
-            uint32_t x[16];
-            load_cols(sS + 16 * g, x);
-            const float4 k = block[g];
+          for (int e0 = 0; e0 < 4; ++e0) {
+            uint32_t y[16];
+            load_cols(sX + 16 * e0, y);
+            const float4 k = block[e0];
 #pragma unroll
-            for (int e = 0; e < 16; ++e) top = fmaxf(top, fmaf(__uint_as_float(x[e]), fmaxf(k.x * c, 1e-37f), k.y));
+            for (int e = 0; e < 16; ++e) top = fmaxf(top, fmaf(__uint_as_float(y[e]), fmaxf(k.x * c, 1e-37f), k.y));
           }
-          ctl->xchg[i][half][me] = make_float2(top, sum >= kMost ? 1.f : 0.f);
-          if (meet(!ok)) break;
-          const float2 other = ctl->xchg[i][half ^ 1][me];
-          if (meet(false)) break;      // (both have read; the flag is never set)
-          const float now = sum >= kMost || other.y != 0.f ? ceilf(fmaxf(top, other.x)) : w, f = ex2_approx(w - now);
+          const float now = sum >= kMost ? ceilf(top) : w, f = ex2_approx(w - now);
           w = now;
           l *= f;
-          if (j > 0) {
+          if (g > 0) {
+            ok = __all_sync(0xffffffffu, kv_wait(o_done(i, h ^ 1), (mine + ((g - 1) >> 1)) & 1));
+            if (!ok) break;
+            tc_fence_after_sync();
 #pragma unroll 1
-            for (int e = 0; e < D / 32; ++e) {
-              uint32_t x[16];
-              load_cols(sO() + 16 * e, x);
+            for (int e0 = 0; e0 < D / 16; ++e0) {
+              uint32_t y[16];
+              load_cols(sO + 16 * e0, y);
 #pragma unroll
-              for (int k = 0; k < 16; ++k) x[k] = __float_as_uint(__uint_as_float(x[k]) * f);
-              tmem_st_32x32b(sO() + 16 * e, x);
+              for (int e = 0; e < 16; ++e) y[e] = __float_as_uint(__uint_as_float(y[e]) * f);
+              tmem_st_32x32b(sO + 16 * e0, y);
             }
             tmem_wait_st();
           }
-        } while (true);
-        if (again) {      // given up, both
-          ok = false;
-          break;
         }
-        tmem_st_32x32b(sS, words[0]);
-        tmem_st_32x32b(sS + 16, words[1]);
+        if (!ok) break;
+        tmem_st_32x32b(sX, words);
         tmem_wait_st();
         tc_fence_before_sync();
         __syncwarp();
-        if (lane == 0) mbar_arrive(p_full(i));
+        if (lane == 0) mbar_arrive(p_full(i, h));
       }
       if (!ok) break;
+      t += n;
+      mine += n;
       // ---- the item's (part of the) output -----------------------------------------------------
-      ctl->xchg[i][half][me].x = l;
-      const bool done = __all_sync(0xffffffffu, kv_wait(o_full(i), o_rounds & 1));
-      ++o_rounds;
-      if (meet(!done)) {
-        ok = false;
-        break;
-      }
-      l = half == 0 ? l + ctl->xchg[i][1][me].x : ctl->xchg[i][0][me].x + l;
+      ok = __all_sync(0xffffffffu, kv_wait(o_done(i, 1), (mine - 1) & 1));
+      if (!ok) break;
       tc_fence_after_sync();
       const float inv = l == 0.f ? 0.f : 1.f / l, lse2 = l == 0.f ? -INFINITY : w + log2f(l);
       const bool complete = it.t0 == 0 && it.t1 == it.span.n;
       const int64_t slot = (2 * static_cast<int64_t>(blockIdx.x) + (it.t0 == 0 ? 1 : 0)) * kManyRows + row;
       const int64_t at = complete ? kv_out_row(a, it, real ? row : 0) : slot;
-      // complete rows go out by way of the q tile, which is done with (this half of this warp's rows, D bytes each), so that lanes write
-      // side by side
-      uint8_t* stage = sQ + i * 2 * C::QTILE + half * C::QTILE + quad * 32 * D;
-      auto place = [&](int r, int chunk) { return r * D + (chunk ^ (D == 128 ? r & 7 : (r >> 1) & 3)) * 16; };
+      // complete rows go out by way of the q tile, which is done with (this warp's rows), so that lanes write side by side
 #pragma unroll 1
-      for (int q = 0; q < D / 64; ++q) {
+      for (int q = 0; q < D / 32; ++q) {
         uint32_t o[32];
-        load_cols(sO() + 32 * q, o);
+        load_cols(sO + 32 * q, o);
         // (a row that saw nothing here is zero, whatever its accumulator holds)
 #pragma unroll
         for (int e = 0; e < 32; ++e) o[e] = l == 0.f ? 0u : __float_as_uint(__uint_as_float(o[e]) * inv);
@@ -501,29 +482,28 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
 #pragma unroll
             for (int k = 0; k < 4; ++k)
               asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(x[k]) : "f"(__uint_as_float(o[e + 2 * k + 1])), "f"(__uint_as_float(o[e + 2 * k])));
-            *reinterpret_cast<uint4*>(stage + place(lane, 4 * q + e / 8)) = make_uint4(x[0], x[1], x[2], x[3]);
+            *reinterpret_cast<uint4*>(place(lane, 4 * q + e / 8)) = make_uint4(x[0], x[1], x[2], x[3]);
           }
         } else if (real) {
 #pragma unroll
-          for (int e = 0; e < 32; e += 4)
-            *reinterpret_cast<uint4*>(a.part + slot * D + half * (D / 2) + 32 * q + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+          for (int e = 0; e < 32; e += 4) *reinterpret_cast<uint4*>(a.part + slot * D + 32 * q + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
         }
       }
       tc_fence_before_sync();
       if (complete) {
         __syncwarp();
-        const unsigned long long to = real ? reinterpret_cast<unsigned long long>(a.out + at * D + half * (D / 2)) : 0;
+        const unsigned long long to = real ? reinterpret_cast<unsigned long long>(a.out + at * D) : 0;
 #pragma unroll 4
         for (int k = 0; k < 32; k += STEP) {
           const unsigned long long dst = __shfl_sync(0xffffffffu, to, k + sub);
-          if (dst != 0) *(reinterpret_cast<uint4*>(dst) + part) = *reinterpret_cast<const uint4*>(stage + place(k + sub, part));
+          if (dst != 0) *(reinterpret_cast<uint4*>(dst) + part) = *reinterpret_cast<const uint4*>(place(k + sub, part));
         }
+        __syncwarp();
       }
-      if (real && half == 0) {
+      if (real) {
         if (!complete) a.part_lse[slot] = lse2;
         else if (a.lse != nullptr) a.lse[at] = lse2 * 0.69314718055994531f;
       }
-      meet(false);      // the exchange and the q tile have been read
     }
     if (!ok && lane == 0) stop(&ctl->abort, status);
     if (threadIdx.x == 4 * 32) kv_write_split(a, share, it);
