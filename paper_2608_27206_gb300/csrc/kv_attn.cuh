@@ -267,10 +267,11 @@ struct KvMaps {
   CUtensorMap k, v;
 };
 
-// mbar_wait with its limit counted in tries (16 million, a quarter of a second at the very least): a few instructions, where the kernels
-// here wait in many places and instructions that are not run push those that are out of the instruction cache.
+// mbar_wait with its limit counted in tries (2^18; the hardware holds one that has to wait for about 4 us, which makes a second): a
+// few instructions, where the kernels here wait in many places and instructions that are not run push those that are out of the
+// instruction cache.
 __device__ __forceinline__ bool kv_wait(uint32_t bar, uint32_t parity) {
-  int left = 1 << 24;
+  int left = 1 << 18;
 #pragma unroll 1
   while (!ptx::mbar_try_wait(bar, parity))
     if (--left == 0) return false;

@@ -380,7 +380,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
       }
       if (bad) break;
       // ---- the item's (part of the) output --------------------------------------------------
-      if (!kv_wait(pv_done, (t - 1) & 1)) stop(&ctl->abort, status);
+      // (S of the last tile says only that the product two tiles before is complete: a phase's parity names one of two, so
+      // the one before the last is waited for as well)
+      if (!kv_wait(pv_done, t & 1) || !kv_wait(pv_done, (t - 1) & 1)) stop(&ctl->abort, status);
 #pragma unroll
       for (int q = 0; q < NQ; ++q) {
         float v = l[q];
