@@ -13,9 +13,11 @@
 // behind: they move only when a weight would pass 2^60 or P 256 (e4m3 ends at 448).  So the usual tile has no maximum and no
 // exchange between threads but one barrier's vote, and O^T stays in TMEM untouched.
 //
-// What bounds it is HBM: per slot and head 2 D bytes.  Roles of a CTA (one per SM): warp 0 fetches tiles of 128 slots
-// (TMA boxes of a page each, scales by 4-byte copies) through a ring of stages, warp 1 issues the MMAs, warps 2-5 own the
-// 128 lanes.
+// What bounds it is HBM: per slot and head 2 D bytes.  From S of a tile to its P takes a group of four warps 1.1 us whatever the
+// number of rows, one and a half times what a tile of 32 KB takes an SM to fetch; so two groups take every other tile, each with its own
+// m, w, l and O^T, and join them at the item's end.  64 sequences of 404-16384 slots, 4 heads of 128: 153 us, 5.8 TB/s (one group: 210 us).
+// Roles of a CTA (one per SM): warp 0 fetches tiles of 128 slots (TMA boxes of a page each, scales by 4-byte copies) through a
+// ring of stages, warp 1 issues the MMAs, warps 2-5 and 6-9 own the 128 lanes of even and odd tiles.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -28,7 +30,7 @@ namespace {
 
 using namespace ptx;
 
-constexpr int kWarps = 6, kThreads = 32 * kWarps;
+constexpr int kWarps = 10, kThreads = 32 * kWarps;
 constexpr float kFar = 60.f;         // how far a score may pass m_q
 constexpr float kOver = 4.f;         // ... and x + log2(vs) may pass w_q
 constexpr float kUnit = 4.f;         // log2 of P at w_q
@@ -36,13 +38,13 @@ constexpr float kUnit = 4.f;         // log2 of P at w_q
 template <int D, int NQ>
 struct DecodeCfg {
   static constexpr int TILE = kKvTile * D;              // bytes of a K or V tile
-  static constexpr int STAGES = D == 128 ? 6 : 12;
+  static constexpr int STAGES = (D == 128 ? 6 : 12) - (NQ == 32 ? 2 - D / 128 : 0);
   static constexpr int QBYTES = 2 * NQ * D;             // hi rows, then lo rows
   static constexpr int PBYTES = 2 * NQ * kKvTile;       // 16 columns of every slot, then the next 16
   static constexpr uint32_t SWIZZLE = D == 128 ? 2 : 4;
   static constexpr uint32_t GROUP = 8 * D;              // bytes of 8 rows
-  static constexpr int COLS = 2 * NQ;                   // TMEM: S twice, then O
-  static constexpr uint32_t TMEM = 6 * NQ <= 64 ? 64 : 6 * NQ <= 128 ? 128 : 256;
+  static constexpr int COLS = 2 * NQ;                   // TMEM: four S, then O of either group
+  static constexpr uint32_t TMEM = NQ == 8 ? 128 : NQ == 16 ? 256 : 512;
   static constexpr uint32_t IDESC_S = idesc_e4m3_f32(128, COLS, false, false);
   static constexpr uint32_t IDESC_O = idesc_e4m3_f32(128, COLS, true, true);
 };
@@ -53,13 +55,13 @@ struct Stat {
 
 template <int D, int NQ>
 struct alignas(16) DecodeCtl {
-  uint64_t full[DecodeCfg<D, NQ>::STAGES], empty[DecodeCfg<D, NQ>::STAGES], s_full[2], p_full[2], q_full, pv_done;
-  Stat stat[NQ];
+  uint64_t full[DecodeCfg<D, NQ>::STAGES], empty[DecodeCfg<D, NQ>::STAGES], s_full[4], p_full[4], pv_done[4], q_full;
+  Stat stat[2][NQ];
   float qc[NQ];             // scale2 * the row's power of two
   int slot_of[NQ];          // slot of the row's query
-  float2 fac[NQ];
+  float2 fac[2][NQ];
   int64_t out_at[NQ];
-  float2 red[4][NQ];
+  float2 red[2][4][NQ];
   float scales[DecodeCfg<D, NQ>::STAGES][16];   // a tile's K scales, then its V scales
   int scan[2 * kWarps];
   KvShare share;
@@ -83,14 +85,15 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* sKV = smem;                         // stages of a K tile and a V tile
   uint8_t* sQ = sKV + ST * 2 * C::TILE;
-  uint8_t* sP = sQ + C::QBYTES;                // two
-  auto* ctl = reinterpret_cast<DecodeCtl<D, NQ>*>(sP + 2 * C::PBYTES);
+  uint8_t* sP = sQ + C::QBYTES;                // four
+  auto* ctl = reinterpret_cast<DecodeCtl<D, NQ>*>(sP + 4 * C::PBYTES);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   auto full = [&](int s) { return smem_u32(&ctl->full[s]); };
   auto empty = [&](int s) { return smem_u32(&ctl->empty[s]); };
   auto s_full = [&](int p) { return smem_u32(&ctl->s_full[p]); };
   auto p_full = [&](int p) { return smem_u32(&ctl->p_full[p]); };
-  const uint32_t q_full = smem_u32(&ctl->q_full), pv_done = smem_u32(&ctl->pv_done);
+  auto pv_done = [&](int p) { return smem_u32(&ctl->pv_done[p]); };
+  const uint32_t q_full = smem_u32(&ctl->q_full);
 
   begin_call();
   const KvShare share = kv_share<NQ, D>(a, ctl->scan, &ctl->share, status);
@@ -105,12 +108,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
       mbar_init(full(s), 33);      // the byte count's arrival and 32 lanes' scales
       mbar_init(empty(s), 1);
     }
-    for (int p = 0; p < 2; ++p) {
+    for (int p = 0; p < 4; ++p) {
       mbar_init(s_full(p), 1);
       mbar_init(p_full(p), 4);
+      mbar_init(pv_done(p), 1);
     }
-    mbar_init(q_full, 4);
-    mbar_init(pv_done, 1);
+    mbar_init(q_full, 8);
     fence_mbar_init();
     ctl->abort = 0;
   }
@@ -139,50 +142,57 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
       int t = 0, items = 0;
       bool ok = true;
       auto weigh = [&](int u, bool first) {     // O += V^T P of tile u
-        if (!kv_wait(p_full(u & 1), (u >> 1) & 1)) return false;
+        if (!kv_wait(p_full(u & 3), (u >> 2) & 1)) return false;
         tc_fence_after_sync();
-        const uint64_t v = dv + static_cast<uint64_t>((u % ST) * 2 * (C::TILE >> 4)), p = dp + static_cast<uint64_t>((u & 1) * (C::PBYTES >> 4));
+        const uint64_t v = dv + static_cast<uint64_t>((u % ST) * 2 * (C::TILE >> 4)), p = dp + static_cast<uint64_t>((u & 3) * (C::PBYTES >> 4));
 #pragma unroll
         for (int k = 0; k < kKvTile / 32; ++k)
-          mma_f8_ss(tmem + 2 * C::COLS, v + static_cast<uint64_t>(k * (32 * D >> 4)), p + static_cast<uint64_t>(k * (32 * 16 >> 4)), C::IDESC_O,
-                    !first || k > 0);
+          mma_f8_ss(tmem + (4 + (u & 1)) * C::COLS, v + static_cast<uint64_t>(k * (32 * D >> 4)), p + static_cast<uint64_t>(k * (32 * 16 >> 4)),
+                    C::IDESC_O, !first || k > 0);
         mma_commit(empty(u % ST));
-        mma_commit(pv_done);
+        mma_commit(pv_done(u & 3));
         return true;
       };
+      // S goes two tiles ahead, so that a group finds its next one when it is done with one.  (S and P of tile t are in place t % 4, and so is the barrier of its P V: a
+      // parity names one of two phases, and of the group's last two products the first need not be complete.
+      // S of tile t comes after P V of tile t - 3, which waited for P of that tile: who sees it complete may overwrite P of tile t - 4.)
       while (ok && walk.next(a)) {
         ok = kv_wait(q_full, items & 1);
         ++items;
         const int n = walk.it.t1 - walk.it.t0;
 #pragma unroll 1
-        for (int i = 0; ok && i < n; ++i, ++t) {
-          ok = kv_wait(full(t % ST), (t / ST) & 1);
-          if (!ok) break;
-          tc_fence_after_sync();
-          const uint64_t k0 = dk + static_cast<uint64_t>((t % ST) * 2 * (C::TILE >> 4));
+        for (int i = 0; ok && i < n + 2; ++i) {
+          if (i < n) {
+            const int u = t + i;
+            ok = kv_wait(full(u % ST), (u / ST) & 1);
+            if (!ok) break;
+            tc_fence_after_sync();
+            const uint64_t k0 = dk + static_cast<uint64_t>((u % ST) * 2 * (C::TILE >> 4));
 #pragma unroll
-          for (int k = 0; k < D / 32; ++k)
-            mma_f8_ss(tmem + (t & 1) * C::COLS, k0 + static_cast<uint64_t>(2 * k), dq + static_cast<uint64_t>(2 * k), C::IDESC_S, k > 0);
-          mma_commit(s_full(t & 1));
-          if (i > 0) ok = weigh(t - 1, i == 1);
+            for (int k = 0; k < D / 32; ++k)
+              mma_f8_ss(tmem + (u & 3) * C::COLS, k0 + static_cast<uint64_t>(2 * k), dq + static_cast<uint64_t>(2 * k), C::IDESC_S, k > 0);
+            mma_commit(s_full(u & 3));
+          }
+          if (i >= 2) ok = weigh(t + i - 2, i < 4);
         }
-        if (ok) ok = weigh(t - 1, n == 1);
+        t += n;
       }
       if (!ok) stop(&ctl->abort, status);
     }
     __syncwarp();
   } else {
     // ---- weights -----------------------------------------------------------------------------
-    const int quad = warp & 3, me = quad * 32 + lane;    // TMEM lane: slot of the tile, then column of the output
+    const int grp = warp >= 6, quad = warp & 3, me = quad * 32 + lane;    // TMEM lane: slot of the tile, then column of the output
     const uint32_t lanes = tmem + (static_cast<uint32_t>(quad * 32) << 16);
+    Stat* stat = ctl->stat[grp];
     int t = 0;
-    bool bad = false;
-    while (!bad && walk.next(a)) {
+    while (walk.next(a)) {
       const KvItem& it = walk.it;
-      named_barrier_sync(1, 128);      // the last item's shared statistics have been read
+      bool bad = false;
+      named_barrier_sync(3, 256);      // the last item's shared statistics have been read
       // q: rows of this item as hi and lo codes (rows past it are zero), the power of two of each
 #pragma unroll 1
-      for (int q = quad; q < NQ; q += 4) {
+      for (int q = warp - 2; q < NQ; q += 8) {
         constexpr int E = D / 32;      // elements of a lane
         float x[E];
 #pragma unroll
@@ -234,22 +244,23 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
           ctl->qc[q] = real ? a.scale2 * __uint_as_float(static_cast<uint32_t>(127 + e2) << 23) : 0.f;
           ctl->slot_of[q] = real ? it.p0 + static_cast<int>(a.by_group(it.row0 + q)) : -1;
           // (rows past the item score 0 and must not ask for anything)
-          ctl->stat[q] = real ? Stat{kNone, kNone, kNone, 0.f} : Stat{-kNone, -kNone, -kNone, 0.f};
+          ctl->stat[0][q] = ctl->stat[1][q] = real ? Stat{kNone, kNone, kNone, 0.f} : Stat{-kNone, -kNone, -kNone, 0.f};
         }
       }
       fence_proxy_async_shared();
       __syncwarp();
       if (lane == 0) mbar_arrive(q_full);
-      named_barrier_sync(1, 128);
+      named_barrier_sync(3, 256);
       float l[NQ];
 #pragma unroll
       for (int q = 0; q < NQ; ++q) l[q] = 0.f;
 #pragma unroll 1
-      for (int i = it.t0; i < it.t1; ++i, ++t) {
-        const int s = t % ST, p = t & 1;
+      for (int i = it.t0 + ((t ^ grp) & 1); i < it.t1; i += 2) {      // the tiles whose number in the CTA's order is the group's, modulo 2
+        const int u = t + i - it.t0, s = u % ST, p = u & 3;
+        const bool begun = i >= it.t0 + 2;
         const int slot0 = it.span.tile(i) * kKvTile, slot = slot0 + me;
-        bool ok = kv_wait(full(s), (t / ST) & 1);        // the tile's scales (and V, below)
-        ok = __all_sync(0xffffffffu, ok && kv_wait(s_full(p), (t >> 1) & 1));
+        bool ok = kv_wait(full(s), (u / ST) & 1);        // the tile's scales (and V, below)
+        ok = __all_sync(0xffffffffu, ok && kv_wait(s_full(p), (u >> 2) & 1));
         if (!ok) {
           if (lane == 0) stop(&ctl->abort, status);
           bad = true;
@@ -298,55 +309,43 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
         const float lv = static_cast<float>(static_cast<int>(__float_as_uint(vs) >> 23) - 127);   // log2(vs), far down for 0
         bool ask = bad;
 #pragma unroll
-        for (int q = 0; q < NQ; ++q) ask = ask || x[q] > fminf(ctl->stat[q].far, ctl->stat[q].w + (kOver - lv));
-        if (named_barrier_any(1, 128, ask)) {
+        for (int q = 0; q < NQ; ++q) ask = ask || x[q] > fminf(stat[q].far, stat[q].w + (kOver - lv));
+        if (named_barrier_any(1 + grp, 128, ask)) {
           // some row's m or w has to move: the tile's maxima over all slots, new values, factors for l and O
 #pragma unroll
           for (int q = 0; q < NQ; ++q) {
             const float mx = warp_max(x[q]), mw = warp_max(x[q] + lv);
-            if (lane == 0) ctl->red[quad][q] = make_float2(mx, mw);
+            if (lane == 0) ctl->red[grp][quad][q] = make_float2(mx, mw);
           }
-          named_barrier_sync(1, 128);
+          named_barrier_sync(1 + grp, 128);
           if (me < NQ) {
-            Stat st = ctl->stat[me];
+            const Stat st = stat[me];
             float mx = kNone, mw = kNone;
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
-              mx = fmaxf(mx, ctl->red[w][me].x);
-              mw = fmaxf(mw, ctl->red[w][me].y);
+              mx = fmaxf(mx, ctl->red[grp][w][me].x);
+              mw = fmaxf(mw, ctl->red[grp][w][me].y);
             }
             const bool move = mx > st.far || mw > st.w + kOver;     // (each row by itself)
             const float m = move ? fmaxf(st.m, mx) : st.m, w = move ? fmaxf(st.w, mw) : st.w;
-            ctl->fac[me] = make_float2(exp2f(st.m - m), exp2f(st.w - w));
-            ctl->stat[me] = Stat{m, w, m + kFar, exp2f(kUnit + m - w)};
+            ctl->fac[grp][me] = make_float2(exp2f(st.m - m), exp2f(st.w - w));
+            stat[me] = Stat{m, w, m + kFar, exp2f(kUnit + m - w)};
           }
-          if (i > it.t0 && !kv_wait(pv_done, (t - 1) & 1)) stop(&ctl->abort, status);
-          named_barrier_sync(1, 128);
-          bad = named_barrier_any(1, 128, stopped(&ctl->abort));
+          if (begun && !kv_wait(pv_done((u - 2) & 3), ((u - 2) >> 2) & 1)) stop(&ctl->abort, status);
+          named_barrier_sync(1 + grp, 128);
+          bad = named_barrier_any(1 + grp, 128, stopped(&ctl->abort));
           if (bad) break;
 #pragma unroll
-          for (int q = 0; q < NQ; ++q) l[q] *= ctl->fac[q].x;
-          if (i > it.t0) {
+          for (int q = 0; q < NQ; ++q) l[q] *= ctl->fac[grp][q].x;
+          if (begun) {
             tc_fence_after_sync();
-            uint32_t o[C::COLS];
-            load_cols(lanes + 2 * C::COLS, o);
+#pragma unroll 1
+            for (int c = 0; c < C::COLS; c += 16) {
+              uint32_t o[16];
+              load_cols(lanes + (4 + grp) * C::COLS + c, o);
 #pragma unroll
-            for (int q = 0; q < NQ; ++q) {
-              const float f = ctl->fac[q].y;
-              o[q] = __float_as_uint(__uint_as_float(o[q]) * f);
-              o[NQ + q] = __float_as_uint(__uint_as_float(o[NQ + q]) * f);
-            }
-            if constexpr (C::COLS == 64) {
-              uint32_t lo[32], hi[32];
-#pragma unroll
-              for (int e = 0; e < 32; ++e) {
-                lo[e] = o[e];
-                hi[e] = o[32 + e];
-              }
-              tmem_st_32x32b(lanes + 2 * C::COLS, lo);
-              tmem_st_32x32b(lanes + 2 * C::COLS + 32, hi);
-            } else {
-              tmem_st_32x32b(lanes + 2 * C::COLS, o);
+              for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * ctl->fac[grp][(c + e) % NQ].y);
+              tmem_st_32x32b(lanes + (4 + grp) * C::COLS + c, o);
             }
             tmem_wait_st();
           }
@@ -358,9 +357,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
           float y[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const float pr = ex2_approx(x[q + e] - ctl->stat[q + e].m);
+            const float pr = ex2_approx(x[q + e] - stat[q + e].m);
             l[q + e] += pr;
-            y[e] = pr * fminf(vs * ctl->stat[q + e].g, 0x1p100f);      // (a bound only where pr is 0: no infinity)
+            y[e] = pr * fminf(vs * stat[q + e].g, 0x1p100f);      // (a bound only where pr is 0: no infinity)
             if (vs != vs && x[q + e] > -INFINITY) y[e] = vs;           // (fminf drops a NaN)
           }
           const uint32_t hi = e4m3x4(y[0], y[1], y[2], y[3]);
@@ -378,48 +377,67 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
         __syncwarp();
         if (lane == 0) mbar_arrive(p_full(p));
       }
-      if (bad) break;
-      // ---- the item's (part of the) output --------------------------------------------------
-      // (S of the last tile says only that the product two tiles before is complete: a phase's parity names one of two, so
-      // the one before the last is waited for as well)
-      if (!kv_wait(pv_done, t & 1) || !kv_wait(pv_done, (t - 1) & 1)) stop(&ctl->abort, status);
+      // ---- the item's (part of the) output, joined from the groups' ---------------------------
+      t += it.t1 - it.t0;
+      const int last = t - 1 - ((t - 1 ^ grp) & 1);      // the group's last tile (not of this item, if it had none)
+      if (!bad && last >= t - (it.t1 - it.t0) && !kv_wait(pv_done(last & 3), (last >> 2) & 1)) stop(&ctl->abort, status);
 #pragma unroll
       for (int q = 0; q < NQ; ++q) {
         float v = l[q];
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-        if (lane == 0) ctl->red[quad][q].x = v;
+        if (lane == 0) ctl->red[grp][quad][q].x = v;
       }
+      if (named_barrier_any(3, 256, bad || stopped(&ctl->abort))) break;
       const bool complete = it.t0 == 0 && it.t1 == it.span.n;
       const int64_t slot = (2 * static_cast<int64_t>(blockIdx.x) + (it.t0 == 0 ? 1 : 0)) * NQ;
-      named_barrier_sync(1, 128);
       if (me < it.rows) {
-        const float sum = (ctl->red[0][me].x + ctl->red[1][me].x) + (ctl->red[2][me].x + ctl->red[3][me].x);
-        const Stat st = ctl->stat[me];
-        const int64_t at = complete ? kv_out_row(a, it, me) : slot + me;
-        ctl->fac[me].x = sum == 0.f ? 0.f : 1.f / (st.g * sum);      // out = O / (g l); a row that saw nothing here is zero
-        ctl->out_at[me] = at * D;
-        float* lse = complete ? a.lse : a.part_lse;
-        if (lse != nullptr) lse[at] = sum == 0.f ? -INFINITY : (st.m + log2f(sum)) * (complete ? 0.69314718055994531f : 1.f);
+        float l2[2], m = kNone;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          l2[k] = (ctl->red[k][0][me].x + ctl->red[k][1][me].x) + (ctl->red[k][2][me].x + ctl->red[k][3][me].x);
+          if (l2[k] != 0.f) m = fmaxf(m, ctl->stat[k][me].m);      // (a group that saw nothing has no say)
+        }
+        const float f0 = l2[0] == 0.f ? 0.f : exp2f(ctl->stat[0][me].m - m), f1 = l2[1] == 0.f ? 0.f : exp2f(ctl->stat[1][me].m - m);
+        const float sum = l2[0] * f0 + l2[1] * f1;
+        const float f = grp == 0 ? f0 : f1;
+        // out = sum over the groups of O f / (g sum); 0 says that the group saw nothing (else O counts however small f is: it may be NaN)
+        float by = f / (stat[me].g * sum);
+        if (by == 0.f) by = 1e-37f;
+        ctl->fac[grp][me].x = (grp == 0 ? l2[0] : l2[1]) == 0.f ? 0.f : by;
+        if (grp == 0) {
+          const int64_t at = complete ? kv_out_row(a, it, me) : slot + me;
+          ctl->out_at[me] = at * D;
+          float* lse = complete ? a.lse : a.part_lse;
+          if (lse != nullptr) lse[at] = sum == 0.f ? -INFINITY : (m + log2f(sum)) * (complete ? 0.69314718055994531f : 1.f);
+        }
       }
-      bad = named_barrier_any(1, 128, stopped(&ctl->abort));
-      if (bad) break;
+      named_barrier_sync(1 + grp, 128);
       tc_fence_after_sync();
       uint32_t o[C::COLS];
-      load_cols(lanes + 2 * C::COLS, o);
+      load_cols(lanes + (4 + grp) * C::COLS, o);
       tc_fence_before_sync();
+      // each group ends half of the rows, with the other's sums by way of P's places (all products have completed)
+      float* join = reinterpret_cast<float*>(sP);
+#pragma unroll
+      for (int q = 0; q < NQ; ++q) {
+        const float f = ctl->fac[grp][q].x;
+        const float v = f == 0.f ? 0.f : fmaf(__uint_as_float(o[NQ + q]), 0.0625f, __uint_as_float(o[q])) * f;
+        o[q] = __float_as_uint(v);
+        if (q / (NQ / 2) != grp && q < it.rows && me < D) join[q * D + me] = v;
+      }
+      named_barrier_sync(3, 256);
       if (me < D) {
 #pragma unroll
         for (int q = 0; q < NQ; ++q) {
-          if (q >= it.rows) break;
-          const float f = ctl->fac[q].x;
-          const float v = f == 0.f ? 0.f : fmaf(__uint_as_float(o[NQ + q]), 0.0625f, __uint_as_float(o[q])) * f;
+          if (q / (NQ / 2) != grp || q >= it.rows) continue;
+          const float v = __uint_as_float(o[q]) + join[q * D + me];
           if (complete) a.out[ctl->out_at[q] + me] = __bfloat16_as_ushort(__float2bfloat16_rn(v));
           else a.part[ctl->out_at[q] + me] = v;
         }
       }
     }
-    if (me == 0) kv_write_split(a, share, walk.it);
+    if (threadIdx.x == 64) kv_write_split(a, share, walk.it);
   }
   // everything issued has completed: the last tile's commit has been waited for, unless the CTA gave up
   tc_fence_before_sync();
@@ -485,7 +503,7 @@ __global__ void __launch_bounds__(256) kv_attn_combine(const __grid_constant__ K
 template <int D, int NQ>
 pace_status_t run_decode(const KvMaps& maps, const KvAttnArgs& a, unsigned grid, int* status, cudaStream_t stream) {
   using C = DecodeCfg<D, NQ>;
-  constexpr size_t smem = 1024 + C::STAGES * 2 * C::TILE + C::QBYTES + 2 * C::PBYTES + sizeof(DecodeCtl<D, NQ>);
+  constexpr size_t smem = 1024 + C::STAGES * 2 * C::TILE + C::QBYTES + 4 * C::PBYTES + sizeof(DecodeCtl<D, NQ>);
   static_assert(smem <= 227 * 1024, "shared memory");
   static DeviceOnce once;
   int dev = 0;
