@@ -452,52 +452,71 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
   if (warp == 1) tmem_dealloc(tmem, C::TMEM);
 }
 
-// Rows of 16 of the items that several CTAs walked: out = sum_c 2^(lse_c - max) o_c / sum_c 2^(lse_c - max), in the CTAs'
-// order.  Sixteen threads per row.
+// The items that several CTAs walked: out = sum_c 2^(lse_c - max) o_c / sum_c 2^(lse_c - max), in the CTAs' order.  A warp per row, so
+// that a long item's parts (one sequence alone makes as many as there are tiles) are many loads in flight.
+constexpr int kJoinRows = 8;
 template <int D>
-__global__ void __launch_bounds__(256) kv_attn_combine(const __grid_constant__ KvAttnArgs a, int tile_rows) {
+__global__ void __launch_bounds__(32 * kJoinRows) kv_attn_combine(const __grid_constant__ KvAttnArgs a, int tile_rows) {
+  constexpr int E = D / 32;      // elements of a lane
   launch_dependents();
   grid_dependency_wait();
-  const int c = blockIdx.x;
+  const int c = blockIdx.x, lane = threadIdx.x & 31;
   const int4 raw = __ldcg(reinterpret_cast<const int4*>(a.split + c));
   const KvSplit sp{raw.x, raw.y, raw.z, raw.w};
   if (sp.followers == 0) return;
-  const int q = blockIdx.y * 16 + threadIdx.x / 16, col = threadIdx.x % 16 * (D / 16);
+  const int q = blockIdx.y * kJoinRows + threadIdx.x / 32;
   const int row = sp.row_tile * tile_rows + q;
-  if (q >= tile_rows || row >= a.s.nq[sp.i] * a.group) return;
+  if (row >= a.s.nq[sp.i] * a.group) return;
   auto at = [&](int j) { return static_cast<int64_t>(j == 0 ? 2 * c + 1 : 2 * (c + j)) * tile_rows + q; };
-  float top = -INFINITY;
-  for (int j = 0; j <= sp.followers; ++j) top = fmaxf(top, __ldcg(a.part_lse + at(j)));
-  const float base = top == -INFINITY ? 0.f : top;
-  float sum = 0.f, o[D / 16];
+  const int parts = sp.followers + 1;
+  float top = -INFINITY, sum = 0.f, o[E];
 #pragma unroll
-  for (int e = 0; e < D / 16; ++e) o[e] = 0.f;
-#pragma unroll 4
-  for (int j = 0; j <= sp.followers; ++j) {
-    const float lse = __ldcg(a.part_lse + at(j));
-    const float w = exp2f(lse - base);
-    const float4* p = reinterpret_cast<const float4*>(a.part + at(j) * D + col);
-    sum += w;
+  for (int e = 0; e < E; ++e) o[e] = 0.f;
+#pragma unroll 1
+  for (int j0 = 0; j0 < parts; j0 += 32) {      // 32 parts at a time
+    const float lse = j0 + lane < parts ? __ldcg(a.part_lse + at(j0 + lane)) : -INFINITY;
+    float now = lse;
 #pragma unroll
-    for (int e = 0; e < D / 64; ++e) {
-      const float4 v = __ldcg(p + e);
-      o[4 * e] = fmaf(w, v.x, o[4 * e]);
-      o[4 * e + 1] = fmaf(w, v.y, o[4 * e + 1]);
-      o[4 * e + 2] = fmaf(w, v.z, o[4 * e + 2]);
-      o[4 * e + 3] = fmaf(w, v.w, o[4 * e + 3]);
+    for (int s = 16; s > 0; s >>= 1) now = fmaxf(now, __shfl_xor_sync(0xffffffffu, now, s));
+    now = fmaxf(now, top);
+    const float base = now == -INFINITY ? 0.f : now, f = exp2f(top - base), mine = exp2f(lse - base);
+    top = now;
+    sum *= f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] *= f;
+    const int n = min(parts - j0, 32);
+#pragma unroll 8
+    for (int j = 0; j < n; ++j) {
+      const float w = __shfl_sync(0xffffffffu, mine, j);
+      const float* p = a.part + at(j0 + j) * D + lane * E;
+      float v[E];
+      if constexpr (E == 4) {
+        const float4 u = __ldcg(reinterpret_cast<const float4*>(p));
+        v[0] = u.x;
+        v[1] = u.y;
+        v[2] = u.z;
+        v[3] = u.w;
+      } else {
+        const float2 u = __ldcg(reinterpret_cast<const float2*>(p));
+        v[0] = u.x;
+        v[1] = u.y;
+      }
+      sum += w;
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] = fmaf(w, v[e], o[e]);
     }
   }
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
   const int token = static_cast<int>(a.by_group(row));
   const int64_t dst = static_cast<int64_t>(a.s.q0[sp.i] + token) * a.q_heads + sp.head * a.group + row - token * a.group;
-  uint32_t w[D / 32];
+  uint32_t w[E / 2];
 #pragma unroll
-  for (int e = 0; e < D / 32; ++e)
+  for (int e = 0; e < E / 2; ++e)
     w[e] = static_cast<uint32_t>(__bfloat16_as_ushort(__float2bfloat16_rn(o[2 * e] * inv))) |
            static_cast<uint32_t>(__bfloat16_as_ushort(__float2bfloat16_rn(o[2 * e + 1] * inv))) << 16;
-  if constexpr (D == 128) *reinterpret_cast<uint4*>(a.out + dst * D + col) = make_uint4(w[0], w[1], w[2], w[3]);
-  else *reinterpret_cast<uint2*>(a.out + dst * D + col) = make_uint2(w[0], w[1]);
-  if (col == 0 && a.lse != nullptr) a.lse[dst] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.69314718055994531f;
+  if constexpr (E == 4) *reinterpret_cast<uint2*>(a.out + dst * D + lane * E) = make_uint2(w[0], w[1]);
+  else *reinterpret_cast<uint32_t*>(a.out + dst * D + lane * E) = w[0];
+  if (lane == 0 && a.lse != nullptr) a.lse[dst] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.69314718055994531f;
 }
 
 template <int D, int NQ>
@@ -527,7 +546,7 @@ pace_status_t launch_kv_decode(const KvMaps& maps, const KvAttnArgs& a, int D, i
 
 pace_status_t launch_kv_combine(const KvAttnArgs& a, int D, int rows, unsigned grid, cudaStream_t stream) {
   auto* kernel = D == 128 ? kv_attn_combine<128> : kv_attn_combine<64>;
-  return launch_dependent(kernel, dim3(grid, static_cast<unsigned>((rows + 15) / 16)), 256, 0, 1, stream, a, rows);
+  return launch_dependent(kernel, dim3(grid, static_cast<unsigned>(rows / kJoinRows)), 32 * kJoinRows, 0, 1, stream, a, rows);
 }
 
 }  // namespace pace
