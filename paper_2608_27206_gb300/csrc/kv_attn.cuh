@@ -203,7 +203,8 @@ __device__ __forceinline__ KvShare kv_share(const KvAttnArgs& a, int* buf, KvSha
       s.ctas = min(static_cast<int>(gridDim.x), total);
       const int c = blockIdx.x;
       if (c >= s.ctas) return s;      // nothing to do (the whole block)
-      s.cost = total >= kItemCost * s.ctas ? kItemCost : 0;      // (few tiles: one each, however dear the rest is)
+      // (few tiles: one each, however dear the rest is; unless items are so few that a CTA need not have parts of two)
+      s.cost = total >= kItemCost * s.ctas || (total > s.ctas && total >= 4 * kItemCost * total_items) ? kItemCost : 0;
       total += s.cost * total_items;
       before += sum - mine + s.cost * (before_items + num - items);
       mine += s.cost * items;

@@ -293,7 +293,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
             if (any) {
 #pragma unroll
               for (int e = 0; e < D / 16; ++e) {
-                const uint4 u = v[e];
+                const uint4 u = v[e ^ (me & (D / 16 - 1))];      // (any order: lanes side by side would meet in one bank)
                 const uint32_t w = (((u.x & 0x7F7F7F7Fu) + 0x01010101u) | ((u.y & 0x7F7F7F7Fu) + 0x01010101u) | ((u.z & 0x7F7F7F7Fu) + 0x01010101u) |
                                     ((u.w & 0x7F7F7F7Fu) + 0x01010101u)) & 0x80808080u;
                 nan = nan || w != 0;
@@ -301,7 +301,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
             }
             if (!any || nan) {
 #pragma unroll
-              for (int e = 0; e < D / 16; ++e) v[e] = make_uint4(0, 0, 0, 0);
+              for (int e = 0; e < D / 16; ++e) v[e ^ (me & (D / 16 - 1))] = make_uint4(0, 0, 0, 0);
             }
             if (nan) vs = NAN;
           }
@@ -452,58 +452,89 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
   if (warp == 1) tmem_dealloc(tmem, C::TMEM);
 }
 
-// The items that several CTAs walked: out = sum_c 2^(lse_c - max) o_c / sum_c 2^(lse_c - max), in the CTAs' order.  A warp per row, so
-// that a long item's parts (one sequence alone makes as many as there are tiles) are many loads in flight.
-constexpr int kJoinRows = 8;
-template <int D>
-__global__ void __launch_bounds__(32 * kJoinRows) kv_attn_combine(const __grid_constant__ KvAttnArgs a, int tile_rows) {
+// The items that several CTAs walked: out = sum_c 2^(lse_c - max) o_c / sum_c 2^(lse_c - max), parts in a fixed order.  What it
+// takes is latency, so all of a warp's loads go out at once.  A row has SPLIT warps: 8 where rows are few (a sequence alone makes as
+// many parts as there are tiles: 38 parts took 8 us with one warp), 1 where they are many and a row has few parts.
+template <int D, int SPLIT>
+__global__ void __launch_bounds__(256) kv_attn_combine(const __grid_constant__ KvAttnArgs a, int tile_rows) {
   constexpr int E = D / 32;      // elements of a lane
+  __shared__ float s_top[8], s_sum[8];
+  __shared__ __align__(16) float s_o[8][D];
   launch_dependents();
   grid_dependency_wait();
-  const int c = blockIdx.x, lane = threadIdx.x & 31;
+  const int c = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int4 raw = __ldcg(reinterpret_cast<const int4*>(a.split + c));
   const KvSplit sp{raw.x, raw.y, raw.z, raw.w};
   if (sp.followers == 0) return;
-  const int q = blockIdx.y * kJoinRows + threadIdx.x / 32;
+  const int q = blockIdx.y * (8 / SPLIT) + warp / SPLIT;
   const int row = sp.row_tile * tile_rows + q;
-  if (row >= a.s.nq[sp.i] * a.group) return;
+  if (row >= a.s.nq[sp.i] * a.group) return;      // (the row's warps all)
   auto at = [&](int j) { return static_cast<int64_t>(j == 0 ? 2 * c + 1 : 2 * (c + j)) * tile_rows + q; };
   const int parts = sp.followers + 1;
   float top = -INFINITY, sum = 0.f, o[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) o[e] = 0.f;
 #pragma unroll 1
-  for (int j0 = 0; j0 < parts; j0 += 32) {      // 32 parts at a time
-    const float lse = j0 + lane < parts ? __ldcg(a.part_lse + at(j0 + lane)) : -INFINITY;
+  for (int j0 = warp % SPLIT; j0 < parts; j0 += 8 * SPLIT) {      // parts j0, j0 + SPLIT, ... : 8 at a time
+    const int j_mine = j0 + (lane & 7) * SPLIT;
+    const float lse = j_mine < parts ? __ldcg(a.part_lse + at(j_mine)) : -INFINITY;
+    float v[8][E];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[k][e] = 0.f;
+      if (j0 + k * SPLIT >= parts) continue;
+      const float* p = a.part + at(j0 + k * SPLIT) * D + lane * E;
+      if constexpr (E == 4) {
+        const float4 u = __ldcg(reinterpret_cast<const float4*>(p));
+        v[k][0] = u.x;
+        v[k][1] = u.y;
+        v[k][2] = u.z;
+        v[k][3] = u.w;
+      } else {
+        const float2 u = __ldcg(reinterpret_cast<const float2*>(p));
+        v[k][0] = u.x;
+        v[k][1] = u.y;
+      }
+    }
     float now = lse;
 #pragma unroll
-    for (int s = 16; s > 0; s >>= 1) now = fmaxf(now, __shfl_xor_sync(0xffffffffu, now, s));
+    for (int s = 4; s > 0; s >>= 1) now = fmaxf(now, __shfl_xor_sync(0xffffffffu, now, s));
     now = fmaxf(now, top);
     const float base = now == -INFINITY ? 0.f : now, f = exp2f(top - base), mine = exp2f(lse - base);
     top = now;
     sum *= f;
 #pragma unroll
     for (int e = 0; e < E; ++e) o[e] *= f;
-    const int n = min(parts - j0, 32);
-#pragma unroll 8
-    for (int j = 0; j < n; ++j) {
-      const float w = __shfl_sync(0xffffffffu, mine, j);
-      const float* p = a.part + at(j0 + j) * D + lane * E;
-      float v[E];
-      if constexpr (E == 4) {
-        const float4 u = __ldcg(reinterpret_cast<const float4*>(p));
-        v[0] = u.x;
-        v[1] = u.y;
-        v[2] = u.z;
-        v[3] = u.w;
-      } else {
-        const float2 u = __ldcg(reinterpret_cast<const float2*>(p));
-        v[0] = u.x;
-        v[1] = u.y;
-      }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float w = __shfl_sync(0xffffffffu, mine, k);
       sum += w;
 #pragma unroll
-      for (int e = 0; e < E; ++e) o[e] = fmaf(w, v[e], o[e]);
+      for (int e = 0; e < E; ++e) o[e] = fmaf(w, v[k][e], o[e]);
+    }
+  }
+  if constexpr (SPLIT > 1) {
+    if (lane == 0) {
+      s_top[warp] = top;
+      s_sum[warp] = sum;
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) s_o[warp][lane * E + e] = o[e];
+    __syncthreads();
+    if (warp > 0) return;
+#pragma unroll
+    for (int k = 1; k < SPLIT; ++k) top = fmaxf(top, s_top[k]);
+    const float base = top == -INFINITY ? 0.f : top;
+    sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = 0.f;
+#pragma unroll
+    for (int k = 0; k < SPLIT; ++k) {
+      const float f = exp2f(s_top[k] - base);
+      sum = fmaf(f, s_sum[k], sum);
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] = fmaf(f, s_o[k][lane * E + e], o[e]);
     }
   }
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
@@ -545,8 +576,11 @@ pace_status_t launch_kv_decode(const KvMaps& maps, const KvAttnArgs& a, int D, i
 }
 
 pace_status_t launch_kv_combine(const KvAttnArgs& a, int D, int rows, unsigned grid, cudaStream_t stream) {
-  auto* kernel = D == 128 ? kv_attn_combine<128> : kv_attn_combine<64>;
-  return launch_dependent(kernel, dim3(grid, static_cast<unsigned>(rows / kJoinRows)), 32 * kJoinRows, 0, 1, stream, a, rows);
+  if (rows == kManyRows)
+    return launch_dependent(D == 128 ? kv_attn_combine<128, 1> : kv_attn_combine<64, 1>, dim3(grid, static_cast<unsigned>(rows / 8)), 256, 0, 1,
+                            stream, a, rows);
+  return launch_dependent(D == 128 ? kv_attn_combine<128, 8> : kv_attn_combine<64, 8>, dim3(grid, static_cast<unsigned>(rows)), 256, 0, 1, stream,
+                          a, rows);
 }
 
 }  // namespace pace
