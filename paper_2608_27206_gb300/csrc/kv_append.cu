@@ -6,8 +6,12 @@
 // of two s that covers the block.  The power costs e4m3 nothing (it is a floating format) and makes
 // the growth of a block's scale, when a later token needs more, an exact factor on its older codes.
 //
-// One CTA per touched block: it stages the tokens' (cos, sin) once for all heads, then a warp takes
-// a head's 16 rows at a time, 16 bytes per lane and load, both halves of a pair in one lane.
+// What bounds it is HBM: a token's rows once in, its codes and turned queries once out; what stands in the way is the chain of loads
+// before them (length, row, position, angles).  One CTA per touched block, three to an SM: it stages the tokens' (cos, sin) once
+// for all heads while the first rows are on their way; a warp takes a head's 16 rows of K or V, 16 bytes per lane and load, both halves
+// of a pair in one lane, 16 bits wide until they are used.  For the queries a lane keeps its row's angles in registers
+// and goes over heads, four in flight.  16 prompts, 44000 tokens of 28 + 8 heads of 128: 137 us, 6.0 TB/s (two CTAs per SM 145,
+// four 149: registers).  A decode step is latency: 64 tokens in 9 us.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -41,41 +45,77 @@ struct AppendArgs {
   int block_prefix[kKvMaxB + 1];   // blocks that a sequence's tokens may touch, at most
 };
 
-struct Eight {
-  float v[8];
+// Eight elements of either half of a row: a[i] and b[i] are a pair.
+struct Raw {
+  uint4 a, b;
 };
-__device__ __forceinline__ Eight load8(const uint16_t* p) {
-  const uint4 u = *reinterpret_cast<const uint4*>(p);
+struct Pairs {
+  float2 a[4], b[4];
+};
+__device__ __forceinline__ void widen(const uint4& u, float2 (&f)[4]) {
   const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-  Eight e;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    e.v[2 * i] = __uint_as_float(w[i] << 16);
-    e.v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-  }
-  return e;
+  for (int i = 0; i < 4; ++i) f[i] = make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u));
 }
 __device__ __forceinline__ uint32_t bf16x2(float lo, float hi) {
-  return static_cast<uint32_t>(__bfloat16_as_ushort(__float2bfloat16_rn(lo))) |
-         (static_cast<uint32_t>(__bfloat16_as_ushort(__float2bfloat16_rn(hi))) << 16);
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ uint4 pack_bf16(const float2 (&f)[4]) {
+  return make_uint4(bf16x2(f[0].x, f[0].y), bf16x2(f[1].x, f[1].y), bf16x2(f[2].x, f[2].y), bf16x2(f[3].x, f[3].y));
 }
 
-// Products and sums rounded one by one, so that a result does not hang on the contraction into FMAs.
-__device__ __forceinline__ void turn(Eight& a, Eight& b, const float2* cs) {
+// (cos, sin) of eight pairs, two at a time.
+struct Turn {
+  float2 c[4], s[4];
+};
+__device__ __forceinline__ Turn load_turn(const float2* cs) {
+  Turn t;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float2 t = cs[i];
-    const float x = a.v[i], y = b.v[i];
-    a.v[i] = __fsub_rn(__fmul_rn(x, t.x), __fmul_rn(y, t.y));
-    b.v[i] = __fadd_rn(__fmul_rn(y, t.x), __fmul_rn(x, t.y));
+  for (int i = 0; i < 4; ++i) {
+    const float4 u = *reinterpret_cast<const float4*>(cs + 2 * i);
+    t.c[i] = make_float2(u.x, u.z);
+    t.s[i] = make_float2(u.y, u.w);
+  }
+  return t;
+}
+// Products and sums rounded one by one, so that a result does not hang on the contraction into FMAs (the difference below is one
+// of finished products, by a factor of -1).
+__device__ __forceinline__ void turn(Pairs& x, const Turn& t) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 ac = ptx::fmul2(x.a[i], t.c[i]), bs = ptx::fmul2(x.b[i], t.s[i]);
+    const float2 bc = ptx::fmul2(x.b[i], t.c[i]), as = ptx::fmul2(x.a[i], t.s[i]);
+    x.a[i] = ptx::ffma2(bs, make_float2(-1.f, -1.f), ac);
+    x.b[i] = ptx::fadd2(bc, as);
+  }
+}
+// Adds a NaN to `all` if an element is not finite, else zeros.
+__device__ __forceinline__ void see_finite(const Pairs& x, float2& all) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    all = ptx::ffma2(x.a[i], make_float2(0.f, 0.f), all);
+    all = ptx::ffma2(x.b[i], make_float2(0.f, 0.f), all);
+  }
+}
+__device__ __forceinline__ void drop_infinite(Pairs& x) {
+  auto fix = [](float& v) { v = fabsf(v) < INFINITY ? v : 0.f; };
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    fix(x.a[i].x);
+    fix(x.a[i].y);
+    fix(x.b[i].x);
+    fix(x.b[i].y);
   }
 }
 
 template <int D>
-__global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(const __grid_constant__ AppendArgs a, int* status) {
+__global__ void __launch_bounds__(kAppendThreads, 3) kv_append_kernel(const __grid_constant__ AppendArgs a, int* status) {
   constexpr int H = D / 2, LPR = D / 16, RPP = 32 / LPR, PASS = kKvBlock / RPP;   // lanes per row, rows per pass
   __shared__ __align__(16) float2 cs[kKvBlock][H];
   __shared__ int64_t src[kKvBlock];   // source row of each slot; -1: no (valid) new token there
+  __shared__ int pos[3][kKvBlock];
   ptx::begin_call();
   int lo = 0, hi = a.nb - 1;
   while (lo < hi) {
@@ -96,10 +136,6 @@ __global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(const __grid_
   const int64_t pi = slot0 >> a.c.page_shift;
   int page = -1;
   if (pi < a.table_stride) page = a.table[(a.b0 + b) * a.table_stride + pi];
-  if (page < 0 || page >= a.c.n_pages) {
-    if (threadIdx.x == 0) record_error(status, PACE_ERR_INVALID_ARG, K_KV_APPEND);
-    page = -1;
-  }
   const int token0 = a.cu[b] + slot0 - first;   // of row 0, where that is a new token
   if (threadIdx.x < kKvBlock) {
     const int r = threadIdx.x;
@@ -109,9 +145,14 @@ __global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(const __grid_
       bool ok = s >= 0 && s < a.n_src;
       if (ok && a.rope != nullptr) {
         const int n_rows = a.sec01 < H ? 3 : a.sec0 < a.sec01 ? 2 : 1;
-        for (int c = 0; c < n_rows; ++c) {
-          const int p = a.pos[c * a.pos_stride + s];
-          ok = ok && p >= 0 && p < a.n_pos;
+        int p[3] = {0, 0, 0};
+#pragma unroll
+        for (int c = 0; c < 3; ++c)
+          if (c < n_rows) p[c] = a.pos[c * a.pos_stride + s];
+#pragma unroll
+        for (int c = 0; c < 3; ++c) {
+          ok = ok && p[c] >= 0 && p[c] < a.n_pos;
+          pos[c][r] = p[c];
         }
       }
       if (!ok) {
@@ -121,68 +162,71 @@ __global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(const __grid_
     }
     src[r] = s;
   }
-  __syncthreads();
-  if (a.rope != nullptr) {
-    for (int i = threadIdx.x; i < kKvBlock * H; i += kAppendThreads) {
-      const int r = i / H, p = i % H;
-      if (src[r] < 0) continue;
-      const int c = p < a.sec0 ? 0 : p < a.sec01 ? 1 : 2;
-      cs[r][p] = a.rope[static_cast<int64_t>(a.pos[c * a.pos_stride + src[r]]) * H + p];
-    }
-    __syncthreads();
+  if (page < 0 || page >= a.c.n_pages) {
+    if (threadIdx.x == 0) record_error(status, PACE_ERR_INVALID_ARG, K_KV_APPEND);
+    page = -1;
   }
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  __syncthreads();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = kAppendThreads / 32;
   const int col = (lane % LPR) * 8, row0 = lane / LPR;
-  const int tasks = 2 * a.c.heads + a.q_heads;
-  for (int task = warp; task < tasks; task += kAppendThreads / 32) {
-    const bool is_q = task >= 2 * a.c.heads, is_v = !is_q && task >= a.c.heads;
-    const int head = is_q ? task - 2 * a.c.heads : is_v ? task - a.c.heads : task;
-    const uint16_t* base = (is_q ? a.Q : is_v ? a.V : a.K) + static_cast<int64_t>(head) * D + col;
-    const int64_t stride = is_q ? a.q_stride : is_v ? a.v_stride : a.k_stride;
-    if (!is_q && page < 0) continue;
-    Eight x[PASS][2];
-#pragma unroll
-    for (int p = 0; p < PASS; ++p) {
-      const int64_t s = src[p * RPP + row0];
-      x[p][0] = x[p][1] = Eight{};
-      if (s >= 0) {
-        x[p][0] = load8(base + s * stride);
-        x[p][1] = load8(base + s * stride + H);
-      }
-    }
-    if (!is_v && a.rope != nullptr) {
-#pragma unroll
-      for (int p = 0; p < PASS; ++p)
-        if (src[p * RPP + row0] >= 0) turn(x[p][0], x[p][1], &cs[p * RPP + row0][col]);
-    }
-    bool bad = false;
-    float amax = 0.f;
-#pragma unroll
-    for (int p = 0; p < PASS; ++p)
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float v = fabsf(x[p][h].v[i]);
-          const bool fin = v < INFINITY;
-          bad |= !fin;
-          amax = fmaxf(amax, fin ? v : 0.f);
-        }
-    if (bad) record_error(status, PACE_ERR_INVALID_ARG, K_KV_APPEND);
-    if (is_q) {
+  const bool turned = a.rope != nullptr;
+  auto load = [&](const uint16_t* from) { return Raw{*reinterpret_cast<const uint4*>(from), *reinterpret_cast<const uint4*>(from + H)}; };
+  // ---- the cache: a warp takes a head's 16 rows of K or V
+  bool staged = !turned;
+#pragma unroll 1
+  for (int task = warp;; task += warps) {
+    const bool is_v = task >= a.c.heads, mine = task < 2 * a.c.heads && page >= 0;
+    const int head = is_v ? task - a.c.heads : task;
+    Raw x[PASS];
+    if (mine) {
+      const uint16_t* base = (is_v ? a.V : a.K) + static_cast<int64_t>(head) * D + col;
+      const int64_t stride = is_v ? a.v_stride : a.k_stride;
 #pragma unroll
       for (int p = 0; p < PASS; ++p) {
-        const int r = p * RPP + row0;
-        if (r < r_lo || r >= r_hi) continue;
-        uint16_t* o = a.q_out + (static_cast<int64_t>(token0 + r) * a.q_heads + head) * D + col;
+        const int64_t s = src[p * RPP + row0];
+        x[p] = Raw{};
+        if (s >= 0) x[p] = load(base + s * stride);
+      }
+    }
+    if (!staged) {      // (while the first rows are on their way)
+      staged = true;
+#pragma unroll 4
+      for (int i = threadIdx.x; i < kKvBlock * H; i += kAppendThreads) {
+        const int r = i / H, p = i % H;
+        if (src[r] < 0) continue;
+        cs[r][p] = a.rope[static_cast<int64_t>(pos[p < a.sec0 ? 0 : p < a.sec01 ? 1 : 2][r]) * H + p];
+      }
+      __syncthreads();
+    }
+    if (!mine) break;
+    auto get = [&](int p, bool strict) {      // pass p's elements as they are to be stored
+      Pairs e;
+      widen(x[p].a, e.a);
+      widen(x[p].b, e.b);
+      if (!is_v && turned && src[p * RPP + row0] >= 0) turn(e, load_turn(&cs[p * RPP + row0][col]));
+      if (strict) drop_infinite(e);
+      return e;
+    };
+    // The rows stay 16 bits wide and are turned twice, for their maximum and for their codes: 32 registers instead of 64
+    float amax = 0.f;
+    bool strict = false;
+#pragma unroll 1
+    while (true) {
+      float2 all = make_float2(0.f, 0.f);
+      amax = 0.f;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const float* v = x[p][h].v;
-          *reinterpret_cast<uint4*>(o + h * H) =
-              make_uint4(bf16x2(v[0], v[1]), bf16x2(v[2], v[3]), bf16x2(v[4], v[5]), bf16x2(v[6], v[7]));
+      for (int p = 0; p < PASS; ++p) {
+        const Pairs e = get(p, strict);
+        see_finite(e, all);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          amax = ptx::max3(amax, fabsf(e.a[i].x), fabsf(e.a[i].y));
+          amax = ptx::max3(amax, fabsf(e.b[i].x), fabsf(e.b[i].y));
         }
       }
-      continue;
+      if (!__any_sync(0xffffffffu, !(all.x + all.y == 0.f))) break;
+      if (lane == 0) record_error(status, PACE_ERR_INVALID_ARG, K_KV_APPEND);
+      strict = true;      // what is not finite counts as 0
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
@@ -201,20 +245,22 @@ __global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(const __grid_
     }
     if (lane == 0) *scale = s;
     const float inv = __frcp_rn(s);   // exact: a power of two from 2^-120 to 2^64
+    const float2 inv2 = make_float2(inv, inv);
 #pragma unroll
     for (int p = 0; p < PASS; ++p) {
       const int r = p * RPP + row0;
       uint8_t* o = codes + r * D;
       if (src[r] >= 0) {
+        Pairs e = get(p, strict);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          float y[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) y[i] = fabsf(x[p][h].v[i]) < INFINITY ? __fmul_rn(x[p][h].v[i], inv) : 0.f;
-          *reinterpret_cast<uint2*>(o + h * H) = make_uint2(e4m3x4(y[0], y[1], y[2], y[3]), e4m3x4(y[4], y[5], y[6], y[7]));
+        for (int i = 0; i < 4; ++i) {
+          e.a[i] = ptx::fmul2(e.a[i], inv2);
+          e.b[i] = ptx::fmul2(e.b[i], inv2);
         }
+        *reinterpret_cast<uint2*>(o) = make_uint2(e4m3x4(e.a[0].x, e.a[0].y, e.a[1].x, e.a[1].y), e4m3x4(e.a[2].x, e.a[2].y, e.a[3].x, e.a[3].y));
+        *reinterpret_cast<uint2*>(o + H) = make_uint2(e4m3x4(e.b[0].x, e.b[0].y, e.b[1].x, e.b[1].y), e4m3x4(e.b[2].x, e.b[2].y, e.b[3].x, e.b[3].y));
       } else if (r < r_lo && ratio != 1.f) {   // an older token under the grown scale
-#pragma unroll
+#pragma unroll 1
         for (int h = 0; h < 2; ++h) {
           const uint2 w = *reinterpret_cast<const uint2*>(o + h * H);
           uint32_t z[2];
@@ -231,6 +277,40 @@ __global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(const __grid_
       }
     }
   }
+  if (a.q_heads == 0) return;
+  // ---- the queries: a warp keeps a pass of rows, with their angles, and goes over heads; warps share out the passes that have rows
+  const int p_lo = r_lo / RPP, live = (r_hi - 1) / RPP - p_lo + 1, over = live > 2 ? 4 : live;
+  const int p = p_lo + warp % over, r = p * RPP + row0;
+  if (p >= PASS || r < r_lo || r >= r_hi) return;
+  const int64_t s = src[r];
+  uint16_t* to = a.q_out + static_cast<int64_t>(token0 + r) * a.q_heads * D + col;
+  const uint16_t* from = a.Q + max(s, static_cast<int64_t>(0)) * a.q_stride + col;
+  Turn t{};
+  if (turned && s >= 0) t = load_turn(&cs[r][col]);
+  float2 all = make_float2(0.f, 0.f);
+  const int step = warps / over;
+#pragma unroll 1
+  for (int h0 = warp / over; h0 < a.q_heads; h0 += 4 * step) {
+    Raw x[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      x[k] = Raw{};      // (the query of a token that could not be found is zero)
+      if (h0 + k * step < a.q_heads && s >= 0) x[k] = load(from + static_cast<int64_t>(h0 + k * step) * D);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (h0 + k * step >= a.q_heads) break;
+      Pairs e;
+      widen(x[k].a, e.a);
+      widen(x[k].b, e.b);
+      if (turned) turn(e, t);
+      see_finite(e, all);
+      uint16_t* o = to + static_cast<int64_t>(h0 + k * step) * D;
+      *reinterpret_cast<uint4*>(o) = turned ? pack_bf16(e.a) : x[k].a;
+      *reinterpret_cast<uint4*>(o + H) = turned ? pack_bf16(e.b) : x[k].b;
+    }
+  }
+  if (!(all.x + all.y == 0.f)) record_error(status, PACE_ERR_INVALID_ARG, K_KV_APPEND);
 }
 
 __global__ void __launch_bounds__(256) rope_table_kernel(float2* table, int64_t n_positions, int half, double step) {
