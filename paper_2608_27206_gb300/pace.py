@@ -661,28 +661,34 @@ def pace_rope_table(n_positions: int, head_dim: int, base: float = 1e6, out: Opt
     return out
 
 
+_BF16, _INT32 = torch.bfloat16, torch.int32
+
+
 def _rows_of(t: torch.Tensor, heads: int, dim: int):
-    """(address, elements between rows) of bf16 [rows, heads, dim] whose rows may lie apart."""
-    if not t.is_cuda or t.dtype != torch.bfloat16:
+    """(address, elements between rows, rows) of bf16 [rows, heads, dim] whose rows may lie apart."""
+    if not t.is_cuda or t.dtype is not _BF16:
         raise ValueError("expected a CUDA tensor of bfloat16")
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim:
-        raise ValueError(f"expected [rows, {heads}, {dim}], got {tuple(t.shape)}")
-    stride = t.stride()
-    if stride[2] != 1 or (heads > 1 and stride[1] != dim):
+    shape = t.shape
+    if len(shape) != 3 or shape[1] != heads or shape[2] != dim:
+        raise ValueError(f"expected [rows, {heads}, {dim}], got {tuple(shape)}")
+    n = shape[0]
+    apart, head, one = t.stride()
+    if one != 1 or (heads > 1 and head != dim):
         raise ValueError("expected contiguous rows")
-    return t.data_ptr(), stride[0] if t.shape[0] > 1 else max(stride[0], heads * dim)
+    return t.data_ptr(), apart if n > 1 else max(apart, heads * dim), n
 
 
 def _int32(t: torch.Tensor, n: int, what: str) -> int:
-    if t.dtype != torch.int32 or not t.is_cuda or not t.is_contiguous() or t.numel() < n:
+    if t.dtype is not _INT32 or not t.is_cuda or not t.is_contiguous() or t.numel() < n:
         raise ValueError(f"{what}: expected at least {n} contiguous int32 on the device")
     return t.data_ptr()
 
 
 def _table(block_table: torch.Tensor, B: int):
-    if block_table.dim() != 2:
+    shape = block_table.shape
+    if len(shape) != 2:
         raise ValueError("block_table: expected [sequences, pages]")
-    return _int32(block_table, B * block_table.shape[1], "block_table"), block_table.shape[1]
+    return _int32(block_table, B * shape[1], "block_table"), shape[1]
 
 
 def pace_kv_append(cache: KvCache, K: torch.Tensor, V: torch.Tensor, cu_new, seq_lens: torch.Tensor,
@@ -698,15 +704,15 @@ def pace_kv_append(cache: KvCache, K: torch.Tensor, V: torch.Tensor, cu_new, seq
     cu, cp, B = _i32(cu_new)
     B -= 1
     n, hk, D = int(cu[-1]), cache.n_kv_heads, cache.head_dim
-    kp, ks = _rows_of(K, hk, D)
-    vp, vs = _rows_of(V, hk, D)
-    src = K.shape[0]
-    if V.shape[0] != src:
+    kp, ks, src = _rows_of(K, hk, D)
+    vp, vs, v_rows = _rows_of(V, hk, D)
+    if v_rows != src:
         raise ValueError("K and V differ in rows")
     tp, ts = _table(block_table, B)
     turn = None
     if rope is not None:
-        if rope.dtype != torch.float32 or rope.dim() != 3 or rope.shape[1] * 2 != D or rope.shape[2] != 2:
+        shape = rope.shape
+        if rope.dtype is not torch.float32 or len(shape) != 3 or shape[1] * 2 != D or shape[2] != 2:
             raise ValueError("rope: expected float32 [positions, D / 2, 2]")
         if positions is None or positions.shape[-1] != src:
             raise ValueError("positions: expected ids of every source row")
@@ -715,16 +721,16 @@ def pace_kv_append(cache: KvCache, K: torch.Tensor, V: torch.Tensor, cu_new, seq
         ids = positions.shape[0] if positions.dim() == 2 else 1
         if len(sec) != 3 or any(s > 0 for s in sec[ids:]):
             raise ValueError("sections: more than rows of ids")
-        turn = Rope(_dev(rope), _int32(positions, ids * src, "positions"), rope.shape[0], src, (ctypes.c_int32 * 3)(*sec))
+        turn = Rope(_dev(rope), _int32(positions, ids * src, "positions"), shape[0], src, tuple(sec))
     qp, qs, hq, op = None, 0, 0, None
     if q is not None:
         hq = q.shape[1]
-        qp, qs = _rows_of(q, hq, D)
-        if q.shape[0] != src:
+        qp, qs, q_rows = _rows_of(q, hq, D)
+        if q_rows != src:
             raise ValueError("K and q differ in rows")
         if q_out is None:
             q_out = torch.empty((n, hq, D), dtype=torch.bfloat16, device=q.device)
-        elif q_out.dtype != torch.bfloat16 or q_out.numel() < n * hq * D:
+        elif q_out.dtype is not _BF16 or q_out.numel() < n * hq * D:
             raise ValueError("q_out: expected bfloat16 [new tokens, heads, D]")
         op = _dev(q_out)
     _check("pace_kv_append",
@@ -751,14 +757,14 @@ def pace_kv_attention(cache: KvCache, Q: torch.Tensor, cu_q, seq_lens: torch.Ten
     B -= 1
     n, D = int(cu[-1]), cache.head_dim
     hq = Q.shape[1]
-    qp, qs = _rows_of(Q, hq, D)
-    if Q.shape[0] < n:
+    qp, qs, q_rows = _rows_of(Q, hq, D)
+    if q_rows < n:
         raise ValueError("fewer queries than cu_q says")
     if scale is None:
         scale = float(D) ** -0.5
     if out is None:
         out = torch.empty((n, hq, D), dtype=torch.bfloat16, device=Q.device)
-    elif out.dtype != torch.bfloat16 or out.numel() < n * hq * D:
+    elif out.dtype is not _BF16 or out.numel() < n * hq * D:
         raise ValueError("out: expected bfloat16 [new tokens, heads, D]")
     if lse is not None and (lse.dtype != torch.float32 or lse.numel() < n * hq):
         raise ValueError("lse: expected float32 [new tokens, heads]")
