@@ -279,6 +279,15 @@ __device__ __forceinline__ bool kv_wait(uint32_t bar, uint32_t parity) {
   return true;
 }
 
+// A warp's wait, which leaves it converged.
+__device__ __forceinline__ bool kv_wait_warp(uint32_t bar, uint32_t parity) {
+  int left = 1 << 18;
+#pragma unroll 1
+  while (!__all_sync(0xffffffffu, ptx::mbar_try_wait(bar, parity)))
+    if (--left == 0) return false;
+  return true;
+}
+
 // A role that gives up on a wait says so here; the others leave as their own waits run out.
 __device__ __forceinline__ bool stopped(const int* abort) { return *reinterpret_cast<const volatile int*>(abort) != 0; }
 __device__ __forceinline__ void stop(int* abort, int* status) {

@@ -44,16 +44,16 @@ struct PrefillCfg {
   static constexpr int VTILE = VCHUNK * D / 64;
   static constexpr uint32_t SWIZZLE = D == 128 ? 2 : 4;
   static constexpr uint32_t GROUP = 8 * D;
-  static constexpr uint32_t IDESC_S = idesc_e4m3_f32(128, kHalf, false, false);
+  static constexpr uint32_t IDESC_S = idesc_e4m3_f32(128, kKvTile, false, false);
   static constexpr uint32_t IDESC_O = idesc_f16_mn_f32(128, D);
 };
 
 template <int D>
 struct alignas(16) PrefillCtl {
   static constexpr int ST = PrefillCfg<D>::STAGES, SV = PrefillCfg<D>::VSTAGES;
-  uint64_t full[ST], empty[ST], v_empty[SV], ready[2], vfree[2], s_full[2][2], p_full[2][2], q_full[2], o_done[2][2];
+  uint64_t full[ST], empty[ST], v_empty[SV], known[4], ready[2], vfree[2], s_full[2], p_full[2][2], q_full[2], o_done[2][2];
   float scales[ST][16];
-  float4 block[2][8];           // per block of 16 slots: K scale, log2(V scale), 1 / V scale
+  float4 block[4][8];           // of the last tiles, per block of 16 slots: K scale, log2(V scale), 1 / V scale
   uint32_t nan[2][4];           // slots of which some row sees a NaN value
   int scan[2 * kThreads / 32];
   KvShare share;
@@ -108,9 +108,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   auto full = [&](int s) { return smem_u32(&ctl->full[s]); };
   auto empty = [&](int s) { return smem_u32(&ctl->empty[s]); };
+  auto known = [&](int b) { return smem_u32(&ctl->known[b]); };
   auto ready = [&](int b) { return smem_u32(&ctl->ready[b]); };
   auto vfree = [&](int b) { return smem_u32(&ctl->vfree[b]); };
-  auto s_full = [&](int i, int h) { return smem_u32(&ctl->s_full[i][h]); };
+  auto s_full = [&](int i) { return smem_u32(&ctl->s_full[i]); };
   auto p_full = [&](int i, int h) { return smem_u32(&ctl->p_full[i][h]); };
   auto q_full = [&](int i) { return smem_u32(&ctl->q_full[i]); };
   auto o_done = [&](int i, int h) { return smem_u32(&ctl->o_done[i][h]); };
@@ -129,11 +130,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
       mbar_init(empty(s), 1);
     }
     for (int s = 0; s < C::VSTAGES; ++s) mbar_init(smem_u32(&ctl->v_empty[s]), 2);
+    for (int b = 0; b < 4; ++b) mbar_init(known(b), 1);
     for (int i = 0; i < 2; ++i) {
       mbar_init(ready(i), 2);
       mbar_init(vfree(i), 1);
+      mbar_init(s_full(i), 1);
       for (int h = 0; h < 2; ++h) {
-        mbar_init(s_full(i, h), 1);
         mbar_init(p_full(i, h), 4);
         mbar_init(o_done(i, h), 1);
       }
@@ -156,8 +158,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
     walk.begin(share);
     kv_fetch<D, ST, C::VSTAGES>(maps, a, walk, KvRings{sK, sC, C::TILE, ctl->full, ctl->empty, ctl->v_empty, ctl->scales}, &ctl->abort, status);
   } else if (warp == 1) {
-    // ---- products: S of a half tile goes ahead of the P V before it, so that neither the tensor pipe nor the rows' owners
-    // wait for the other; A and B in turn -----------------------------------------------------------
+    // ---- products: P V of a slot tile, half by half as the weights come, then S of the next; A and B in turn ----------
+    // The warp stays converged: operands of these instructions are registers of the whole warp, and in one lane's branch each took 80
+    // clocks.
     KvWalk<kManyRows> walk;
     walk.begin(share);
     const KvItem& it = walk.it;
@@ -168,19 +171,22 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
     int t = 0, done_a = 0, done_b = 0, items_a = 0, items_b = 0;      // slot tiles; of a row tile: slot tiles, items
     bool ok = true;
     auto wait = [&](uint32_t bar, int round) {
-      ok = __all_sync(0xffffffffu, kv_wait(bar, round & 1));
+      ok = kv_wait_warp(bar, round & 1);
       return ok;
     };
-    auto scores = [&](int i, int u, int h) {      // S of half h of slot tile u
+    auto commit = [&](uint32_t bar) {
+      if (issue) mma_commit(bar);
+    };
+    auto scores = [&](int i, int u) {      // S of slot tile u
       const uint64_t q = dq + static_cast<uint64_t>(i * 2 * (C::QTILE >> 4));
-      const uint64_t k0 = dk + static_cast<uint64_t>((u % ST) * (C::TILE >> 4) + h * (kHalf * D >> 4));
+      const uint64_t k0 = dk + static_cast<uint64_t>((u % ST) * (C::TILE >> 4));
 #pragma unroll
       for (int part = 0; part < 2; ++part)
 #pragma unroll
         for (int k = 0; k < D / 32; ++k)
-          mma_f8_ss(tmem + i * 128 + h * kHalf, q + static_cast<uint64_t>(part * (C::QTILE >> 4) + 2 * k), k0 + static_cast<uint64_t>(2 * k), C::IDESC_S,
+          mma_f8_ss(tmem + i * 128, q + static_cast<uint64_t>(part * (C::QTILE >> 4) + 2 * k), k0 + static_cast<uint64_t>(2 * k), C::IDESC_S,
                     part > 0 || k > 0, issue);
-      if (issue) mma_commit(s_full(i, h));
+      commit(s_full(i));
     };
     while (ok && walk.next(a)) {
       const int n = it.t1 - it.t0, two = it.rows > 128;
@@ -189,31 +195,35 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
       for (int i = 0; i <= two; ++i) {
         if (!wait(q_full(i), i == 0 ? items_a++ : items_b++)) break;
         tc_fence_after_sync();
-        scores(i, t, 0);
-        scores(i, t, 1);
+        scores(i, t);
       }
       if (!ok) break;
-      if (issue) mma_commit(empty(t % ST));
+      commit(empty(t % ST));
+      if ((n > 1 && !wait(full((t + 1) % ST), (t + 1) / ST)) || !wait(ready(t & 1), t >> 1)) break;
 #pragma unroll 1
-      for (int g = 0; ok && g < 2 * n; ++g) {      // P V of half tile g, S of half tile g + 2
-        const int u = t + (g >> 1), h = g & 1;
-        const bool more = g + 2 < 2 * n;
-        if (h == 0 && !wait(ready(u & 1), u >> 1)) break;
-        if (h == 0 && more && !wait(full((u + 1) % ST), (u + 1) / ST)) break;
-#pragma unroll 1
-        for (int i = 0; i <= two; ++i) {
-          if (!wait(p_full(i, h), (i == 0 ? done_a : done_b) + (g >> 1))) break;
-          tc_fence_after_sync();
-          const uint64_t v = dv + static_cast<uint64_t>((u & 1) * (C::VTILE >> 4) + h * (kHalf * 128 >> 4));
+      for (int u = t; ok && u < t + n; ++u) {
+        const bool more = u + 1 < t + n;
+        const uint64_t v = dv + static_cast<uint64_t>((u & 1) * (C::VTILE >> 4));
 #pragma unroll
-          for (int k = 0; k < kHalf / 16; ++k)
-            mma_f16_ts(tmem + 256 + i * 128, tmem + i * 128 + h * kHalf + k * 8, v + static_cast<uint64_t>(k * (2048 >> 4)), C::IDESC_O, g > 0 || k > 0, issue);
-          if (issue) mma_commit(o_done(i, h));
-          if (more) scores(i, u + 1, h);
+        for (int i = 0; i < 2; ++i) {
+          if (!ok || i > two) break;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            if (!wait(p_full(i, h), (i == 0 ? done_a : done_b) + u - t)) break;
+            tc_fence_after_sync();
+#pragma unroll
+            for (int k = 0; k < kHalf / 16; ++k)
+              mma_f16_ts(tmem + 256 + i * 128, tmem + i * 128 + h * kHalf + k * 8, v + static_cast<uint64_t>((h * 4 + k) * (2048 >> 4)), C::IDESC_O,
+                         u > t || h > 0 || k > 0, issue);
+            commit(o_done(i, h));
+          }
+          if (ok && more) scores(i, u + 1);
         }
-        if (ok && issue && h == 1) {
-          mma_commit(vfree(u & 1));
-          if (more) mma_commit(empty((u + 1) % ST));
+        if (!ok) break;
+        commit(vfree(u & 1));
+        if (more) {
+          commit(empty((u + 1) % ST));
+          if ((u + 2 < t + n && !wait(full((u + 2) % ST), (u + 2) / ST)) || !wait(ready((u + 1) & 1), (u + 1) >> 1)) break;
         }
       }
       t += n;
@@ -233,8 +243,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
 #pragma unroll 1
       for (int j = it.t0; ok && j < it.t1; ++j, ++t) {
         const int s = t % ST, b = t & 1, slot0 = it.span.tile(j) * kKvTile;
-        ok = kv_wait(full(s), (t / ST) & 1) && (t < 2 || kv_wait(vfree(b), ((t >> 1) - 1) & 1));
-        ok = __all_sync(0xffffffffu, ok);
+        ok = __all_sync(0xffffffffu, kv_wait(full(s), (t / ST) & 1));
         if (!ok) break;
         // 0 * NaN is NaN: no slot of V that some row does not see may hold one.  Slots that nobody sees become zero; where rows
         // differ, so does a slot with a NaN, and rows that see it take a NaN weight for it.
@@ -243,8 +252,14 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
         if (warp == 2 && lane < 8) {      // (where the slots are not there, or rows differ, no scale may be NaN either)
           float ks = ctl->scales[s][lane], vs = ctl->scales[s][8 + lane];
           if (!whole && (slot0 + lane * kKvBlock > it.p_last || !usable(ks) || !usable(vs))) ks = vs = 1.f;
-          ctl->block[b][lane] = make_float4(ks, log2f(vs), 1.f / vs, 0.f);
+          ctl->block[t & 3][lane] = make_float4(ks, log2f(vs), 1.f / vs, 0.f);
         }
+        // (known before V is: the rows' owners need it first.  Their last use of this place, four tiles ago, was over when `vfree` of
+        // the tile before the last but one was waited for)
+        __syncwarp();
+        if (warp == 2 && lane == 0) mbar_arrive(known(t & 3));
+        ok = __all_sync(0xffffffffu, t < 2 || kv_wait(vfree(b), ((t >> 1) - 1) & 1));
+        if (!ok) break;
 #pragma unroll 1
         for (int part = warp - 2; part < 4; part += 2) {
           const int row = part * 32 + lane, slot = slot0 + row;      // a slot of the tile
@@ -316,7 +331,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
       };
       float c;                  // scale2 * the row's power of two
       {
-        // q as hi and lo codes.  A row waits in its places in the hi and the lo tile until its owner turns it into them
+        // q as hi and lo codes.  A row waits in its places until its owner turns it into them, 16 elements at a time and in place: of a
+        // pair of chunks the first is in the hi tile and the second in the lo tile
         {
           const unsigned long long from = real ? reinterpret_cast<unsigned long long>(kv_query(a, it, row, D)) : 0;
           uint4 u[32 / STEP];
@@ -326,24 +342,24 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
             u[k] = src != 0 ? *(reinterpret_cast<const uint4*>(src) + part) : make_uint4(0, 0, 0, 0);
           }
 #pragma unroll
-          for (int k = 0; k < 32 / STEP; ++k) *reinterpret_cast<uint4*>(place(k * STEP + sub, part)) = u[k];
+          for (int k = 0; k < 32 / STEP; ++k) *reinterpret_cast<uint4*>(place(k * STEP + sub, part / 2 + (part & 1) * (D / 16))) = u[k];
         }
         __syncwarp();
-        uint4 u[D / 8];
         uint32_t most = 0;      // largest magnitude, as the bits of two bf16 without their signs
-#pragma unroll
+#pragma unroll 4
         for (int e = 0; e < D / 8; ++e) {
-          u[e] = *reinterpret_cast<const uint4*>(place(lane, e));
-          most = __vmaxu2(__vmaxu2(most, __vmaxu2(u[e].x & 0x7FFF7FFFu, u[e].y & 0x7FFF7FFFu)), __vmaxu2(u[e].z & 0x7FFF7FFFu, u[e].w & 0x7FFF7FFFu));
+          const uint4 u = *reinterpret_cast<const uint4*>(place(lane, e));
+          most = __vmaxu2(__vmaxu2(most, __vmaxu2(u.x & 0x7FFF7FFFu, u.y & 0x7FFF7FFFu)), __vmaxu2(u.z & 0x7FFF7FFFu, u.w & 0x7FFF7FFFu));
         }
         const uint32_t top = max(most & 0xFFFFu, most >> 16);
         const bool fin = top < 0x7F80u;
         const int e2 = fin ? max(static_cast<int>(top >> 7) - 127 - 7, -110) : 0;      // top 2^-e2 in [128, 256)
         const float inv = fin ? __uint_as_float(static_cast<uint32_t>(127 - e2) << 23) : NAN;      // (a row that is not finite: NaN throughout)
         c = a.scale2 * __uint_as_float(static_cast<uint32_t>(127 + e2) << 23);
-#pragma unroll
-        for (int e = 0; e < D / 16; ++e) {      // 16 elements at a time: by way of f16, which holds them (and 2^-24 where e4m3 ends at 2^-9)
-          const uint32_t w[8] = {u[2 * e].x, u[2 * e].y, u[2 * e].z, u[2 * e].w, u[2 * e + 1].x, u[2 * e + 1].y, u[2 * e + 1].z, u[2 * e + 1].w};
+#pragma unroll 2
+        for (int e = 0; e < D / 16; ++e) {      // by way of f16, which holds them (and 2^-24 where e4m3 ends at 2^-9)
+          const uint4 u0 = *reinterpret_cast<const uint4*>(place(lane, e)), u1 = *reinterpret_cast<const uint4*>(place(lane, e + D / 16));
+          const uint32_t w[8] = {u0.x, u0.y, u0.z, u0.w, u1.x, u1.y, u1.z, u1.w};
           uint32_t hi[4], lo[4];
 #pragma unroll
           for (int k = 0; k < 4; ++k) split_e4m3(pair_f16(w[2 * k], inv), pair_f16(w[2 * k + 1], inv), hi[k], lo[k]);
@@ -356,17 +372,23 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
       }
       float w = kNone, l = 0.f;
       const int n = it.t1 - it.t0;
+      int slot0 = 0;
+      bool whole = true;
 #pragma unroll 1
       for (int g = 0; g < 2 * n; ++g) {      // half tiles
-        const int h = g & 1, u = t + (g >> 1), b = u & 1, slot0 = it.span.tile(it.t0 + (g >> 1)) * kKvTile;
+        const int h = g & 1, u = t + (g >> 1), b = u & 1;
         const uint32_t sX = sS + h * kHalf;
-        // (S first: a row tile that left items out may be rounds ahead of the others until its products run)
-        ok = kv_wait(s_full(i, h), (mine + (g >> 1)) & 1) && (h == 1 || kv_wait(ready(b), (u >> 1) & 1));
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) break;
-        tc_fence_after_sync();
-        const float4* block = &ctl->block[b][4 * h];
-        if (!kv_whole(slot0, p_lo, p_hi, a.window, a.sinks)) {      // what the row does not see becomes -inf
+        if (h == 0) {
+          slot0 = it.span.tile(it.t0 + (g >> 1)) * kKvTile;
+          whole = kv_whole(slot0, p_lo, p_hi, a.window, a.sinks);
+          // (S first: a row tile that left items out may be rounds ahead of the others until its products run)
+          ok = kv_wait(s_full(i), (mine + (g >> 1)) & 1) && kv_wait(known(u & 3), (u >> 2) & 1) && (whole || kv_wait(ready(b), (u >> 1) & 1));
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          tc_fence_after_sync();
+        }
+        const float4* block = &ctl->block[u & 3][4 * h];
+        if (!whole) {      // what the row does not see becomes -inf
           // (it sees slots up to p that are past `from` or before `few`)
           const int from = a.window > 0 ? p - a.window : -1, few = a.window > 0 ? a.sinks : INT32_MAX;
           auto below = [](int m) { return m >= 32 ? 0xFFFFFFFFu : m <= 0 ? 0u : (1u << m) - 1u; };      // columns 0 .. m - 1
@@ -388,11 +410,49 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
           tmem_wait_st();
         }
         uint32_t words[32];
+        bool over = g == 0;      // the row's w has to move
+        float sum = INFINITY;    // (by how much: not known)
 #pragma unroll 1
         while (true) {
+          if (__any_sync(0xffffffffu, over)) {
+            // w moves in the rows that need it, and O (once its products have completed) and l with it: to a power that covers the sum
+            // of the weights, or to the scores' maximum where that is not known.  The weights start (again) from S, which is whole.
+            float now = over ? w + static_cast<float>(static_cast<int>(__float_as_uint(sum) >> 23) - 126) : w;
+            if (__any_sync(0xffffffffu, over && !(sum < INFINITY))) {
+              float top = kNone;
+#pragma unroll 1
+              for (int e0 = 0; e0 < 4; ++e0) {
+                uint32_t y[16];
+                load_cols(sX + 16 * e0, y);
+                const float4 k = block[e0];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) top = fmaxf(top, fmaf(__uint_as_float(y[e]), fmaxf(k.x * c, 1e-37f), k.y));
+              }
+              if (over && !(sum < INFINITY)) now = ceilf(top);
+            }
+            const float f = ex2_approx(w - now);
+            w = now;
+            l *= f;
+            if (g > 0) {
+              // (S of the tile is complete, so the products of the tiles before are)
+              if (h == 1) ok = __all_sync(0xffffffffu, kv_wait(o_done(i, 0), (mine + (g >> 1)) & 1));
+              if (!ok) break;
+              tc_fence_after_sync();
+#pragma unroll 1
+              for (int e0 = 0; e0 < D / 32; ++e0) {
+                uint32_t y[32];
+                load_cols(sO + 32 * e0, y);
+#pragma unroll
+                for (int e = 0; e < 32; ++e) y[e] = __float_as_uint(__uint_as_float(y[e]) * f);
+                tmem_st_32x32b(sO + 32 * e0, y);
+              }
+              tmem_wait_st();
+            }
+          }
           uint32_t x[64];
           load_cols(sX, x);
-          float sum = 0.f, dl = 0.f;
+          float dl = 0.f;
+          sum = 0.f;
 #pragma unroll
           for (int e0 = 0; e0 < 4; ++e0) {      // a block's columns
             const float4 k = block[e0];
@@ -416,37 +476,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
             sum += all;
             dl = fmaf(all, k.z, dl);
           }
-          if (!__any_sync(0xffffffffu, sum >= kMost)) {
+          over = sum >= kMost;
+          if (!__any_sync(0xffffffffu, over)) {
             l += dl;
             break;
-          }
-          // w moves to the maximum, in the rows that need it, and O (once its products have completed) and l with it; the
-          // weights start again from S, which is still whole
-          float top = kNone;
-#pragma unroll 1
-          for (int e0 = 0; e0 < 4; ++e0) {
-            uint32_t y[16];
-            load_cols(sX + 16 * e0, y);
-            const float4 k = block[e0];
-#pragma unroll
-            for (int e = 0; e < 16; ++e) top = fmaxf(top, fmaf(__uint_as_float(y[e]), fmaxf(k.x * c, 1e-37f), k.y));
-          }
-          const float now = sum >= kMost ? ceilf(top) : w, f = ex2_approx(w - now);
-          w = now;
-          l *= f;
-          if (g > 0) {
-            ok = __all_sync(0xffffffffu, kv_wait(o_done(i, h ^ 1), (mine + ((g - 1) >> 1)) & 1));
-            if (!ok) break;
-            tc_fence_after_sync();
-#pragma unroll 1
-            for (int e0 = 0; e0 < D / 16; ++e0) {
-              uint32_t y[16];
-              load_cols(sO + 16 * e0, y);
-#pragma unroll
-              for (int e = 0; e < 16; ++e) y[e] = __float_as_uint(__uint_as_float(y[e]) * f);
-              tmem_st_32x32b(sO + 16 * e0, y);
-            }
-            tmem_wait_st();
           }
         }
         if (!ok) break;

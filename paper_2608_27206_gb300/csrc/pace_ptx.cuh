@@ -295,7 +295,7 @@ __host__ __device__ constexpr uint32_t idesc_f16_mn_f32(int M, int N) {
 
 // D[tmem] (+)= A[tmem] * B[smem]^T, 16-bit, 16 elements along K, issued likewise; A: row r in lane r, two elements per column.
 __device__ __forceinline__ void mma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accumulate,
-                                           uint32_t issue) {
+                                           uint32_t issue = 1) {
   asm volatile(
       "{\n\t.reg .pred p, q;\n\t"
       "setp.ne.b32 p, %4, 0;\n\t"
