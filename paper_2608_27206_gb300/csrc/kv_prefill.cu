@@ -370,7 +370,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
         __syncwarp();
         if (lane == 0) mbar_arrive(q_full(i));
       }
-      float w = kNone, l = 0.f;
+      float w = kNone, l = 0.f, peak = 0.f;      // peak: the largest sum of 64 weights under w
       const int n = it.t1 - it.t0;
       int slot0 = 0;
       bool whole = true;
@@ -417,7 +417,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
           if (__any_sync(0xffffffffu, over)) {
             // w moves in the rows that need it, and O (once its products have completed) and l with it: to a power that covers the sum
             // of the weights, or to the scores' maximum where that is not known.  The weights start (again) from S, which is whole.
-            float now = over ? w + static_cast<float>(static_cast<int>(__float_as_uint(sum) >> 23) - 126) : w;
+            // (A move costs the same for a row and for 32: those that have outgrown their w by less come along, which leaves them
+            // further from the next)
+            peak = over ? sum : peak;
+            float now = peak >= 2.f ? w + static_cast<float>(static_cast<int>(__float_as_uint(peak) >> 23) - 126) : w;
             if (__any_sync(0xffffffffu, over && !(sum < INFINITY))) {
               float top = kNone;
 #pragma unroll 1
@@ -433,18 +436,25 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
             const float f = ex2_approx(w - now);
             w = now;
             l *= f;
+            peak = 0.f;
             if (g > 0) {
               // (S of the tile is complete, so the products of the tiles before are)
               if (h == 1) ok = __all_sync(0xffffffffu, kv_wait(o_done(i, 0), (mine + (g >> 1)) & 1));
               if (!ok) break;
               tc_fence_after_sync();
 #pragma unroll 1
-              for (int e0 = 0; e0 < D / 32; ++e0) {
-                uint32_t y[32];
-                load_cols(sO + 32 * e0, y);
+              for (int e0 = 0; e0 < D / 64; ++e0) {
+                uint32_t y[32], z[32];
+                tmem_ld_32x32b(sO + 64 * e0, y);
+                load_cols(sO + 64 * e0 + 32, z);
+                reg_fence(y);
 #pragma unroll
-                for (int e = 0; e < 32; ++e) y[e] = __float_as_uint(__uint_as_float(y[e]) * f);
-                tmem_st_32x32b(sO + 32 * e0, y);
+                for (int e = 0; e < 32; ++e) {
+                  y[e] = __float_as_uint(__uint_as_float(y[e]) * f);
+                  z[e] = __float_as_uint(__uint_as_float(z[e]) * f);
+                }
+                tmem_st_32x32b(sO + 64 * e0, y);
+                tmem_st_32x32b(sO + 64 * e0 + 32, z);
               }
               tmem_wait_st();
             }
@@ -479,6 +489,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
           over = sum >= kMost;
           if (!__any_sync(0xffffffffu, over)) {
             l += dl;
+            peak = fmaxf(peak, sum);
             break;
           }
         }
