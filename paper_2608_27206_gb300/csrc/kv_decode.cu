@@ -453,65 +453,78 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
 }
 
 // The items that several CTAs walked: out = sum_c 2^(lse_c - max) o_c / sum_c 2^(lse_c - max), parts in a fixed order.  What it
-// takes is latency, so all of a warp's loads go out at once.  A row has SPLIT warps: 8 where rows are few (a sequence alone makes as
-// many parts as there are tiles: 38 parts took 8 us with one warp), 1 where they are many and a row has few parts.
-template <int D, int SPLIT>
+// takes is latency, so a warp's loads go out together, PARTS parts of ROWS rows at a time.  Where rows are few a row has 8 warps (a
+// sequence alone makes as many parts as there are tiles: 38 of them took 8 us with one warp); where they are many and a row has few
+// parts, a warp has 4 rows (a call of 517 tokens: 97 us in all, with one row 99).
+template <int D, int ROWS, int PARTS, int SPLIT>
 __global__ void __launch_bounds__(256) kv_attn_combine(const __grid_constant__ KvAttnArgs a, int tile_rows) {
   constexpr int E = D / 32;      // elements of a lane
+  static_assert(ROWS == 1 || SPLIT == 1, "a warp has several rows or a row several warps");
   __shared__ float s_top[8], s_sum[8];
-  __shared__ __align__(16) float s_o[8][D];
+  __shared__ __align__(16) float s_o[SPLIT > 1 ? 8 : 1][D];
   launch_dependents();
   grid_dependency_wait();
   const int c = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int4 raw = __ldcg(reinterpret_cast<const int4*>(a.split + c));
   const KvSplit sp{raw.x, raw.y, raw.z, raw.w};
   if (sp.followers == 0) return;
-  const int q = blockIdx.y * (8 / SPLIT) + warp / SPLIT;
-  const int row = sp.row_tile * tile_rows + q;
-  if (row >= a.s.nq[sp.i] * a.group) return;      // (the row's warps all)
-  auto at = [&](int j) { return static_cast<int64_t>(j == 0 ? 2 * c + 1 : 2 * (c + j)) * tile_rows + q; };
+  const int q0 = (blockIdx.y * (8 / SPLIT) + warp / SPLIT) * ROWS;
+  const int live = min(ROWS, a.s.nq[sp.i] * a.group - sp.row_tile * tile_rows - q0);      // rows of this warp
+  if (live <= 0) return;      // (a row's warps all)
+  auto at = [&](int j, int r) { return static_cast<int64_t>(j == 0 ? 2 * c + 1 : 2 * (c + j)) * tile_rows + q0 + r; };
   const int parts = sp.followers + 1;
-  float top = -INFINITY, sum = 0.f, o[E];
+  float top = -INFINITY, sum = 0.f, o[ROWS][E];      // of row lane / PARTS (the same in its PARTS lanes); of every row
 #pragma unroll
-  for (int e = 0; e < E; ++e) o[e] = 0.f;
+  for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[r][e] = 0.f;
 #pragma unroll 1
-  for (int j0 = warp % SPLIT; j0 < parts; j0 += 8 * SPLIT) {      // parts j0, j0 + SPLIT, ... : 8 at a time
-    const int j_mine = j0 + (lane & 7) * SPLIT;
-    const float lse = j_mine < parts ? __ldcg(a.part_lse + at(j_mine)) : -INFINITY;
-    float v[8][E];
+  for (int j0 = warp % SPLIT; j0 < parts; j0 += PARTS * SPLIT) {      // parts j0, j0 + SPLIT, ...
+    const int j_mine = j0 + lane % PARTS * SPLIT, r_mine = lane / PARTS;
+    const float lse = j_mine < parts && r_mine < live ? __ldcg(a.part_lse + at(j_mine, r_mine)) : -INFINITY;
+    float v[ROWS][PARTS][E];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int r = 0; r < ROWS; ++r)
 #pragma unroll
-      for (int e = 0; e < E; ++e) v[k][e] = 0.f;
-      if (j0 + k * SPLIT >= parts) continue;
-      const float* p = a.part + at(j0 + k * SPLIT) * D + lane * E;
-      if constexpr (E == 4) {
-        const float4 u = __ldcg(reinterpret_cast<const float4*>(p));
-        v[k][0] = u.x;
-        v[k][1] = u.y;
-        v[k][2] = u.z;
-        v[k][3] = u.w;
-      } else {
-        const float2 u = __ldcg(reinterpret_cast<const float2*>(p));
-        v[k][0] = u.x;
-        v[k][1] = u.y;
+      for (int k = 0; k < PARTS; ++k) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[r][k][e] = 0.f;
+        if (j0 + k * SPLIT >= parts || r >= live) continue;
+        const float* p = a.part + at(j0 + k * SPLIT, r) * D + lane * E;
+        if constexpr (E == 4) {
+          const float4 u = __ldcg(reinterpret_cast<const float4*>(p));
+          v[r][k][0] = u.x;
+          v[r][k][1] = u.y;
+          v[r][k][2] = u.z;
+          v[r][k][3] = u.w;
+        } else {
+          const float2 u = __ldcg(reinterpret_cast<const float2*>(p));
+          v[r][k][0] = u.x;
+          v[r][k][1] = u.y;
+        }
       }
-    }
     float now = lse;
 #pragma unroll
-    for (int s = 4; s > 0; s >>= 1) now = fmaxf(now, __shfl_xor_sync(0xffffffffu, now, s));
+    for (int s = PARTS / 2; s > 0; s >>= 1) now = fmaxf(now, __shfl_xor_sync(0xffffffffu, now, s));
     now = fmaxf(now, top);
     const float base = now == -INFINITY ? 0.f : now, f = exp2f(top - base), mine = exp2f(lse - base);
     top = now;
     sum *= f;
+    float all = mine;
 #pragma unroll
-    for (int e = 0; e < E; ++e) o[e] *= f;
+    for (int s = PARTS / 2; s > 0; s >>= 1) all += __shfl_xor_sync(0xffffffffu, all, s);
+    sum += all;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const float w = __shfl_sync(0xffffffffu, mine, k);
-      sum += w;
+    for (int r = 0; r < ROWS; ++r) {
+      const float fr = __shfl_sync(0xffffffffu, f, r * PARTS);
 #pragma unroll
-      for (int e = 0; e < E; ++e) o[e] = fmaf(w, v[k][e], o[e]);
+      for (int e = 0; e < E; ++e) o[r][e] *= fr;
+#pragma unroll
+      for (int k = 0; k < PARTS; ++k) {
+        const float w = __shfl_sync(0xffffffffu, mine, r * PARTS + k);
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[r][e] = fmaf(w, v[r][k][e], o[r][e]);
+      }
     }
   }
   if constexpr (SPLIT > 1) {
@@ -520,34 +533,40 @@ __global__ void __launch_bounds__(256) kv_attn_combine(const __grid_constant__ K
       s_sum[warp] = sum;
     }
 #pragma unroll
-    for (int e = 0; e < E; ++e) s_o[warp][lane * E + e] = o[e];
+    for (int e = 0; e < E; ++e) s_o[warp][lane * E + e] = o[0][e];
     __syncthreads();
     if (warp > 0) return;
+    top = s_top[0];
 #pragma unroll
     for (int k = 1; k < SPLIT; ++k) top = fmaxf(top, s_top[k]);
     const float base = top == -INFINITY ? 0.f : top;
     sum = 0.f;
 #pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = 0.f;
+    for (int e = 0; e < E; ++e) o[0][e] = 0.f;
 #pragma unroll
     for (int k = 0; k < SPLIT; ++k) {
       const float f = exp2f(s_top[k] - base);
       sum = fmaf(f, s_sum[k], sum);
 #pragma unroll
-      for (int e = 0; e < E; ++e) o[e] = fmaf(f, s_o[k][lane * E + e], o[e]);
+      for (int e = 0; e < E; ++e) o[0][e] = fmaf(f, s_o[k][lane * E + e], o[0][e]);
     }
   }
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  const int token = static_cast<int>(a.by_group(row));
-  const int64_t dst = static_cast<int64_t>(a.s.q0[sp.i] + token) * a.q_heads + sp.head * a.group + row - token * a.group;
-  uint32_t w[E / 2];
 #pragma unroll
-  for (int e = 0; e < E / 2; ++e)
-    w[e] = static_cast<uint32_t>(__bfloat16_as_ushort(__float2bfloat16_rn(o[2 * e] * inv))) |
-           static_cast<uint32_t>(__bfloat16_as_ushort(__float2bfloat16_rn(o[2 * e + 1] * inv))) << 16;
-  if constexpr (E == 4) *reinterpret_cast<uint2*>(a.out + dst * D + lane * E) = make_uint2(w[0], w[1]);
-  else *reinterpret_cast<uint32_t*>(a.out + dst * D + lane * E) = w[0];
-  if (lane == 0 && a.lse != nullptr) a.lse[dst] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.69314718055994531f;
+  for (int r = 0; r < ROWS; ++r) {
+    if (r >= live) break;
+    const float s = __shfl_sync(0xffffffffu, sum, r * PARTS), m = __shfl_sync(0xffffffffu, top, r * PARTS);
+    const float inv = s == 0.f ? 0.f : 1.f / s;
+    const int row = sp.row_tile * tile_rows + q0 + r, token = static_cast<int>(a.by_group(row));
+    const int64_t dst = static_cast<int64_t>(a.s.q0[sp.i] + token) * a.q_heads + sp.head * a.group + row - token * a.group;
+    uint32_t w[E / 2];
+#pragma unroll
+    for (int e = 0; e < E / 2; ++e)
+      w[e] = static_cast<uint32_t>(__bfloat16_as_ushort(__float2bfloat16_rn(o[r][2 * e] * inv))) |
+             static_cast<uint32_t>(__bfloat16_as_ushort(__float2bfloat16_rn(o[r][2 * e + 1] * inv))) << 16;
+    if constexpr (E == 4) *reinterpret_cast<uint2*>(a.out + dst * D + lane * E) = make_uint2(w[0], w[1]);
+    else *reinterpret_cast<uint32_t*>(a.out + dst * D + lane * E) = w[0];
+    if (lane == 0 && a.lse != nullptr) a.lse[dst] = s == 0.f ? -INFINITY : (m + log2f(s)) * 0.69314718055994531f;
+  }
 }
 
 template <int D, int NQ>
@@ -577,10 +596,10 @@ pace_status_t launch_kv_decode(const KvMaps& maps, const KvAttnArgs& a, int D, i
 
 pace_status_t launch_kv_combine(const KvAttnArgs& a, int D, int rows, unsigned grid, cudaStream_t stream) {
   if (rows == kManyRows)
-    return launch_dependent(D == 128 ? kv_attn_combine<128, 1> : kv_attn_combine<64, 1>, dim3(grid, static_cast<unsigned>(rows / 8)), 256, 0, 1,
-                            stream, a, rows);
-  return launch_dependent(D == 128 ? kv_attn_combine<128, 8> : kv_attn_combine<64, 8>, dim3(grid, static_cast<unsigned>(rows)), 256, 0, 1, stream,
-                          a, rows);
+    return launch_dependent(D == 128 ? kv_attn_combine<128, 4, 4, 1> : kv_attn_combine<64, 4, 4, 1>, dim3(grid, static_cast<unsigned>(rows / 32)),
+                            256, 0, 1, stream, a, rows);
+  return launch_dependent(D == 128 ? kv_attn_combine<128, 1, 8, 8> : kv_attn_combine<64, 1, 8, 8>, dim3(grid, static_cast<unsigned>(rows)), 256, 0, 1,
+                          stream, a, rows);
 }
 
 }  // namespace pace
