@@ -248,7 +248,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
         // 0 * NaN is NaN: no slot of V that some row does not see may hold one.  Slots that nobody sees become zero; where rows
         // differ, so does a slot with a NaN, and rows that see it take a NaN weight for it.
         const bool whole = kv_whole(slot0, it.p_first, it.p_last, a.window, a.sinks);
-        auto usable = [](float x) { return x > 0.f && x < INFINITY; };
+        auto usable = [](float x) { return x >= 0x1p-120f && x <= 0x1p124f; };      // (1 / x and log2 x are finite)
         if (warp == 2 && lane < 8) {      // (where the slots are not there, or rows differ, no scale may be NaN either)
           float ks = ctl->scales[s][lane], vs = ctl->scales[s][8 + lane];
           if (!whole && (slot0 + lane * kKvBlock > it.p_last || !usable(ks) || !usable(vs))) ks = vs = 1.f;
