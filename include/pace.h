@@ -597,10 +597,11 @@ PACE_API size_t pace_kv_attention_workspace_size(const pace_kv_cache* cache, con
  *   lse = ln sum_j exp(scale q . k_j).
  * A query that sees nothing (a sequence shorter than its new tokens, or empty) gives out = 0 and
  * lse = -inf.  What slots hold that a query does not see has no influence on it, be it NaN; a
- * query that sees a NaN code or scale has no meaningful result.  Products are formed in e4m3 with
- * q and the softmax weights as sums of two e4m3 terms (q exactly, weights to 8 bits), sums and
- * softmax statistics in fp32; results do not depend on anything but the arguments (no atomics on
- * values).
+ * query that sees a NaN code or scale has no meaningful result.  Scores are products in e4m3 with q
+ * as the sum of two e4m3 terms, which is exact.  The softmax weights are held to 8 bits as two e4m3
+ * terms where a sequence has at most 32 query rows per KV head (n_b * n_q_heads / n_kv_heads), else
+ * to the 11 bits of f16; what is 2^-18 (2^-25) below the largest may be lost.  Sums and softmax
+ * statistics are fp32; results do not depend on anything but the arguments (no atomics on values).
  *
  *  Q            device  bf16 [cu_q[B], n_q_heads, D], rows q_row_stride elements apart (a multiple
  *                       of 8), 16-byte aligned
@@ -616,6 +617,8 @@ PACE_API size_t pace_kv_attention_workspace_size(const pace_kv_cache* cache, con
  *  A page number out of range or a length above max_len records PACE_ERR_INVALID_ARG (kernel id
  *  15) in the device status word; that sequence's results are then not meaningful.
  *  n_q_heads % n_kv_heads == 0, n_q_heads / n_kv_heads <= 64.
+ *  A call takes at most 2^30 query rows per KV head (cu_q[B] * n_q_heads / n_kv_heads), and 2^31 tiles
+ *  of 128 slots in a launch (query row tiles * n_kv_heads * tiles of max_len), else PACE_ERR_INVALID_ARG.
  */
 PACE_API pace_status_t pace_kv_attention(const pace_kv_cache* cache, const void* Q, int64_t q_row_stride, const int32_t* cu_q,
                                          int B, int n_q_heads, const int32_t* seq_lens, const int32_t* block_table,

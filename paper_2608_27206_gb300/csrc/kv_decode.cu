@@ -15,7 +15,7 @@
 //
 // What bounds it is HBM: per slot and head 2 D bytes.  From S of a tile to its P takes a group of four warps 1.1 us whatever the
 // number of rows, one and a half times what a tile of 32 KB takes an SM to fetch; so two groups take every other tile, each with its own
-// m, w, l and O^T, and join them at the item's end.  64 sequences of 404-16384 slots, 4 heads of 128: 153 us, 5.8 TB/s (one group: 210 us).
+// m, w, l and O^T, and join them at the item's end.  64 sequences of 5001-28007 slots, 4 heads of 128: 150 us, 5.9 TB/s (one group: 210 us).
 // Roles of a CTA (one per SM): warp 0 fetches tiles of 128 slots (TMA boxes of a page each, scales by 4-byte copies) through a
 // ring of stages, warp 1 issues the MMAs, warps 2-5 and 6-9 own the 128 lanes of even and odd tiles.
 #include <cuda_bf16.h>
