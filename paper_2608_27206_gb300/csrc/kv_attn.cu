@@ -63,7 +63,7 @@ struct Workspace {
 Workspace workspace(int rows, int D) {
   Workspace w{};
   w.lse = align_up(kPlanCtas * sizeof(KvSplit), 256);
-  w.part = w.lse + align_up(static_cast<size_t>(2) * kPlanCtas * rows * sizeof(float), 256);
+  w.part = w.lse + align_up(static_cast<size_t>(2) * kPlanCtas * rows * sizeof(float2), 256);
   w.total = w.part + static_cast<size_t>(2) * kPlanCtas * rows * D * sizeof(float);
   return w;
 }
@@ -110,7 +110,7 @@ extern "C" pace_status_t pace_kv_attention(const pace_kv_cache* cache, const voi
   a.lens = seq_lens;
   a.table = block_table;
   a.split = static_cast<KvSplit*>(ws);
-  a.part_lse = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + w.lse);
+  a.part_lse = reinterpret_cast<float2*>(static_cast<uint8_t*>(ws) + w.lse);
   a.part = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + w.part);
   a.scale2 = static_cast<float>(static_cast<double>(scale) * 1.4426950408889634);
   a.q_heads = n_q_heads;

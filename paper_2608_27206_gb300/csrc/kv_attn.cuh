@@ -8,7 +8,8 @@
 // every CTA has the same work to a tile, whatever the lengths are, and at most its first and its last (row
 // tile, head) are shared with others: those leave a normalised partial output and its log-sum-exp per row
 // (slot 2 c: it begins inside, 2 c + 1: it begins there and goes on elsewhere), which kv_attn_combine weighs
-// together.
+// together.  The log-sum-exp stays in two terms, a score and the logarithm of a sum relative to it: of large scores 32 bits
+// would not hold the sum of both (at 2^20 to an eighth).
 #pragma once
 #include <cuda.h>
 
@@ -46,7 +47,7 @@ struct KvAttnArgs {
   const int32_t* lens;
   const int32_t* table;
   KvSplit* split;       // [CTAs]
-  float* part_lse;      // [2 CTAs][rows of a tile], base 2
+  float2* part_lse;     // [2 CTAs][rows of a tile], base 2: score, logarithm relative to it (-inf: saw nothing)
   float* part;          // [2 CTAs][rows of a tile][D]
   float scale2;         // scale * log2(e)
   int q_heads, group, window, sinks, max_len;

@@ -408,8 +408,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
         if (grp == 0) {
           const int64_t at = complete ? kv_out_row(a, it, me) : slot + me;
           ctl->out_at[me] = at * D;
-          float* lse = complete ? a.lse : a.part_lse;
-          if (lse != nullptr) lse[at] = sum == 0.f ? -INFINITY : (m + log2f(sum)) * (complete ? 0.69314718055994531f : 1.f);
+          const float rel = sum == 0.f ? -INFINITY : log2f(sum);
+          if (!complete) a.part_lse[at] = make_float2(m, rel);
+          else if (a.lse != nullptr) a.lse[at] = (m + rel) * 0.69314718055994531f;
         }
       }
       named_barrier_sync(1 + grp, 128);
@@ -452,7 +453,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
   if (warp == 1) tmem_dealloc(tmem, C::TMEM);
 }
 
-// The items that several CTAs walked: out = sum_c 2^(lse_c - max) o_c / sum_c 2^(lse_c - max), parts in a fixed order.  What it
+// The items that several CTAs walked: out = sum_c 2^(lse_c - max) o_c / sum_c 2^(lse_c - max), parts in a fixed order; lse_c = b_c + r_c,
+// and differences are of b by itself first, which leaves them exact where the scores b are close.  What it
 // takes is latency, so a warp's loads go out together, PARTS parts of ROWS rows at a time.  Where rows are few a row has 8 warps (a
 // sequence alone makes as many parts as there are tiles: 38 of them took 8 us with one warp); where they are many and a row has few
 // parts, a warp has 4 rows (a call of 517 tokens: 97 us in all, with one row 99).
@@ -460,7 +462,7 @@ template <int D, int ROWS, int PARTS, int SPLIT>
 __global__ void __launch_bounds__(256) kv_attn_combine(const __grid_constant__ KvAttnArgs a, int tile_rows) {
   constexpr int E = D / 32;      // elements of a lane
   static_assert(ROWS == 1 || SPLIT == 1, "a warp has several rows or a row several warps");
-  __shared__ float s_top[8], s_sum[8];
+  __shared__ float s_base[8], s_top[8], s_sum[8];
   __shared__ __align__(16) float s_o[SPLIT > 1 ? 8 : 1][D];
   launch_dependents();
   grid_dependency_wait();
@@ -473,7 +475,9 @@ __global__ void __launch_bounds__(256) kv_attn_combine(const __grid_constant__ K
   if (live <= 0) return;      // (a row's warps all)
   auto at = [&](int j, int r) { return static_cast<int64_t>(j == 0 ? 2 * c + 1 : 2 * (c + j)) * tile_rows + q0 + r; };
   const int parts = sp.followers + 1;
-  float top = -INFINITY, sum = 0.f, o[ROWS][E];      // of row lane / PARTS (the same in its PARTS lanes); of every row
+  // of row lane / PARTS (the same in its PARTS lanes): the largest b, the largest lse relative to it, the sum; of every row o
+  float base = -INFINITY, top = -INFINITY, sum = 0.f, o[ROWS][E];
+  auto finite = [](float x) { return x == -INFINITY ? 0.f : x; };      // (where nothing was seen: 2^(-inf - 0), no NaN)
 #pragma unroll
   for (int r = 0; r < ROWS; ++r)
 #pragma unroll
@@ -481,7 +485,9 @@ __global__ void __launch_bounds__(256) kv_attn_combine(const __grid_constant__ K
 #pragma unroll 1
   for (int j0 = warp % SPLIT; j0 < parts; j0 += PARTS * SPLIT) {      // parts j0, j0 + SPLIT, ...
     const int j_mine = j0 + lane % PARTS * SPLIT, r_mine = lane / PARTS;
-    const float lse = j_mine < parts && r_mine < live ? __ldcg(a.part_lse + at(j_mine, r_mine)) : -INFINITY;
+    float2 lse = make_float2(-INFINITY, -INFINITY);
+    if (j_mine < parts && r_mine < live) lse = __ldcg(a.part_lse + at(j_mine, r_mine));
+    if (lse.y == -INFINITY) lse.x = -INFINITY;
     float v[ROWS][PARTS][E];
 #pragma unroll
     for (int r = 0; r < ROWS; ++r)
@@ -503,11 +509,15 @@ __global__ void __launch_bounds__(256) kv_attn_combine(const __grid_constant__ K
           v[r][k][1] = u.y;
         }
       }
-    float now = lse;
+    float b = fmaxf(lse.x, base);
+#pragma unroll
+    for (int s = PARTS / 2; s > 0; s >>= 1) b = fmaxf(b, __shfl_xor_sync(0xffffffffu, b, s));
+    const float rel = lse.x - finite(b) + lse.y, was = base - finite(b) + top;
+    float now = fmaxf(rel, was);
 #pragma unroll
     for (int s = PARTS / 2; s > 0; s >>= 1) now = fmaxf(now, __shfl_xor_sync(0xffffffffu, now, s));
-    now = fmaxf(now, top);
-    const float base = now == -INFINITY ? 0.f : now, f = exp2f(top - base), mine = exp2f(lse - base);
+    const float f = exp2f(was - finite(now)), mine = exp2f(rel - finite(now));
+    base = b;
     top = now;
     sum *= f;
     float all = mine;
@@ -529,6 +539,7 @@ __global__ void __launch_bounds__(256) kv_attn_combine(const __grid_constant__ K
   }
   if constexpr (SPLIT > 1) {
     if (lane == 0) {
+      s_base[warp] = base;
       s_top[warp] = top;
       s_sum[warp] = sum;
     }
@@ -536,16 +547,18 @@ __global__ void __launch_bounds__(256) kv_attn_combine(const __grid_constant__ K
     for (int e = 0; e < E; ++e) s_o[warp][lane * E + e] = o[0][e];
     __syncthreads();
     if (warp > 0) return;
-    top = s_top[0];
+    base = s_base[0];
 #pragma unroll
-    for (int k = 1; k < SPLIT; ++k) top = fmaxf(top, s_top[k]);
-    const float base = top == -INFINITY ? 0.f : top;
+    for (int k = 1; k < SPLIT; ++k) base = fmaxf(base, s_base[k]);
+    top = -INFINITY;
+#pragma unroll
+    for (int k = 0; k < SPLIT; ++k) top = fmaxf(top, s_base[k] - finite(base) + s_top[k]);
     sum = 0.f;
 #pragma unroll
     for (int e = 0; e < E; ++e) o[0][e] = 0.f;
 #pragma unroll
     for (int k = 0; k < SPLIT; ++k) {
-      const float f = exp2f(s_top[k] - base);
+      const float f = exp2f(s_base[k] - finite(base) + s_top[k] - finite(top));
       sum = fmaf(f, s_sum[k], sum);
 #pragma unroll
       for (int e = 0; e < E; ++e) o[0][e] = fmaf(f, s_o[k][lane * E + e], o[0][e]);
@@ -554,7 +567,7 @@ __global__ void __launch_bounds__(256) kv_attn_combine(const __grid_constant__ K
 #pragma unroll
   for (int r = 0; r < ROWS; ++r) {
     if (r >= live) break;
-    const float s = __shfl_sync(0xffffffffu, sum, r * PARTS), m = __shfl_sync(0xffffffffu, top, r * PARTS);
+    const float s = __shfl_sync(0xffffffffu, sum, r * PARTS), m = __shfl_sync(0xffffffffu, base + top, r * PARTS);
     const float inv = s == 0.f ? 0.f : 1.f / s;
     const int row = sp.row_tile * tile_rows + q0 + r, token = static_cast<int>(a.by_group(row));
     const int64_t dst = static_cast<int64_t>(a.s.q0[sp.i] + token) * a.q_heads + sp.head * a.group + row - token * a.group;

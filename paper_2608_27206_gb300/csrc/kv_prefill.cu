@@ -511,7 +511,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
       ok = __all_sync(0xffffffffu, kv_wait(o_done(i, 1), (mine - 1) & 1));
       if (!ok) break;
       tc_fence_after_sync();
-      const float inv = l == 0.f ? 0.f : 1.f / l, lse2 = l == 0.f ? -INFINITY : w + log2f(l);
+      const float inv = l == 0.f ? 0.f : 1.f / l, rel = l == 0.f ? -INFINITY : log2f(l);
       const bool complete = it.t0 == 0 && it.t1 == it.span.n;
       const int64_t slot = (2 * static_cast<int64_t>(blockIdx.x) + (it.t0 == 0 ? 1 : 0)) * kManyRows + row;
       const int64_t at = complete ? kv_out_row(a, it, real ? row : 0) : slot;
@@ -549,8 +549,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
         __syncwarp();
       }
       if (real) {
-        if (!complete) a.part_lse[slot] = lse2;
-        else if (a.lse != nullptr) a.lse[at] = lse2 * 0.69314718055994531f;
+        if (!complete) a.part_lse[slot] = make_float2(w, rel);
+        else if (a.lse != nullptr) a.lse[at] = (w + rel) * 0.69314718055994531f;
       }
     }
     if (!ok && lane == 0) stop(&ctl->abort, status);

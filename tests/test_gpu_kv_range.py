@@ -1,0 +1,69 @@
+"""Attention over the paged cache at scores of every size that 32 bits hold.
+
+Keys are code * (+-1, the same pattern in every slot) and queries a power of two on that pattern, so scores are whole multiples of one
+number: equal codes give equal scores to the last bit, in the kernels and in 64 bits, and where scores are large others are too far
+away to count.  So the weights have no error of their scores in them, and the bounds here leave none for it."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import pace_oracle as O
+from test_gpu_kv import BF16, Pool, _cu, _f64, _upload, pace  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def _codes(x):
+    return torch.from_numpy(x).clamp(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8).numpy()
+
+
+def _set_keys(pool, pattern, curve, exponent):
+    """Key j is curve[j], as a code, times the pattern [heads, D] times 2^exponent."""
+    page_size = pool.raw["k"].shape[2]
+    for p, page in enumerate(pool.pages[0]):
+        at = np.arange(page_size * p, min(page_size * (p + 1), len(curve)))
+        blocks = -(-len(at) // 16)
+        pool.s["k"][page, :, :blocks] = 2.0 ** exponent
+        pool.raw["k"][page, :, :len(at)] = _codes(pattern[:, None, :] * curve[at][None, :, None])
+
+
+def check_exact_scores(P, pool, Q, count, scale, window=0, sinks=0):
+    """out and lse of one sequence's last `count` queries.
+
+    out: one rounding to bf16 (2^-9) and weights of 8 bits (2^-9 each, of numerator and denominator alike), twice over for the joins in
+    fp32; what is far below the largest is off by 2^-18 of that.  lse: rounded from two terms to fp32, the score's scale by 2^-23."""
+    n, hq, _ = Q.shape
+    length = pool.host_lens[0]
+    lse = torch.full((n, hq), 7.0, device="cuda")
+    out = P.pace_kv_attention(pool.cache, Q, _cu([count]), pool.lens, pool.table, length, scale=scale, window=window, sinks=sinks, lse=lse)
+    see = O.kv_visible(length, count, window, sinks)
+    r = O.kv_attention(_f64(Q), pool.read("k", 0), pool.read("v", 0), see, scale)
+    err = np.abs(_f64(out) - r["out"])
+    tol = 2.0 ** -8 * np.abs(r["out"]) + 2.0 ** -8 * r["abs_out"] + 2.0 ** -17 * r["peak"][..., None]
+    assert np.all(err <= tol), (float((err - tol).max()), float(err.max()))
+    off = np.abs(lse.cpu().numpy().astype(np.float64) - r["lse"])
+    assert np.all(off <= 2.0 ** -22 * np.abs(r["lse"]) + 2.0 ** -18), float(off.max())
+    return out
+
+
+def _pattern(heads, dim):
+    return np.random.default_rng(40).choice([-1.0, 1.0], size=(heads, dim))
+
+
+# Equal scores in two CTAs' parts, with 128 and 80 slots: the parts weigh as their slots do, however large the score
+@pytest.mark.parametrize("log2_score", [4, 18, 21])
+@pytest.mark.parametrize("count,group", [(1, 4), (30, 2)])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_parts_of_equal_scores(pace, log2_score, count, group, dim):  # noqa: F811
+    length = 128 + 80
+    pool = Pool(pace, 41, [length], 1, dim, 16)
+    u = _pattern(1, dim)
+    _set_keys(pool, u, np.full(length, 1.375), 0)
+    for p, page in enumerate(pool.pages[0]):      # values near 1 in the first tile, near -1 in the second
+        pool.raw["v"][page] = _codes((1 if p < 8 else -1) * np.random.default_rng(p).choice([1.0, 1.125, 1.25], size=pool.raw["v"][page].shape))
+        pool.s["v"][page] = 1.0
+    _upload(pool)
+    Q = torch.from_numpy(np.broadcast_to(u, (count, group, dim)) * 1.0).to(BF16).cuda()
+    check_exact_scores(pace, pool, Q, count, math.log(2) * 2.0 ** log2_score / dim)
