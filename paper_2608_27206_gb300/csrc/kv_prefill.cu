@@ -36,6 +36,7 @@ using namespace ptx;
 constexpr int kThreads = 384;
 constexpr int kHalf = 64;          // columns of S at a time
 constexpr float kMost = 32768.f;   // sum of 64 weights at which w moves
+constexpr float kFar = 0x1p22f;    // a row's maximum from which on its scores are taken relative to one of them
 constexpr uint32_t kTmem = 512;    // S of A and B, then O of A and B, 128 columns each
 
 template <int D>
@@ -375,6 +376,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
         if (lane == 0) mbar_arrive(q_full(i));
       }
       float w = kNone, l = 0.f, peak = 0.f;      // peak: the largest sum of 64 weights under w
+      // A maximum below kFar is a whole number, and so are the logarithms of the scales: x + (log2(vs) - w) has one rounding, of
+      // a small result.  Beyond it log2(vs) - w would lose bits, scores that are equal come out different, and weights under a w that
+      // is their maximum pass 1 by any factor.  There (`far`) S of the half tile is first turned into x - m, x rounded like any score
+      // and m a score of the row that is the largest so far to within 2^20, so that what w is about is small again.
+      bool far = false;
+      float m = 0.f;      // (0 of other rows)
       const int n = it.t1 - it.t0;
       int slot0 = 0;
       bool whole = true;
@@ -413,11 +420,42 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
           }
           tmem_wait_st();
         }
+        float back = 0.f;        // old m less new
+        auto level = [&](bool mine, float least) {      // S of rows that are `mine` becomes x - m, m the largest x if that is far above `least`
+          float top = -INFINITY;
+#pragma unroll 1
+          for (int e0 = 0; e0 < 8; ++e0) {      // four times 16 columns for the largest, and again
+            uint32_t y[16];
+            load_cols(sX + 16 * (e0 & 3), y);
+            const float mul = fmaxf(block[e0 & 3].x * c, 1e-37f);
+            if (e0 == 4 && mine) {
+              const float to = top > least + 0x1p20f ? top : least;
+              back = m - to;
+              m = to;
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const float x = __fmul_rn(__uint_as_float(y[e]), mul);
+              top = fmaxf(top, x);
+              y[e] = mine ? __float_as_uint(x - m) : y[e];
+            }
+            if (e0 >= 4) tmem_st_32x32b(sX + 16 * (e0 & 3), y);
+          }
+          tmem_wait_st();
+        };
+        if (__any_sync(0xffffffffu, far)) level(far, m);
         uint32_t words[32];
-        bool over = g == 0;      // the row's w has to move
-        float sum = INFINITY;    // (by how much: not known)
+        bool over = g == 0 || back != 0.f;      // the row's w has to move
+        float sum = INFINITY;                   // (by how much: not known)
+        // Two rounds at most: a move leaves a sum of 64 weights of at most 2^0.5 each.  (Below kFar the largest weight's exponent is
+        // exact to 2^-1; of a far row x - m is at most 0 where m has just moved, else below 2^20.)
+        int rounds = 4;
 #pragma unroll 1
         while (true) {
+          if (--rounds == 0) {
+            ok = false;
+            break;
+          }
           if (__any_sync(0xffffffffu, over)) {
             // w moves in the rows that need it, and O (once its products have completed) and l with it: to a power that covers the sum
             // of the weights, or to the scores' maximum where that is not known.  The weights start (again) from S, which is whole.
@@ -425,19 +463,28 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
             // further from the next)
             peak = over ? sum : peak;
             float now = peak >= 2.f ? w + static_cast<float>(static_cast<int>(__float_as_uint(peak) >> 23) - 126) : w;
-            if (__any_sync(0xffffffffu, over && !(sum < INFINITY))) {
+            bool find = over && !(sum < INFINITY && fabsf(now) < kFar);
+            if (!over && !(fabsf(now) < kFar)) now = w;
+#pragma unroll 1
+            while (__any_sync(0xffffffffu, find)) {
               float top = kNone;
 #pragma unroll 1
               for (int e0 = 0; e0 < 4; ++e0) {
                 uint32_t y[16];
                 load_cols(sX + 16 * e0, y);
                 const float4 k = block[e0];
+                const float mul = far ? 1.f : fmaxf(k.x * c, 1e-37f);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) top = fmaxf(top, fmaf(__uint_as_float(y[e]), fmaxf(k.x * c, 1e-37f), k.y));
+                for (int e = 0; e < 16; ++e) top = fmaxf(top, fmaf(__uint_as_float(y[e]), mul, k.y));
               }
-              if (over && !(sum < INFINITY)) now = ceilf(top);
+              if (find) now = ceilf(top);
+              find = find && !far && top > kNone && !(fabsf(top) < kFar);
+              if (!__any_sync(0xffffffffu, find)) break;
+              level(find, -INFINITY);      // (once: these are far now)
+              far = far || find;
             }
-            const float f = ex2_approx(w - now);
+            const float f = ex2_approx((w + back) - now);
+            back = 0.f;
             w = now;
             l *= f;
             peak = 0.f;
@@ -470,7 +517,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
 #pragma unroll
           for (int e0 = 0; e0 < 4; ++e0) {      // a block's columns
             const float4 k = block[e0];
-            const float mul = fmaxf(k.x * c, 1e-37f), add = k.y - w;      // (not 0: -inf stays what it is)
+            const float mul = far ? 1.f : fmaxf(k.x * c, 1e-37f), add = k.y - w;      // (not 0: -inf stays what it is)
             const float2 mul2 = make_float2(mul, mul), add2 = make_float2(add, add);
             float2 s0 = make_float2(0.f, 0.f), s1 = s0;
 #pragma unroll
@@ -549,8 +596,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
         __syncwarp();
       }
       if (real) {
-        if (!complete) a.part_lse[slot] = make_float2(w, rel);
-        else if (a.lse != nullptr) a.lse[at] = (w + rel) * 0.69314718055994531f;
+        if (!complete) a.part_lse[slot] = far ? make_float2(m, w + rel) : make_float2(w, rel);
+        else if (a.lse != nullptr) a.lse[at] = (m + (w + rel)) * 0.69314718055994531f;
       }
     }
     if (!ok && lane == 0) stop(&ctl->abort, status);

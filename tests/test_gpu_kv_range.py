@@ -33,8 +33,10 @@ def check_exact_scores(P, pool, Q, count, scale, window=0, sinks=0):
     """out and lse of one sequence's last `count` queries.
 
     out: one rounding to bf16 (2^-9) and weights of 8 bits (2^-9 each, of numerator and denominator alike), twice over for the joins in
-    fp32; what is far below the largest is off by 2^-18 of that.  lse: rounded from two terms to fp32, the score's scale by 2^-23."""
+    fp32; what is far below the largest is off by 2^-18 of that.  lse: five roundings to fp32 (the scale, the score, the sum of two terms, a
+    constant and the product with it)."""
     n, hq, _ = Q.shape
+    scale = float(np.float32(scale))
     length = pool.host_lens[0]
     lse = torch.full((n, hq), 7.0, device="cuda")
     out = P.pace_kv_attention(pool.cache, Q, _cu([count]), pool.lens, pool.table, length, scale=scale, window=window, sinks=sinks, lse=lse)
@@ -44,7 +46,7 @@ def check_exact_scores(P, pool, Q, count, scale, window=0, sinks=0):
     tol = 2.0 ** -8 * np.abs(r["out"]) + 2.0 ** -8 * r["abs_out"] + 2.0 ** -17 * r["peak"][..., None]
     assert np.all(err <= tol), (float((err - tol).max()), float(err.max()))
     off = np.abs(lse.cpu().numpy().astype(np.float64) - r["lse"])
-    assert np.all(off <= 2.0 ** -22 * np.abs(r["lse"]) + 2.0 ** -18), float(off.max())
+    assert np.all(off <= 2.0 ** -21 * np.abs(r["lse"]) + 2.0 ** -18), float(off.max())
     return out
 
 
@@ -67,3 +69,23 @@ def test_parts_of_equal_scores(pace, log2_score, count, group, dim):  # noqa: F8
     _upload(pool)
     Q = torch.from_numpy(np.broadcast_to(u, (count, group, dim)) * 1.0).to(BF16).cuda()
     check_exact_scores(pace, pool, Q, count, math.log(2) * 2.0 ** log2_score / dim)
+
+
+# Scores in base 2 of up to +-2^log2_size that climb, fall or jump along the sequence, other rows the other way round or less steep: a
+# call returns, and what it returns is right, however far the maximum of a row moves
+@pytest.mark.parametrize("log2_size", [16, 21, 23, 26, 28, 32, 40, 80, 110])
+@pytest.mark.parametrize("shape", ["rise", "fall", "saw", "steps"])
+@pytest.mark.parametrize("count,hq,hkv,dim", [(90, 14, 2, 128), (50, 8, 8, 64)])
+def test_scores_of_any_size(pace, shape, log2_size, count, hq, hkv, dim):  # noqa: F811
+    length = 1300
+    pool = Pool(pace, 42, [length], hkv, dim, 64, spread=3)
+    j = np.arange(length)
+    curve = {"rise": j / length * 2 - 1, "fall": 1 - j / length * 2, "saw": (j % 170) / 170 * (0.2 + 0.8 * j / length),
+             "steps": np.floor(j / 97) / np.floor(length / 97) * np.where(j % 97 == 50, 1, 0.9)}[shape]
+    u = _pattern(hkv, dim)
+    of_scale, of_q = log2_size // 2 - 8, log2_size // 4
+    _set_keys(pool, u, curve * 256, log2_size - 8 - of_scale - of_q)
+    _upload(pool)
+    steep = np.resize([1.0, -1.0, 0.125, 0.5, -0.25], count * hq).reshape(count, hq, 1)
+    Q = torch.from_numpy(steep * 2.0 ** of_q * np.repeat(u, hq // hkv, axis=0)[None]).to(BF16).cuda()
+    check_exact_scores(pace, pool, Q, count, math.log(2) * 2.0 ** of_scale / dim)
