@@ -8,10 +8,11 @@
 // weights P.  The two terms are two columns of the same product, so they cost nothing while N is small.
 //
 // A TMEM lane of S^T is a slot.  Its thread applies the block's K scale and the mask, and turns the score x
-// (base 2) of row q into the weight 2^(x - m_q), which it sums, and into P = 16 * 2^(x - m_q) vs 2^(m_q - w_q),
-// vs being the block's V scale.  m_q and w_q stand for the largest x and the largest x + log2(vs) so far, but lag
+// (base 2) of row q into the weight 2^(x - m_q), which it sums, and into P = 16 * 2^(x - m_q) vs 2^-r_q,
+// vs being the block's V scale.  m_q and m_q + r_q stand for the largest x and the largest x + log2(vs) so far, but lag
 // behind: they move only when a weight would pass 2^60 or P 256 (e4m3 ends at 448).  So the usual tile has no maximum and no
-// exchange between threads but one barrier's vote, and O^T stays in TMEM untouched.
+// exchange between threads but one barrier's vote, and O^T stays in TMEM untouched.  Whatever x is, log2(vs) is only ever added to
+// a difference of scores: added to a score of 2^24 and more it would be rounded.
 //
 // What bounds it is HBM: per slot and head 2 D bytes.  From S of a tile to its P takes a group of four warps 1.1 us whatever the
 // number of rows, one and a half times what a tile of 32 KB takes an SM to fetch; so two groups take every other tile, each with its own
@@ -32,8 +33,8 @@ using namespace ptx;
 
 constexpr int kWarps = 10, kThreads = 32 * kWarps;
 constexpr float kFar = 60.f;         // how far a score may pass m_q
-constexpr float kOver = 4.f;         // ... and x + log2(vs) may pass w_q
-constexpr float kUnit = 4.f;         // log2 of P at w_q
+constexpr float kOver = 4.f;         // ... and x + log2(vs) may pass m_q + r_q
+constexpr float kUnit = 4.f;         // log2 of P at m_q + r_q
 
 template <int D, int NQ>
 struct DecodeCfg {
@@ -50,7 +51,7 @@ struct DecodeCfg {
 };
 
 struct Stat {
-  float m, w, far, g;     // m_q, w_q, m_q + kFar, 2^(kUnit + m_q - w_q)
+  float m, r, over, g;     // m_q, r_q, r_q + kOver, 2^(kUnit - r_q)
 };
 
 template <int D, int NQ>
@@ -309,27 +310,31 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
         const float lv = static_cast<float>(static_cast<int>(__float_as_uint(vs) >> 23) - 127);   // log2(vs), far down for 0
         bool ask = bad;
 #pragma unroll
-        for (int q = 0; q < NQ; ++q) ask = ask || x[q] > fminf(stat[q].far, stat[q].w + (kOver - lv));
+        for (int q = 0; q < NQ; ++q) ask = ask || x[q] - stat[q].m > fminf(kFar, stat[q].over - lv);
         if (named_barrier_any(1 + grp, 128, ask)) {
-          // some row's m or w has to move: the tile's maxima over all slots, new values, factors for l and O
+          // some row's m or r has to move: the tile's maxima over all slots (a warp's second one relative to its first), new values,
+          // factors for l and O
 #pragma unroll
           for (int q = 0; q < NQ; ++q) {
-            const float mx = warp_max(x[q]), mw = warp_max(x[q] + lv);
+            const float mx = fmaxf(warp_max(x[q]), kNone), mw = warp_max(x[q] - mx + lv);
             if (lane == 0) ctl->red[grp][quad][q] = make_float2(mx, mw);
           }
           named_barrier_sync(1 + grp, 128);
           if (me < NQ) {
             const Stat st = stat[me];
-            float mx = kNone, mw = kNone;
+            float mx = kNone;
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
-              mx = fmaxf(mx, ctl->red[grp][w][me].x);
-              mw = fmaxf(mw, ctl->red[grp][w][me].y);
-            }
-            const bool move = mx > st.far || mw > st.w + kOver;     // (each row by itself)
-            const float m = move ? fmaxf(st.m, mx) : st.m, w = move ? fmaxf(st.w, mw) : st.w;
-            ctl->fac[grp][me] = make_float2(exp2f(st.m - m), exp2f(st.w - w));
-            stat[me] = Stat{m, w, m + kFar, exp2f(kUnit + m - w)};
+            for (int w = 0; w < 4; ++w) mx = fmaxf(mx, ctl->red[grp][w][me].x);
+            auto weighted = [&](float base) {      // largest x + log2(vs) of the tile, less base
+              float r = -INFINITY;
+#pragma unroll
+              for (int w = 0; w < 4; ++w) r = fmaxf(r, ctl->red[grp][w][me].x - base + ctl->red[grp][w][me].y);
+              return r;
+            };
+            const bool move = mx - st.m > kFar || weighted(st.m) > st.over;     // (each row by itself)
+            const float m = move ? fmaxf(st.m, mx) : st.m, r = move ? fmaxf(st.m - m + st.r, weighted(m)) : st.r;
+            ctl->fac[grp][me] = make_float2(exp2f(st.m - m), exp2f((st.m - m) + (st.r - r)));
+            stat[me] = Stat{m, r, r + kOver, exp2f(kUnit - r)};
           }
           if (begun && !kv_wait(pv_done((u - 2) & 3), ((u - 2) >> 2) & 1)) stop(&ctl->abort, status);
           named_barrier_sync(1 + grp, 128);
@@ -359,7 +364,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
           for (int e = 0; e < 4; ++e) {
             const float pr = ex2_approx(x[q + e] - stat[q + e].m);
             l[q + e] += pr;
-            y[e] = pr * fminf(vs * stat[q + e].g, 0x1p100f);      // (a bound only where pr is 0: no infinity)
+            y[e] = pr * fminf(vs * stat[q + e].g, 0x1p100f);      // (the bound: pr is 0 or all but 0 there, and 0 times infinity)
             if (vs != vs && x[q + e] > -INFINITY) y[e] = vs;           // (fminf drops a NaN)
           }
           const uint32_t hi = e4m3x4(y[0], y[1], y[2], y[3]);

@@ -71,14 +71,9 @@ def test_parts_of_equal_scores(pace, log2_score, count, group, dim):  # noqa: F8
     check_exact_scores(pace, pool, Q, count, math.log(2) * 2.0 ** log2_score / dim)
 
 
-# Scores in base 2 of up to +-2^log2_size that climb, fall or jump along the sequence, other rows the other way round or less steep: a
-# call returns, and what it returns is right, however far the maximum of a row moves
-@pytest.mark.parametrize("log2_size", [16, 21, 23, 26, 28, 32, 40, 80, 110])
-@pytest.mark.parametrize("shape", ["rise", "fall", "saw", "steps"])
-@pytest.mark.parametrize("count,hq,hkv,dim", [(90, 14, 2, 128), (50, 8, 8, 64)])
-def test_scores_of_any_size(pace, shape, log2_size, count, hq, hkv, dim):  # noqa: F811
+def _any_size(P, shape, log2_size, mantissa, count, hq, hkv, dim):
     length = 1300
-    pool = Pool(pace, 42, [length], hkv, dim, 64, spread=3)
+    pool = Pool(P, 42, [length], hkv, dim, 64, spread=8)
     j = np.arange(length)
     curve = {"rise": j / length * 2 - 1, "fall": 1 - j / length * 2, "saw": (j % 170) / 170 * (0.2 + 0.8 * j / length),
              "steps": np.floor(j / 97) / np.floor(length / 97) * np.where(j % 97 == 50, 1, 0.9)}[shape]
@@ -88,4 +83,23 @@ def test_scores_of_any_size(pace, shape, log2_size, count, hq, hkv, dim):  # noq
     _upload(pool)
     steep = np.resize([1.0, -1.0, 0.125, 0.5, -0.25], count * hq).reshape(count, hq, 1)
     Q = torch.from_numpy(steep * 2.0 ** of_q * np.repeat(u, hq // hkv, axis=0)[None]).to(BF16).cuda()
-    check_exact_scores(pace, pool, Q, count, math.log(2) * 2.0 ** of_scale / dim)
+    check_exact_scores(P, pool, Q, count, mantissa * math.log(2) * 2.0 ** of_scale / dim)
+
+
+# Scores in base 2 of up to +-mantissa 2^log2_size that climb, fall or jump along the sequence, other rows the other way round or less
+# steep, V scales of 2^-8 to 2^8: a call returns, and what it returns is right, however far the maximum of a row moves
+@pytest.mark.parametrize("log2_size,mantissa", [(16, 1.3), (21, 1.9), (23, 1.0), (26, 1.7320508), (28, 1.2345678), (32, 1.0), (40, 1.6), (80, 1.3),
+                                                (110, 1.1)])
+@pytest.mark.parametrize("shape", ["rise", "fall", "saw", "steps"])
+@pytest.mark.parametrize("count,hq,hkv,dim", [(90, 14, 2, 128), (50, 8, 8, 64)])
+def test_scores_of_any_size(pace, shape, log2_size, mantissa, count, hq, hkv, dim):  # noqa: F811
+    _any_size(pace, shape, log2_size, mantissa, count, hq, hkv, dim)
+
+
+# likewise where rows are few; from 2^26 to 2^27 a score's last bit is 8
+@pytest.mark.parametrize("log2_size,mantissa", [(16, 1.3), (24, 1.2), (26, 1.05), (26, 1.2345678), (26, 1.4142135), (26, 1.7320508), (26, 1.9), (28, 1.3),
+                                                (40, 1.6), (110, 1.1)])
+@pytest.mark.parametrize("shape", ["rise", "fall", "saw", "steps"])
+@pytest.mark.parametrize("count,hq,hkv,dim", [(1, 14, 2, 128), (3, 8, 8, 64), (2, 14, 1, 128)])
+def test_scores_of_any_size_few_rows(pace, shape, log2_size, mantissa, count, hq, hkv, dim):  # noqa: F811
+    _any_size(pace, shape, log2_size, mantissa, count, hq, hkv, dim)
