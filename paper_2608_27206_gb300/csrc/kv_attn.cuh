@@ -19,7 +19,7 @@
 namespace pace {
 
 constexpr int kKvTile = 128;      // slots of one tile
-constexpr float kNone = -1e30f;   // a row's maximum before its first slot (finite: x - kNone is never NaN)
+constexpr float kNone = -0x1p127f;   // a row's maximum before its first slot, below any score (and finite: x - kNone is never NaN)
 constexpr int kManyRows = 256;    // rows of a tile of the form for many
 constexpr int kItemCost = 3;      // slot tiles that the queries and the output of a (row tile, head) are worth
 constexpr int kPlanCtas = 152;    // CTAs of a launch at most: an SM each (the size queries need no device)

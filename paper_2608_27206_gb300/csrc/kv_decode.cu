@@ -332,9 +332,13 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
               return r;
             };
             const bool move = mx - st.m > kFar || weighted(st.m) > st.over;     // (each row by itself)
-            const float m = move ? fmaxf(st.m, mx) : st.m, r = move ? fmaxf(st.m - m + st.r, weighted(m)) : st.r;
-            ctl->fac[grp][me] = make_float2(exp2f(st.m - m), exp2f((st.m - m) + (st.r - r)));
-            stat[me] = Stat{m, r, r + kOver, exp2f(kUnit - r)};
+            float2 fac = make_float2(1.f, 1.f);
+            if (move) {
+              const float m = fmaxf(st.m, mx), r = fmaxf(st.m - m + st.r, weighted(m));
+              fac = make_float2(exp2f(st.m - m), exp2f((st.m - m) + (st.r - r)));
+              stat[me] = Stat{m, r, r + kOver, exp2f(kUnit - r)};
+            }
+            ctl->fac[grp][me] = fac;
           }
           if (begun && !kv_wait(pv_done((u - 2) & 3), ((u - 2) >> 2) & 1)) stop(&ctl->abort, status);
           named_barrier_sync(1 + grp, 128);

@@ -103,3 +103,16 @@ def test_scores_of_any_size(pace, shape, log2_size, mantissa, count, hq, hkv, di
 @pytest.mark.parametrize("count,hq,hkv,dim", [(1, 14, 2, 128), (3, 8, 8, 64), (2, 14, 1, 128)])
 def test_scores_of_any_size_few_rows(pace, shape, log2_size, mantissa, count, hq, hkv, dim):  # noqa: F811
     _any_size(pace, shape, log2_size, mantissa, count, hq, hkv, dim)
+
+
+# a row whose every score is far below 0 (-2^90 to -2^120 in base 2) is still a softmax of them
+@pytest.mark.parametrize("log2_size", [90, 98, 101, 110, 120])
+@pytest.mark.parametrize("count,hq,hkv,dim", [(1, 14, 2, 128), (2, 14, 1, 64), (50, 8, 2, 64), (90, 14, 2, 128)])
+def test_scores_far_below_zero(pace, log2_size, count, hq, hkv, dim):  # noqa: F811
+    length = 600
+    pool = Pool(pace, 43, [length], hkv, dim, 64)
+    u = _pattern(hkv, dim)
+    _set_keys(pool, u, np.where(np.arange(length) % 7 == 3, -1.0, -1.5), 40)
+    _upload(pool)
+    Q = torch.from_numpy(2.0 ** 30 * np.broadcast_to(np.repeat(u, hq // hkv, axis=0)[None], (count, hq, dim))).to(BF16).cuda()
+    check_exact_scores(pace, pool, Q, count, math.log(2) * 2.0 ** (log2_size - 70) / dim)
