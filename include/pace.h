@@ -598,10 +598,12 @@ PACE_API size_t pace_kv_attention_workspace_size(const pace_kv_cache* cache, con
  * A query that sees nothing (a sequence shorter than its new tokens, or empty) gives out = 0 and
  * lse = -inf.  What slots hold that a query does not see has no influence on it, be it NaN; a
  * query that sees a NaN code or scale has no meaningful result.  Scores are products in e4m3 with q
- * as the sum of two e4m3 terms, which is exact.  The softmax weights are held to 8 bits as two e4m3
- * terms where a sequence has at most 32 query rows per KV head (n_b * n_q_heads / n_kv_heads), else
- * to the 11 bits of f16; what is 2^-18 (2^-25) below the largest may be lost.  Sums and softmax
- * statistics are fp32; results do not depend on anything but the arguments (no atomics on values).
+ * as the sum of two e4m3 terms, which is exact.  Where a sequence has at most 32 query rows per KV
+ * head (n_b * n_q_heads / n_kv_heads), a softmax weight is held to 8 bits, as two e4m3 terms of one
+ * of two ranges, down to 2^-22 of the query's largest (weight times V scale of its block) and to
+ * 2^-31 of that below; else to the 11 bits of f16, and what is 2^-25 below the largest may be lost.
+ * Sums and softmax statistics are fp32; results do not depend on anything but the arguments (no
+ * atomics on values).
  *
  *  Q            device  bf16 [cu_q[B], n_q_heads, D], rows q_row_stride elements apart (a multiple
  *                       of 8), 16-byte aligned

@@ -5,7 +5,11 @@
 //   S^T [128 slots x rows] = K [slots x D] q^T         O^T [D x rows] += V^T [D x slots] P^T
 // A 16-bit factor enters as two e4m3 terms side by side, x = hi + lo / 16: exactly for bf16 q (8 significant
 // bits are two times 4; each row of q is first brought under 256 by a power of two), to 8 bits for the
-// weights P.  The two terms are two columns of the same product, so they cost nothing while N is small.
+// weights P.  Terms are columns of the same product, so they cost little while N is small.
+// Two terms hold 8 bits of P from 2^-5 to 448 only, 2^-9 to 1 of the largest weight.  A context of tens of thousands of slots of which
+// one draws half of the weight has nearly all of its others below that, and they make up the output where that one's value is
+// small: held to a floor of 2^-18 of the largest they cost it percents.  So weights below 2^-5 go into two more columns, times 2^13: 8
+// bits down to 2^-22 of the largest, and an absolute error of 2^-31 below.
 //
 // A TMEM lane of S^T is a slot.  Its thread applies the block's K scale and the mask, and turns the score x
 // (base 2) of row q into the weight 2^(x - m_q), which it sums, and into P = 16 * 2^(x - m_q) vs 2^-r_q,
@@ -35,19 +39,21 @@ constexpr int kWarps = 10, kThreads = 32 * kWarps;
 constexpr float kFar = 60.f;         // how far a score may pass m_q
 constexpr float kOver = 4.f;         // ... and x + log2(vs) may pass m_q + r_q
 constexpr float kUnit = 4.f;         // log2 of P at m_q + r_q
+constexpr float kSmall = 0x1p-5f, kTimes = 0x1p13f;      // P below the first takes the second pair of columns, times the second
 
 template <int D, int NQ>
 struct DecodeCfg {
   static constexpr int TILE = kKvTile * D;              // bytes of a K or V tile
-  static constexpr int STAGES = (D == 128 ? 6 : 12) - (NQ == 32 ? 2 - D / 128 : 0);
+  static constexpr int STAGES = D == 128 ? (NQ == 8 ? 6 : NQ == 16 ? 5 : 4) : (NQ == 8 ? 12 : NQ == 16 ? 11 : 9);      // what fits
   static constexpr int QBYTES = 2 * NQ * D;             // hi rows, then lo rows
-  static constexpr int PBYTES = 2 * NQ * kKvTile;       // 16 columns of every slot, then the next 16
+  static constexpr int PBYTES = 4 * NQ * kKvTile;       // 16 columns of every slot, then the next 16
   static constexpr uint32_t SWIZZLE = D == 128 ? 2 : 4;
   static constexpr uint32_t GROUP = 8 * D;              // bytes of 8 rows
-  static constexpr int COLS = 2 * NQ;                   // TMEM: four S, then O of either group
+  static constexpr int COLS = 2 * NQ, OCOLS = 4 * NQ;   // TMEM: four S, then O of either group
+  static constexpr uint32_t O_AT = 4 * COLS;
   static constexpr uint32_t TMEM = NQ == 8 ? 128 : NQ == 16 ? 256 : 512;
   static constexpr uint32_t IDESC_S = idesc_e4m3_f32(128, COLS, false, false);
-  static constexpr uint32_t IDESC_O = idesc_e4m3_f32(128, COLS, true, true);
+  static constexpr uint32_t IDESC_O = idesc_e4m3_f32(128, OCOLS, true, true);
 };
 
 struct Stat {
@@ -139,7 +145,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
       // the same codes again and is not used.)
       const uint64_t dk = smem_desc(smem_u32(sKV), 16, C::GROUP, C::SWIZZLE);
       const uint64_t dv = smem_desc(smem_u32(sKV + C::TILE), 0, C::GROUP, C::SWIZZLE);
-      const uint64_t dp = smem_desc(smem_u32(sP), 8 * 16, NQ == 8 ? 8 * 16 : 16 * kKvTile, 0);
+      const uint64_t dp = smem_desc(smem_u32(sP), 8 * 16, 16 * kKvTile, 0);
       int t = 0, items = 0;
       bool ok = true;
       auto weigh = [&](int u, bool first) {     // O += V^T P of tile u
@@ -148,7 +154,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
         const uint64_t v = dv + static_cast<uint64_t>((u % ST) * 2 * (C::TILE >> 4)), p = dp + static_cast<uint64_t>((u & 3) * (C::PBYTES >> 4));
 #pragma unroll
         for (int k = 0; k < kKvTile / 32; ++k)
-          mma_f8_ss(tmem + (4 + (u & 1)) * C::COLS, v + static_cast<uint64_t>(k * (32 * D >> 4)), p + static_cast<uint64_t>(k * (32 * 16 >> 4)),
+          mma_f8_ss(tmem + C::O_AT + (u & 1) * C::OCOLS, v + static_cast<uint64_t>(k * (32 * D >> 4)), p + static_cast<uint64_t>(k * (32 * 16 >> 4)),
                     C::IDESC_O, !first || k > 0);
         mma_commit(empty(u % ST));
         mma_commit(pv_done(u & 3));
@@ -349,18 +355,18 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
           if (begun) {
             tc_fence_after_sync();
 #pragma unroll 1
-            for (int c = 0; c < C::COLS; c += 16) {
+            for (int c = 0; c < C::OCOLS; c += 16) {
               uint32_t o[16];
-              load_cols(lanes + (4 + grp) * C::COLS + c, o);
+              load_cols(lanes + C::O_AT + grp * C::OCOLS + c, o);
 #pragma unroll
               for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * ctl->fac[grp][(c + e) % NQ].y);
-              tmem_st_32x32b(lanes + (4 + grp) * C::COLS + c, o);
+              tmem_st_32x32b(lanes + C::O_AT + grp * C::OCOLS + c, o);
             }
             tmem_wait_st();
           }
         }
-        // weights, and P as hi and lo codes: 16 columns of this slot at a time
-        uint32_t w[2 * NQ / 4];
+        // weights, and P as hi and lo codes, in the columns of its size: 16 columns of this slot at a time
+        uint32_t w[4 * NQ / 4];
 #pragma unroll
         for (int q = 0; q < NQ; q += 4) {
           float y[4];
@@ -371,15 +377,25 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
             y[e] = pr * fminf(vs * stat[q + e].g, 0x1p100f);      // (the bound: pr is 0 or all but 0 there, and 0 times infinity)
             if (vs != vs && x[q + e] > -INFINITY) y[e] = vs;           // (fminf drops a NaN)
           }
+          uint32_t small = 0;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const bool is = y[e] < kSmall;
+            y[e] *= is ? kTimes : 1.f;
+            small |= is ? 0xFFu << 8 * e : 0u;
+          }
           const uint32_t hi = e4m3x4(y[0], y[1], y[2], y[3]);
           const uint32_t f0 = e4m3x2_to_f16x2(hi & 0xFFFFu), f1 = e4m3x2_to_f16x2(hi >> 16);
           const float2 g0 = __half22float2(*reinterpret_cast<const __half2*>(&f0)), g1 = __half22float2(*reinterpret_cast<const __half2*>(&f1));
-          w[q / 4] = hi;
-          w[NQ / 4 + q / 4] = e4m3x4((y[0] - g0.x) * 16.f, (y[1] - g0.y) * 16.f, (y[2] - g1.x) * 16.f, (y[3] - g1.y) * 16.f);
+          const uint32_t lo = e4m3x4((y[0] - g0.x) * 16.f, (y[1] - g0.y) * 16.f, (y[2] - g1.x) * 16.f, (y[3] - g1.y) * 16.f);
+          w[q / 4] = hi & ~small;
+          w[NQ / 4 + q / 4] = lo & ~small;
+          w[2 * NQ / 4 + q / 4] = hi & small;
+          w[3 * NQ / 4 + q / 4] = lo & small;
         }
         uint8_t* dst = sP + p * C::PBYTES + me * 16;
 #pragma unroll
-        for (int c = 0; c < C::COLS / 16; ++c)
+        for (int c = 0; c < C::OCOLS / 16; ++c)
           *reinterpret_cast<uint4*>(dst + c * 16 * kKvTile) = make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
         fence_proxy_async_shared();
         tc_fence_before_sync();
@@ -424,26 +440,36 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
       }
       named_barrier_sync(1 + grp, 128);
       tc_fence_after_sync();
-      uint32_t o[C::COLS];
-      load_cols(lanes + (4 + grp) * C::COLS, o);
+      float v[NQ];
+#pragma unroll
+      for (int q = 0; q < NQ; ++q) v[q] = 0.f;
+#pragma unroll
+      for (int c = 0; c < C::OCOLS; c += 16) {
+        uint32_t o[16];
+        load_cols(lanes + C::O_AT + grp * C::OCOLS + c, o);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          constexpr float unit[4] = {1.f, 0.0625f, 1.f / kTimes, 0.0625f / kTimes};
+          v[(c + e) % NQ] = fmaf(__uint_as_float(o[e]), unit[(c + e) / NQ], v[(c + e) % NQ]);
+        }
+      }
       tc_fence_before_sync();
       // each group ends half of the rows, with the other's sums by way of P's places (all products have completed)
       float* join = reinterpret_cast<float*>(sP);
 #pragma unroll
       for (int q = 0; q < NQ; ++q) {
         const float f = ctl->fac[grp][q].x;
-        const float v = f == 0.f ? 0.f : fmaf(__uint_as_float(o[NQ + q]), 0.0625f, __uint_as_float(o[q])) * f;
-        o[q] = __float_as_uint(v);
-        if (q / (NQ / 2) != grp && q < it.rows && me < D) join[q * D + me] = v;
+        v[q] = f == 0.f ? 0.f : v[q] * f;
+        if (q / (NQ / 2) != grp && q < it.rows && me < D) join[q * D + me] = v[q];
       }
       named_barrier_sync(3, 256);
       if (me < D) {
 #pragma unroll
         for (int q = 0; q < NQ; ++q) {
           if (q / (NQ / 2) != grp || q >= it.rows) continue;
-          const float v = __uint_as_float(o[q]) + join[q * D + me];
-          if (complete) a.out[ctl->out_at[q] + me] = __bfloat16_as_ushort(__float2bfloat16_rn(v));
-          else a.part[ctl->out_at[q] + me] = v;
+          const float sum = v[q] + join[q * D + me];
+          if (complete) a.out[ctl->out_at[q] + me] = __bfloat16_as_ushort(__float2bfloat16_rn(sum));
+          else a.part[ctl->out_at[q] + me] = sum;
         }
       }
     }

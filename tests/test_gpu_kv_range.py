@@ -116,3 +116,56 @@ def test_scores_far_below_zero(pace, log2_size, count, hq, hkv, dim):  # noqa: F
     _upload(pool)
     Q = torch.from_numpy(2.0 ** 30 * np.broadcast_to(np.repeat(u, hq // hkv, axis=0)[None], (count, hq, dim))).to(BF16).cuda()
     check_exact_scores(pace, pool, Q, count, math.log(2) * 2.0 ** (log2_size - 70) / dim)
+
+
+def _first_token(P, length, weight, size, hq, hkv, dim):
+    """A sequence whose first token draws about `weight` of every head's softmax, with values `size` times the others' (N(0, 1)) in a block
+    whose scale goes by its other tokens; a query."""
+    pool = Pool(P, 44, [length], hkv, dim, 64, poison=False)
+    rng, first = np.random.default_rng(45), pool.pages[0][0]
+    for n in "kv":
+        x = rng.normal(size=pool.raw[n].shape).astype(np.float32)
+        if n == "k":
+            x[..., 0] = 0      # channel 0 is the first token's alone
+            x[first, :, 0] = 0
+            x[first, :, 0, 0] = 6
+        else:
+            x[first, :, 0] *= size
+        pool.raw[n], pool.s[n] = _codes(x * 64), np.full(pool.s[n].shape, 2.0 ** -6)
+    _upload(pool)
+    lead = math.log(weight / (1 - weight)) + math.log(length) + 0.5      # a softmax of N(0, 1) scores sums up to about length e^(1/2)
+    g = torch.Generator().manual_seed(46)
+    Q = torch.randn(1, hq, dim, generator=g)
+    Q[..., 0] = lead * math.sqrt(dim) / 6
+    return pool, Q.to(BF16).cuda()
+
+
+def check_in_norm(P, pool, Q, bits, copies):
+    """The output's error over all its elements (2-norm): every weight is rounded by itself to `bits` bits, 2^-(bits + 1) of it at most, and the
+    output once to bf16, so it is at most 2^-9 |out| + 2^-(bits + 1) |sqrt(sum_j (p_j v_j)^2)|; twice that for joins and sums.
+
+    The sequence is called for `copies` times at once, so many that a copy is walked in one piece or two."""
+    length, n = pool.host_lens[0], len(Q)
+    got = P.pace_kv_attention(pool.cache, Q.repeat(copies, 1, 1), [n * i for i in range(copies + 1)], pool.lens.repeat(copies),
+                              pool.table.repeat(copies, 1), length)
+    k, v = pool.read("k", 0), pool.read("v", 0)
+    see = O.kv_visible(length, n)
+    scale = Q.shape[2] ** -0.5
+    r = O.kv_attention(_f64(Q), k, v, see, scale)
+    group = Q.shape[1] // k.shape[1]
+    each = np.zeros(r["out"].shape)
+    for t in range(n):
+        for h in range(Q.shape[1]):
+            s = np.where(see[t], scale * (k[:, h // group] @ _f64(Q)[t, h]), -np.inf)
+            each[t, h] = np.sqrt((np.exp(s - r["lse"][t, h]) ** 2) @ v[:, h // group] ** 2)
+    err = max(np.linalg.norm(_f64(x) - r["out"]) for x in got.split(n))
+    size = np.linalg.norm(r["out"])
+    bound = 2 * (2.0 ** -9 * size + 2.0 ** -(bits + 1) * np.linalg.norm(each))
+    assert err <= bound, (err / size, bound / size)
+
+
+# a first token that draws most of the weight and has next to no value: the others make up the output
+@pytest.mark.parametrize("weight,size", [(0.3, 0.02), (0.6, 0.02), (0.6, 0.002), (0.9, 0.002), (0.99, 0.0002)])
+@pytest.mark.parametrize("length,hq,hkv,dim", [(10825, 14, 2, 128), (28000, 8, 1, 128), (20011, 16, 1, 64), (20011, 32, 1, 64)])
+def test_first_token_draws_the_weight(pace, weight, size, length, hq, hkv, dim):  # noqa: F811
+    check_in_norm(pace, *_first_token(pace, length, weight, size, hq, hkv, dim), bits=8, copies=152 // hkv + 3)
