@@ -601,7 +601,7 @@ PACE_API size_t pace_kv_attention_workspace_size(const pace_kv_cache* cache, con
  * as the sum of two e4m3 terms, which is exact.  Where a sequence has at most 32 query rows per KV
  * head (n_b * n_q_heads / n_kv_heads), a softmax weight is held to 8 bits, as two e4m3 terms of one
  * of two ranges, down to 2^-22 of the query's largest (weight times V scale of its block) and to
- * 2^-31 of that below; else to the 11 bits of f16, and what is 2^-25 below the largest may be lost.
+ * 2^-31 of that below; else to the 11 bits of f16 down to 2^-13 and to 2^-24 of the largest below.
  * Sums and softmax statistics are fp32; results do not depend on anything but the arguments (no
  * atomics on values).
  *

@@ -9,9 +9,11 @@
 // weights are P = 2^(x + log2(vs) - w) and l = sum P / vs; both scales are constants of 16 columns, so a weight costs
 // one multiply-add, one exponential, one addition and half a conversion.  w is a whole number, the maximum of the row's first
 // 64 slots rounded up, and then stays: f16 has room for weights up to 2^15 above it, and below it 14 binary orders keep all their bits
-// and what is lost is under 2^-24.  Only when the weights of 64 columns sum up to more does w move, and O, l and the tile's weights so
-// far with it.  There is no maximum in the common path.  (Weights of blocks whose V scale is below 2^-110 of the largest are
-// lost to l.)
+// and what is lost is under 2^-25.  Only when the weights of 64 columns sum up to more does w move, and O, l and the tile's weights so
+// far with it, to where that sum is 2^5 to 2^6: then, as at first, the largest weight is 1/2 at least, and what is lost under 2^-24 of it.
+// (Down to a sum of 1 a row would move less often, but 64 equal weights would be 2^-6 each: a call of 517 tokens 98-100 us, so 101-102; with the
+// largest weight at 2^4 instead it would be 108.)  There is no maximum in the common path.  (Weights of blocks whose V scale is below
+// 2^-110 of the largest are lost to l.)
 //
 // The tensor pipe needs 2048 clocks per slot tile of 2 x 128 rows at D = 128, the exponentials 1024, and a slot tile takes 3600:
 // what bounds it is the chain from S to P to P V, 45 % tensor active.  Two row tiles A and B share every K and V tile (a V tile turned
@@ -36,6 +38,7 @@ using namespace ptx;
 constexpr int kThreads = 384;
 constexpr int kHalf = 64;          // columns of S at a time
 constexpr float kMost = 32768.f;   // sum of 64 weights at which w moves
+constexpr int kAfter = 6;          // log2 of what that sum is when w has moved, at most (so the largest weight is 2^-1 at least)
 constexpr float kFar = 0x1p22f;    // a row's maximum from which on its scores are taken relative to one of them
 constexpr uint32_t kTmem = 512;    // S of A and B, then O of A and B, 128 columns each
 
@@ -462,7 +465,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
             // (A move costs the same for a row and for 32: those that have outgrown their w by less come along, which leaves them
             // further from the next)
             peak = over ? sum : peak;
-            float now = peak >= 2.f ? w + static_cast<float>(static_cast<int>(__float_as_uint(peak) >> 23) - 126) : w;
+            float now = peak >= static_cast<float>(2 << kAfter) ? w + static_cast<float>(static_cast<int>(__float_as_uint(peak) >> 23) - 126 - kAfter) : w;
             bool find = over && !(sum < INFINITY && fabsf(now) < kFar);
             if (!over && !(fabsf(now) < kFar)) now = w;
 #pragma unroll 1

@@ -118,31 +118,33 @@ def test_scores_far_below_zero(pace, log2_size, count, hq, hkv, dim):  # noqa: F
     check_exact_scores(pace, pool, Q, count, math.log(2) * 2.0 ** (log2_size - 70) / dim)
 
 
-def _first_token(P, length, weight, size, hq, hkv, dim):
-    """A sequence whose first token draws about `weight` of every head's softmax, with values `size` times the others' (N(0, 1)) in a block
-    whose scale goes by its other tokens; a query."""
+def _heavy_tokens(P, length, weight, size, hq, hkv, dim, tokens=slice(0, 1), count=1):
+    """A sequence in which a few tokens draw about `weight` of every head's softmax, each as much, with values `size` times the others'
+    (N(0, 1)) in blocks whose scale is theirs; queries."""
     pool = Pool(P, 44, [length], hkv, dim, 64, poison=False)
-    rng, first = np.random.default_rng(45), pool.pages[0][0]
+    rng, page = np.random.default_rng(45), tokens.start // 64
+    heavy = (pool.pages[0][page], slice(None), slice(tokens.start - 64 * page, tokens.stop - 64 * page))
     for n in "kv":
         x = rng.normal(size=pool.raw[n].shape).astype(np.float32)
         if n == "k":
-            x[..., 0] = 0      # channel 0 is the first token's alone
-            x[first, :, 0] = 0
-            x[first, :, 0, 0] = 6
+            x[..., 0] = 0      # channel 0 is theirs alone
+            x[heavy] = 0
+            x[heavy + (0,)] = 6
         else:
-            x[first, :, 0] *= size
+            x[heavy] *= size
         pool.raw[n], pool.s[n] = _codes(x * 64), np.full(pool.s[n].shape, 2.0 ** -6)
     _upload(pool)
-    lead = math.log(weight / (1 - weight)) + math.log(length) + 0.5      # a softmax of N(0, 1) scores sums up to about length e^(1/2)
+    lead = math.log(weight / (1 - weight)) + math.log(length / (tokens.stop - tokens.start)) + 0.5      # a softmax of N(0, 1) scores sums up to about length e^(1/2)
     g = torch.Generator().manual_seed(46)
-    Q = torch.randn(1, hq, dim, generator=g)
+    Q = torch.randn(count, hq, dim, generator=g)
     Q[..., 0] = lead * math.sqrt(dim) / 6
     return pool, Q.to(BF16).cuda()
 
 
-def check_in_norm(P, pool, Q, bits, copies):
-    """The output's error over all its elements (2-norm): every weight is rounded by itself to `bits` bits, 2^-(bits + 1) of it at most, and the
-    output once to bf16, so it is at most 2^-9 |out| + 2^-(bits + 1) |sqrt(sum_j (p_j v_j)^2)|; twice that for joins and sums.
+def check_in_norm(P, pool, Q, bits, floor, copies):
+    """The output's error over all its elements (2-norm): every weight is rounded by itself to `bits` bits, 2^-(bits + 1) of it at most, or to
+    `floor` of the largest (scales are all alike here), and the output once to bf16, so it is at most
+    2^-9 |out| + 2^-(bits + 1) |sqrt(sum_j (p_j v_j)^2)| + floor |max p sqrt(sum_j v_j^2)|; twice that for joins and sums.
 
     The sequence is called for `copies` times at once, so many that a copy is walked in one piece or two."""
     length, n = pool.host_lens[0], len(Q)
@@ -157,10 +159,11 @@ def check_in_norm(P, pool, Q, bits, copies):
     for t in range(n):
         for h in range(Q.shape[1]):
             s = np.where(see[t], scale * (k[:, h // group] @ _f64(Q)[t, h]), -np.inf)
-            each[t, h] = np.sqrt((np.exp(s - r["lse"][t, h]) ** 2) @ v[:, h // group] ** 2)
+            p, v2 = np.exp(s - r["lse"][t, h]), v[:, h // group] ** 2
+            each[t, h] = 2.0 ** -(bits + 1) * np.sqrt(p ** 2 @ v2) + floor * p.max() * np.sqrt(v2.sum(0))
     err = max(np.linalg.norm(_f64(x) - r["out"]) for x in got.split(n))
     size = np.linalg.norm(r["out"])
-    bound = 2 * (2.0 ** -9 * size + 2.0 ** -(bits + 1) * np.linalg.norm(each))
+    bound = 2 * (2.0 ** -9 * size + np.linalg.norm(each))
     assert err <= bound, (err / size, bound / size)
 
 
@@ -168,4 +171,12 @@ def check_in_norm(P, pool, Q, bits, copies):
 @pytest.mark.parametrize("weight,size", [(0.3, 0.02), (0.6, 0.02), (0.6, 0.002), (0.9, 0.002), (0.99, 0.0002)])
 @pytest.mark.parametrize("length,hq,hkv,dim", [(10825, 14, 2, 128), (28000, 8, 1, 128), (20011, 16, 1, 64), (20011, 32, 1, 64)])
 def test_first_token_draws_the_weight(pace, weight, size, length, hq, hkv, dim):  # noqa: F811
-    check_in_norm(pace, *_first_token(pace, length, weight, size, hq, hkv, dim), bits=8, copies=152 // hkv + 3)
+    check_in_norm(pace, *_heavy_tokens(pace, length, weight, size, hq, hkv, dim), bits=8, floor=2.0 ** -31, copies=152 // hkv + 3)
+
+
+# the same where rows are many, and with 64 such tokens behind 64 others: the weights of the 64 first slots are passed by 2^9, all at once
+@pytest.mark.parametrize("weight,size,tokens", [(0.3, 0.02, slice(0, 1)), (0.9, 0.002, slice(0, 1)), (0.8, 0.002, slice(64, 128)),
+                                                (0.95, 0.002, slice(64, 128)), (0.99, 0.0002, slice(64, 128))])
+@pytest.mark.parametrize("length,count,hq,hkv,dim", [(20011, 17, 2, 1, 128), (12000, 10, 8, 2, 64)])
+def test_few_tokens_draw_the_weight_of_many_rows(pace, weight, size, tokens, length, count, hq, hkv, dim):  # noqa: F811
+    check_in_norm(pace, *_heavy_tokens(pace, length, weight, size, hq, hkv, dim, tokens, count), bits=11, floor=2.0 ** -24, copies=152 // hkv + 3)
