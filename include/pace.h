@@ -597,8 +597,9 @@ PACE_API size_t pace_kv_attention_workspace_size(const pace_kv_cache* cache, con
  *   lse = ln sum_j exp(scale q . k_j).
  * A query that sees nothing (a sequence shorter than its new tokens, or empty) gives out = 0 and
  * lse = -inf.  What slots hold that a query does not see has no influence on it, be it NaN; a
- * query that sees a NaN code or scale has no meaningful result.  Scores are products in e4m3 with q
- * as the sum of two e4m3 terms, which is exact.  Where a sequence has at most 32 query rows per KV
+ * query that sees a NaN code or scale has no meaningful result.  Scores are products in 8 bits with q
+ * as the sum of two terms: exact for elements of at least 2^-13 of a query's largest, the others are
+ * off by at most 2^-21 of that.  Where a sequence has at most 32 query rows per KV
  * head (n_b * n_q_heads / n_kv_heads), a softmax weight is held to 8 bits, as two e4m3 terms of one
  * of two ranges, down to 2^-22 of the query's largest (weight times V scale of its block) and to
  * 2^-31 of that below; else to the 11 bits of f16 down to 2^-13 and to 2^-24 of the largest below.

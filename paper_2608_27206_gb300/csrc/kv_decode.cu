@@ -3,9 +3,9 @@
 // K and V cross HBM once and go to the tensor cores as the 8-bit codes they are.  With so few rows the
 // codes are the large operand of both products, so both are formed transposed:
 //   S^T [128 slots x rows] = K [slots x D] q^T         O^T [D x rows] += V^T [D x slots] P^T
-// A 16-bit factor enters as two e4m3 terms side by side, x = hi + lo / 16: exactly for bf16 q (8 significant
-// bits are two times 4; each row of q is first brought under 256 by a power of two), to 8 bits for the
-// weights P.  Terms are columns of the same product, so they cost little while N is small.
+// A 16-bit factor enters as two e4m3 terms side by side, x = hi + lo / 16: to 8 bits for the weights P; of bf16 q (8
+// significant bits are two times 4; each row is first brought under 256 by a power of two, to 128 at least) exactly for elements
+// of 2^-6 and more, smaller ones, those under 2^-13 of the row's largest, are off by 2^-14 at most.  Terms are columns of the same product, so they cost little while N is small.
 // Two terms hold 8 bits of P from 2^-5 to 448 only, 2^-9 to 1 of the largest weight.  A context of tens of thousands of slots of which
 // one draws half of the weight has nearly all of its others below that, and they make up the output where that one's value is
 // small: held to a floor of 2^-18 of the largest they cost it percents.  So weights below 2^-5 go into two more columns, times 2^13: 8

@@ -1,9 +1,12 @@
 // Serve: attention over the paged cache for many query rows per KV head (prefill, whole or in chunks).
 //
 //   S [128 rows x 128 slots] = q K^T        O [128 rows x D] += P V
-// S is formed in 8 bits: K as the codes it is stored as, bf16 q as two e4m3 terms, which is exact (8 significant bits are two
-// times 4; each row is first brought under 256 by a power of two).  Two e4m3 products cost what one of 16 bits would, at half the
-// shared memory and with no work on K.  P V is formed in f16, which holds every e4m3 number, and a weight to 11 bits.
+// S is formed in 8 bits: K as the codes it is stored as, bf16 q as an e4m3 term and an e5m2 term for what is left of it.  Each row is
+// first brought under 256 by a power of two, to 128 at least; of an element of 2^-6 or more the first term then takes 4 of its 8
+// significant bits, what is left are 8 units of its last bit at most, and e5m2 holds that exactly (3 significant bits, down to 2^-16; e4m3,
+// which ends at 2^-9, would lose bits from 2^-3 on).  Smaller elements, those under 2^-13 of the row's largest, are off by 2^-14 at most, 2^-21 of
+// it.  Two 8-bit products cost what one of 16 bits would, at half the shared memory and with no work on K.  P V is formed in f16,
+// which holds every e4m3 number, and a weight to 11 bits.
 //
 // A TMEM lane of S is a query row and one thread's.  With x the score in base 2 and vs the V scale of a slot's block, the row's
 // weights are P = 2^(x + log2(vs) - w) and l = sum P / vs; both scales are constants of 16 columns, so a weight costs
@@ -52,7 +55,7 @@ struct PrefillCfg {
   static constexpr int VTILE = VCHUNK * D / 64;
   static constexpr uint32_t SWIZZLE = D == 128 ? 2 : 4;
   static constexpr uint32_t GROUP = 8 * D;
-  static constexpr uint32_t IDESC_S = idesc_e4m3_f32(128, kKvTile, false, false);
+  static constexpr uint32_t IDESC_HI = idesc_e4m3_f32(128, kKvTile, false, false), IDESC_LO = idesc_e4m3_f32(128, kKvTile, false, false, true);
   static constexpr uint32_t IDESC_O = idesc_f16_mn_f32(128, D);
 };
 
@@ -84,21 +87,23 @@ __device__ __forceinline__ uint32_t f16x2(float lo, float hi) {
 __device__ __forceinline__ uint32_t pair_f16(uint32_t two, float by) {
   return f16x2(__uint_as_float(two << 16) * by, __uint_as_float(two & 0xFFFF0000u) * by);
 }
-// Four f16 as e4m3 terms: hi, and what is left of them.
-__device__ __forceinline__ void split_e4m3(uint32_t a, uint32_t b, uint32_t& hi, uint32_t& lo) {
+// Four f16 as two terms: e4m3, and what is left of them in e5m2.
+__device__ __forceinline__ void split_8bit(uint32_t a, uint32_t b, uint32_t& hi, uint32_t& lo) {
   auto code = [](uint32_t two) {
     uint16_t r;
     asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(r) : "r"(two));
     return static_cast<uint32_t>(r);
   };
   auto rest = [](uint32_t two, uint32_t codes) {
-    uint32_t r;
-    asm("sub.f16x2 %0, %1, %2;" : "=r"(r) : "r"(two), "r"(e4m3x2_to_f16x2(codes)));
-    return r;
+    uint32_t d;
+    uint16_t r;
+    asm("sub.f16x2 %0, %1, %2;" : "=r"(d) : "r"(two), "r"(e4m3x2_to_f16x2(codes)));
+    asm("cvt.rn.satfinite.e5m2x2.f16x2 %0, %1;" : "=h"(r) : "r"(d));
+    return static_cast<uint32_t>(r);
   };
   const uint32_t ca = code(a), cb = code(b);
   hi = ca | cb << 16;
-  lo = code(rest(a, ca)) | code(rest(b, cb)) << 16;
+  lo = rest(a, ca) | rest(b, cb) << 16;
 }
 
 template <int D>
@@ -192,8 +197,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
       for (int part = 0; part < 2; ++part)
 #pragma unroll
         for (int k = 0; k < D / 32; ++k)
-          mma_f8_ss(tmem + i * 128, q + static_cast<uint64_t>(part * (C::QTILE >> 4) + 2 * k), k0 + static_cast<uint64_t>(2 * k), C::IDESC_S,
-                    part > 0 || k > 0, issue);
+          mma_f8_ss(tmem + i * 128, q + static_cast<uint64_t>(part * (C::QTILE >> 4) + 2 * k), k0 + static_cast<uint64_t>(2 * k),
+                    part == 0 ? C::IDESC_HI : C::IDESC_LO,                    part > 0 || k > 0, issue);
       commit(s_full(i));
     };
     while (ok && walk.next(a)) {
@@ -365,12 +370,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
         const float inv = fin ? __uint_as_float(static_cast<uint32_t>(127 - e2) << 23) : NAN;      // (a row that is not finite: NaN throughout)
         c = a.scale2 * __uint_as_float(static_cast<uint32_t>(127 + e2) << 23);
 #pragma unroll 2
-        for (int e = 0; e < D / 16; ++e) {      // by way of f16, which holds them (and 2^-24 where e4m3 ends at 2^-9)
+        for (int e = 0; e < D / 16; ++e) {      // by way of f16, which holds them (and 2^-24 where e5m2 ends at 2^-16)
           const uint4 u0 = *reinterpret_cast<const uint4*>(place(lane, e)), u1 = *reinterpret_cast<const uint4*>(place(lane, e + D / 16));
           const uint32_t w[8] = {u0.x, u0.y, u0.z, u0.w, u1.x, u1.y, u1.z, u1.w};
           uint32_t hi[4], lo[4];
 #pragma unroll
-          for (int k = 0; k < 4; ++k) split_e4m3(pair_f16(w[2 * k], inv), pair_f16(w[2 * k + 1], inv), hi[k], lo[k]);
+          for (int k = 0; k < 4; ++k) split_8bit(pair_f16(w[2 * k], inv), pair_f16(w[2 * k + 1], inv), hi[k], lo[k]);
           *reinterpret_cast<uint4*>(place(lane, e)) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
           *reinterpret_cast<uint4*>(place(lane, e + D / 16)) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
         }

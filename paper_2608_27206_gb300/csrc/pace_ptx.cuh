@@ -266,10 +266,11 @@ __device__ __forceinline__ void reg_fence(uint32_t (&r)[32]) {
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// Instruction descriptor, kind::f8f6f4: e4m3 A and B, fp32 accumulator, M x N; an operand is K-major, or
-// MN-major where its flag is set.
-__host__ __device__ constexpr uint32_t idesc_e4m3_f32(int M, int N, bool a_mn, bool b_mn) {
+// Instruction descriptor, kind::f8f6f4: e4m3 A (e5m2 where its flag is set) and B, fp32 accumulator, M x N; an operand is
+// K-major, or MN-major where its flag is set.
+__host__ __device__ constexpr uint32_t idesc_e4m3_f32(int M, int N, bool a_mn, bool b_mn, bool a_e5m2 = false) {
   return (1u << 4)                                   // D format: f32 (A and B format 0: e4m3)
+         | (a_e5m2 ? 1u << 7 : 0u)                   // A format
          | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u)
          | (static_cast<uint32_t>(N >> 3) << 17)     // N / 8
          | (static_cast<uint32_t>(M >> 4) << 24);    // M / 16

@@ -180,3 +180,32 @@ def test_first_token_draws_the_weight(pace, weight, size, length, hq, hkv, dim):
 @pytest.mark.parametrize("length,count,hq,hkv,dim", [(20011, 17, 2, 1, 128), (12000, 10, 8, 2, 64)])
 def test_few_tokens_draw_the_weight_of_many_rows(pace, weight, size, tokens, length, count, hq, hkv, dim):  # noqa: F811
     check_in_norm(pace, *_heavy_tokens(pace, length, weight, size, hq, hkv, dim, tokens, count), bits=11, floor=2.0 ** -24, copies=152 // hkv + 3)
+
+
+# One channel of q stands out by far, and the keys have nothing there: the others' bits are all that scores are made of.  (With a window of
+# one slot lse is the score.)  Elements under 2^-13 of the largest are off by 2^-21 of it at most; a score is a sum of D products in fp32.
+@pytest.mark.parametrize("outlier", [100.0, 300.0, 1024.0, 3000.0, 8192.0])
+@pytest.mark.parametrize("count,hq,hkv", [(4, 8, 2), (60, 8, 2), (33, 2, 2)])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_queries_with_an_outlying_channel(pace, outlier, count, hq, hkv, dim):  # noqa: F811
+    length = 300
+    pool = Pool(pace, 47, [length], hkv, dim, 32, poison=False)
+    x = np.random.default_rng(48).normal(size=pool.raw["k"].shape).astype(np.float32)
+    x[..., 5] = 0
+    pool.raw["k"], pool.s["k"] = _codes(x * 64), np.full(pool.s["k"].shape, 2.0 ** -6)
+    _upload(pool)
+    Q = torch.randn(count, hq, dim, generator=torch.Generator().manual_seed(49))
+    Q[..., 5] = outlier
+    Q = Q.to(BF16).cuda()
+    k, q, scale = pool.read("k", 0), _f64(Q), dim ** -0.5
+    for window in (1, 0):
+        see = O.kv_visible(length, count, window, 0)
+        lse = torch.empty(count, hq, device="cuda")
+        out = pace.pace_kv_attention(pool.cache, Q, [0, count], pool.lens, pool.table, length, window=window, lse=lse)
+        r = O.kv_attention(q, k, pool.read("v", 0), see, scale)
+        most = np.abs(k[length - count if window else 0:]).sum(2).max(0).repeat(hq // hkv)      # of the slots seen, sum_d |k_d|
+        score = scale * 2.0 ** -21 * outlier * most + 2.0 ** -23 * (dim + 8) * r["abs_score"] + 2.0 ** -20
+        off = np.abs(lse.cpu().numpy() - r["lse"])
+        assert np.all(off <= score + 2.0 ** -21 * np.abs(r["lse"])), float((off / score).max())
+        tol = 2.0 ** -8 * np.abs(r["out"]) + (2.0 ** -8 + 2 * score[..., None]) * r["abs_out"] + 2.0 ** -17 * r["peak"][..., None]
+        assert np.all(np.abs(_f64(out) - r["out"]) <= tol)
