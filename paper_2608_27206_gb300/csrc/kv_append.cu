@@ -80,15 +80,15 @@ __device__ __forceinline__ Turn load_turn(const float2* cs) {
   }
   return t;
 }
-// Products and sums rounded one by one, so that a result does not hang on the contraction into FMAs (the difference below is one
-// of finished products, by a factor of -1).
+// Products and sums rounded one by one, so that a result does not hang on the contraction into FMAs.  The sums are scalar: ptxas joins a
+// packed sum (add, or an FMA by 1) with the packed product before it, rounding modifiers or not.
 __device__ __forceinline__ void turn(Pairs& x, const Turn& t) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const float2 ac = ptx::fmul2(x.a[i], t.c[i]), bs = ptx::fmul2(x.b[i], t.s[i]);
     const float2 bc = ptx::fmul2(x.b[i], t.c[i]), as = ptx::fmul2(x.a[i], t.s[i]);
-    x.a[i] = ptx::ffma2(bs, make_float2(-1.f, -1.f), ac);
-    x.b[i] = ptx::fadd2(bc, as);
+    x.a[i] = make_float2(__fsub_rn(ac.x, bs.x), __fsub_rn(ac.y, bs.y));
+    x.b[i] = make_float2(__fadd_rn(bc.x, as.x), __fadd_rn(bc.y, as.y));
   }
 }
 // Adds a NaN to `all` if an element is not finite, else zeros.
