@@ -610,7 +610,8 @@ PACE_API size_t pace_kv_attention_workspace_size(const pace_kv_cache* cache, con
  *                       of 8), 16-byte aligned
  *  cu_q         host    int32 [B+1] prefix of the queries per sequence (0 allowed)
  *  seq_lens     device  int32 [B], the queries' own tokens included; each 0 .. max_len
- *  block_table  device  int32 [B][table_stride], as for pace_kv_append
+ *  block_table  device  int32 [B][table_stride], as for pace_kv_append; the entry of a page none of whose
+ *                       slots any query of the call sees is of no consequence
  *  max_len      host    bound on seq_lens, at most table_stride * page_size; the workspace and the
  *                       launch depend on it and on cu_q alone, so that a captured call can be
  *                       replayed while the sequences grow

@@ -334,12 +334,13 @@ __device__ __forceinline__ void kv_fetch(const KvMaps& maps, const KvAttnArgs& a
   while (!stopped(abort) && walk.next(a)) {
     const KvItem& it = walk.it;
     const int32_t* table = a.table + static_cast<int64_t>(a.s.seq[it.i]) * a.table_stride;
-    const int last = it.p_last;
+    // (slots that no query of the item sees: behind the last one's own, and from the first ones to the first query's window)
+    const int last = it.p_last, before = a.window > 0 ? it.p_first - a.window : -1;
     auto page_of = [&](int tile_i) {         // of box lane % boxes of tile tile_i + lane / boxes
       const int i = tile_i + lane / boxes;
       if (i >= it.t1) return -2;
       const int slot = it.span.tile(i) * kKvTile + (lane % boxes) * box_rows;
-      if (slot > last) return -2;            // nothing there
+      if (slot > last || (slot >= a.sinks && slot + box_rows - 1 <= before)) return -2;      // nothing there that counts
       const int page = table[slot >> a.c.page_shift];
       return page >= 0 && page < a.c.n_pages ? page : -1;
     };
@@ -372,7 +373,7 @@ __device__ __forceinline__ void kv_fetch(const KvMaps& maps, const KvAttnArgs& a
       const int blk = lane & 7;
       const int bpage = __shfl_sync(0xffffffffu, page, blk * kKvBlock >> shift);
       const int row = (slot0 + blk * kKvBlock) & ((1 << a.c.page_shift) - 1);
-      if (lane < 16 && slot0 + blk * kKvBlock <= last)
+      if (lane < 16 && bpage >= 0 && slot0 + blk * kKvBlock <= last)
         cp_async4(smem_u32(&ring.scales[s][lane]),
                   (lane < 8 ? a.c.ks : a.c.vs) + bpage * a.c.scale_stride + (static_cast<int64_t>(it.head) << (a.c.page_shift - 4)) + row / kKvBlock);
       cp_async_arrive(smem_u32(&ring.full[s]));
