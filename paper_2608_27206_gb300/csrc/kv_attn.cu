@@ -116,7 +116,7 @@ extern "C" pace_status_t pace_kv_attention(const pace_kv_cache* cache, const voi
   a.q_heads = n_q_heads;
   a.group = group;
   a.by_group = fast_div(static_cast<uint32_t>(group));
-  a.window = window;
+  a.window = window < max_len ? window : 0;      // (one of max_len leaves nothing out; smaller ones keep slot - window within 32 bits)
   a.sinks = sinks;
   a.max_len = max_len;
   int* status = device_status_word();
