@@ -124,19 +124,20 @@ __global__ void __launch_bounds__(kAppendThreads, 3) kv_append_kernel(const __gr
     else hi = mid - 1;
   }
   const int b = lo, n = a.cu[b + 1] - a.cu[b];
-  const int len = a.lens[a.b0 + b], first = len - n;
+  // (a length may be anything: slots in 64 bits until they are known to be in the table)
+  const int64_t len = a.lens[a.b0 + b], first = len - n;
   if (first < 0) {
     if (threadIdx.x == 0) record_error(status, PACE_ERR_INVALID_ARG, K_KV_APPEND);
   }
   // (of a sequence shorter than its new tokens those before its first slot are dropped)
-  const int blk = (first < 0 ? 0 : first / kKvBlock) + static_cast<int>(blockIdx.x) - a.block_prefix[b];
-  const int slot0 = blk * kKvBlock;
+  const int64_t slot0 = (first < 0 ? 0 : first / kKvBlock * kKvBlock) + static_cast<int64_t>(blockIdx.x - a.block_prefix[b]) * kKvBlock;
   if (slot0 >= len) return;
-  const int r_lo = max(first - slot0, 0), r_hi = min(len - slot0, kKvBlock);
+  const int r_lo = static_cast<int>(max(first - slot0, int64_t{0})), r_hi = static_cast<int>(min(len - slot0, int64_t{kKvBlock}));
   const int64_t pi = slot0 >> a.c.page_shift;
+  const int slot = static_cast<int>(slot0) & ((1 << a.c.page_shift) - 1);      // of row 0, in its page
   int page = -1;
   if (pi < a.table_stride) page = a.table[(a.b0 + b) * a.table_stride + pi];
-  const int token0 = a.cu[b] + slot0 - first;   // of row 0, where that is a new token
+  const int token0 = a.cu[b] + static_cast<int>(slot0 - first);   // of row 0, where that is a new token
   if (threadIdx.x < kKvBlock) {
     const int r = threadIdx.x;
     int64_t s = -1;
@@ -230,7 +231,7 @@ __global__ void __launch_bounds__(kAppendThreads, 3) kv_append_kernel(const __gr
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-    const int slot = slot0 & ((1 << a.c.page_shift) - 1), blocks = 1 << (a.c.page_shift - 4);
+    const int blocks = 1 << (a.c.page_shift - 4);
     float* scale = (is_v ? a.c.vs : a.c.ks) + page * a.c.scale_stride + head * blocks + slot / kKvBlock;
     uint8_t* codes = (is_v ? a.c.v : a.c.k) + page * a.c.page_stride +
                      ((static_cast<int64_t>(head) << a.c.page_shift) + slot) * D + col;
