@@ -621,8 +621,11 @@ PACE_API size_t pace_kv_attention_workspace_size(const pace_kv_cache* cache, con
  *  A page number out of range or a length above max_len records PACE_ERR_INVALID_ARG (kernel id
  *  15) in the device status word; that sequence's results are then not meaningful.
  *  n_q_heads % n_kv_heads == 0, n_q_heads / n_kv_heads <= 64.
- *  A call takes at most 2^30 query rows per KV head (cu_q[B] * n_q_heads / n_kv_heads), and 2^31 tiles
- *  of 128 slots in a launch (query row tiles * n_kv_heads * tiles of max_len), else PACE_ERR_INVALID_ARG.
+ *  A call takes at most 2^30 query rows per KV head (cu_q[B] * n_q_heads / n_kv_heads).  Sequences go 256
+ *  to a launch, in order, those of at most 32 query rows per KV head apart from the others; a launch
+ *  takes row tiles * n_kv_heads * (tiles of 128 slots in max_len + 3) < 2^31, where a row tile has 256
+ *  rows, or for the former 8, 16 or 32, what the largest of them needs.  Else PACE_ERR_INVALID_ARG, and
+ *  nothing is launched.
  */
 PACE_API pace_status_t pace_kv_attention(const pace_kv_cache* cache, const void* Q, int64_t q_row_stride, const int32_t* cu_q,
                                          int B, int n_q_heads, const int32_t* seq_lens, const int32_t* block_table,

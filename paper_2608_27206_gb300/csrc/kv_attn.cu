@@ -28,15 +28,6 @@ pace_status_t make_map(CUtensorMap* m, const pace_kv_cache* c, void* codes) {
   return r == CUDA_SUCCESS ? PACE_OK : PACE_ERR_INVALID_ARG;
 }
 
-pace_status_t check_attention(const pace_kv_cache* cache, const int32_t* cu_q, int B, int n_q_heads, int max_len) {
-  PACE_CHECK(check_cache(cache));
-  PACE_CHECK(check_prefix(cu_q, B));
-  if (n_q_heads < 1 || n_q_heads % cache->n_kv_heads != 0 || n_q_heads / cache->n_kv_heads > 64) return PACE_ERR_INVALID_ARG;
-  if (max_len < 0 || max_len > (1 << 30)) return PACE_ERR_INVALID_ARG;
-  if (cu_q[B] > (1 << 30) / (n_q_heads / cache->n_kv_heads)) return PACE_ERR_INVALID_ARG;
-  return PACE_OK;
-}
-
 // Sequences of at most kFewRows query rows per KV head take the transposed products of kv_decode.cu.
 constexpr int kFewRows = 32;
 
@@ -55,6 +46,47 @@ int most_rows(const int32_t* cu_q, int B, int group) {
   for (int b = 0; b < B; ++b)
     if (static_cast<int64_t>(cu_q[b + 1] - cu_q[b]) * group > kFewRows) return kManyRows;
   return few_rows(cu_q, B, group);
+}
+
+int64_t slot_tiles(int max_len) { return std::max(1, (max_len + kKvTile - 1) / kKvTile); }
+
+// The sequences of a form that the next launch takes, from b on (b: the first that it leaves); its row tiles.
+int64_t next_launch(const int32_t* cu_q, int B, int group, bool is_few, int rows, int& b, KvSeqs* s) {
+  int64_t tiles = 0;
+  int nb = 0;
+  for (; b < B && nb < kKvMaxB; ++b) {
+    const int n = cu_q[b + 1] - cu_q[b];
+    const int64_t r = static_cast<int64_t>(n) * group;
+    if (n == 0 || (r <= kFewRows) != is_few) continue;
+    tiles += (r + rows - 1) / rows;
+    if (s != nullptr) {
+      s->seq[nb] = b;
+      s->q0[nb] = cu_q[b];
+      s->nq[nb] = n;
+      s->tile0[nb + 1] = static_cast<int>(tiles);
+    }
+    ++nb;
+  }
+  if (s != nullptr) {
+    s->nb = nb;
+    s->tile0[0] = 0;
+  }
+  return tiles;
+}
+
+// What the size query and the call refuse alike, and before anything is launched.
+pace_status_t check_attention(const pace_kv_cache* cache, const int32_t* cu_q, int B, int n_q_heads, int max_len) {
+  PACE_CHECK(check_cache(cache));
+  PACE_CHECK(check_prefix(cu_q, B));
+  if (n_q_heads < 1 || n_q_heads % cache->n_kv_heads != 0 || n_q_heads / cache->n_kv_heads > 64) return PACE_ERR_INVALID_ARG;
+  if (max_len < 0 || max_len > (1 << 30)) return PACE_ERR_INVALID_ARG;
+  const int group = n_q_heads / cache->n_kv_heads;
+  if (cu_q[B] > (1 << 30) / group) return PACE_ERR_INVALID_ARG;
+  const int64_t most = INT32_MAX / (cache->n_kv_heads * (slot_tiles(max_len) + kItemCost));      // row tiles of a launch
+  for (const bool is_few : {true, false})
+    for (int b = 0; b < B;)
+      if (next_launch(cu_q, B, group, is_few, is_few ? few_rows(cu_q, B, group) : kManyRows, b, nullptr) > most) return PACE_ERR_INVALID_ARG;
+  return PACE_OK;
 }
 
 struct Workspace {
@@ -122,31 +154,15 @@ extern "C" pace_status_t pace_kv_attention(const pace_kv_cache* cache, const voi
   int* status = device_status_word();
   int sms = 0;
   PACE_CHECK(sm_count(&sms));
-  const int64_t slot_tiles = std::max(1, (max_len + kKvTile - 1) / kKvTile);
   for (const bool is_few : {true, false}) {
     const int rows = is_few ? few : kManyRows;
     for (int b = 0; b < B;) {
-      a.s.nb = 0;
-      a.s.tile0[0] = 0;
-      int64_t tiles = 0;
-      for (; b < B && a.s.nb < kKvMaxB; ++b) {
-        const int n = cu_q[b + 1] - cu_q[b];
-        const int64_t r = static_cast<int64_t>(n) * group;
-        if (n == 0 || (r <= kFewRows) != is_few) continue;
-        const int i = a.s.nb++;
-        a.s.seq[i] = b;
-        a.s.q0[i] = cu_q[b];
-        a.s.nq[i] = n;
-        tiles += (r + rows - 1) / rows;
-        a.s.tile0[i + 1] = static_cast<int>(tiles);
-      }
-      if (a.s.nb == 0) break;
-      const int64_t most = tiles * cache->n_kv_heads * (slot_tiles + kItemCost);
-      if (most > INT32_MAX) return PACE_ERR_INVALID_ARG;
-      const unsigned grid = static_cast<unsigned>(std::min<int64_t>({tiles * cache->n_kv_heads * slot_tiles, sms, kPlanCtas}));
+      const int64_t tiles = next_launch(cu_q, B, group, is_few, rows, b, &a.s);
+      if (tiles == 0) break;
+      const unsigned grid = static_cast<unsigned>(std::min<int64_t>({tiles * cache->n_kv_heads * slot_tiles(max_len), sms, kPlanCtas}));
       if (is_few) PACE_CHECK(launch_kv_decode(maps, a, D, rows, grid, status, stream));
       else PACE_CHECK(launch_kv_prefill(maps, a, D, grid, status, stream));
-      if (slot_tiles > 1) PACE_CHECK(launch_kv_combine(a, D, rows, grid, stream));
+      if (slot_tiles(max_len) > 1) PACE_CHECK(launch_kv_combine(a, D, rows, grid, stream));
     }
   }
   return PACE_OK;
