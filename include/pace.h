@@ -618,8 +618,8 @@ PACE_API size_t pace_kv_attention_workspace_size(const pace_kv_cache* cache, con
  *  window       <= 0: every earlier slot;  sinks >= 0: the first slots that stay visible
  *  out          device  bf16 [cu_q[B], n_q_heads, D] contiguous, 16-byte aligned
  *  lse          device  float [cu_q[B], n_q_heads] or NULL
- *  A page number out of range or a length above max_len records PACE_ERR_INVALID_ARG (kernel id
- *  15) in the device status word; that sequence's results are then not meaningful.
+ *  A page number out of range or a length above max_len or below 0 records PACE_ERR_INVALID_ARG
+ *  (kernel id 15) in the device status word; that sequence's results are then not meaningful.
  *  n_q_heads % n_kv_heads == 0, n_q_heads / n_kv_heads <= 64.
  *  A call takes at most 2^30 query rows per KV head (cu_q[B] * n_q_heads / n_kv_heads).  Sequences go 256
  *  to a launch, in order, those of at most 32 query rows per KV head apart from the others; a launch

@@ -236,7 +236,7 @@ __device__ __forceinline__ KvShare kv_share(const KvAttnArgs& a, int* buf, KvSha
       }
       mine += n;
       items += n > 0 ? a.c.heads : 0;
-      if (blockIdx.x == 0 && it.row_tile == 0 && a.lens[a.s.seq[i]] > a.max_len) record_error(status, PACE_ERR_INVALID_ARG, K_KV_ATTN);
+      if (blockIdx.x == 0 && it.row_tile == 0 && static_cast<uint32_t>(a.lens[a.s.seq[i]]) > static_cast<uint32_t>(a.max_len)) record_error(status, PACE_ERR_INVALID_ARG, K_KV_ATTN);
       if (n == 0 && t % gridDim.x == blockIdx.x) {
 #pragma unroll 1
         for (it.head = 0; it.head < a.c.heads; ++it.head)
