@@ -217,10 +217,17 @@ def _stream(stream):
     return torch.cuda.current_stream().cuda_stream
 
 
-def _workspace(size, args, ws: Optional[torch.Tensor], device):
+def _used(t: torch.Tensor, stream) -> torch.Tensor:
+    """A tensor that a call on `stream` has allocated (on the current one): the allocator keeps its memory until the stream is done with it."""
+    if stream is not None:
+        t.record_stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream.cuda_stream))
+    return t
+
+
+def _workspace(size, args, ws: Optional[torch.Tensor], device, stream):
     """The workspace tensor and its bytes: the caller's, or a new one of size(*args) bytes."""
     if ws is None:
-        ws = torch.empty(max(int(size(*args)), 16), dtype=torch.uint8, device=device)
+        ws = _used(torch.empty(max(int(size(*args)), 16), dtype=torch.uint8, device=device), stream)
     return ws, ws.numel() * ws.element_size()
 
 
@@ -302,7 +309,7 @@ def pace_apc_density(img: torch.Tensor, img_off, H, W, params: Optional[ApcParam
     n = _n_patches(h, w)
     d_out, stats = _density_outputs(n, B, img.device, d_out, stats)
     L = lib()
-    buf, nbytes = _workspace(L.pace_apc_density_workspace_size, (B, hp, wp), ws, img.device)
+    buf, nbytes = _workspace(L.pace_apc_density_workspace_size, (B, hp, wp), ws, img.device, stream)
     _check_ws("pace_apc_density", L.pace_apc_density(_dev(img), op, hp, wp, B, _params(params), _dev(d_out), _dev(stats),
                                                      _dev(buf), nbytes, _stream(stream)), ws)
     return _first(d_out, n), _first(stats, B)
@@ -338,7 +345,7 @@ def pace_apc_density_pixel(img: torch.Tensor, img_off, H, W, feature, params: Op
     n = _n_patches(h, w)
     d_out, stats = _density_outputs(n, B, img.device, d_out, stats)
     L = lib()
-    buf, nbytes = _workspace(L.pace_apc_density_pixel_workspace_size, (B, hp, wp), ws, img.device)
+    buf, nbytes = _workspace(L.pace_apc_density_pixel_workspace_size, (B, hp, wp), ws, img.device, stream)
     _check_ws("pace_apc_density_pixel",
               L.pace_apc_density_pixel(_dev(img), op, hp, wp, B, _feature(feature), _params(params), _dev(d_out), _dev(stats),
                                        _dev(buf), nbytes, _stream(stream)), ws)
@@ -381,7 +388,7 @@ def pace_apc_density_tokens(T: torch.Tensor, cu_tokens, H, W, params: Optional[A
     d_out, stats = _density_outputs(n, B, T.device, d_out, stats)
     L = lib()
     if ws is None:
-        ws = torch.empty(max(int(L.pace_apc_density_tokens_workspace_size(B, cp, D)), 16), dtype=torch.uint8, device=T.device)
+        ws = _used(torch.empty(max(int(L.pace_apc_density_tokens_workspace_size(B, cp, D)), 16), dtype=torch.uint8, device=T.device), stream)
     _check("pace_apc_density_tokens", L.pace_apc_density_tokens(_dev(T), cp, B, D, hp, wp, _params(params), _dev(d_out),
                                                                 _dev(stats), _dev(ws), ws.numel(), _stream(stream)))
     return _first(d_out, n), _first(stats, B)
@@ -472,7 +479,7 @@ def pace_vit_attn_importance(Q: torch.Tensor, K: torch.Tensor, cu_seqlens, scale
     if out is None:
         out = torch.empty(max(n, 1), dtype=torch.float32, device=Q.device)
     L = lib()
-    buf, nbytes = _workspace(L.pace_vit_attn_importance_workspace_size, (B, cp, Hh), ws, Q.device)
+    buf, nbytes = _workspace(L.pace_vit_attn_importance_workspace_size, (B, cp, Hh), ws, Q.device, stream)
     _check_ws("pace_vit_attn_importance",
               L.pace_vit_attn_importance(_dev(Q), _dev(K), cp, B, Hh, D, float(scale), int(merge), _dev(out), _dev(buf),
                                          nbytes, _stream(stream)), ws)
@@ -514,7 +521,7 @@ def pace_vit_attn_importance_chunked(Q: torch.Tensor, K: torch.Tensor, cu_seqlen
         raise ValueError("one event per chunk")
     evs = (ctypes.c_void_p * max(n_ends, 1))(*[int(e.cuda_event) for e in chunk_ready])
     L = lib()
-    buf, nbytes = _workspace(L.pace_vit_attn_importance_workspace_size, (B, cp, Hh), ws, Q.device)
+    buf, nbytes = _workspace(L.pace_vit_attn_importance_workspace_size, (B, cp, Hh), ws, Q.device, stream)
     _check_ws("pace_vit_attn_importance_chunked",
               L.pace_vit_attn_importance_chunked(_dev(Q), _dev(K), cp, B, Hh, D, float(scale), int(merge), _dev(out),
                                                  _dev(buf), nbytes, n_ends, ep, evs, _stream(stream)), ws)
@@ -540,7 +547,7 @@ def pace_llm_text_visual_importance(Q: torch.Tensor, K: torch.Tensor, cu_q, cu_k
     if out is None:
         out = torch.empty(max(n, 1), dtype=torch.float32, device=Q.device)
     L = lib()
-    buf, nbytes = _workspace(L.pace_llm_text_visual_importance_workspace_size, (B, qp, kp, Hq, Hkv), ws, Q.device)
+    buf, nbytes = _workspace(L.pace_llm_text_visual_importance_workspace_size, (B, qp, kp, Hq, Hkv), ws, Q.device, stream)
     _check_ws("pace_llm_text_visual_importance",
               L.pace_llm_text_visual_importance(_dev(Q), _dev(K), qp, kp, B, Hq, Hkv, D, float(scale), _dev(out), _dev(buf),
                                                 nbytes, _stream(stream)), ws)
@@ -575,7 +582,7 @@ def pace_llm_sequence_importance(Q: torch.Tensor, K: torch.Tensor, cu_seq, vis_s
     if out is None:
         out = torch.empty(max(total, 1), dtype=torch.float32, device=Q.device)
     L = lib()
-    buf, nbytes = _workspace(L.pace_llm_sequence_importance_workspace_size, (B, cp, vp, np_, Hq, Hkv, qs), ws, Q.device)
+    buf, nbytes = _workspace(L.pace_llm_sequence_importance_workspace_size, (B, cp, vp, np_, Hq, Hkv, qs), ws, Q.device, stream)
     _check_ws("pace_llm_sequence_importance",
               L.pace_llm_sequence_importance(_dev(Q), _dev(K), cp, vp, np_, B, Hq, Hkv, D, float(scale), qs, _dev(out),
                                              _dev(buf), nbytes, _stream(stream)), ws)
@@ -729,7 +736,7 @@ def pace_kv_append(cache: KvCache, K: torch.Tensor, V: torch.Tensor, cu_new, seq
         if q_rows != src:
             raise ValueError("K and q differ in rows")
         if q_out is None:
-            q_out = torch.empty((n, hq, D), dtype=torch.bfloat16, device=q.device)
+            q_out = _used(torch.empty((n, hq, D), dtype=torch.bfloat16, device=q.device), stream)
         elif q_out.dtype is not _BF16 or q_out.numel() < n * hq * D:
             raise ValueError("q_out: expected bfloat16 [new tokens, heads, D]")
         op = _dev(q_out)
@@ -763,14 +770,14 @@ def pace_kv_attention(cache: KvCache, Q: torch.Tensor, cu_q, seq_lens: torch.Ten
     if scale is None:
         scale = float(D) ** -0.5
     if out is None:
-        out = torch.empty((n, hq, D), dtype=torch.bfloat16, device=Q.device)
+        out = _used(torch.empty((n, hq, D), dtype=torch.bfloat16, device=Q.device), stream)
     elif out.dtype is not _BF16 or out.numel() < n * hq * D:
         raise ValueError("out: expected bfloat16 [new tokens, heads, D]")
     if lse is not None and (lse.dtype != torch.float32 or lse.numel() < n * hq):
         raise ValueError("lse: expected float32 [new tokens, heads]")
     tp, ts = _table(block_table, B)
     L = lib()
-    buf, nbytes = _workspace(L.pace_kv_attention_workspace_size, (cache._address, cp, B, hq, int(max_len)), ws, Q.device)
+    buf, nbytes = _workspace(L.pace_kv_attention_workspace_size, (cache._address, cp, B, hq, int(max_len)), ws, Q.device, stream)
     _check_ws("pace_kv_attention",
               L.pace_kv_attention(cache._address, qp, qs, cp, B, hq, _int32(seq_lens, B, "seq_lens"), tp, ts, int(max_len),
                                   float(scale), int(window), int(sinks), _dev(out), _dev(lse), _dev(buf), nbytes,
