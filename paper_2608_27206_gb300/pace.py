@@ -217,10 +217,14 @@ def _stream(stream):
     return torch.cuda.current_stream().cuda_stream
 
 
+def _torch_stream(stream) -> torch.cuda.Stream:
+    return stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream.cuda_stream)
+
+
 def _used(t: torch.Tensor, stream) -> torch.Tensor:
     """A tensor that a call on `stream` has allocated (on the current one): the allocator keeps its memory until the stream is done with it."""
     if stream is not None:
-        t.record_stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream.cuda_stream))
+        t.record_stream(_torch_stream(stream))
     return t
 
 
@@ -289,11 +293,16 @@ def pace_apc_density_workspace_size(H: Sequence[int], W: Sequence[int]) -> int:
     return int(lib().pace_apc_density_workspace_size(B, hp, wp))
 
 
-def _density_outputs(n: int, B: int, dev, d_out, stats):
+def _density_outputs(n: int, B: int, dev, d_out, stats, stream):
     if d_out is None:
         d_out = torch.empty(max(n, 1), dtype=torch.float32, device=dev)
     if stats is None:
-        stats = torch.zeros((max(B, 1), 10), dtype=torch.int32, device=dev)
+        if stream is None:
+            stats = torch.zeros((max(B, 1), 10), dtype=torch.int32, device=dev)
+        else:       # zeroed on the call's own stream: on the current one the zeros could come after the results
+            stats = _used(torch.empty((max(B, 1), 10), dtype=torch.int32, device=dev), stream)
+            with torch.cuda.stream(_torch_stream(stream)):
+                stats.zero_()
     return d_out, stats
 
 
@@ -307,7 +316,7 @@ def pace_apc_density(img: torch.Tensor, img_off, H, W, params: Optional[ApcParam
     """APC density of B packed uint8 images.  Returns (d [sum N] float32, stats [B, 10] int32 view)."""
     (_o, op, _), (h, hp, B), (w, wp, _) = _i64(img_off), _i32(H), _i32(W)
     n = _n_patches(h, w)
-    d_out, stats = _density_outputs(n, B, img.device, d_out, stats)
+    d_out, stats = _density_outputs(n, B, img.device, d_out, stats, stream)
     L = lib()
     buf, nbytes = _workspace(L.pace_apc_density_workspace_size, (B, hp, wp), ws, img.device, stream)
     _check_ws("pace_apc_density", L.pace_apc_density(_dev(img), op, hp, wp, B, _params(params), _dev(d_out), _dev(stats),
@@ -343,7 +352,7 @@ def pace_apc_density_pixel(img: torch.Tensor, img_off, H, W, feature, params: Op
     """APC density with a pixel-statistic preview.  Returns (d [sum N], stats [B, 10])."""
     (_o, op, _), (h, hp, B), (w, wp, _) = _i64(img_off), _i32(H), _i32(W)
     n = _n_patches(h, w)
-    d_out, stats = _density_outputs(n, B, img.device, d_out, stats)
+    d_out, stats = _density_outputs(n, B, img.device, d_out, stats, stream)
     L = lib()
     buf, nbytes = _workspace(L.pace_apc_density_pixel_workspace_size, (B, hp, wp), ws, img.device, stream)
     _check_ws("pace_apc_density_pixel",
@@ -367,7 +376,7 @@ def pace_apc_density_static(img: torch.Tensor, img_off, H, W, params: Optional[A
     """
     (_o, op, _), (h, hp, B), (w, wp, _) = _i64(img_off), _i32(H), _i32(W)
     n = _n_patches(h, w)
-    d_out, stats = _density_outputs(n, B, img.device, d_out, stats)
+    d_out, stats = _density_outputs(n, B, img.device, d_out, stats, stream)
     _check("pace_apc_density_static", lib().pace_apc_density_static(_dev(img), op, hp, wp, B, _params(params), _dev(d_out),
                                                                     _dev(stats), _stream(stream)))
     return _first(d_out, n), _first(stats, B)
@@ -385,7 +394,7 @@ def pace_apc_density_tokens(T: torch.Tensor, cu_tokens, H, W, params: Optional[A
     (cu, cp, B), (_h, hp, _), (_w, wp, _) = _i32(cu_tokens), _i32(H), _i32(W)
     B -= 1
     n, D = int(cu[-1]), int(T.shape[-1])
-    d_out, stats = _density_outputs(n, B, T.device, d_out, stats)
+    d_out, stats = _density_outputs(n, B, T.device, d_out, stats, stream)
     L = lib()
     if ws is None:
         ws = _used(torch.empty(max(int(L.pace_apc_density_tokens_workspace_size(B, cp, D)), 16), dtype=torch.uint8, device=T.device), stream)

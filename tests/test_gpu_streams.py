@@ -1,4 +1,4 @@
-"""Calls on another stream than the current one: what they allocate themselves stays theirs until they are done."""
+"""Calls on another stream than the current one: what they allocate themselves is theirs from their first kernel to their last."""
 import pytest
 import torch
 
@@ -42,3 +42,16 @@ def test_scratch_and_outputs_are_kept(pace, monkeypatch, count):  # noqa: F811
 
     assert _taken_early(make) == []
     assert pace.pace_device_status(clear=True) == (0, 0)
+
+
+def test_statistics_are_not_zeroed_after_the_call(pace):  # noqa: F811
+    g = torch.Generator().manual_seed(82)
+    img = torch.randint(0, 256, (224 * 224 * 3,), dtype=torch.uint8, generator=g).cuda()
+    d, stats = pace.pace_apc_density(img, [0], [224], [224])
+    want = stats.clone()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda._sleep(100_000_000)      # the current stream is busy for some 50 ms
+    _, got = pace.pace_apc_density(img, [0], [224], [224], stream=side)
+    torch.cuda.synchronize()
+    assert want.any() and torch.equal(got, want)
