@@ -7,7 +7,9 @@ calls of a serving loop:
     step    append one token per sequence and attend: a decode step
 
 Everything is allocated once, and what a step needs is on the device, lengths included, so a step
-can be captured in a CUDA graph and replayed while the sequences grow.
+can be captured in a CUDA graph and replayed while the sequences grow.  The host counts along: a call
+or a replay that would take a sequence past max_len raises before it issues anything.  What the
+kernels report (numbers out of range, values that are not finite) shows in check().
 
     python -m paper_2608_27206_gb300.serve
 
@@ -26,8 +28,20 @@ from . import pace as P
 from . import synth
 
 
+class CapturedStep(torch.cuda.CUDAGraph):
+    """A captured step of a ServeLayer, whose replays count like its steps."""
+
+    layer: "ServeLayer"
+
+    def replay(self) -> None:
+        self.layer._take_one()
+        super().replay()
+
+
 class ServeLayer:
-    """max_len bounds a sequence's slots; sections are the pairs that each row of position ids turns."""
+    """max_len bounds a sequence's slots; sections are the pairs that each row of position ids turns.
+
+    lens, on the device, are the sequences' lengths: prompt, step, replay and reset change them, nobody else may."""
 
     def __init__(self, max_seqs: int, max_len: int, page_size: int = 64, n_q_heads: int = synth.LLM_QHEADS,
                  n_kv_heads: int = synth.LLM_KVHEADS, head_dim: int = synth.LLM_DIM, sections: Optional[Sequence[int]] = None,
@@ -40,6 +54,7 @@ class ServeLayer:
         # each sequence has the pages of max_len slots for itself (a program short of memory hands them out as sequences grow)
         self.table = torch.arange(max_seqs * pages, dtype=torch.int32, device=device).view(max_seqs, pages)
         self.lens = torch.zeros(max_seqs, dtype=torch.int32, device=device)
+        self._of_prompts, self._steps = [0] * max_seqs, 0      # the same on the host: tokens of prompts, and of steps
         self.rope = P.pace_rope_table(max_positions or max_len, head_dim, rope_base, device=device)
         self.one = list(range(max_seqs + 1))
         self.q = torch.empty((max_seqs, n_q_heads, head_dim), dtype=torch.bfloat16, device=device)
@@ -47,11 +62,33 @@ class ServeLayer:
         n = P.pace_kv_attention_workspace_size(self.cache, self.one, n_q_heads, max_len)
         self.ws = torch.empty(max(n, 16), dtype=torch.uint8, device=device)
 
+    def _take_one(self) -> None:
+        if max(self._of_prompts) + self._steps >= self.max_len:
+            raise ValueError(f"a step past max_len ({self.max_len})")
+        self._steps += 1
+
+    def reset(self) -> None:
+        """Empties the sequences."""
+        self.lens.zero_()
+        self._of_prompts, self._steps = [0] * self.B, 0
+
+    def check(self) -> None:
+        """Waits for the device and raises if a call since the last check has reported an error."""
+        code, where = P.pace_device_status(clear=True)
+        if code != P.PACE_OK:
+            raise RuntimeError(f"{P.status_string(code)} (device status {code} from kernel {where})")
+
     def prompt(self, K: torch.Tensor, V: torch.Tensor, Q: torch.Tensor, cu_new: Sequence[int], positions: torch.Tensor,
                rows: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Appends cu_new[b + 1] - cu_new[b] tokens to every sequence b (0: none) and attends from each of them: a whole prompt, a
         chunk of one or a chat's next turn.  rows picks the tokens out of K, V, Q and positions.  bf16 [cu_new[-1], heads, D]."""
-        new = [b - a for a, b in zip(cu_new, cu_new[1:])]
+        new = [int(b) - int(a) for a, b in zip(cu_new, cu_new[1:])]
+        if len(new) != self.B or min(new) < 0:
+            raise ValueError(f"cu_new: expected a prefix of {self.B} numbers of tokens")
+        taken = [a + b for a, b in zip(self._of_prompts, new)]
+        if max(taken) + self._steps > self.max_len:
+            raise ValueError(f"a prompt past max_len ({self.max_len})")
+        self._of_prompts = taken
         self.lens += torch.tensor(new, dtype=torch.int32, device=self.lens.device)
         q = P.pace_kv_append(self.cache, K, V, cu_new, self.lens, self.table, rows=rows, rope=self.rope, positions=positions,
                              sections=self.sections, q=Q)
@@ -59,17 +96,22 @@ class ServeLayer:
 
     def step(self, K: torch.Tensor, V: torch.Tensor, Q: torch.Tensor, positions: torch.Tensor) -> torch.Tensor:
         """One token for every sequence: row b of K, V, Q and of the position ids.  The result is overwritten by the next step."""
+        self._take_one()
+        return self._step(K, V, Q, positions)
+
+    def _step(self, K: torch.Tensor, V: torch.Tensor, Q: torch.Tensor, positions: torch.Tensor) -> torch.Tensor:
         self.lens += 1
         P.pace_kv_append(self.cache, K, V, self.one, self.lens, self.table, rope=self.rope, positions=positions,
                          sections=self.sections, q=Q, q_out=self.q)
         return P.pace_kv_attention(self.cache, self.q, self.one, self.lens, self.table, self.max_len, window=self.window,
                                    sinks=self.sinks, out=self.out, ws=self.ws)
 
-    def capture_step(self, K: torch.Tensor, V: torch.Tensor, Q: torch.Tensor, positions: torch.Tensor) -> torch.cuda.CUDAGraph:
+    def capture_step(self, K: torch.Tensor, V: torch.Tensor, Q: torch.Tensor, positions: torch.Tensor) -> CapturedStep:
         """A graph of step() on these tensors; a replay reads what they hold then.  (Capturing runs nothing.)"""
-        graph = torch.cuda.CUDAGraph()
+        graph = CapturedStep()
+        graph.layer = self
         with torch.cuda.graph(graph):
-            self.step(K, V, Q, positions)
+            self._step(K, V, Q, positions)
         return graph
 
 
@@ -106,7 +148,7 @@ def main(argv=None) -> None:
     layer.prompt(K, V, Q, [0, len(rows)], ids, rows=rows)
     torch.cuda.synchronize()
     t0 = time.perf_counter()
-    layer.lens.zero_()
+    layer.reset()
     layer.prompt(K, V, Q, [0, len(rows)], ids, rows=rows)
     torch.cuda.synchronize()
     prompt_us = 1e6 * (time.perf_counter() - t0)
@@ -121,9 +163,7 @@ def main(argv=None) -> None:
         graph.replay()
     end.record()
     torch.cuda.synchronize()
-    code, where = P.pace_device_status(clear=True)
-    if code != 0:
-        raise RuntimeError(f"device status {code} from kernel {where}")
+    layer.check()
     print(f"prompt: {len(rows)} of {n} tokens appended and attended in {prompt_us:.0f} us; "
           f"then {args.steps - 1} decode steps, {1e3 * start.elapsed_time(end) / max(args.steps - 1, 1):.1f} us each; "
           f"{int(layer.lens[0])} slots in use")
