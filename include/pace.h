@@ -565,7 +565,7 @@ PACE_API pace_status_t pace_rope_table(float* table, int64_t n_positions, int he
  *
  *  K, V          device  bf16 [n_src_rows, n_kv_heads, D]; consecutive rows k_row_stride,
  *                        v_row_stride elements apart (a fused projection's output will do); the
- *                        strides multiples of 8, the pointers 16-byte aligned
+ *                        strides multiples of 8 and at most 2^31, the pointers 16-byte aligned
  *  cu_new        host    int32 [B+1] prefix of the new tokens per sequence (0 allowed)
  *  seq_lens      device  int32 [B]
  *  block_table   device  int32 [B][table_stride]: page of slots page_size * i ..; entries behind
@@ -574,7 +574,8 @@ PACE_API pace_status_t pace_rope_table(float* table, int64_t n_positions, int he
  *  rope          host    NULL for no rotation
  *  Q, q_out      device  bf16 [n_src_rows, n_q_heads, D] with rows q_row_stride apart, and
  *                        [cu_new[B], n_q_heads, D] contiguous; both NULL: keys and values only.
- *                        q_out may be Q itself where that is contiguous and rows is NULL
+ *                        q_out may be Q itself where that is contiguous and rows is NULL;
+ *                        n_q_heads 1 .. 16384
  *  No two sequences may share a page that the call writes.
  */
 PACE_API pace_status_t pace_kv_append(const pace_kv_cache* cache, const void* K, const void* V, int64_t k_row_stride,
@@ -607,7 +608,7 @@ PACE_API size_t pace_kv_attention_workspace_size(const pace_kv_cache* cache, con
  * atomics on values).
  *
  *  Q            device  bf16 [cu_q[B], n_q_heads, D], rows q_row_stride elements apart (a multiple
- *                       of 8), 16-byte aligned
+ *                       of 8, at most 2^31), 16-byte aligned
  *  cu_q         host    int32 [B+1] prefix of the queries per sequence (0 allowed)
  *  seq_lens     device  int32 [B], the queries' own tokens included; each 0 .. max_len
  *  block_table  device  int32 [B][table_stride], as for pace_kv_append; the entry of a page none of whose

@@ -357,7 +357,7 @@ extern "C" pace_status_t pace_kv_append(const pace_kv_cache* cache, const void* 
     return PACE_ERR_INVALID_ARG;
   if (rows == nullptr && n_src_rows < cu_new[B]) return PACE_ERR_INVALID_ARG;
   if ((Q == nullptr) != (q_out == nullptr)) return PACE_ERR_INVALID_ARG;
-  if (Q != nullptr && (n_q_heads < 1 || n_q_heads > 256 || !rows_ok(Q, q_row_stride, n_q_heads, D) ||
+  if (Q != nullptr && (n_q_heads < 1 || n_q_heads > kKvMaxQHeads || !rows_ok(Q, q_row_stride, n_q_heads, D) ||
                        reinterpret_cast<uintptr_t>(q_out) % 16 != 0))
     return PACE_ERR_INVALID_ARG;
   AppendArgs a{};

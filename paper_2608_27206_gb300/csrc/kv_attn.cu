@@ -78,7 +78,7 @@ int64_t next_launch(const int32_t* cu_q, int B, int group, bool is_few, int rows
 pace_status_t check_attention(const pace_kv_cache* cache, const int32_t* cu_q, int B, int n_q_heads, int max_len) {
   PACE_CHECK(check_cache(cache));
   PACE_CHECK(check_prefix(cu_q, B));
-  if (n_q_heads < 1 || n_q_heads % cache->n_kv_heads != 0 || n_q_heads / cache->n_kv_heads > 64) return PACE_ERR_INVALID_ARG;
+  if (n_q_heads < 1 || n_q_heads % cache->n_kv_heads != 0 || n_q_heads / cache->n_kv_heads > kKvMaxGroup) return PACE_ERR_INVALID_ARG;
   if (max_len < 0 || max_len > (1 << 30)) return PACE_ERR_INVALID_ARG;
   const int group = n_q_heads / cache->n_kv_heads;
   if (cu_q[B] > (1 << 30) / group) return PACE_ERR_INVALID_ARG;

@@ -8,6 +8,7 @@ namespace pace {
 
 constexpr int kKvMaxB = 256;          // sequences of one launch
 constexpr int kKvBlock = PACE_KV_BLOCK;
+constexpr int kKvMaxGroup = 64, kKvMaxQHeads = 256 * kKvMaxGroup;      // query heads per KV head, in all
 
 // The cache as the kernels take it.
 struct KvView {

@@ -34,3 +34,13 @@ def test_rotated_keys_and_queries(pace, heads, dim, first, count):  # noqa: F811
         np.testing.assert_array_equal(O.e4m3_values()[codes], values)
     want = torch.from_numpy(_turn32(_f64(q), cs)).to(BF16)
     assert torch.equal(q_out.cpu(), want)
+
+
+# as many query heads as attention takes
+@pytest.mark.parametrize("hq", [256, 257, 320, 1000, 16384])
+def test_queries_of_many_heads(pace, hq):  # noqa: F811
+    pool = Pool(pace, 65, [19, 3], 1, 64, 16, poison=False)
+    K, q = _tokens(66, 22, 1, 64), _tokens(67, 22, hq, 64)
+    kw, angles = rotation(pace, 64, 22, 68)
+    q_out = pace.pace_kv_append(pool.cache, K, K, [0, 19, 22], pool.lens, pool.table, q=q, **kw)
+    assert torch.equal(q_out.cpu(), torch.from_numpy(_turn32(_f64(q), angles(np.arange(22)))).to(BF16))
