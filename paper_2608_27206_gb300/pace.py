@@ -648,10 +648,14 @@ class KvCache:
                 raise ValueError("k, v and their scales do not fit together")
             if not (t.is_cuda and s.is_cuda):
                 raise ValueError("expected CUDA tensors")
+            if t.numel() == 0:
+                raise ValueError("expected at least one page")
             if not (t[0].is_contiguous() and s[0].is_contiguous()):
                 raise ValueError("expected contiguous pages")
             if t.stride(0) != k.stride(0) or s.stride(0) != k_scale.stride(0):
                 raise ValueError("k and v differ in the distance between their pages")
+            if t.shape[0] > 1 and (t.stride(0) < t[0].numel() or s.stride(0) < s[0].numel()):
+                raise ValueError("pages overlap")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         n, self.n_kv_heads, self.page_size, self.head_dim = k.shape
         self.n_pages = n
