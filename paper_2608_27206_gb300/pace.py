@@ -676,7 +676,9 @@ def pace_rope_table(n_positions: int, head_dim: int, base: float = 1e6, out: Opt
                     stream=None) -> torch.Tensor:
     """Rotation table float32 [n_positions, head_dim / 2, 2] of (cos, sin)."""
     if out is None:
-        out = torch.empty((n_positions, head_dim // 2, 2), dtype=torch.float32, device=device)
+        out = _used(torch.empty((n_positions, head_dim // 2, 2), dtype=torch.float32, device=device), stream)
+    elif out.dtype != torch.float32 or out.numel() < n_positions * head_dim:
+        raise ValueError("out: expected float32 [positions, D / 2, 2]")
     _check("pace_rope_table", lib().pace_rope_table(_dev(out), n_positions, head_dim, float(base), _stream(stream)))
     return out
 

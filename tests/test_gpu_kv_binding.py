@@ -16,3 +16,11 @@ def test_caches_whose_pages_overlap(pace):  # noqa: F811
     for k, s in ((same, scales), (near, scales[:3]), (codes, scales[:1].expand(6, -1, -1)), (codes[:0], scales[:0])):
         with pytest.raises(ValueError):
             pace.KvCache(k, k, s, s)
+
+
+def test_rotation_tables_that_do_not_fit(pace):  # noqa: F811
+    good = torch.empty(10, 32, 2, device="cuda")
+    assert pace.pace_rope_table(10, 64, out=good) is good
+    for bad in (good[:9], good.to(torch.bfloat16), good.double()):
+        with pytest.raises(ValueError):
+            pace.pace_rope_table(10, 64, out=bad)
