@@ -286,13 +286,6 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
 #pragma unroll
             for (int q = 0; q < NQ; ++q) any = any || kv_sees(slot, ctl->slot_of[q], a.window, a.sinks);
             if (!any) ks = vs = 0.f;     // (what is there may be NaN)
-          }
-#pragma unroll
-          for (int q = 0; q < NQ; ++q) {
-            x[q] = fmaf(__uint_as_float(sv[NQ + q]), 0.0625f, __uint_as_float(sv[q])) * (ks * ctl->qc[q]);
-            if (!whole && !kv_sees(slot, ctl->slot_of[q], a.window, a.sinks)) x[q] = -INFINITY;
-          }
-          if (!whole) {
             // 0 * NaN is NaN: a slot of V that some row does not see must not hold one.  Slots that nobody sees are
             // cleared; where rows differ, a slot with a NaN code is cleared and those that see it get a NaN weight.
             uint4* v = reinterpret_cast<uint4*>(sKV + (2 * s + 1) * C::TILE + me * D);
@@ -311,6 +304,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
               for (int e = 0; e < D / 16; ++e) v[e ^ (me & (D / 16 - 1))] = make_uint4(0, 0, 0, 0);
             }
             if (nan) vs = NAN;
+          }
+          if (vs != vs) ks = vs;      // (by way of its score: the products below drop a NaN scale)
+#pragma unroll
+          for (int q = 0; q < NQ; ++q) {
+            x[q] = fmaf(__uint_as_float(sv[NQ + q]), 0.0625f, __uint_as_float(sv[q])) * (ks * ctl->qc[q]);
+            if (!whole && !kv_sees(slot, ctl->slot_of[q], a.window, a.sinks)) x[q] = -INFINITY;
           }
         }
         const float lv = static_cast<float>(static_cast<int>(__float_as_uint(vs) >> 23) - 127);   // log2(vs), far down for 0
@@ -375,14 +374,14 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
             const float pr = ex2_approx(x[q + e] - stat[q + e].m);
             l[q + e] += pr;
             y[e] = pr * fminf(vs * stat[q + e].g, 0x1p100f);      // (the bound: pr is 0 or all but 0 there, and 0 times infinity)
-            if (vs != vs && x[q + e] > -INFINITY) y[e] = vs;           // (fminf drops a NaN)
           }
           uint32_t small = 0;
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const bool is = y[e] < kSmall;
-            y[e] *= is ? kTimes : 1.f;
-            small |= is ? 0xFFu << 8 * e : 0u;
+            if (y[e] < kSmall) {
+              y[e] *= kTimes;
+              small |= 0xFFu << 8 * e;
+            }
           }
           const uint32_t hi = e4m3x4(y[0], y[1], y[2], y[3]);
           const uint32_t f0 = e4m3x2_to_f16x2(hi & 0xFFFFu), f1 = e4m3x2_to_f16x2(hi >> 16);
