@@ -605,7 +605,8 @@ PACE_API size_t pace_kv_attention_workspace_size(const pace_kv_cache* cache, con
  * of two ranges, down to 2^-22 of the query's largest (weight times V scale of its block) and to
  * 2^-31 of that below; else to the 11 bits of f16 down to 2^-13 and to 2^-24 of the largest below.
  * Sums and softmax statistics are fp32; results do not depend on anything but the arguments (no
- * atomics on values).
+ * atomics on values).  Scores may be as large as fp32 holds (below 2^127 in base 2, else the result
+ * is NaN); V scales that a query sees are to lie within 2^90 of each other.
  *
  *  Q            device  bf16 [cu_q[B], n_q_heads, D], rows q_row_stride elements apart (a multiple
  *                       of 8, at most 2^31), 16-byte aligned

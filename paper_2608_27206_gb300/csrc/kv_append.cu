@@ -10,7 +10,7 @@
 // before them (length, row, position, angles).  One CTA per touched block, three to an SM: it stages the tokens' (cos, sin) once
 // for all heads while the first rows are on their way; a warp takes a head's 16 rows of K or V, 16 bytes per lane and load, both halves
 // of a pair in one lane, 16 bits wide until they are used.  For the queries a lane keeps its row's angles in registers
-// and goes over heads, four in flight.  16 prompts, 44000 tokens of 28 + 8 heads of 128: 137 us, 6.0 TB/s (two CTAs per SM 145,
+// and goes over heads, four in flight.  16 prompts, 44000 tokens of 28 + 8 heads of 128: 137 us, 5.9 TB/s (two CTAs per SM 145,
 // four 149: registers).  A decode step is latency: 64 tokens in 9 us.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>

@@ -18,9 +18,11 @@
 // exchange between threads but one barrier's vote, and O^T stays in TMEM untouched.  Whatever x is, log2(vs) is only ever added to
 // a difference of scores: added to a score of 2^24 and more it would be rounded.
 //
-// What bounds it is HBM: per slot and head 2 D bytes.  From S of a tile to its P takes a group of four warps 1.1 us whatever the
-// number of rows, one and a half times what a tile of 32 KB takes an SM to fetch; so two groups take every other tile, each with its own
-// m, w, l and O^T, and join them at the item's end.  64 sequences of 5001-28007 slots, 4 heads of 128: 150 us, 5.9 TB/s (one group: 210 us).
+// What bounds it is HBM where rows are few: per slot and head 2 D bytes.  From S of a tile to its P takes a group of four warps more than
+// a microsecond, one and a half times what a tile of 32 KB takes an SM to fetch; so two groups take every other tile, each with its own
+// m, r, l and O^T, and join them at the item's end.  64 sequences of 5001-28007 slots, 4 heads of 128, 7 rows: 156 us, 5.6 TB/s (with one
+// pair of columns for P 153; one group took 210 against 150).  With 32 rows it is the groups: 463 us, 34 us of it the second pair's
+// stores and products of twice the columns.
 // Roles of a CTA (one per SM): warp 0 fetches tiles of 128 slots (TMA boxes of a page each, scales by 4-byte copies) through a
 // ring of stages, warp 1 issues the MMAs, warps 2-5 and 6-9 own the 128 lanes of even and odd tiles.
 #include <cuda_bf16.h>
@@ -491,7 +493,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
 // and differences are of b by itself first, which leaves them exact where the scores b are close.  What it
 // takes is latency, so a warp's loads go out together, PARTS parts of ROWS rows at a time.  Where rows are few a row has 8 warps (a
 // sequence alone makes as many parts as there are tiles: 38 of them took 8 us with one warp); where they are many and a row has few
-// parts, a warp has 4 rows (a call of 517 tokens: 97 us in all, with one row 99).
+// parts, a warp has 4 rows (2 us less in a call of 517 tokens than with one row).
 template <int D, int ROWS, int PARTS, int SPLIT>
 __global__ void __launch_bounds__(256) kv_attn_combine(const __grid_constant__ KvAttnArgs a, int tile_rows) {
   constexpr int E = D / 32;      // elements of a lane

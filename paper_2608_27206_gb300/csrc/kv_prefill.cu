@@ -18,12 +18,13 @@
 // largest weight at 2^4 instead it would be 108.)  There is no maximum in the common path.  (Weights of blocks whose V scale is below
 // 2^-110 of the largest are lost to l.)
 //
-// The tensor pipe needs 2048 clocks per slot tile of 2 x 128 rows at D = 128, the exponentials 1024, and a slot tile takes 3600:
-// what bounds it is the chain from S to P to P V, 45 % tensor active.  Two row tiles A and B share every K and V tile (a V tile turned
-// into f16 once for both) and take turns: while one's weights are worked out, the other's products run.  P overwrites its S
-// in TMEM.  Measured: a prompt of 10825 tokens, 28 + 4 heads of 128: 790-815 us, 1.03-1.06 PFLOP/s; 517 tokens at the end of 11342: 97 us.  Tried
-// and slower: S by halves of 64 columns (A is read twice as often: 844 us), two threads per row on four warps per
-// scheduler (908), a warp of MMAs per row tile (872), a single row tile with S ahead (1013; the short call 89).
+// The tensor pipe needs 2048 clocks per slot tile of 2 x 128 rows at D = 128 (1024 at D = 64), the exponentials 1024 at either, and in a
+// long prompt a slot tile takes 4060 all told: what bounds it is the chain from S to P to P V, 50 % tensor active (a call of 517 tokens
+// 43 %, prompts of D = 64 with a window 18 %, where items are short and change often).  Two row tiles A and B share every K and V tile (a V
+// tile turned into f16 once for both) and take turns: while one's weights are worked out, the other's products run.  P overwrites its
+// S in TMEM.  Measured: a prompt of 10825 tokens, 28 + 4 heads of 128: 815-830 us, 1.01-1.03 PFLOP/s; 517 tokens at the end of 11342:
+// 102 us.  Tried and slower, when these were 790-815 and 97: S by halves of 64 columns (A is read twice as often: 844 us), two threads per
+// row on four warps per scheduler (908), a warp of MMAs per row tile (872), a single row tile with S ahead (1013; the short call 89).
 // Roles of a CTA (one per SM): warp 0 fetches, warp 1 issues the MMAs, warps 2-3 turn V into f16 (they also see to NaN that must
 // not reach rows that do not look at it), warps 4-7 and 8-11 own the rows of A and B.
 #include <cuda_bf16.h>

@@ -10,7 +10,7 @@ import pytest
 import torch
 
 from oracle import pace_oracle as O
-from test_gpu_kv import BF16, Pool, _cu, _f64, _upload, pace  # noqa: F401
+from test_gpu_kv import BF16, Pool, _cu, _f64, _tokens, _upload, check_attention, pace  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -209,3 +209,13 @@ def test_queries_with_an_outlying_channel(pace, outlier, count, hq, hkv, dim):  
         assert np.all(off <= score + 2.0 ** -21 * np.abs(r["lse"])), float((off / score).max())
         tol = 2.0 ** -8 * np.abs(r["out"]) + (2.0 ** -8 + 2 * score[..., None]) * r["abs_out"] + 2.0 ** -17 * r["peak"][..., None]
         assert np.all(np.abs(_f64(out) - r["out"]) <= tol)
+
+
+# V scales of blocks up to 2^80 apart: neither the sum of the weights nor the large blocks' part of the output suffers
+@pytest.mark.parametrize("lens,new", [((900, 300), (1, 2)), ((400,), (120,)), ((2000, 70), (70, 3))])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_v_scales_far_apart(pace, lens, new, dim):  # noqa: F811
+    pool = Pool(pace, 50, list(lens), 2, dim, 16)
+    pool.s["v"] = pool.s["v"] * 2.0 ** np.random.default_rng(51).integers(-40, 41, pool.s["v"].shape)
+    _upload(pool)
+    check_attention(pace, pool, _tokens(52, sum(new), 14, dim), list(new))
