@@ -199,7 +199,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
 #pragma unroll
         for (int k = 0; k < D / 32; ++k)
           mma_f8_ss(tmem + i * 128, q + static_cast<uint64_t>(part * (C::QTILE >> 4) + 2 * k), k0 + static_cast<uint64_t>(2 * k),
-                    part == 0 ? C::IDESC_HI : C::IDESC_LO,                    part > 0 || k > 0, issue);
+                    part == 0 ? C::IDESC_HI : C::IDESC_LO, part > 0 || k > 0, issue);
       commit(s_full(i));
     };
     while (ok && walk.next(a)) {
