@@ -634,6 +634,87 @@ PACE_API pace_status_t pace_kv_attention(const pace_kv_cache* cache, const void*
                                          int64_t table_stride, int max_len, float scale, int window, int sinks, void* out,
                                          float* lse, void* ws, size_t ws_bytes, pace_stream_t stream);
 
+/* ---- drafted tokens ------------------------------------------------------------------------ */
+
+/* Nodes that a tree of pace_kv_tree_attention may have. */
+#define PACE_TREE_MAX 1024
+
+/* Scratch bytes for pace_kv_tree_attention (host cu_q [B+1]); 0 if the arguments are invalid. */
+PACE_API size_t pace_kv_tree_attention_workspace_size(const pace_kv_cache* cache, const int32_t* cu_q, int B, int n_q_heads,
+                                                      int max_len);
+
+/*
+ * pace_kv_attention from the nodes of a tree of drafted tokens.  The n_b newest slots of a sequence, from base = seq_lens[b] - n_b
+ * on, are the nodes of a tree (or of several: a forest): node t's parent is node parents[cu_q[b] + t], before it, or -1 where it
+ * follows the slots before the tree.  With depth e(t), the number of its ancestors, node t's position is base + e(t), and so is its
+ * slot's; a slot j < base has position j.  Node t sees its ancestors, itself and the slots before base, of them those with
+ * window <= 0 or position > base + e(t) - window or position < sinks: what it would see if the path to it were the sequence's end.
+ * (Keys and queries are rotated by such positions when they are appended: the caller's ids say so.)
+ *
+ *  parents  device  int32 [cu_q[B]]; an entry below -1 or not before its node counts as -1 and records PACE_ERR_INVALID_ARG
+ *                   (kernel id 16) in the device status word
+ *  n_b at most PACE_TREE_MAX.  Everything else, formats, limits and errors, as for pace_kv_attention; a page none of whose slots any node
+ *  sees may be anything.  A sequence shorter than its nodes has its first ones before slot 0: nobody sees those, and a node that sees
+ *  nothing gives out = 0 and lse = -inf.
+ */
+PACE_API pace_status_t pace_kv_tree_attention(const pace_kv_cache* cache, const void* Q, int64_t q_row_stride, const int32_t* cu_q,
+                                              int B, int n_q_heads, const int32_t* parents, const int32_t* seq_lens,
+                                              const int32_t* block_table, int64_t table_stride, int max_len, float scale, int window,
+                                              int sinks, void* out, float* lse, void* ws, size_t ws_bytes, pace_stream_t stream);
+
+/*
+ * The drafted tokens that are accepted.  Node 0 of sequence b's tree is accepted (the token that the model picked last); after it, from
+ * the node come to, the first child (lowest number) whose token is the one picked after that node, until there is none.
+ *
+ *  tokens       device  int32 [cu_nodes[B]] the nodes' tokens (node 0's is not looked at)
+ *  parents      device  int32 [cu_nodes[B]] as for pace_kv_tree_attention (a node without a parent other than node 0 is
+ *                       never accepted); an entry below -1 or not before its node counts as -1 and records PACE_ERR_INVALID_ARG
+ *                       (kernel id 17)
+ *  picked       device  int32 [cu_nodes[B]] the token that the model picks after each node
+ *  cu_nodes     host    int32 [B+1] prefix of the nodes per sequence (0 allowed; no limit on one)
+ *  rows         device  int32 [cu_nodes[B]]: from cu_nodes[b] on the accepted nodes of sequence b, as rows cu_nodes[b] + t of the
+ *                       packed batch, ascending; the rest of its cu_nodes[b + 1] - cu_nodes[b] entries -1
+ *  counts       device  int32 [B] how many (0 for a sequence without nodes)
+ *  next_tokens  device  int32 [B] the token picked after the last of them (-1 for a sequence without nodes)
+ *  No output may overlap another one or an input.
+ */
+PACE_API pace_status_t pace_draft_accept(const int32_t* tokens, const int32_t* parents, const int32_t* picked, const int32_t* cu_nodes, int B,
+                                         int32_t* rows, int32_t* counts, int32_t* next_tokens, pace_stream_t stream);
+
+/*
+ * Keeps some of the newest tokens of each sequence and moves them together, in every layer.  Of the n_b = cu_new[b+1] - cu_new[b]
+ * newest tokens of sequence b, at slots base = seq_lens[b] - n_b on, the kept are those that a list of rows names, row cu_new[b] + t
+ * standing for token t: accepted drafts as pace_draft_accept lists them, or a pruned prompt as pace_prune_index does.  Kept token
+ * i goes to slot base + i of the pages that dst_table names, or of the sequence's own (in place).
+ *
+ * Every block that a kept token goes to gets a new scale, the smallest power of two that covers what it then holds
+ * (amax <= 448 s; between 2^-64 and 2^120): kept tokens, and earlier ones in slots below base of its first block (those of dst_table's
+ * page).  Codes are multiplied by the ratio of their scales and rounded once more, ties to even (where the ratio is 1 or
+ * above, exactly).  Slots behind the last kept token hold what they held, under the new scale: nothing.
+ *
+ * A kept token with a NaN code or a scale that is not a finite positive number is stored as 0 (that head of K or V) and records
+ * PACE_ERR_INVALID_ARG (kernel id 18) in the device status word; so does a row that is out of range or not above the one before it,
+ * or whose page number is out of range.  A page number of dst_table out of range records it, and that block is not
+ * stored.  A count out of range, or a sequence shorter than n_b, records it; nothing of that sequence moves, and its new length is its length.
+ *
+ *  layers       host    [n_layers] caches alike in everything but their addresses (any number)
+ *  cu_new       host    int32 [B+1] prefix of the newest tokens per sequence that are looked at (0 allowed)
+ *  seq_lens     device  int32 [B], those tokens included
+ *  block_table  device  int32 [B][table_stride] as for pace_kv_append; entries of pages that hold no token to be read are not read
+ *  cu_rows      host    int32 [B+1] prefix of the rows' places; at most n_b for a sequence.  NULL: cu_new
+ *  rows         device  int32 [cu_rows[B]], the list of sequence b from cu_rows[b] on, strictly ascending.  NULL: token i is kept token i
+ *  counts       device  int32 [B] how many of them count, at most cu_rows[b+1] - cu_rows[b].  NULL: all
+ *  dst_table    device  int32 [B][dst_stride], or NULL (or block_table itself): in place.  Else no page that is written may be one
+ *                       that is read.  A shared prefix may stand in both: pages of slots below base are not written, but for the one that base
+ *                       lies in
+ *  new_lens     device  int32 [B]: base + the number kept.  May not overlap any other array
+ *  No two sequences may write the same page, or one write what another reads.
+ */
+PACE_API pace_status_t pace_kv_compact(const pace_kv_cache* layers, int n_layers, const int32_t* cu_new, int B, const int32_t* seq_lens,
+                                       const int32_t* block_table, int64_t table_stride, const int32_t* cu_rows, const int32_t* rows,
+                                       const int32_t* counts, const int32_t* dst_table, int64_t dst_stride, int32_t* new_lens,
+                                       pace_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

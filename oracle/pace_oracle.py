@@ -531,3 +531,62 @@ def kv_attention(Q: np.ndarray, K: np.ndarray, V: np.ndarray, visible: np.ndarra
             score[t, h] = scale * (np.abs(K[j, g]) @ np.abs(Q[t, h])).max()
             peak[t, h] = np.sqrt(j.size) * (w * np.abs(V[j, g]).max(axis=1)).max()
     return dict(out=out, lse=lse, abs_out=absout, abs_score=score, peak=peak)
+
+
+def tree_family(parents: Sequence[int]) -> List[List[int]]:
+    """Of every node itself and its ancestors, ascending; parents come before their children, -1 is none."""
+    family: List[List[int]] = []
+    for t, p in enumerate(parents):
+        family.append((family[p] if p >= 0 else []) + [t])
+    return family
+
+
+def kv_tree_visible(length: int, parents: Sequence[int], window: int = 0, sinks: int = 0) -> np.ndarray:
+    """[nodes, length]: the slots that each node of a tree in a sequence's newest slots sees.  Positions: a slot's number before the
+    tree, base + depth in it."""
+    family = tree_family(parents)
+    n = len(family)
+    base = length - n
+    depth = np.array([len(f) - 1 for f in family])
+    slot = np.arange(length)
+    at = np.where(slot < base, slot, base + depth[np.clip(slot - base, 0, n - 1)])
+    see = np.zeros((n, length), dtype=bool)
+    for t, f in enumerate(family):
+        mine = slot < base
+        mine[[base + u for u in f if base + u >= 0]] = True
+        see[t] = mine & ((window <= 0) | (at > base + depth[t] - window) | (at < sinks))
+    return see
+
+
+def draft_accept(tokens: Sequence[int], parents: Sequence[int], picked: Sequence[int]) -> List[int]:
+    """The accepted path of one tree: from node 0 the first child whose token was picked after its parent, until there is none."""
+    path = [0] if len(tokens) else []
+    while path:
+        child = [t for t in range(len(tokens)) if parents[t] == path[-1] and tokens[t] == picked[path[-1]]]
+        if not child:
+            break
+        path.append(child[0])
+    return path
+
+
+def kv_compact(values: np.ndarray, scales: np.ndarray, source: Sequence[int], target: Sequence[int], base: int, kept: Sequence[int]) -> None:
+    """Moves a sequence's tokens at slots base + kept[i] of pages `source` to slots base + i of pages `target`, in place in
+    values and scales (as kv_append has them): each block written under the smallest scale that covers it, earlier tokens included."""
+    page = values.shape[2]
+    if len(kept) == 0:
+        return
+    lead = base % KV_BLOCK
+
+    def read(pages, slots):
+        pg, at = np.asarray(pages)[slots // page], slots % page
+        return values[pg, :, at] * scales[pg, :, at // KV_BLOCK][..., None]
+    early = np.arange(base - lead, base)
+    x = read(source, base + np.asarray(kept))
+    if lead:
+        x = np.concatenate([read(target, early), x])
+    for i in range(0, len(x), KV_BLOCK):
+        part, slot = x[i:i + KV_BLOCK], base - lead + i
+        s = kv_scale(np.abs(part).max(axis=(0, 2)))
+        pg, at = target[slot // page], slot % page
+        values[pg, :, at:at + len(part)] = e4m3_round(part / s[None, :, None]).transpose(1, 0, 2)
+        scales[pg, :, at // KV_BLOCK] = s

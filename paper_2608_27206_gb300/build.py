@@ -22,7 +22,8 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libpace.so")
-SOURCES = ["pace_api.cu", "apc.cu", "attn.cu", "ddae.cu", "kv_append.cu", "kv_attn.cu", "kv_decode.cu", "kv_prefill.cu"]
+SOURCES = ["pace_api.cu", "apc.cu", "attn.cu", "ddae.cu", "kv_append.cu", "kv_attn.cu", "kv_decode.cu", "kv_prefill.cu", "kv_tree.cu",
+           "kv_compact.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

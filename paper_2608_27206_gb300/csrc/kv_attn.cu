@@ -90,35 +90,47 @@ pace_status_t check_attention(const pace_kv_cache* cache, const int32_t* cu_q, i
 }
 
 struct Workspace {
-  size_t lse, part, total;
+  size_t lse, part, depth, family, total;
+  int words;
 };
-Workspace workspace(int rows, int D) {
+Workspace workspace(int rows, int D, const int32_t* cu_q, int B, bool tree) {
   Workspace w{};
   w.lse = align_up(kPlanCtas * sizeof(KvSplit), 256);
   w.part = w.lse + align_up(static_cast<size_t>(2) * kPlanCtas * rows * sizeof(float2), 256);
   w.total = w.part + static_cast<size_t>(2) * kPlanCtas * rows * D * sizeof(float);
+  if (tree) {
+    int most = 1;
+    for (int b = 0; b < B; ++b) most = std::max(most, cu_q[b + 1] - cu_q[b]);
+    w.words = (most + 62) / 32;      // (wherever in a word the first bit lands)
+    w.depth = w.total;
+    w.family = w.depth + align_up(static_cast<size_t>(cu_q[B]) * sizeof(int32_t), 256);
+    w.total = w.family + static_cast<size_t>(cu_q[B]) * w.words * sizeof(uint32_t);
+  }
   return w;
 }
 
-}  // namespace
-}  // namespace pace
-
-using namespace pace;
-
-extern "C" size_t pace_kv_attention_workspace_size(const pace_kv_cache* cache, const int32_t* cu_q, int B, int n_q_heads,
-                                                   int max_len) {
-  if (B <= 0 || check_attention(cache, cu_q, B, n_q_heads, max_len) != PACE_OK) return 0;
-  return workspace(most_rows(cu_q, B, n_q_heads / cache->n_kv_heads), cache->head_dim).total;
+// Trees have at most PACE_TREE_MAX nodes.
+pace_status_t check_tree(const int32_t* cu_q, int B) {
+  for (int b = 0; b < B; ++b)
+    if (cu_q[b + 1] - cu_q[b] > PACE_TREE_MAX) return PACE_ERR_INVALID_ARG;
+  return PACE_OK;
 }
 
-extern "C" pace_status_t pace_kv_attention(const pace_kv_cache* cache, const void* Q, int64_t q_row_stride, const int32_t* cu_q,
-                                           int B, int n_q_heads, const int32_t* seq_lens, const int32_t* block_table,
-                                           int64_t table_stride, int max_len, float scale, int window, int sinks, void* out,
-                                           float* lse, void* ws, size_t ws_bytes, pace_stream_t stream) {
+size_t workspace_size(const pace_kv_cache* cache, const int32_t* cu_q, int B, int n_q_heads, int max_len, bool tree) {
+  if (B <= 0 || check_attention(cache, cu_q, B, n_q_heads, max_len) != PACE_OK || (tree && check_tree(cu_q, B) != PACE_OK)) return 0;
+  return workspace(most_rows(cu_q, B, n_q_heads / cache->n_kv_heads), cache->head_dim, cu_q, B, tree).total;
+}
+
+// Both calls; parents null: the queries follow one another.
+pace_status_t attend(const pace_kv_cache* cache, const void* Q, int64_t q_row_stride, const int32_t* cu_q, int B, int n_q_heads,
+                     const int32_t* parents, bool tree, const int32_t* seq_lens, const int32_t* block_table, int64_t table_stride, int max_len,
+                     float scale, int window, int sinks, void* out, float* lse, void* ws, size_t ws_bytes, cudaStream_t stream) {
   if (B < 0) return PACE_ERR_INVALID_ARG;
   if (B == 0) return PACE_OK;
   PACE_CHECK(check_attention(cache, cu_q, B, n_q_heads, max_len));
+  if (tree) PACE_CHECK(check_tree(cu_q, B));
   if (cu_q[B] == 0) return PACE_OK;
+  if (tree && (parents == nullptr || reinterpret_cast<uintptr_t>(parents) % 4 != 0)) return PACE_ERR_INVALID_ARG;
   const int D = cache->head_dim, group = n_q_heads / cache->n_kv_heads;
   if (!rows_ok(Q, q_row_stride, n_q_heads, D) || out == nullptr || reinterpret_cast<uintptr_t>(out) % 16 != 0)
     return PACE_ERR_INVALID_ARG;
@@ -126,7 +138,7 @@ extern "C" pace_status_t pace_kv_attention(const pace_kv_cache* cache, const voi
   if (max_len > table_stride * cache->page_size) return PACE_ERR_INVALID_ARG;
   if (!(scale > 0.f) || !std::isfinite(scale)) return PACE_ERR_INVALID_ARG;
   const int few = few_rows(cu_q, B, group);
-  const Workspace w = workspace(most_rows(cu_q, B, group), D);
+  const Workspace w = workspace(most_rows(cu_q, B, group), D, cu_q, B, tree);
   if (ws == nullptr || reinterpret_cast<uintptr_t>(ws) % 16 != 0 || ws_bytes < w.total) return PACE_ERR_WORKSPACE;
   PACE_CHECK(check_device());
   KvMaps maps;
@@ -154,6 +166,13 @@ extern "C" pace_status_t pace_kv_attention(const pace_kv_cache* cache, const voi
   int* status = device_status_word();
   int sms = 0;
   PACE_CHECK(sm_count(&sms));
+  if (tree) {
+    KvTree t{parents, reinterpret_cast<int32_t*>(static_cast<uint8_t*>(ws) + w.depth), reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(ws) + w.family), w.words};
+    PACE_CHECK(launch_kv_tree(t, cu_q, B, seq_lens, max_len, a.window, sinks, status, stream));
+    a.depth = t.depth;
+    a.family = t.family;
+    a.words = t.words;
+  }
   for (const bool is_few : {true, false}) {
     const int rows = is_few ? few : kManyRows;
     for (int b = 0; b < B;) {
@@ -166,4 +185,35 @@ extern "C" pace_status_t pace_kv_attention(const pace_kv_cache* cache, const voi
     }
   }
   return PACE_OK;
+}
+
+}  // namespace
+}  // namespace pace
+
+using namespace pace;
+
+extern "C" size_t pace_kv_attention_workspace_size(const pace_kv_cache* cache, const int32_t* cu_q, int B, int n_q_heads,
+                                                   int max_len) {
+  return workspace_size(cache, cu_q, B, n_q_heads, max_len, false);
+}
+
+extern "C" size_t pace_kv_tree_attention_workspace_size(const pace_kv_cache* cache, const int32_t* cu_q, int B, int n_q_heads,
+                                                        int max_len) {
+  return workspace_size(cache, cu_q, B, n_q_heads, max_len, true);
+}
+
+extern "C" pace_status_t pace_kv_attention(const pace_kv_cache* cache, const void* Q, int64_t q_row_stride, const int32_t* cu_q,
+                                           int B, int n_q_heads, const int32_t* seq_lens, const int32_t* block_table,
+                                           int64_t table_stride, int max_len, float scale, int window, int sinks, void* out,
+                                           float* lse, void* ws, size_t ws_bytes, pace_stream_t stream) {
+  return attend(cache, Q, q_row_stride, cu_q, B, n_q_heads, nullptr, false, seq_lens, block_table, table_stride, max_len, scale, window, sinks, out,
+                lse, ws, ws_bytes, stream);
+}
+
+extern "C" pace_status_t pace_kv_tree_attention(const pace_kv_cache* cache, const void* Q, int64_t q_row_stride, const int32_t* cu_q,
+                                                int B, int n_q_heads, const int32_t* parents, const int32_t* seq_lens,
+                                                const int32_t* block_table, int64_t table_stride, int max_len, float scale, int window,
+                                                int sinks, void* out, float* lse, void* ws, size_t ws_bytes, pace_stream_t stream) {
+  return attend(cache, Q, q_row_stride, cu_q, B, n_q_heads, parents, true, seq_lens, block_table, table_stride, max_len, scale, window, sinks, out,
+                lse, ws, ws_bytes, stream);
 }

@@ -10,6 +10,9 @@
 // (slot 2 c: it begins inside, 2 c + 1: it begins there and goes on elsewhere), which kv_attn_combine weighs
 // together.  The log-sum-exp stays in two terms, a score and the logarithm of a sum relative to it: of large scores 32 bits
 // would not hold the sum of both (at 2^20 to an eighth).
+//
+// The kernels have a second form, TREE, for queries that are nodes of a tree of drafted tokens: a node sees the slots before the tree
+// (as far as the window around its position, base + its depth, lets it) and of the tree's those whose bits kv_tree.cu has set for it.
 #pragma once
 #include <cuda.h>
 
@@ -53,6 +56,10 @@ struct KvAttnArgs {
   int q_heads, group, window, sinks, max_len;
   FastDiv by_group;
   KvSeqs s;
+  // of a tree, else null:
+  const int32_t* depth;     // [queries] a node's ancestors
+  const uint32_t* family;   // [queries][words]: word k stands for slots 32 (base / 32 + k) .., rounded down
+  int words;
 };
 
 __device__ __forceinline__ bool kv_sees(int j, int p, int window, int sinks) {
@@ -82,18 +89,20 @@ struct KvItem {
   int i, row_tile, head, t0, t1;
   int row0, rows;           // its query rows
   int p0;                   // slot of the sequence's query 0
-  int p_first, p_last;      // slots of the tile's first and last query
+  int p_first, p_last;      // slots of the tile's first and last query (of a tree: of its node 0, a position that none is before, and of the last)
+  int p_all;                // the last slot that all rows see, as far as the window lets them
   KvSpan span;
 };
 
-template <int ROWS>
+template <int ROWS, bool TREE>
 __device__ __forceinline__ void kv_item_rows(const KvAttnArgs& a, int i, int row_tile, KvItem& it) {
   it.i = i;
   it.row_tile = row_tile;
   it.p0 = min(max(a.lens[a.s.seq[i]], 0), a.max_len) - a.s.nq[i];
   it.row0 = row_tile * ROWS;
   it.rows = min(a.s.nq[i] * a.group - it.row0, ROWS);
-  it.p_first = it.p0 + static_cast<int>(a.by_group(it.row0));
+  it.p_first = TREE ? it.p0 : it.p0 + static_cast<int>(a.by_group(it.row0));
+  it.p_all = TREE ? it.p0 - 1 : it.p_first;
   it.p_last = it.p0 + static_cast<int>(a.by_group(it.row0 + it.rows - 1));
   it.span = kv_span(it.p_first, it.p_last, a.window, a.sinks);
 }
@@ -109,6 +118,16 @@ __device__ __forceinline__ const uint16_t* kv_query(const KvAttnArgs& a, const K
   return a.Q + (a.s.q0[it.i] + token) * a.q_stride + static_cast<int64_t>(it.head * a.group + row - token * a.group) * D;
 }
 
+// Bits of a number of columns up to m (0 .. m - 1) out of 32.
+__device__ __forceinline__ uint32_t below(int m) { return m >= 32 ? 0xFFFFFFFFu : m <= 0 ? 0u : (1u << m) - 1u; }
+
+// Of slots at .. at + 31 (at >= 0, a multiple of 32) those that a node sees: `node` its query, p its position.
+__device__ __forceinline__ uint32_t kv_tree_sees(const KvAttnArgs& a, int base, int64_t node, int p, int at) {
+  const uint32_t near = a.window > 0 ? ~below(p - a.window + 1 - at) | below(a.sinks - at) : 0xFFFFFFFFu;
+  const int k = (at >> 5) - (base >> 5);
+  return (below(base - at) & near) | (k >= 0 && k < a.words ? a.family[node * a.words + k] : 0u);
+}
+
 // Where a CTA's share lies; the same for all its threads.  CTA c of a line of total = each * ctas + more tiles begins at
 // c * each + min(c, more).  (The call keeps a launch below 2^31 tiles.)
 struct KvShare {
@@ -120,7 +139,7 @@ struct KvShare {
 };
 
 // Walks a share (item) by item.
-template <int ROWS>
+template <int ROWS, bool TREE>
 struct KvWalk {
   KvShare s;
   KvItem it;
@@ -134,7 +153,7 @@ struct KvWalk {
 #pragma unroll 1
     while (true) {
       if (!have) {
-        kv_item_rows<ROWS>(a, s.i, s.row_tile, it);
+        kv_item_rows<ROWS, TREE>(a, s.i, s.row_tile, it);
         have = true;
       }
       const uint32_t off = s.pos - s.base, n = it.span.n > 0 ? it.span.n + s.cost : 0;
@@ -160,7 +179,7 @@ struct KvWalk {
 
 // Every thread of the block (whole warps, at most 32) calls this once; `buf` holds two ints per warp.  Row tiles that see
 // nothing get their zeros here.
-template <int ROWS, int D>
+template <int ROWS, int D, bool TREE>
 __device__ __forceinline__ KvShare kv_share(const KvAttnArgs& a, int* buf, KvShare* found, int* status) {
   const int threads = blockDim.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int tiles = a.s.tile0[a.s.nb], per = (tiles + threads - 1) / threads;
@@ -221,7 +240,7 @@ __device__ __forceinline__ KvShare kv_share(const KvAttnArgs& a, int* buf, KvSha
 #pragma unroll 1
       while (t >= a.s.tile0[i + 1]) ++i;
       KvItem it;
-      kv_item_rows<ROWS>(a, i, t - a.s.tile0[i], it);
+      kv_item_rows<ROWS, TREE>(a, i, t - a.s.tile0[i], it);
       const int n = it.span.n > 0 ? (it.span.n + s.cost) * a.c.heads : 0;
       if (round == 1) {
         if (s.pos < before + n) {
@@ -323,8 +342,8 @@ struct KvRings {
 
 // Warp 0 of a CTA: fetches the slot tiles of its share, K and V in boxes of a page, at most 128 rows, each by TMA; the tile's 8 K
 // and 8 V scales by 4-byte copies.
-template <int D, int ST, int SV, int ROWS>
-__device__ __forceinline__ void kv_fetch(const KvMaps& maps, const KvAttnArgs& a, KvWalk<ROWS>& walk, const KvRings& ring, int* abort,
+template <int D, int ST, int SV, typename Walk>
+__device__ __forceinline__ void kv_fetch(const KvMaps& maps, const KvAttnArgs& a, Walk& walk, const KvRings& ring, int* abort,
                                          int* status) {
   using namespace ptx;
   const int lane = threadIdx.x & 31;
@@ -387,9 +406,20 @@ __device__ __forceinline__ void kv_fetch(const KvMaps& maps, const KvAttnArgs& a
   }
 }
 
-// Launches of the two forms (rows of a tile: 8, 16 or 32, and kManyRows); `grid` CTAs, then the combine kernel.
+// Launches of the two forms (rows of a tile: 8, 16 or 32, and kManyRows; nodes of trees where a.family is set); `grid` CTAs, then the
+// combine kernel.
 pace_status_t launch_kv_decode(const KvMaps& maps, const KvAttnArgs& a, int D, int rows, unsigned grid, int* status, cudaStream_t stream);
 pace_status_t launch_kv_prefill(const KvMaps& maps, const KvAttnArgs& a, int D, unsigned grid, int* status, cudaStream_t stream);
 pace_status_t launch_kv_combine(const KvAttnArgs& a, int D, int rows, unsigned grid, cudaStream_t stream);
+
+// Depths and family bits of the nodes of trees (host prefix cu_q), as KvAttnArgs has them.
+struct KvTree {
+  const int32_t* parents;
+  int32_t* depth;
+  uint32_t* family;
+  int words;
+};
+pace_status_t launch_kv_tree(const KvTree& t, const int32_t* cu_q, int B, const int32_t* lens, int max_len, int window, int sinks, int* status,
+                             cudaStream_t stream);
 
 }  // namespace pace

@@ -85,7 +85,7 @@ __device__ __forceinline__ float warp_max(float x) {
   return r;
 }
 
-template <int D, int NQ>
+template <int D, int NQ, bool TREE>
 __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_constant__ KvMaps maps, const __grid_constant__ KvAttnArgs a,
                                                                 int* status) {
   using C = DecodeCfg<D, NQ>;
@@ -105,7 +105,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
   const uint32_t q_full = smem_u32(&ctl->q_full);
 
   begin_call();
-  const KvShare share = kv_share<NQ, D>(a, ctl->scan, &ctl->share, status);
+  const KvShare share = kv_share<NQ, D, TREE>(a, ctl->scan, &ctl->share, status);
   if (static_cast<int>(blockIdx.x) >= share.ctas) {
     if (threadIdx.x == 0) a.split[blockIdx.x] = KvSplit{0, 0, 0, 0};
     return;
@@ -134,7 +134,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
   __syncthreads();
   tc_fence_after_sync();
   const uint32_t tmem = ctl->tmem;
-  KvWalk<NQ> walk;
+  KvWalk<NQ, TREE> walk;
   walk.begin(share);
 
   if (warp == 0) {
@@ -260,6 +260,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
       __syncwarp();
       if (lane == 0) mbar_arrive(q_full);
       named_barrier_sync(3, 256);
+      int64_t node = -1;      // of a tree: row `lane`'s query, and its position
+      int place = 0;
+      if (TREE && lane < it.rows) {
+        node = a.s.q0[it.i] + static_cast<int>(a.by_group(it.row0 + lane));
+        place = it.p0 + a.depth[node];
+      }
       float l[NQ];
 #pragma unroll
       for (int q = 0; q < NQ; ++q) l[q] = 0.f;
@@ -276,7 +282,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
         }
         tc_fence_after_sync();
         // every row sees the whole tile?
-        const bool whole = slot0 + kKvTile - 1 <= it.p_first &&
+        const bool whole = slot0 + kKvTile - 1 <= it.p_all &&
                            (a.window <= 0 || slot0 > it.p_last - a.window || slot0 + kKvTile <= a.sinks);
         float ks = ctl->scales[s][me >> 4], vs = ctl->scales[s][8 + (me >> 4)];
         float x[NQ];
@@ -284,9 +290,16 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
           uint32_t sv[C::COLS];
           load_cols(lanes + p * C::COLS, sv);
           bool any = whole;
+          uint32_t by = 0;      // rows of a tree that see the slot
+          auto sees = [&](int q) { return TREE ? (by >> q & 1) != 0 : kv_sees(slot, ctl->slot_of[q], a.window, a.sinks); };
           if (!whole) {
+            if constexpr (TREE) {      // (a lane looks up the warp's 32 slots for one row)
+              const uint32_t word = node >= 0 ? kv_tree_sees(a, it.p0, node, place, slot0 + quad * 32) : 0u;
 #pragma unroll
-            for (int q = 0; q < NQ; ++q) any = any || kv_sees(slot, ctl->slot_of[q], a.window, a.sinks);
+              for (int q = 0; q < NQ; ++q) by |= (__shfl_sync(0xffffffffu, word, q) >> lane & 1) << q;
+            }
+#pragma unroll
+            for (int q = 0; q < NQ; ++q) any = any || sees(q);
             if (!any) ks = vs = 0.f;     // (what is there may be NaN)
             // 0 * NaN is NaN: a slot of V that some row does not see must not hold one.  Slots that nobody sees are
             // cleared; where rows differ, a slot with a NaN code is cleared and those that see it get a NaN weight.
@@ -311,7 +324,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
 #pragma unroll
           for (int q = 0; q < NQ; ++q) {
             x[q] = fmaf(__uint_as_float(sv[NQ + q]), 0.0625f, __uint_as_float(sv[q])) * (ks * ctl->qc[q]);
-            if (!whole && !kv_sees(slot, ctl->slot_of[q], a.window, a.sinks)) x[q] = -INFINITY;
+            if (!whole && !sees(q)) x[q] = -INFINITY;
           }
         }
         const float lv = static_cast<float>(static_cast<int>(__float_as_uint(vs) >> 23) - 127);   // log2(vs), far down for 0
@@ -618,7 +631,7 @@ __global__ void __launch_bounds__(256) kv_attn_combine(const __grid_constant__ K
   }
 }
 
-template <int D, int NQ>
+template <int D, int NQ, bool TREE>
 pace_status_t run_decode(const KvMaps& maps, const KvAttnArgs& a, unsigned grid, int* status, cudaStream_t stream) {
   using C = DecodeCfg<D, NQ>;
   constexpr size_t smem = 1024 + C::STAGES * 2 * C::TILE + C::QBYTES + 4 * C::PBYTES + sizeof(DecodeCtl<D, NQ>);
@@ -627,20 +640,28 @@ pace_status_t run_decode(const KvMaps& maps, const KvAttnArgs& a, unsigned grid,
   int dev = 0;
   PACE_CUDA(cudaGetDevice(&dev));
   if (!once.done(dev)) {
-    PACE_CUDA(cudaFuncSetAttribute(kv_decode_kernel<D, NQ>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
+    PACE_CUDA(cudaFuncSetAttribute(kv_decode_kernel<D, NQ, TREE>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
     once.mark(dev);
   }
-  return launch_dependent(kv_decode_kernel<D, NQ>, grid, kThreads, smem, 1, stream, maps, a, status);
+  return launch_dependent(kv_decode_kernel<D, NQ, TREE>, grid, kThreads, smem, 1, stream, maps, a, status);
+}
+
+}  // namespace
+
+namespace {
+
+template <int D, bool TREE>
+pace_status_t run_rows(const KvMaps& maps, const KvAttnArgs& a, int rows, unsigned grid, int* status, cudaStream_t stream) {
+  return rows == 8 ? run_decode<D, 8, TREE>(maps, a, grid, status, stream) : rows == 16 ? run_decode<D, 16, TREE>(maps, a, grid, status, stream)
+                                                                                    : run_decode<D, 32, TREE>(maps, a, grid, status, stream);
 }
 
 }  // namespace
 
 pace_status_t launch_kv_decode(const KvMaps& maps, const KvAttnArgs& a, int D, int rows, unsigned grid, int* status, cudaStream_t stream) {
-  if (D == 128)
-    return rows == 8 ? run_decode<128, 8>(maps, a, grid, status, stream) : rows == 16 ? run_decode<128, 16>(maps, a, grid, status, stream)
-                                                                                   : run_decode<128, 32>(maps, a, grid, status, stream);
-  return rows == 8 ? run_decode<64, 8>(maps, a, grid, status, stream) : rows == 16 ? run_decode<64, 16>(maps, a, grid, status, stream)
-                                                                                 : run_decode<64, 32>(maps, a, grid, status, stream);
+  if (a.family != nullptr)
+    return D == 128 ? run_rows<128, true>(maps, a, rows, grid, status, stream) : run_rows<64, true>(maps, a, rows, grid, status, stream);
+  return D == 128 ? run_rows<128, false>(maps, a, rows, grid, status, stream) : run_rows<64, false>(maps, a, rows, grid, status, stream);
 }
 
 pace_status_t launch_kv_combine(const KvAttnArgs& a, int D, int rows, unsigned grid, cudaStream_t stream) {

@@ -73,9 +73,9 @@ struct alignas(16) PrefillCtl {
   int abort;
 };
 
-// A tile that rows at slots p_first .. p_last all see whole.
-__device__ __forceinline__ bool kv_whole(int slot0, int p_first, int p_last, int window, int sinks) {
-  return slot0 + kKvTile - 1 <= p_first && (window <= 0 || slot0 > p_last - window || slot0 + kKvTile <= sinks);
+// A tile that rows at slots up to p_last, which see every slot up to p_all but for the window, all see whole.
+__device__ __forceinline__ bool kv_whole(int slot0, int p_all, int p_last, int window, int sinks) {
+  return slot0 + kKvTile - 1 <= p_all && (window <= 0 || slot0 > p_last - window || slot0 + kKvTile <= sinks);
 }
 
 __device__ __forceinline__ uint32_t f16x2(float lo, float hi) {
@@ -107,7 +107,7 @@ __device__ __forceinline__ void split_8bit(uint32_t a, uint32_t b, uint32_t& hi,
   lo = rest(a, ca) | rest(b, cb) << 16;
 }
 
-template <int D>
+template <int D, bool TREE>
 __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_constant__ KvMaps maps, const __grid_constant__ KvAttnArgs a,
                                                                  int* status) {
   using C = PrefillCfg<D>;
@@ -131,7 +131,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
   auto o_done = [&](int i, int h) { return smem_u32(&ctl->o_done[i][h]); };
 
   begin_call();
-  const KvShare share = kv_share<kManyRows, D>(a, ctl->scan, &ctl->share, status);
+  const KvShare share = kv_share<kManyRows, D, TREE>(a, ctl->scan, &ctl->share, status);
   if (static_cast<int>(blockIdx.x) >= share.ctas) {
     if (threadIdx.x == 0) a.split[blockIdx.x] = KvSplit{0, 0, 0, 0};
     return;
@@ -168,14 +168,14 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
   const uint32_t tmem = ctl->tmem;
 
   if (warp == 0) {
-    KvWalk<kManyRows> walk;
+    KvWalk<kManyRows, TREE> walk;
     walk.begin(share);
     kv_fetch<D, ST, C::VSTAGES>(maps, a, walk, KvRings{sK, sC, C::TILE, ctl->full, ctl->empty, ctl->v_empty, ctl->scales}, &ctl->abort, status);
   } else if (warp == 1) {
     // ---- products: P V of a slot tile, half by half as the weights come, then S of the next; A and B in turn ----------
     // The warp stays converged: operands of these instructions are registers of the whole warp, and in one lane's branch each took 80
     // clocks.
-    KvWalk<kManyRows> walk;
+    KvWalk<kManyRows, TREE> walk;
     walk.begin(share);
     const KvItem& it = walk.it;
     const uint32_t issue = elect_one();
@@ -248,7 +248,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
     __syncwarp();
   } else if (warp < 4) {
     // ---- V of a slot tile as f16, and the tile's constants ---------------------------------------
-    KvWalk<kManyRows> walk;
+    KvWalk<kManyRows, TREE> walk;
     walk.begin(share);
     const KvItem& it = walk.it;
     int t = 0;
@@ -261,7 +261,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
         if (!ok) break;
         // 0 * NaN is NaN: no slot of V that some row does not see may hold one.  Slots that nobody sees become zero; where rows
         // differ, so does a slot with a NaN, and rows that see it take a NaN weight for it.
-        const bool whole = kv_whole(slot0, it.p_first, it.p_last, a.window, a.sinks);
+        const bool whole = kv_whole(slot0, it.p_all, it.p_last, a.window, a.sinks);
         auto usable = [](float x) { return x >= 0x1p-120f && x <= 0x1p124f; };      // (1 / x and log2 x are finite)
         if (warp == 2 && lane < 8) {      // (where the slots are not there, or rows differ, no scale may be NaN either)
           float ks = ctl->scales[s][lane], vs = ctl->scales[s][8 + lane];
@@ -322,7 +322,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
     // ---- weights: a thread owns a row -------------------------------------------------------------
     const int i = (warp - 4) >> 2, quad = warp & 3, me = quad * 32 + lane;
     const uint32_t sS = tmem + (static_cast<uint32_t>(quad * 32) << 16) + i * 128, sO = sS + 256;
-    KvWalk<kManyRows> walk;
+    KvWalk<kManyRows, TREE> walk;
     walk.begin(share);
     const KvItem& it = walk.it;
     int t = 0, mine = 0;      // slot tiles of the CTA, of this row tile
@@ -335,7 +335,13 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
       const int row = i * 128 + me;
       const bool real = row < it.rows;
       auto slot_of = [&](int r) { return it.p0 + static_cast<int>(a.by_group(it.row0 + min(r, it.rows - 1))); };
-      const int p = slot_of(row), p_lo = slot_of(i * 128), p_hi = slot_of(i * 128 + 127);      // of the row, of the tile's first and last
+      int p = slot_of(row);      // of the row (of a tree's node: its position)
+      const int p_lo = TREE ? it.p_all : slot_of(i * 128), p_hi = slot_of(i * 128 + 127);      // of the tile's first and last
+      int64_t node = 0;
+      if constexpr (TREE) {
+        node = a.s.q0[it.i] + p - it.p0;
+        p = it.p0 + a.depth[node];
+      }
       constexpr int LANES = D / 8, STEP = 32 / LANES;      // lanes that move a row, rows at a time
       const int sub = lane / LANES, part = lane % LANES;
       uint8_t* tile = sQ + i * 2 * C::QTILE + quad * 32 * D;
@@ -411,11 +417,11 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
         if (!whole) {      // what the row does not see becomes -inf
           // (it sees slots up to p that are past `from` or before `few`)
           const int from = a.window > 0 ? p - a.window : -1, few = a.window > 0 ? a.sinks : INT32_MAX;
-          auto below = [](int m) { return m >= 32 ? 0xFFFFFFFFu : m <= 0 ? 0u : (1u << m) - 1u; };      // columns 0 .. m - 1
 #pragma unroll 1
           for (int q = 0; q < 2; ++q) {
             const int at = slot0 + kHalf * h + 32 * q;
-            const uint32_t see = below(p + 1 - at) & (~below(from + 1 - at) | below(few - at)), nan = ctl->nan[b][2 * h + q] & see;
+            const uint32_t see = TREE ? kv_tree_sees(a, it.p0, node, p, at) : below(p + 1 - at) & (~below(from + 1 - at) | below(few - at));
+            const uint32_t nan = ctl->nan[b][2 * h + q] & see;
             if (__all_sync(0xffffffffu, (see & ~nan) == 0xFFFFFFFFu)) continue;
             uint32_t x[32];
             load_cols(sX + 32 * q, x);
@@ -624,7 +630,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
   if (warp == 1) tmem_dealloc(tmem, kTmem);
 }
 
-template <int D>
+template <int D, bool TREE>
 pace_status_t run_prefill(const KvMaps& maps, const KvAttnArgs& a, unsigned grid, int* status, cudaStream_t stream) {
   using C = PrefillCfg<D>;
   constexpr size_t smem = 1024 + (C::STAGES + C::VSTAGES) * C::TILE + 2 * C::VTILE + 4 * C::QTILE + sizeof(PrefillCtl<D>);
@@ -633,16 +639,17 @@ pace_status_t run_prefill(const KvMaps& maps, const KvAttnArgs& a, unsigned grid
   int dev = 0;
   PACE_CUDA(cudaGetDevice(&dev));
   if (!once.done(dev)) {
-    PACE_CUDA(cudaFuncSetAttribute(kv_prefill_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
+    PACE_CUDA(cudaFuncSetAttribute(kv_prefill_kernel<D, TREE>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
     once.mark(dev);
   }
-  return launch_dependent(kv_prefill_kernel<D>, grid, kThreads, smem, 1, stream, maps, a, status);
+  return launch_dependent(kv_prefill_kernel<D, TREE>, grid, kThreads, smem, 1, stream, maps, a, status);
 }
 
 }  // namespace
 
 pace_status_t launch_kv_prefill(const KvMaps& maps, const KvAttnArgs& a, int D, unsigned grid, int* status, cudaStream_t stream) {
-  return D == 128 ? run_prefill<128>(maps, a, grid, status, stream) : run_prefill<64>(maps, a, grid, status, stream);
+  if (a.family != nullptr) return D == 128 ? run_prefill<128, true>(maps, a, grid, status, stream) : run_prefill<64, true>(maps, a, grid, status, stream);
+  return D == 128 ? run_prefill<128, false>(maps, a, grid, status, stream) : run_prefill<64, false>(maps, a, grid, status, stream);
 }
 
 }  // namespace pace

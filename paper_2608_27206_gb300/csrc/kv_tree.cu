@@ -1,0 +1,183 @@
+// Serve: trees of drafted tokens: who sees whom, and the walk along the tokens that are accepted.
+//
+// kv_tree_kernel: of every node its depth and, as bits over the tree's slots, which of them it sees: its ancestors and itself, as far
+// as the window around its position lets it.  The attention kernels read a word of bits where they would compare slots.  A thread goes
+// up from a node twice, for its depth and for its bits; parents lie in shared memory.  All latency: a tree of 26 nodes takes 3 us, most of
+// it the launch.
+//
+// draft_accept_kernel: a warp walks a tree.  A child comes after its parent, so one pass over the nodes in order finds the path: of each
+// 32 nodes, those that agree with what was picked after their parent are known at once, and a ballot finds the first child of the node
+// that the walk has come to.
+#include <algorithm>
+
+#include "kv_attn.cuh"
+
+namespace pace {
+namespace {
+
+struct TreeArgs {
+  KvTree t;
+  const int32_t* lens;
+  int max_len, window, sinks;
+  int b0;                      // the launch's first sequence
+  int cu[kKvMaxB + 1];
+};
+
+constexpr int kTreeThreads = 256;
+
+__global__ void __launch_bounds__(kTreeThreads) kv_tree_kernel(const __grid_constant__ TreeArgs a, int* status) {
+  __shared__ int16_t up[PACE_TREE_MAX];
+  ptx::begin_call();
+  const int b = blockIdx.x, at = a.cu[b], n = a.cu[b + 1] - at;
+  const int base = min(max(a.lens[a.b0 + b], 0), a.max_len) - n;
+  for (int t = threadIdx.x; t < n; t += kTreeThreads) {
+    int p = a.t.parents[at + t];
+    if (p < -1 || p >= t) {
+      record_error(status, PACE_ERR_INVALID_ARG, K_KV_TREE);
+      p = -1;
+    }
+    up[t] = static_cast<int16_t>(p);
+  }
+  __syncthreads();
+  for (int t = threadIdx.x; t < n; t += kTreeThreads) {
+    int depth = 0;
+    for (int p = up[t]; p >= 0; p = up[p]) ++depth;
+    a.t.depth[at + t] = depth;
+    // ancestors come in falling order, and so do the words of their slots
+    uint32_t* row = a.t.family + static_cast<int64_t>(at + t) * a.t.words;
+    int k = a.t.words - 1, place = base + depth;
+    uint32_t bits = 0;
+    for (int p = t, far = 0; p >= 0; p = up[p], ++far, --place) {
+      if (base + p < 0 || (a.window > 0 && far >= a.window && place >= a.sinks)) continue;
+      const int word = ((base + p) >> 5) - (base >> 5);
+      for (; k > word; --k) {
+        row[k] = bits;
+        bits = 0;
+      }
+      bits |= 1u << ((base + p) & 31);
+    }
+    for (; k >= 0; --k) {
+      row[k] = bits;
+      bits = 0;
+    }
+  }
+}
+
+constexpr int kAcceptMaxB = 1024;     // sequences of one launch
+constexpr int kAcceptWarps = 4;
+
+struct AcceptArgs {
+  const int32_t* tokens;
+  const int32_t* parents;
+  const int32_t* picked;
+  int32_t* rows;
+  int32_t* counts;
+  int32_t* next;
+  int b0, nb;
+  int cu[kAcceptMaxB + 1];
+};
+
+__global__ void __launch_bounds__(32 * kAcceptWarps) draft_accept_kernel(const __grid_constant__ AcceptArgs a, int* status) {
+  ptx::begin_call();
+  const int b = blockIdx.x * kAcceptWarps + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  if (b >= a.nb) return;
+  const int at = a.cu[b], n = a.cu[b + 1] - at;
+  int now = 0, count = 0;        // the node that the walk has come to; how many have been accepted
+  if (n > 0) {
+    if (lane == 0) a.rows[at] = at;
+    count = 1;
+  }
+  constexpr int U = 4;           // 32 nodes each, loaded together
+#pragma unroll 1
+  for (int t0 = 0; t0 < n; t0 += 32 * U) {
+    int parent[U];
+    bool agrees[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int t = t0 + 32 * u + lane;
+      parent[u] = t < n ? a.parents[at + t] : -1;
+      if (parent[u] < -1 || parent[u] >= t) {
+        record_error(status, PACE_ERR_INVALID_ARG, K_DRAFT_ACCEPT);
+        parent[u] = -1;
+      }
+      agrees[u] = t < n && parent[u] >= 0 && a.tokens[at + t] == a.picked[at + parent[u]];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      uint32_t child;
+      while ((child = __ballot_sync(0xffffffffu, agrees[u] && parent[u] == now)) != 0) {
+        now = t0 + 32 * u + __ffs(child) - 1;
+        if (lane == 0) a.rows[at + count] = at + now;
+        ++count;
+      }
+    }
+  }
+  for (int i = count + lane; i < n; i += 32) a.rows[at + i] = -1;
+  if (lane == 0) {
+    a.counts[a.b0 + b] = count;
+    a.next[a.b0 + b] = n > 0 ? a.picked[at + now] : -1;
+  }
+}
+
+// Whether [p, p + np) and [q, q + nq), in int32, have a part in common.
+bool overlap(const int32_t* p, int64_t np, const int32_t* q, int64_t nq) {
+  const auto a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+  return np > 0 && nq > 0 && a < b + 4 * static_cast<uintptr_t>(nq) && b < a + 4 * static_cast<uintptr_t>(np);
+}
+
+}  // namespace
+
+pace_status_t launch_kv_tree(const KvTree& t, const int32_t* cu_q, int B, const int32_t* lens, int max_len, int window, int sinks, int* status,
+                             cudaStream_t stream) {
+  TreeArgs a{};
+  a.t = t;
+  a.lens = lens;
+  a.max_len = max_len;
+  a.window = window;
+  a.sinks = sinks;
+  for (int b0 = 0; b0 < B; b0 += kKvMaxB) {
+    const int nb = std::min(kKvMaxB, B - b0);
+    a.b0 = b0;
+    for (int i = 0; i <= nb; ++i) a.cu[i] = cu_q[b0 + i];
+    if (a.cu[nb] == a.cu[0]) continue;
+    PACE_CHECK(launch_dependent(kv_tree_kernel, static_cast<unsigned>(nb), kTreeThreads, 0, 1, stream, a, status));
+  }
+  return PACE_OK;
+}
+
+}  // namespace pace
+
+using namespace pace;
+
+extern "C" pace_status_t pace_draft_accept(const int32_t* tokens, const int32_t* parents, const int32_t* picked, const int32_t* cu_nodes, int B,
+                                           int32_t* rows, int32_t* counts, int32_t* next_tokens, pace_stream_t stream) {
+  if (B < 0) return PACE_ERR_INVALID_ARG;
+  if (B == 0) return PACE_OK;
+  PACE_CHECK(check_prefix(cu_nodes, B));
+  const int64_t n = cu_nodes[B];
+  if (n > 0 && (tokens == nullptr || parents == nullptr || picked == nullptr || rows == nullptr)) return PACE_ERR_INVALID_ARG;
+  if (counts == nullptr || next_tokens == nullptr) return PACE_ERR_INVALID_ARG;
+  for (const int32_t* p : {tokens, parents, picked, static_cast<const int32_t*>(rows), static_cast<const int32_t*>(counts),
+                           static_cast<const int32_t*>(next_tokens)})
+    if (reinterpret_cast<uintptr_t>(p) % 4 != 0) return PACE_ERR_INVALID_ARG;
+  for (const int32_t* p : {tokens, parents, picked})
+    if (overlap(rows, n, p, n) || overlap(counts, B, p, n) || overlap(next_tokens, B, p, n)) return PACE_ERR_INVALID_ARG;
+  if (overlap(rows, n, counts, B) || overlap(rows, n, next_tokens, B) || overlap(counts, B, next_tokens, B)) return PACE_ERR_INVALID_ARG;
+  PACE_CHECK(check_device());
+  int* status = device_status_word();
+  AcceptArgs a{};
+  a.tokens = tokens;
+  a.parents = parents;
+  a.picked = picked;
+  a.rows = rows;
+  a.counts = counts;
+  a.next = next_tokens;
+  for (int b0 = 0; b0 < B; b0 += kAcceptMaxB) {
+    a.b0 = b0;
+    a.nb = std::min(kAcceptMaxB, B - b0);
+    for (int i = 0; i <= a.nb; ++i) a.cu[i] = cu_nodes[b0 + i];
+    PACE_CHECK(launch_dependent(draft_accept_kernel, static_cast<unsigned>((a.nb + kAcceptWarps - 1) / kAcceptWarps), 32 * kAcceptWarps, 0, 1,
+                                stream, a, status));
+  }
+  return PACE_OK;
+}

@@ -27,6 +27,9 @@ enum KernelId : int {
   K_GATHER_MULTI = 13,
   K_KV_APPEND = 14,
   K_KV_ATTN = 15,
+  K_KV_TREE = 16,
+  K_DRAFT_ACCEPT = 17,
+  K_KV_COMPACT = 18,
 };
 
 // Device status word layout: [0] = code (pace_status_t), [1] = kernel id.

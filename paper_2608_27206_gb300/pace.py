@@ -123,6 +123,13 @@ _SIGS = {
     "pace_kv_attention": (ctypes.c_int, [_P, _P, ctypes.c_int64, _P, ctypes.c_int, ctypes.c_int, _P, _P, ctypes.c_int64,
                                          ctypes.c_int, ctypes.c_float, ctypes.c_int, ctypes.c_int, _P, _P, _P,
                                          ctypes.c_size_t, _P]),
+    "pace_kv_tree_attention_workspace_size": (ctypes.c_size_t, [_P, _P, ctypes.c_int, ctypes.c_int, ctypes.c_int]),
+    "pace_kv_tree_attention": (ctypes.c_int, [_P, _P, ctypes.c_int64, _P, ctypes.c_int, ctypes.c_int, _P, _P, _P, ctypes.c_int64,
+                                              ctypes.c_int, ctypes.c_float, ctypes.c_int, ctypes.c_int, _P, _P, _P,
+                                              ctypes.c_size_t, _P]),
+    "pace_draft_accept": (ctypes.c_int, [_P, _P, _P, _P, ctypes.c_int, _P, _P, _P, _P]),
+    "pace_kv_compact": (ctypes.c_int, [_P, ctypes.c_int, _P, ctypes.c_int, _P, _P, ctypes.c_int64, _P, _P, _P, _P, ctypes.c_int64, _P,
+                                       _P]),
 }
 
 _lib = None
@@ -767,14 +774,8 @@ def pace_kv_attention_workspace_size(cache: KvCache, cu_q, n_q_heads: int, max_l
     return int(lib().pace_kv_attention_workspace_size(cache._address, cp, n - 1, int(n_q_heads), int(max_len)))
 
 
-def pace_kv_attention(cache: KvCache, Q: torch.Tensor, cu_q, seq_lens: torch.Tensor, block_table: torch.Tensor, max_len: int,
-                      scale: Optional[float] = None, window: int = 0, sinks: int = 0, out: Optional[torch.Tensor] = None,
-                      lse: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
-    """Causal attention of Q (bf16 [new tokens, heads, D]) over the cache: bf16 [new tokens, heads, D].
-
-    The queries are the last of their sequences' seq_lens (device int32, none above max_len) slots; with
-    window > 0 one sees the last `window` slots up to its own and the first `sinks`.  lse (float32 [new
-    tokens, heads]) receives the log-sum-exp of the scores."""
+def _attend(fn: str, cache: KvCache, Q, cu_q, parents, seq_lens, block_table, max_len, scale, window, sinks, out, lse, ws, stream):
+    """pace_kv_attention, or (parents: a tuple of one tensor) pace_kv_tree_attention."""
     cu, cp, B = _i32(cu_q)
     B -= 1
     n, D = int(cu[-1]), cache.head_dim
@@ -792,9 +793,97 @@ def pace_kv_attention(cache: KvCache, Q: torch.Tensor, cu_q, seq_lens: torch.Ten
         raise ValueError("lse: expected float32 [new tokens, heads]")
     tp, ts = _table(block_table, B)
     L = lib()
-    buf, nbytes = _workspace(L.pace_kv_attention_workspace_size, (cache._address, cp, B, hq, int(max_len)), ws, Q.device, stream)
-    _check_ws("pace_kv_attention",
-              L.pace_kv_attention(cache._address, qp, qs, cp, B, hq, _int32(seq_lens, B, "seq_lens"), tp, ts, int(max_len),
-                                  float(scale), int(window), int(sinks), _dev(out), _dev(lse), _dev(buf), nbytes,
-                                  _stream(stream)), ws)
+    buf, nbytes = _workspace(getattr(L, fn + "_workspace_size"), (cache._address, cp, B, hq, int(max_len)), ws, Q.device, stream)
+    tree = [_int32(p, n, "parents") for p in parents]
+    _check_ws(fn, getattr(L, fn)(cache._address, qp, qs, cp, B, hq, *tree, _int32(seq_lens, B, "seq_lens"), tp, ts, int(max_len),
+                                 float(scale), int(window), int(sinks), _dev(out), _dev(lse), _dev(buf), nbytes, _stream(stream)), ws)
     return out
+
+
+def pace_kv_attention(cache: KvCache, Q: torch.Tensor, cu_q, seq_lens: torch.Tensor, block_table: torch.Tensor, max_len: int,
+                      scale: Optional[float] = None, window: int = 0, sinks: int = 0, out: Optional[torch.Tensor] = None,
+                      lse: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Causal attention of Q (bf16 [new tokens, heads, D]) over the cache: bf16 [new tokens, heads, D].
+
+    The queries are the last of their sequences' seq_lens (device int32, none above max_len) slots; with
+    window > 0 one sees the last `window` slots up to its own and the first `sinks`.  lse (float32 [new
+    tokens, heads]) receives the log-sum-exp of the scores."""
+    return _attend("pace_kv_attention", cache, Q, cu_q, (), seq_lens, block_table, max_len, scale, window, sinks, out, lse, ws, stream)
+
+
+# ---- drafted tokens --------------------------------------------------------------------------
+TREE_MAX = 1024   # nodes of a tree
+
+
+def pace_kv_tree_attention_workspace_size(cache: KvCache, cu_q, n_q_heads: int, max_len: int) -> int:
+    _c, cp, n = _i32(cu_q)
+    return int(lib().pace_kv_tree_attention_workspace_size(cache._address, cp, n - 1, int(n_q_heads), int(max_len)))
+
+
+def pace_kv_tree_attention(cache: KvCache, Q: torch.Tensor, cu_q, parents: torch.Tensor, seq_lens: torch.Tensor,
+                           block_table: torch.Tensor, max_len: int, scale: Optional[float] = None, window: int = 0, sinks: int = 0,
+                           out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
+                           stream=None) -> torch.Tensor:
+    """pace_kv_attention from the nodes of trees: the queries are a sequence's newest slots, parents (device int32 [nodes]) the number
+    of each one's parent in its own tree, before it, or -1.  A node sees the slots before the tree, its ancestors and
+    itself; a window counts in positions, which are depths within the tree."""
+    return _attend("pace_kv_tree_attention", cache, Q, cu_q, (parents,), seq_lens, block_table, max_len, scale, window, sinks, out, lse,
+                   ws, stream)
+
+
+def _out_int32(t: Optional[torch.Tensor], n: int, what: str, device, stream) -> torch.Tensor:
+    if t is None:
+        return _used(torch.empty(n, dtype=torch.int32, device=device), stream)
+    _int32(t, n, what)
+    return t
+
+
+def pace_draft_accept(tokens: torch.Tensor, parents: torch.Tensor, picked: torch.Tensor, cu_nodes, rows: Optional[torch.Tensor] = None,
+                      counts: Optional[torch.Tensor] = None, next_tokens: Optional[torch.Tensor] = None, stream=None):
+    """The accepted path of each sequence's tree: from node 0 on the first child whose token (tokens, device int32 [nodes]) is the one
+    picked after its parent (picked, likewise).  Returns (rows [nodes], counts [sequences], next_tokens [sequences]): the accepted
+    nodes' rows of the batch from cu_nodes[b] on, -1 behind them; how many; the token picked after the last."""
+    cu, cp, B = _i32(cu_nodes)
+    B -= 1
+    n = int(cu[-1]) if B >= 0 else 0
+    dev = tokens.device
+    tp, pp, kp = _int32(tokens, n, "tokens"), _int32(parents, n, "parents"), _int32(picked, n, "picked")
+    rows = _out_int32(rows, n, "rows", dev, stream)
+    counts, next_tokens = _out_int32(counts, B, "counts", dev, stream), _out_int32(next_tokens, B, "next_tokens", dev, stream)
+    _check("pace_draft_accept", lib().pace_draft_accept(tp, pp, kp, cp, B, rows.data_ptr(), counts.data_ptr(), next_tokens.data_ptr(),
+                                                        _stream(stream)))
+    return rows, counts, next_tokens
+
+
+class KvLayers:
+    """Handle of the caches of several layers, alike but for their addresses, whose sequences share a block table."""
+
+    def __init__(self, caches: Sequence[KvCache]):
+        self.caches = list(caches)
+        if any(not isinstance(c, KvCache) for c in self.caches):
+            raise ValueError("expected caches")
+        self.views = (KvCacheView * max(len(self.caches), 1))(*[c.view for c in self.caches])
+        self._address = ctypes.addressof(self.views)
+
+
+def pace_kv_compact(cache, cu_new, seq_lens: torch.Tensor, block_table: torch.Tensor, cu_rows=None, rows: Optional[torch.Tensor] = None,
+                    counts: Optional[torch.Tensor] = None, dst_table: Optional[torch.Tensor] = None,
+                    new_lens: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Of each sequence's newest cu_new[b + 1] - cu_new[b] tokens keeps those in `rows` (device int32, rows of that packed batch, list b
+    from cu_rows[b] on; default cu_new, and all of them), the first counts[b] (device int32), and moves them together, in place or
+    to dst_table's pages.  cache: a KvCache, or KvLayers.  Returns the sequences' new lengths, device int32 [B]."""
+    layers = len(cache.caches) if isinstance(cache, KvLayers) else 1
+    _cu, cp, B = _i32(cu_new)
+    B -= 1
+    keep, kp, n_keep = (_cu, cp, B + 1) if cu_rows is None else _i32(cu_rows)
+    if n_keep != B + 1:
+        raise ValueError("cu_rows: expected as many sequences as cu_new has")
+    tp, ts = _table(block_table, B)
+    dp, ds = (None, 0) if dst_table is None else _table(dst_table, B)
+    lens = _int32(seq_lens, B, "seq_lens")
+    rp = None if rows is None else _int32(rows, int(keep[-1]), "rows")
+    np_ = None if counts is None else _int32(counts, B, "counts")
+    new_lens = _out_int32(new_lens, B, "new_lens", seq_lens.device, stream)
+    _check("pace_kv_compact", lib().pace_kv_compact(cache._address, layers, cp, B, lens, tp, ts, kp, rp, np_, dp, ds, new_lens.data_ptr(),
+                                                    _stream(stream)))
+    return new_lens
