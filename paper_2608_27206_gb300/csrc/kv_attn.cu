@@ -172,6 +172,7 @@ pace_status_t attend(const pace_kv_cache* cache, const void* Q, int64_t q_row_st
     a.depth = t.depth;
     a.family = t.family;
     a.words = t.words;
+    a.after_tree = 1;
   }
   for (const bool is_few : {true, false}) {
     const int rows = is_few ? few : kManyRows;
@@ -181,7 +182,8 @@ pace_status_t attend(const pace_kv_cache* cache, const void* Q, int64_t q_row_st
       const unsigned grid = static_cast<unsigned>(std::min<int64_t>({tiles * cache->n_kv_heads * slot_tiles(max_len), sms, kPlanCtas}));
       if (is_few) PACE_CHECK(launch_kv_decode(maps, a, D, rows, grid, status, stream));
       else PACE_CHECK(launch_kv_prefill(maps, a, D, grid, status, stream));
-      if (slot_tiles(max_len) > 1) PACE_CHECK(launch_kv_combine(a, D, rows, grid, stream));
+      a.after_tree = 0;
+      if (slot_tiles(max_len) > 1) PACE_CHECK(launch_kv_combine(a, D, rows, grid, tiles * cache->n_kv_heads, stream));
     }
   }
   return PACE_OK;

@@ -60,6 +60,7 @@ struct KvAttnArgs {
   const int32_t* depth;     // [queries] a node's ancestors
   const uint32_t* family;   // [queries][words]: word k stands for slots 32 (base / 32 + k) .., rounded down
   int words;
+  int after_tree;           // the launch follows kv_tree_kernel, and waits for it only where it reads depth and family
 };
 
 __device__ __forceinline__ bool kv_sees(int j, int p, int window, int sinks) {
@@ -288,6 +289,17 @@ struct KvMaps {
   CUtensorMap k, v;
 };
 
+// The start of a launch.  kv_tree_kernel, which needs some microseconds for what is read last, starts when all work before it is
+// complete: a launch that follows it need not wait for that again, and waits for it in the threads that read what it writes.
+template <bool TREE>
+__device__ __forceinline__ void kv_begin(const KvAttnArgs& a) {
+  if (!TREE || !a.after_tree) ptx::begin_call();
+}
+template <bool TREE>
+__device__ __forceinline__ void kv_tree_ready(const KvAttnArgs& a) {
+  if (TREE && a.after_tree) ptx::begin_call();
+}
+
 // mbar_wait with its limit counted in tries (2^18; the hardware holds one that has to wait for about 4 us, which makes a second): a
 // few instructions, where the kernels here wait in many places and instructions that are not run push those that are out of the
 // instruction cache.
@@ -410,7 +422,7 @@ __device__ __forceinline__ void kv_fetch(const KvMaps& maps, const KvAttnArgs& a
 // combine kernel.
 pace_status_t launch_kv_decode(const KvMaps& maps, const KvAttnArgs& a, int D, int rows, unsigned grid, int* status, cudaStream_t stream);
 pace_status_t launch_kv_prefill(const KvMaps& maps, const KvAttnArgs& a, int D, unsigned grid, int* status, cudaStream_t stream);
-pace_status_t launch_kv_combine(const KvAttnArgs& a, int D, int rows, unsigned grid, cudaStream_t stream);
+pace_status_t launch_kv_combine(const KvAttnArgs& a, int D, int rows, unsigned grid, int64_t items, cudaStream_t stream);
 
 // Depths and family bits of the nodes of trees (host prefix cu_q), as KvAttnArgs has them.
 struct KvTree {

@@ -104,9 +104,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
   auto pv_done = [&](int p) { return smem_u32(&ctl->pv_done[p]); };
   const uint32_t q_full = smem_u32(&ctl->q_full);
 
-  begin_call();
+  kv_begin<TREE>(a);
   const KvShare share = kv_share<NQ, D, TREE>(a, ctl->scan, &ctl->share, status);
   if (static_cast<int>(blockIdx.x) >= share.ctas) {
+    kv_tree_ready<TREE>(a);      // (a launch does not end before the one that it follows)
     if (threadIdx.x == 0) a.split[blockIdx.x] = KvSplit{0, 0, 0, 0};
     return;
   }
@@ -194,6 +195,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
     const int grp = warp >= 6, quad = warp & 3, me = quad * 32 + lane;    // TMEM lane: slot of the tile, then column of the output
     const uint32_t lanes = tmem + (static_cast<uint32_t>(quad * 32) << 16);
     Stat* stat = ctl->stat[grp];
+    kv_tree_ready<TREE>(a);
     int t = 0;
     while (walk.next(a)) {
       const KvItem& it = walk.it;
@@ -507,19 +509,15 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
 // takes is latency, so a warp's loads go out together, PARTS parts of ROWS rows at a time.  Where rows are few a row has 8 warps (a
 // sequence alone makes as many parts as there are tiles: 38 of them took 8 us with one warp); where they are many and a row has few
 // parts, a warp has 4 rows (2 us less in a call of 517 tokens than with one row).
+// Rows from `first` on of the item that CTA c began.
 template <int D, int ROWS, int PARTS, int SPLIT>
-__global__ void __launch_bounds__(256) kv_attn_combine(const __grid_constant__ KvAttnArgs a, int tile_rows) {
+__device__ __forceinline__ void join_rows(const KvAttnArgs& a, int tile_rows, int c, const KvSplit& sp, int first) {
   constexpr int E = D / 32;      // elements of a lane
   static_assert(ROWS == 1 || SPLIT == 1, "a warp has several rows or a row several warps");
   __shared__ float s_base[8], s_top[8], s_sum[8];
   __shared__ __align__(16) float s_o[SPLIT > 1 ? 8 : 1][D];
-  launch_dependents();
-  grid_dependency_wait();
-  const int c = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int4 raw = __ldcg(reinterpret_cast<const int4*>(a.split + c));
-  const KvSplit sp{raw.x, raw.y, raw.z, raw.w};
-  if (sp.followers == 0) return;
-  const int q0 = (blockIdx.y * (8 / SPLIT) + warp / SPLIT) * ROWS;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int q0 = first + warp / SPLIT * ROWS;
   const int live = min(ROWS, a.s.nq[sp.i] * a.group - sp.row_tile * tile_rows - q0);      // rows of this warp
   if (live <= 0) return;      // (a row's warps all)
   auto at = [&](int j, int r) { return static_cast<int64_t>(j == 0 ? 2 * c + 1 : 2 * (c + j)) * tile_rows + q0 + r; };
@@ -631,6 +629,53 @@ __global__ void __launch_bounds__(256) kv_attn_combine(const __grid_constant__ K
   }
 }
 
+template <int D, int ROWS, int PARTS, int SPLIT>
+__global__ void __launch_bounds__(256) kv_attn_combine(const __grid_constant__ KvAttnArgs a, int tile_rows) {
+  launch_dependents();
+  grid_dependency_wait();
+  const int4 raw = __ldcg(reinterpret_cast<const int4*>(a.split + blockIdx.x));
+  const KvSplit sp{raw.x, raw.y, raw.z, raw.w};
+  if (sp.followers == 0) return;
+  join_rows<D, ROWS, PARTS, SPLIT>(a, tile_rows, blockIdx.x, sp, blockIdx.y * (8 / SPLIT) * ROWS);
+}
+
+// The same where a few items have many parts and many rows each (a tree on one long sequence: 4 items of 182 rows in 38 parts): every block
+// lists the rows of all split items and takes its share of them, a row at a time, with eight warps.
+template <int D>
+__global__ void __launch_bounds__(256) kv_attn_combine_list(const __grid_constant__ KvAttnArgs a, int tile_rows, int ctas) {
+  static_assert(kPlanCtas <= 256, "a thread per CTA of the launch");
+  __shared__ int s_end[8][32], s_warp[8];      // rows up to each CTA's item, within its warp; of each warp
+  launch_dependents();
+  grid_dependency_wait();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int rows = 0;
+  if (static_cast<int>(threadIdx.x) < ctas) {
+    const int4 raw = __ldcg(reinterpret_cast<const int4*>(a.split + threadIdx.x));
+    if (raw.w > 0) rows = min(a.s.nq[raw.x] * a.group - raw.y * tile_rows, tile_rows);
+  }
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int x = __shfl_up_sync(0xffffffffu, rows, o);
+    if (lane >= o) rows += x;
+  }
+  s_end[warp][lane] = rows;
+  if (lane == 31) s_warp[warp] = rows;
+  __syncthreads();
+  int total = 0;
+#pragma unroll
+  for (int w = 0; w < 8; ++w) total += s_warp[w];
+#pragma unroll 1
+  for (int task = blockIdx.x; task < total; task += gridDim.x) {
+    int w = 0, left = task;
+    while (left >= s_warp[w]) left -= s_warp[w++];
+    const uint32_t after = __ballot_sync(0xffffffffu, s_end[w][lane] > left);      // the first whose rows reach it
+    const int k = __ffs(after) - 1, c = 32 * w + k;
+    const int4 raw = __ldcg(reinterpret_cast<const int4*>(a.split + c));
+    join_rows<D, 1, 8, 8>(a, tile_rows, c, KvSplit{raw.x, raw.y, raw.z, raw.w}, left - (k > 0 ? s_end[w][k - 1] : 0));
+    __syncthreads();      // (the joined sums' places are used again)
+  }
+}
+
 template <int D, int NQ, bool TREE>
 pace_status_t run_decode(const KvMaps& maps, const KvAttnArgs& a, unsigned grid, int* status, cudaStream_t stream) {
   using C = DecodeCfg<D, NQ>;
@@ -664,7 +709,11 @@ pace_status_t launch_kv_decode(const KvMaps& maps, const KvAttnArgs& a, int D, i
   return D == 128 ? run_rows<128, false>(maps, a, rows, grid, status, stream) : run_rows<64, false>(maps, a, rows, grid, status, stream);
 }
 
-pace_status_t launch_kv_combine(const KvAttnArgs& a, int D, int rows, unsigned grid, cudaStream_t stream) {
+pace_status_t launch_kv_combine(const KvAttnArgs& a, int D, int rows, unsigned grid, int64_t items, cudaStream_t stream) {
+  // Nodes of trees, eight parts or more to an item: rows one by one on every SM.
+  if (a.family != nullptr && rows == kManyRows && grid >= 8 * items)
+    return launch_dependent(D == 128 ? kv_attn_combine_list<128> : kv_attn_combine_list<64>, static_cast<unsigned>(std::min<int64_t>(items * rows, kPlanCtas * 6)),
+                            256, 0, 1, stream, a, rows, static_cast<int>(grid));
   if (rows == kManyRows)
     return launch_dependent(D == 128 ? kv_attn_combine<128, 4, 4, 1> : kv_attn_combine<64, 4, 4, 1>, dim3(grid, static_cast<unsigned>(rows / 32)),
                             256, 0, 1, stream, a, rows);

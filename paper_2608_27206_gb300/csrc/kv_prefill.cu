@@ -130,9 +130,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
   auto q_full = [&](int i) { return smem_u32(&ctl->q_full[i]); };
   auto o_done = [&](int i, int h) { return smem_u32(&ctl->o_done[i][h]); };
 
-  begin_call();
+  kv_begin<TREE>(a);
   const KvShare share = kv_share<kManyRows, D, TREE>(a, ctl->scan, &ctl->share, status);
   if (static_cast<int>(blockIdx.x) >= share.ctas) {
+    kv_tree_ready<TREE>(a);      // (a launch does not end before the one that it follows)
     if (threadIdx.x == 0) a.split[blockIdx.x] = KvSplit{0, 0, 0, 0};
     return;
   }
@@ -320,6 +321,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
     if (!ok && lane == 0) stop(&ctl->abort, status);
   } else {
     // ---- weights: a thread owns a row -------------------------------------------------------------
+    kv_tree_ready<TREE>(a);
     const int i = (warp - 4) >> 2, quad = warp & 3, me = quad * 32 + lane;
     const uint32_t sS = tmem + (static_cast<uint32_t>(quad * 32) << 16) + i * 128, sO = sS + 256;
     KvWalk<kManyRows, TREE> walk;
