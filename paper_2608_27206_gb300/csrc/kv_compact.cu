@@ -5,10 +5,12 @@
 // c s / s' rounded to e4m3.  s' is at most the largest s, so c' = c wherever the scale stays (most blocks of one source block, and those are
 // copied as they are); a token from under a smaller scale loses bits only below 2^-6 of s', as it would have had it been appended there.
 //
-// What bounds it is HBM: a kept token's codes once in and once out.  One CTA per written block and layer finds its 16 source rows once for
-// all heads (length, list, page table: a chain of loads that other CTAs of the SM hide); a warp takes a head's 16 rows of K or V, 16 bytes
-// per lane and load.  In place, blocks are written in order: what block i overwrites are sources of blocks up to i, which have
-// been read, since r_i >= i.  So a CTA goes over a sequence's blocks by itself, a head's K or V always in the same warp, and needs no other order.
+// What bounds it is HBM: a kept token's codes once in and once out.  A warp takes a head's 16 rows of K or V, 16 bytes per lane and
+// load; a block's 16 source rows are looked up (list, page table: a chain of loads) once for all heads and layers.  To other pages the
+// written blocks of all sequences form a line, block by block and in it layer by layer, of which every CTA takes an equal
+// share, as the lengths and counts on the device have it.  In place, blocks are written in order: what block i overwrites are
+// sources of blocks up to i, which have been read, since r_i >= i.  So a warp goes over a sequence's blocks of one head by itself, with the rows of
+// the next blocks on their way (reading ahead takes nothing away: only earlier blocks have been written), and needs no other order.
 #include <cuda_fp16.h>
 
 #include <algorithm>
@@ -19,14 +21,18 @@
 namespace pace {
 namespace {
 
-constexpr int kCompactThreads = 256;
-constexpr int kMaxLayers = 64;        // of one launch
+constexpr int kMoveThreads = 256, kMoveCtas = 4;      // to other pages: threads of a CTA, CTAs of an SM
+constexpr int kSlideThreads = 128;                    // in place, a warp per head's K or V
+constexpr int kSlideBlocks = 4;                       // ... whose blocks are looked up so many at a time
+constexpr int kWideWarps = 16;                        // in place, a CTA per head's K or V
+constexpr int kMaxLayers = 64;                        // of one launch
 
 struct CompactArgs {
   uint8_t* codes[2][kMaxLayers];      // K and V of each layer
   float* scales[2][kMaxLayers];
   int64_t page_stride, scale_stride, src_stride, dst_stride;
-  int n_pages, page_shift, heads;
+  int n_pages, page_shift, heads, layers;
+  FastDiv by_tasks;                   // 2 heads
   const int32_t* lens;
   const int32_t* src_table;
   const int32_t* dst_table;
@@ -36,8 +42,57 @@ struct CompactArgs {
   int b0, nb;
   int cu[kKvMaxB + 1];                // newest tokens of each sequence
   int cu_rows[kKvMaxB + 1];           // its list
-  int block_prefix[kKvMaxB + 1];      // blocks that it may write (in place: 1 where it may write any)
 };
+
+// Where a sequence's newest tokens begin, and how many of them are kept; -1: what its numbers say cannot be.
+struct Kept {
+  int base, count;
+};
+__device__ __forceinline__ Kept kept_of(const CompactArgs& a, int b) {
+  const int len = a.lens[a.b0 + b], n = a.cu[b + 1] - a.cu[b], room = a.cu_rows[b + 1] - a.cu_rows[b];
+  const int count = a.counts != nullptr ? a.counts[a.b0 + b] : room;
+  return len < n || count < 0 || count > room ? Kept{len, -1} : Kept{len - n, count};
+}
+// Its new length, which one thread of the launch writes.
+__device__ __forceinline__ void put_length(const CompactArgs& a, int b, const Kept& k, int* status) {
+  if (k.count < 0) record_error(status, PACE_ERR_INVALID_ARG, K_KV_COMPACT);
+  if (a.new_lens != nullptr) a.new_lens[a.b0 + b] = k.base + max(k.count, 0);
+}
+
+// Where slot `slot` of a sequence gets its token from: places of its codes and scale in head 0; code -1: zeros, -2: nothing goes there.
+struct alignas(16) Source {
+  int64_t code, scale;
+};
+__device__ __forceinline__ Source place_of(const CompactArgs& a, int page, int64_t slot, int D) {
+  const int at = static_cast<int>(slot) & ((1 << a.page_shift) - 1);
+  return Source{page * a.page_stride + at * D, page * a.scale_stride + at / kKvBlock};
+}
+__device__ __forceinline__ Source source_of(const CompactArgs& a, int b, const Kept& k, int64_t slot, int dst_page, int D, int* status) {
+  const int64_t i = slot - k.base;      // which of the kept tokens
+  if (i < 0) return dst_page < 0 ? Source{-1, 0} : place_of(a, dst_page, slot, D);      // there already
+  if (i >= k.count) return Source{-2, 0};
+  int64_t row = i;
+  bool ok = true;
+  if (a.rows != nullptr) {
+    const int32_t* list = a.rows + a.cu_rows[b];
+    const int mine = list[i], before = i > 0 ? list[i - 1] : -1;
+    row = static_cast<int64_t>(mine) - a.cu[b];
+    ok = row >= i && row < a.cu[b + 1] - a.cu[b] && mine > before;
+  }
+  const int64_t s = k.base + row, pi = s >> a.page_shift;
+  const int page = ok && pi < a.src_stride ? a.src_table[(a.b0 + b) * a.src_stride + pi] : -1;
+  if (page >= 0 && page < a.n_pages) return place_of(a, page, s, D);
+  record_error(status, PACE_ERR_INVALID_ARG, K_KV_COMPACT);
+  return Source{-1, 0};
+}
+// The page that a block goes to; -1: none.
+__device__ __forceinline__ int target_of(const CompactArgs& a, int b, int64_t block, int* status, bool say) {
+  const int64_t pi = block * kKvBlock >> a.page_shift;
+  const int page = pi < a.dst_stride ? a.dst_table[(a.b0 + b) * a.dst_stride + pi] : -1;
+  if (page >= 0 && page < a.n_pages) return page;
+  if (say) record_error(status, PACE_ERR_INVALID_ARG, K_KV_COMPACT);
+  return -1;
+}
 
 // Codes times a ratio, rounded again.
 __device__ __forceinline__ uint32_t times(uint32_t u, float ratio) {
@@ -45,132 +100,256 @@ __device__ __forceinline__ uint32_t times(uint32_t u, float ratio) {
   const float2 g0 = __half22float2(*reinterpret_cast<const __half2*>(&f0)), g1 = __half22float2(*reinterpret_cast<const __half2*>(&f1));
   return e4m3x4(g0.x * ratio, g0.y * ratio, g1.x * ratio, g1.y * ratio);
 }
-
-template <int D, bool IN_PLACE>
-__global__ void __launch_bounds__(kCompactThreads) kv_compact_kernel(const __grid_constant__ CompactArgs a, int* status) {
-  constexpr int LPR = D / 16, RPP = 32 / LPR, PASS = kKvBlock / RPP;      // lanes per row, rows per pass
-  __shared__ int src_page[kKvBlock], src_slot[kKvBlock];      // of each slot of the block; page -1: zeros, -2: nothing there
-  ptx::begin_call();
-  // the kept tokens of a sequence; -1: what its numbers say cannot be
-  auto kept = [&](int b, int64_t len, int n) {
-    const int room = a.cu_rows[b + 1] - a.cu_rows[b], count = a.counts != nullptr ? a.counts[a.b0 + b] : room;
-    return len < n || count < 0 || count > room ? -1 : count;
+// The same for a power of two, as the product of two f16 that are.  f16 holds every product of a code down to its last bit at 2^-24,
+// 2^-14 of half a step of the smallest codes: what is lost below decides nothing.
+__device__ __forceinline__ uint32_t times_pow2(uint32_t u, uint32_t f, uint32_t g) {
+  auto two = [&](uint32_t codes) {
+    uint32_t x = e4m3x2_to_f16x2(codes);
+    uint16_t r;
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(x) : "r"(x), "r"(f));
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(x) : "r"(x), "r"(g));
+    asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(r) : "r"(x));
+    return static_cast<uint32_t>(r);
   };
-  if (a.new_lens != nullptr && blockIdx.x == 0 && blockIdx.y == 0) {
-    for (int b = threadIdx.x; b < a.nb; b += kCompactThreads) {
-      const int len = a.lens[a.b0 + b], n = a.cu[b + 1] - a.cu[b], count = kept(b, len, n);
-      if (count < 0) record_error(status, PACE_ERR_INVALID_ARG, K_KV_COMPACT);
-      a.new_lens[a.b0 + b] = count < 0 ? len : len - n + count;
+  return two(u & 0xFFFFu) | two(u >> 16) << 16;
+}
+
+// A block's rows of one head, K or V, as a warp holds them: 16 codes of PASS rows in a lane, and their scales.
+template <int D>
+struct Rows {
+  static constexpr int LPR = D / 16, RPP = 32 / LPR, PASS = kKvBlock / RPP;      // lanes per row, rows per pass
+  uint4 x[PASS];
+  float s[PASS];
+};
+struct HeadOf {      // of a layer
+  uint8_t* codes;
+  float* scales;
+  int head;
+};
+__device__ __forceinline__ HeadOf head_of(const CompactArgs& a, int layer, int task) {
+  const bool is_v = task >= a.heads;
+  return HeadOf{a.codes[is_v][layer], a.scales[is_v][layer], is_v ? task - a.heads : task};
+}
+
+template <int D>
+__device__ __forceinline__ void get_rows(const CompactArgs& a, const HeadOf& h, const Source* from, Rows<D>& r) {
+  using R = Rows<D>;
+  const int lane = threadIdx.x & 31, col = lane % R::LPR * 16, row0 = lane / R::LPR;
+  const uint8_t* codes = h.codes + (static_cast<int64_t>(h.head) << a.page_shift) * D + col;
+  const float* scales = h.scales + (static_cast<int64_t>(h.head) << (a.page_shift - 4));
+#pragma unroll
+  for (int p = 0; p < R::PASS; ++p) {
+    const Source f = from[p * R::RPP + row0];
+    r.x[p] = make_uint4(0, 0, 0, 0);
+    r.s[p] = 1.f;
+    if (f.code >= 0) {
+      r.x[p] = *reinterpret_cast<const uint4*>(codes + f.code);
+      r.s[p] = scales[f.scale];
     }
   }
-  int lo = 0, hi = a.nb - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (a.block_prefix[mid] <= static_cast<int>(blockIdx.x)) lo = mid;
-    else hi = mid - 1;
+}
+
+// ... to the slots of a page that begin at `to_place` (in head 0), `n` of them, under their scale.
+template <int D>
+__device__ __forceinline__ void put_rows(const CompactArgs& a, const HeadOf& h, Rows<D>& r, const Source& to_place, int n, int* status) {
+  using R = Rows<D>;
+  const int lane = threadIdx.x & 31, col = lane % R::LPR * 16, row0 = lane / R::LPR;
+  // the largest magnitude of sixteen codes is the largest of their low seven bits, 0x7F a NaN; a byte for each pass
+  uint32_t most = 0;
+#pragma unroll
+  for (int p = 0; p < R::PASS; ++p) {
+    const uint4 x = r.x[p];
+    uint32_t m = __vmaxu4(__vmaxu4(x.x & 0x7F7F7F7Fu, x.y & 0x7F7F7F7Fu), __vmaxu4(x.z & 0x7F7F7F7Fu, x.w & 0x7F7F7F7Fu));
+    m = __vmaxu4(m, m >> 16);
+    most |= max(m & 0xFFu, m >> 8 & 0xFFu) << 8 * p;
   }
-  const int b = lo, n = a.cu[b + 1] - a.cu[b];
-  if (static_cast<int>(blockIdx.x) >= a.block_prefix[a.nb]) return;      // (a launch for the lengths alone)
-  // (a length may be anything: slots in 64 bits until they are known to be in the table)
-  const int64_t len = a.lens[a.b0 + b], base = len - n;
-  const int count = kept(b, len, n);
-  if (count <= 0) return;
-  const int64_t first = base / kKvBlock, last = (base + count - 1) / kKvBlock;
-  const int64_t begin = IN_PLACE ? first : first + (blockIdx.x - a.block_prefix[b]), end = IN_PLACE ? last : min(begin, last);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = kCompactThreads / 32, layer = blockIdx.y;
-  const int col = (lane % LPR) * 16, row0 = lane / LPR, blocks = 1 << (a.page_shift - 4), page_slots = 1 << a.page_shift;
-#pragma unroll 1
-  for (int64_t block = begin; block <= end; ++block) {
-    const int64_t slot0 = block * kKvBlock, pi = slot0 >> a.page_shift;
-    const int slot = static_cast<int>(slot0) & (page_slots - 1);      // of row 0, in its page
-    int page = pi < a.dst_stride ? a.dst_table[(a.b0 + b) * a.dst_stride + pi] : -1;
-    if (page < 0 || page >= a.n_pages) {
-      if (threadIdx.x == 0) record_error(status, PACE_ERR_INVALID_ARG, K_KV_COMPACT);
-      page = -1;
+#pragma unroll
+  for (int o = 1; o < R::LPR; o <<= 1) most = __vmaxu4(most, __shfl_xor_sync(0xffffffffu, most, o));
+  float amax = 0.f;
+  bool bad = false;
+#pragma unroll
+  for (int p = 0; p < R::PASS; ++p) {
+    uint32_t m = most >> 8 * p & 0xFFu;
+    if (m == 0x7Fu || !(r.s[p] > 0.f && r.s[p] < INFINITY)) {      // the whole row (its LPR lanes)
+      bad = true;
+      r.x[p] = make_uint4(0, 0, 0, 0);
+      r.s[p] = 1.f;
+      m = 0;
     }
-    if (threadIdx.x < kKvBlock) {
-      const int r = threadIdx.x;
-      const int64_t i = slot0 + r - base;      // which of the kept tokens
-      int from = -2, at = slot + r;
-      if (i < 0) {
-        from = page;      // there already
-      } else if (i < count) {
-        int64_t row = i;
-        bool ok = true;
-        if (a.rows != nullptr) {
-          const int32_t* list = a.rows + a.cu_rows[b];
-          row = static_cast<int64_t>(list[i]) - a.cu[b];
-          ok = row >= i && row < n && (i == 0 || list[i] > list[i - 1]);
-        }
-        const int64_t s = base + row, sp = s >> a.page_shift;
-        at = static_cast<int>(s) & (page_slots - 1);
-        from = ok && sp < a.src_stride ? a.src_table[(a.b0 + b) * a.src_stride + sp] : -1;
-        if (from < 0 || from >= a.n_pages) {
-          record_error(status, PACE_ERR_INVALID_ARG, K_KV_COMPACT);
-          from = -1;
-        }
+    const uint32_t f = e4m3x2_to_f16x2(m);
+    amax = fmaxf(amax, __low2float(*reinterpret_cast<const __half2*>(&f)) * r.s[p]);
+  }
+  if (bad) record_error(status, PACE_ERR_INVALID_ARG, K_KV_COMPACT);
+  amax = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(amax)));      // (none is negative; the lanes have their rows and scales)
+  const float to = scale_for(amax);
+  uint8_t* codes = h.codes + to_place.code + (static_cast<int64_t>(h.head) << a.page_shift) * D + col;
+#pragma unroll
+  for (int p = 0; p < R::PASS; ++p) {
+    const int at = p * R::RPP + row0;
+    uint4 x = r.x[p];
+    const uint32_t was = __float_as_uint(r.s[p]), now = __float_as_uint(to);
+    if (was != now) {
+      if ((was & 0x7FFFFFu) == 0) {
+        // the power 2^e, e = e0 + e1 (above 18 every code is 0, as none passes 448; from -24 on nothing is left of any)
+        const int e = min(max(static_cast<int>(was >> 23) - static_cast<int>(now >> 23), -24), 18), e0 = e >> 1, e1 = e - e0;
+        const uint32_t f = static_cast<uint32_t>(15 + e0) << 10, g = static_cast<uint32_t>(15 + e1) << 10;
+        const uint32_t f2 = f | f << 16, g2 = g | g << 16;
+        x = make_uint4(times_pow2(x.x, f2, g2), times_pow2(x.y, f2, g2), times_pow2(x.z, f2, g2), times_pow2(x.w, f2, g2));
+      } else {      // (a scale that this library has not made, or below 2^-126)
+        const float ratio = __fdiv_rn(r.s[p], to);
+        x = make_uint4(times(x.x, ratio), times(x.y, ratio), times(x.z, ratio), times(x.w, ratio));
       }
-      src_page[r] = from;
-      src_slot[r] = at;
+    }
+    if (at < n) *reinterpret_cast<uint4*>(codes + at * D) = x;
+  }
+  if (lane == 0) h.scales[to_place.scale + (static_cast<int64_t>(h.head) << (a.page_shift - 4))] = to;
+}
+
+// Of a block's slots those that hold a token when it is written.
+__device__ __forceinline__ int slots_of(const Kept& k, int64_t block) {
+  return static_cast<int>(min(static_cast<int64_t>(k.base) + k.count - block * kKvBlock, static_cast<int64_t>(kKvBlock)));
+}
+
+// To other pages.
+template <int D>
+__global__ void __launch_bounds__(kMoveThreads, kMoveCtas) kv_move_kernel(const __grid_constant__ CompactArgs a, int* status) {
+  static_assert(kMoveThreads >= kKvMaxB, "a thread per sequence");
+  __shared__ int s_base[kKvMaxB], s_count[kKvMaxB], s_end[kKvMaxB], s_warp[kMoveThreads / 32], s_page;
+  __shared__ Source s_from[kKvBlock];
+  ptx::begin_call();
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, warps = kMoveThreads / 32;
+  {      // the line: blocks up to each sequence's end
+    int blocks = 0;
+    if (tid < a.nb) {
+      const Kept k = kept_of(a, tid);
+      if (blockIdx.x == 0) put_length(a, tid, k, status);
+      s_base[tid] = k.base;
+      s_count[tid] = k.count;
+      if (k.count > 0) blocks = (k.base + k.count - 1) / kKvBlock - k.base / kKvBlock + 1;
+    }
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, blocks, o);
+      if (lane >= o) blocks += x;
+    }
+    if (lane == 31) s_warp[warp] = blocks;
+    __syncthreads();
+    for (int w = 0; w < warp; ++w) blocks += s_warp[w];
+    if (tid < a.nb) s_end[tid] = blocks;
+    __syncthreads();
+  }
+  const int64_t total = static_cast<int64_t>(s_end[a.nb - 1]) * a.layers;
+  int64_t u = total * blockIdx.x / gridDim.x;
+  const int64_t end = total * (blockIdx.x + 1) / gridDim.x;
+#pragma unroll 1
+  while (u < end) {
+    const int at = static_cast<int>(u / a.layers), from_layer = static_cast<int>(u - static_cast<int64_t>(at) * a.layers);
+    const int n_layers = static_cast<int>(min(static_cast<int64_t>(a.layers - from_layer), end - u));
+    int b = 0, hi = a.nb - 1;      // the first sequence whose end is past it
+    while (b < hi) {
+      const int mid = (b + hi) >> 1;
+      if (s_end[mid] > at) hi = mid;
+      else b = mid + 1;
+    }
+    const Kept k{s_base[b], s_count[b]};
+    const int64_t block = k.base / kKvBlock + at - (b > 0 ? s_end[b - 1] : 0);
+    if (tid < kKvBlock) {
+      const int page = target_of(a, b, block, status, tid == 0);
+      s_from[tid] = source_of(a, b, k, block * kKvBlock + tid, page, D, status);
+      if (tid == 0) s_page = page;
     }
     __syncthreads();
-    if (page >= 0) {
+    const Source to = place_of(a, max(s_page, 0), block * kKvBlock, D);
+    const int tasks = s_page >= 0 ? n_layers * 2 * a.heads : 0, n = slots_of(k, block);
 #pragma unroll 1
-      for (int task = warp; task < 2 * a.heads; task += warps) {
-        const bool is_v = task >= a.heads;
-        const int head = is_v ? task - a.heads : task;
-        uint8_t* codes = a.codes[is_v][layer];
-        float* scales = a.scales[is_v][layer];
-        uint4 x[PASS];
-        float s[PASS];
+    for (int t = warp; t < tasks; t += warps) {
+      const int l = static_cast<int>(a.by_tasks(t));
+      const HeadOf h = head_of(a, from_layer + l, t - l * 2 * a.heads);
+      Rows<D> r;
+      get_rows<D>(a, h, s_from, r);
+      put_rows<D>(a, h, r, to, n, status);
+    }
+    __syncthreads();      // (the rows' sources have been used)
+    u += n_layers;
+  }
+}
+
+// In place, few blocks of a sequence: a warp per head's K or V.
+template <int D>
+__global__ void __launch_bounds__(kSlideThreads) kv_slide_kernel(const __grid_constant__ CompactArgs a, int* status) {
+  constexpr int WARPS = kSlideThreads / 32;
+  __shared__ Source s_from[kSlideBlocks][kKvBlock];
+  __shared__ int s_page[kSlideBlocks];
+  ptx::begin_call();
+  const int b = blockIdx.x, tid = threadIdx.x;
+  const Kept k = kept_of(a, b);
+  if (blockIdx.y == 0 && tid == 0) put_length(a, b, k, status);
+  if (k.count <= 0) return;
+  const int task = blockIdx.y * WARPS + (tid >> 5), layer = static_cast<int>(a.by_tasks(task));
+  const bool mine = layer < a.layers;
+  const HeadOf h = head_of(a, mine ? layer : 0, mine ? task - layer * 2 * a.heads : 0);
+  const int64_t first = k.base / kKvBlock, last = (static_cast<int64_t>(k.base) + k.count - 1) / kKvBlock;
+#pragma unroll 1
+  for (int64_t block0 = first; block0 <= last; block0 += kSlideBlocks) {
+    const int n = static_cast<int>(min(last - block0 + 1, static_cast<int64_t>(kSlideBlocks)));
+    for (int i = tid; i < n * kKvBlock; i += kSlideThreads) {
+      const int64_t block = block0 + i / kKvBlock;
+      const int page = target_of(a, b, block, status, i % kKvBlock == 0);
+      s_from[i / kKvBlock][i % kKvBlock] = source_of(a, b, k, block0 * kKvBlock + i, page, D, status);
+      if (i % kKvBlock == 0) s_page[i / kKvBlock] = page;
+    }
+    __syncthreads();
+    if (mine) {
+      Rows<D> r[2];
+      get_rows<D>(a, h, s_from[0], r[0]);
 #pragma unroll
-        for (int p = 0; p < PASS; ++p) {
-          const int r = p * RPP + row0, from = src_page[r], at = src_slot[r];
-          x[p] = make_uint4(0, 0, 0, 0);
-          s[p] = 1.f;
-          if (from >= 0) {
-            x[p] = *reinterpret_cast<const uint4*>(codes + from * a.page_stride + ((static_cast<int64_t>(head) << a.page_shift) + at) * D + col);
-            s[p] = scales[from * a.scale_stride + head * blocks + at / kKvBlock];
-          }
-        }
-        float amax = 0.f;
-        bool bad = false;
-#pragma unroll
-        for (int p = 0; p < PASS; ++p) {
-          // the largest magnitude of sixteen codes is the largest of their low seven bits, 0x7F a NaN
-          uint32_t m = __vmaxu4(__vmaxu4(x[p].x & 0x7F7F7F7Fu, x[p].y & 0x7F7F7F7Fu), __vmaxu4(x[p].z & 0x7F7F7F7Fu, x[p].w & 0x7F7F7F7Fu));
-          m = __vmaxu4(m, m >> 16);
-          m = max(m & 0xFFu, m >> 8 & 0xFFu);
-#pragma unroll
-          for (int o = 1; o < LPR; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-          if (m == 0x7Fu || !(s[p] > 0.f && s[p] < INFINITY)) {      // the whole row (its LPR lanes)
-            bad = true;
-            x[p] = make_uint4(0, 0, 0, 0);
-            m = 0;
-            s[p] = 1.f;
-          }
-          const uint32_t f = e4m3x2_to_f16x2(m);
-          amax = fmaxf(amax, __low2float(*reinterpret_cast<const __half2*>(&f)) * s[p]);
-        }
-#pragma unroll
-        for (int o = LPR; o < 32; o <<= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-        if (bad) record_error(status, PACE_ERR_INVALID_ARG, K_KV_COMPACT);
-        const float to = scale_for(amax);
-        __syncwarp();      // every lane has its rows and their scales: in place they may go
-#pragma unroll
-        for (int p = 0; p < PASS; ++p) {
-          const int r = p * RPP + row0;
-          if (src_page[r] == -2) continue;
-          if (s[p] != to) {
-            const float ratio = __fdiv_rn(s[p], to);
-            x[p] = make_uint4(times(x[p].x, ratio), times(x[p].y, ratio), times(x[p].z, ratio), times(x[p].w, ratio));
-          }
-          *reinterpret_cast<uint4*>(codes + page * a.page_stride + ((static_cast<int64_t>(head) << a.page_shift) + slot + r) * D + col) = x[p];
-        }
-        if (lane == 0) scales[page * a.scale_stride + head * blocks + slot / kKvBlock] = to;
+      for (int j = 0; j < kSlideBlocks; ++j) {
+        if (j >= n) break;
+        if (j + 1 < n) get_rows<D>(a, h, s_from[j + 1], r[(j + 1) & 1]);
+        if (s_page[j] >= 0) put_rows<D>(a, h, r[j & 1], place_of(a, s_page[j], (block0 + j) * kKvBlock, D), slots_of(k, block0 + j), status);
       }
     }
-    if (IN_PLACE) __syncthreads();      // (the rows' sources have been used)
+    __syncthreads();      // (the rows' sources have been used)
+  }
+}
+
+// In place, many blocks: a CTA per head's K or V, a warp per block of a round of kWideWarps.  All read a round's rows before one
+// writes them, and the next round's before they write: what a round overwrites are sources of rounds up to it.
+template <int D>
+__global__ void __launch_bounds__(32 * kWideWarps) kv_slide_wide_kernel(const __grid_constant__ CompactArgs a, int* status) {
+  __shared__ Source s_from[3][kWideWarps][kKvBlock];
+  __shared__ int s_page[3][kWideWarps];
+  ptx::begin_call();
+  const int b = blockIdx.x, tid = threadIdx.x, warp = tid >> 5;
+  const Kept k = kept_of(a, b);
+  if (blockIdx.y == 0 && tid == 0) put_length(a, b, k, status);
+  if (k.count <= 0) return;
+  const int layer = static_cast<int>(a.by_tasks(blockIdx.y));
+  const HeadOf h = head_of(a, layer, static_cast<int>(blockIdx.y) - layer * 2 * a.heads);
+  const int64_t first = k.base / kKvBlock, last = (static_cast<int64_t>(k.base) + k.count - 1) / kKvBlock;
+  const int rounds = static_cast<int>((last - first) / kWideWarps) + 1;
+  auto look_up = [&](int round) {      // (three rounds' places: a warp may still write one round when another looks up the next but one)
+    if (round >= rounds || tid >= kWideWarps * kKvBlock) return;
+    const int64_t block = first + static_cast<int64_t>(round) * kWideWarps + tid / kKvBlock;
+    if (block > last) return;
+    const int page = target_of(a, b, block, status, tid % kKvBlock == 0);
+    s_from[round % 3][tid / kKvBlock][tid % kKvBlock] = source_of(a, b, k, block * kKvBlock + tid % kKvBlock, page, D, status);
+    if (tid % kKvBlock == 0) s_page[round % 3][tid / kKvBlock] = page;
+  };
+  auto block_of = [&](int round) { return first + static_cast<int64_t>(round) * kWideWarps + warp; };
+  Rows<D> r, next;
+  look_up(0);
+  __syncthreads();
+  if (block_of(0) <= last) get_rows<D>(a, h, s_from[0][warp], next);
+#pragma unroll 1
+  for (int round = 0; round < rounds; ++round) {
+    r = next;
+    look_up(round + 1);
+    __syncthreads();      // every warp has this round's rows
+    if (round + 1 < rounds && block_of(round + 1) <= last) get_rows<D>(a, h, s_from[(round + 1) % 3][warp], next);
+    const int64_t block = block_of(round);
+    const int page = block <= last ? s_page[round % 3][warp] : -1;
+    if (page >= 0) put_rows<D>(a, h, r, place_of(a, page, block * kKvBlock, D), slots_of(k, block), status);
   }
 }
 
@@ -222,6 +401,7 @@ extern "C" pace_status_t pace_kv_compact(const pace_kv_cache* layers, int n_laye
   a.n_pages = v.n_pages;
   a.page_shift = v.page_shift;
   a.heads = v.heads;
+  a.by_tasks = fast_div(2 * static_cast<uint32_t>(v.heads));
   a.src_stride = table_stride;
   a.dst_stride = in_place ? table_stride : dst_stride;
   a.lens = seq_lens;
@@ -230,9 +410,11 @@ extern "C" pace_status_t pace_kv_compact(const pace_kv_cache* layers, int n_laye
   a.rows = rows;
   a.counts = counts;
   int* status = device_status_word();
+  int sms = 0;
+  PACE_CHECK(sm_count(&sms));
   for (int l0 = 0; l0 < n_layers; l0 += kMaxLayers) {
-    const int nl = std::min(kMaxLayers, n_layers - l0);
-    for (int l = 0; l < nl; ++l) {
+    a.layers = std::min(kMaxLayers, n_layers - l0);
+    for (int l = 0; l < a.layers; ++l) {
       const pace_kv_cache& c = layers[l0 + l];
       a.codes[0][l] = static_cast<uint8_t*>(c.k);
       a.codes[1][l] = static_cast<uint8_t*>(c.v);
@@ -243,20 +425,29 @@ extern "C" pace_status_t pace_kv_compact(const pace_kv_cache* layers, int n_laye
     for (int b0 = 0; b0 < B; b0 += kKvMaxB) {
       a.b0 = b0;
       a.nb = std::min(kKvMaxB, B - b0);
-      int64_t blocks = 0;
       for (int i = 0; i <= a.nb; ++i) {
         a.cu[i] = cu_new[b0 + i];
         a.cu_rows[i] = cu_rows[b0 + i];
-        a.block_prefix[i] = static_cast<int>(blocks);
-        if (i == a.nb) break;
-        const int most = cu_rows[b0 + i + 1] - cu_rows[b0 + i];
-        if (most > 0) blocks += in_place ? 1 : (most + 2 * (kKvBlock - 1)) / kKvBlock;      // wherever in a block the first one lands
       }
-      if (blocks == 0 && l0 > 0) continue;
-      auto* kernel = layers->head_dim == 128 ? (in_place ? kv_compact_kernel<128, true> : kv_compact_kernel<128, false>)
-                                             : (in_place ? kv_compact_kernel<64, true> : kv_compact_kernel<64, false>);
-      PACE_CHECK(launch_dependent(kernel, dim3(static_cast<unsigned>(std::max<int64_t>(blocks, 1)), static_cast<unsigned>(nl)), kCompactThreads, 0, 1,
-                                  stream, a, status));
+      if (in_place) {
+        // A warp by itself moves a block in a microsecond, a round of a CTA takes little more: few blocks of many sequences go by warps, which
+        // waste none, more than kSlideBlocks by CTAs.
+        int most = 0;
+        for (int i = 0; i < a.nb; ++i) most = std::max(most, a.cu_rows[i + 1] - a.cu_rows[i]);
+        const unsigned tasks = static_cast<unsigned>(a.layers * 2 * a.heads), warps = kSlideThreads / 32, nb = static_cast<unsigned>(a.nb);
+        if (most <= (kSlideBlocks - 1) * kKvBlock + 1)
+          PACE_CHECK(launch_dependent(layers->head_dim == 128 ? kv_slide_kernel<128> : kv_slide_kernel<64>, dim3(nb, (tasks + warps - 1) / warps),
+                                      kSlideThreads, 0, 1, stream, a, status));
+        else
+          PACE_CHECK(launch_dependent(layers->head_dim == 128 ? kv_slide_wide_kernel<128> : kv_slide_wide_kernel<64>, dim3(nb, tasks), 32 * kWideWarps,
+                                      0, 1, stream, a, status));
+      } else {
+        int64_t blocks = 0;      // at most, wherever in a block a sequence's first token lands
+        for (int i = 0; i < a.nb; ++i)
+          if (a.cu_rows[i + 1] > a.cu_rows[i]) blocks += (a.cu_rows[i + 1] - a.cu_rows[i] + 2 * (kKvBlock - 1)) / kKvBlock;
+        const unsigned grid = static_cast<unsigned>(std::max<int64_t>(1, std::min<int64_t>(blocks * a.layers, static_cast<int64_t>(sms) * kMoveCtas)));
+        PACE_CHECK(launch_dependent(layers->head_dim == 128 ? kv_move_kernel<128> : kv_move_kernel<64>, grid, kMoveThreads, 0, 1, stream, a, status));
+      }
     }
   }
   return PACE_OK;

@@ -328,3 +328,16 @@ def test_a_step_of_drafts(pace):  # noqa: F811
     # and the accepted nodes' outputs are what they would have been in a line
     line = pace.pace_kv_attention(plain.cache, Q[torch.from_numpy(pick).cuda()], few, now, plain.table, 135)
     np.testing.assert_allclose(_f64(out)[pick], _f64(line), rtol=2.0 ** -7, atol=2.0 ** -7)
+
+
+@pytest.mark.parametrize("away", [False, True])
+def test_zeros_under_a_large_scale_join_a_small_one(pace, away):  # noqa: F811
+    """A block of zeros (of either sign) may have any scale: its tokens are zeros still beside others 2^150 below."""
+    case = Case(pace, 48, (96,), (96,), (40,), 2, 64, 16, away=away)
+    pool, pages = case.pools[0], case.source[0]
+    for n in "kv":
+        pool.raw[n][pages[2]] = np.where(pool.raw[n][pages[2]] & 1, 0x80, 0)
+        pool.s[n][pages] = 2.0 ** -40
+        pool.s[n][pages[2]] = 2.0 ** 110
+    _upload(pool)
+    case.check(case.call())
