@@ -100,18 +100,30 @@ __device__ __forceinline__ uint32_t times(uint32_t u, float ratio) {
   const float2 g0 = __half22float2(*reinterpret_cast<const __half2*>(&f0)), g1 = __half22float2(*reinterpret_cast<const __half2*>(&f1));
   return e4m3x4(g0.x * ratio, g0.y * ratio, g1.x * ratio, g1.y * ratio);
 }
-// The same for a power of two, as the product of two f16 that are.  f16 holds every product of a code down to its last bit at 2^-24,
-// 2^-14 of half a step of the smallest codes: what is lost below decides nothing.
-__device__ __forceinline__ uint32_t times_pow2(uint32_t u, uint32_t f, uint32_t g) {
+// The same for 2^e, -24 <= e <= 18, in f16, which holds every product of a code down to its last bit at 2^-24, 2^-14 of half a step of
+// the smallest codes: what is lost below decides nothing.
+__device__ __forceinline__ uint4 times_pow2(uint4 u, int e) {
+  const int e0 = min(max(e, -14), 15), e1 = e - e0;      // (f16 has no larger powers, and no smaller ones without its shift)
+  const uint32_t f = static_cast<uint32_t>(15 + e0) * 0x04000400u;
   auto two = [&](uint32_t codes) {
     uint32_t x = e4m3x2_to_f16x2(codes);
     uint16_t r;
     asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(x) : "r"(x), "r"(f));
-    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(x) : "r"(x), "r"(g));
+    if (e1 != 0) asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(x) : "r"(x), "r"(static_cast<uint32_t>(15 + e1) * 0x04000400u));
     asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(r) : "r"(x));
     return static_cast<uint32_t>(r);
   };
-  return two(u & 0xFFFFu) | two(u >> 16) << 16;
+  auto four = [&](uint32_t codes) { return two(codes & 0xFFFFu) | two(codes >> 16) << 16; };
+  return make_uint4(four(u.x), four(u.y), four(u.z), four(u.w));
+}
+
+// The largest magnitude of sixteen codes: of their low seven bits, 0x7F a NaN.  (Sixteen bits at a time the upper byte decides; the
+// lower bytes go by themselves.)
+__device__ __forceinline__ uint32_t largest(const uint4& x) {
+  const uint32_t up = __vmaxu2(__vimax3_u16x2(x.x & 0x7F7F7F7Fu, x.y & 0x7F7F7F7Fu, x.z & 0x7F7F7F7Fu), x.w & 0x7F7F7F7Fu);
+  const uint32_t lo = __vmaxu2(__vimax3_u16x2(x.x & 0x007F007Fu, x.y & 0x007F007Fu, x.z & 0x007F007Fu), x.w & 0x007F007Fu);
+  const uint32_t m = __vmaxu2(up >> 8 & 0x007F007Fu, lo);
+  return max(m & 0xFFFFu, m >> 16);
 }
 
 // A block's rows of one head, K or V, as a warp holds them: 16 codes of PASS rows in a lane, and their scales.
@@ -154,32 +166,35 @@ template <int D>
 __device__ __forceinline__ void put_rows(const CompactArgs& a, const HeadOf& h, Rows<D>& r, const Source& to_place, int n, int* status) {
   using R = Rows<D>;
   const int lane = threadIdx.x & 31, col = lane % R::LPR * 16, row0 = lane / R::LPR;
-  // the largest magnitude of sixteen codes is the largest of their low seven bits, 0x7F a NaN; a byte for each pass
-  uint32_t most = 0;
-#pragma unroll
-  for (int p = 0; p < R::PASS; ++p) {
-    const uint4 x = r.x[p];
-    uint32_t m = __vmaxu4(__vmaxu4(x.x & 0x7F7F7F7Fu, x.y & 0x7F7F7F7Fu), __vmaxu4(x.z & 0x7F7F7F7Fu, x.w & 0x7F7F7F7Fu));
-    m = __vmaxu4(m, m >> 16);
-    most |= max(m & 0xFFu, m >> 8 & 0xFFu) << 8 * p;
-  }
-#pragma unroll
-  for (int o = 1; o < R::LPR; o <<= 1) most = __vmaxu4(most, __shfl_xor_sync(0xffffffffu, most, o));
   float amax = 0.f;
+  auto bad_scale = [](float x) { return !(x > 0.f && x < INFINITY); };
+  auto value = [](uint32_t m) {
+    const uint32_t f = e4m3x2_to_f16x2(m);
+    return __low2float(*reinterpret_cast<const __half2*>(&f));
+  };
   bool bad = false;
 #pragma unroll
   for (int p = 0; p < R::PASS; ++p) {
-    uint32_t m = most >> 8 * p & 0xFFu;
-    if (m == 0x7Fu || !(r.s[p] > 0.f && r.s[p] < INFINITY)) {      // the whole row (its LPR lanes)
-      bad = true;
-      r.x[p] = make_uint4(0, 0, 0, 0);
-      r.s[p] = 1.f;
-      m = 0;
-    }
-    const uint32_t f = e4m3x2_to_f16x2(m);
-    amax = fmaxf(amax, __low2float(*reinterpret_cast<const __half2*>(&f)) * r.s[p]);
+    const uint32_t m = largest(r.x[p]);
+    bad = bad || m == 0x7Fu || bad_scale(r.s[p]);
+    amax = fmaxf(amax, value(m) * r.s[p]);
   }
-  if (bad) record_error(status, PACE_ERR_INVALID_ARG, K_KV_COMPACT);
+  if (__any_sync(0xffffffffu, bad)) {      // rows (of LPR lanes) with a NaN or a scale that is none become zeros
+    if (bad) record_error(status, PACE_ERR_INVALID_ARG, K_KV_COMPACT);
+    amax = 0.f;
+#pragma unroll
+    for (int p = 0; p < R::PASS; ++p) {
+      uint32_t m = bad_scale(r.s[p]) ? 0x7Fu : largest(r.x[p]);
+#pragma unroll
+      for (int o = 1; o < R::LPR; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+      if (m == 0x7Fu) {
+        r.x[p] = make_uint4(0, 0, 0, 0);
+        r.s[p] = 1.f;
+        m = 0;
+      }
+      amax = fmaxf(amax, value(m) * r.s[p]);
+    }
+  }
   amax = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(amax)));      // (none is negative; the lanes have their rows and scales)
   const float to = scale_for(amax);
   uint8_t* codes = h.codes + to_place.code + (static_cast<int64_t>(h.head) << a.page_shift) * D + col;
@@ -189,12 +204,8 @@ __device__ __forceinline__ void put_rows(const CompactArgs& a, const HeadOf& h, 
     uint4 x = r.x[p];
     const uint32_t was = __float_as_uint(r.s[p]), now = __float_as_uint(to);
     if (was != now) {
-      if ((was & 0x7FFFFFu) == 0) {
-        // the power 2^e, e = e0 + e1 (above 18 every code is 0, as none passes 448; from -24 on nothing is left of any)
-        const int e = min(max(static_cast<int>(was >> 23) - static_cast<int>(now >> 23), -24), 18), e0 = e >> 1, e1 = e - e0;
-        const uint32_t f = static_cast<uint32_t>(15 + e0) << 10, g = static_cast<uint32_t>(15 + e1) << 10;
-        const uint32_t f2 = f | f << 16, g2 = g | g << 16;
-        x = make_uint4(times_pow2(x.x, f2, g2), times_pow2(x.y, f2, g2), times_pow2(x.z, f2, g2), times_pow2(x.w, f2, g2));
+      if ((was & 0x7FFFFFu) == 0) {      // (above 2^18 every code is 0, as none passes 448; from 2^-24 on nothing is left of any)
+        x = times_pow2(x, min(max(static_cast<int>(was >> 23) - static_cast<int>(now >> 23), -24), 18));
       } else {      // (a scale that this library has not made, or below 2^-126)
         const float ratio = __fdiv_rn(r.s[p], to);
         x = make_uint4(times(x.x, ratio), times(x.y, ratio), times(x.z, ratio), times(x.w, ratio));
