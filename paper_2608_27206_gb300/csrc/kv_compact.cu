@@ -326,8 +326,8 @@ __global__ void __launch_bounds__(kSlideThreads) kv_slide_kernel(const __grid_co
 
 // In place, many blocks: a CTA per head's K or V, a warp per block of a round of kWideWarps.  All read a round's rows before one
 // writes them, and the next round's before they write: what a round overwrites are sources of rounds up to it.
-template <int D>
-__global__ void __launch_bounds__(32 * kWideWarps) kv_slide_wide_kernel(const __grid_constant__ CompactArgs a, int* status) {
+template <int D, int CTAS>
+__global__ void __launch_bounds__(32 * kWideWarps, CTAS) kv_slide_wide_kernel(const __grid_constant__ CompactArgs a, int* status) {
   __shared__ Source s_from[3][kWideWarps][kKvBlock];
   __shared__ int s_page[3][kWideWarps];
   ptx::begin_call();
@@ -339,7 +339,7 @@ __global__ void __launch_bounds__(32 * kWideWarps) kv_slide_wide_kernel(const __
   const HeadOf h = head_of(a, layer, static_cast<int>(blockIdx.y) - layer * 2 * a.heads);
   const int64_t first = k.base / kKvBlock, last = (static_cast<int64_t>(k.base) + k.count - 1) / kKvBlock;
   const int rounds = static_cast<int>((last - first) / kWideWarps) + 1;
-  auto look_up = [&](int round) {      // (three rounds' places: a warp may still write one round when another looks up the next but one)
+  auto look_up = [&](int round) {      // (three rounds' places: one is written, the next one's rows are fetched, and the one after is looked up)
     if (round >= rounds || tid >= kWideWarps * kKvBlock) return;
     const int64_t block = first + static_cast<int64_t>(round) * kWideWarps + tid / kKvBlock;
     if (block > last) return;
@@ -350,14 +350,15 @@ __global__ void __launch_bounds__(32 * kWideWarps) kv_slide_wide_kernel(const __
   auto block_of = [&](int round) { return first + static_cast<int64_t>(round) * kWideWarps + warp; };
   Rows<D> r, next;
   look_up(0);
+  look_up(1);
   __syncthreads();
   if (block_of(0) <= last) get_rows<D>(a, h, s_from[0][warp], next);
 #pragma unroll 1
   for (int round = 0; round < rounds; ++round) {
     r = next;
-    look_up(round + 1);
-    __syncthreads();      // every warp has this round's rows
+    __syncthreads();      // every warp has this round's rows, and the next one's places are known
     if (round + 1 < rounds && block_of(round + 1) <= last) get_rows<D>(a, h, s_from[(round + 1) % 3][warp], next);
+    look_up(round + 2);
     const int64_t block = block_of(round);
     const int page = block <= last ? s_page[round % 3][warp] : -1;
     if (page >= 0) put_rows<D>(a, h, r, place_of(a, page, block * kKvBlock, D), slots_of(k, block), status);
@@ -450,8 +451,9 @@ extern "C" pace_status_t pace_kv_compact(const pace_kv_cache* layers, int n_laye
           PACE_CHECK(launch_dependent(layers->head_dim == 128 ? kv_slide_kernel<128> : kv_slide_kernel<64>, dim3(nb, (tasks + warps - 1) / warps),
                                       kSlideThreads, 0, 1, stream, a, status));
         else
-          PACE_CHECK(launch_dependent(layers->head_dim == 128 ? kv_slide_wide_kernel<128> : kv_slide_wide_kernel<64>, dim3(nb, tasks), 32 * kWideWarps,
-                                      0, 1, stream, a, status));
+          // (28 layers of 4 heads: 75 us with two CTAs to an SM, 88 with one and more registers; 2 layers: 42 and 36)
+          PACE_CHECK(launch_dependent(layers->head_dim == 64 ? kv_slide_wide_kernel<64, 2> : nb * static_cast<int64_t>(tasks) > sms ? kv_slide_wide_kernel<128, 2> : kv_slide_wide_kernel<128, 1>,
+                                      dim3(nb, tasks), 32 * kWideWarps, 0, 1, stream, a, status));
       } else {
         int64_t blocks = 0;      // at most, wherever in a block a sequence's first token lands
         for (int i = 0; i < a.nb; ++i)
