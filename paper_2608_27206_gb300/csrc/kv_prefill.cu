@@ -44,6 +44,7 @@ constexpr int kHalf = 64;          // columns of S at a time
 constexpr float kMost = 32768.f;   // sum of 64 weights at which w moves
 constexpr int kAfter = 6;          // log2 of what that sum is when w has moved, at most (so the largest weight is 2^-1 at least)
 constexpr float kFar = 0x1p22f;    // a row's maximum from which on its scores are taken relative to one of them
+constexpr bool kOrder = true;
 constexpr uint32_t kTmem = 512;    // S of A and B, then O of A and B, 128 columns each
 
 template <int D>
@@ -57,13 +58,14 @@ struct PrefillCfg {
   static constexpr uint32_t SWIZZLE = D == 128 ? 2 : 4;
   static constexpr uint32_t GROUP = 8 * D;
   static constexpr uint32_t IDESC_HI = idesc_e4m3_f32(128, kKvTile, false, false), IDESC_LO = idesc_e4m3_f32(128, kKvTile, false, false, true);
+  static constexpr uint32_t HALF_HI = idesc_e4m3_f32(128, kHalf, false, false), HALF_LO = idesc_e4m3_f32(128, kHalf, false, false, true);
   static constexpr uint32_t IDESC_O = idesc_f16_mn_f32(128, D);
 };
 
 template <int D>
 struct alignas(16) PrefillCtl {
   static constexpr int ST = PrefillCfg<D>::STAGES, SV = PrefillCfg<D>::VSTAGES;
-  uint64_t full[ST], empty[ST], v_empty[SV], known[4], ready[2], vfree[2], s_full[2], p_full[2][2], q_full[2], o_done[2][2];
+  uint64_t full[ST], empty[ST], v_empty[SV], known[4], ready[2], vfree[2], s_full[2][2], p_full[2][2], q_full[2], o_done[2][2];
   float scales[ST][16];
   float4 block[4][8];           // of the last tiles, per block of 16 slots: K scale, log2(V scale), 1 / V scale
   uint32_t nan[2][4];           // slots of which some row sees a NaN value
@@ -125,7 +127,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
   auto known = [&](int b) { return smem_u32(&ctl->known[b]); };
   auto ready = [&](int b) { return smem_u32(&ctl->ready[b]); };
   auto vfree = [&](int b) { return smem_u32(&ctl->vfree[b]); };
-  auto s_full = [&](int i) { return smem_u32(&ctl->s_full[i]); };
+  auto s_full = [&](int i, int h) { return smem_u32(&ctl->s_full[i][h]); };
   auto p_full = [&](int i, int h) { return smem_u32(&ctl->p_full[i][h]); };
   auto q_full = [&](int i) { return smem_u32(&ctl->q_full[i]); };
   auto o_done = [&](int i, int h) { return smem_u32(&ctl->o_done[i][h]); };
@@ -149,8 +151,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
     for (int i = 0; i < 2; ++i) {
       mbar_init(ready(i), 2);
       mbar_init(vfree(i), 1);
-      mbar_init(s_full(i), 1);
       for (int h = 0; h < 2; ++h) {
+        mbar_init(s_full(i, h), 1);
         mbar_init(p_full(i, h), 4);
         mbar_init(o_done(i, h), 1);
       }
@@ -201,7 +203,18 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
         for (int k = 0; k < D / 32; ++k)
           mma_f8_ss(tmem + i * 128, q + static_cast<uint64_t>(part * (C::QTILE >> 4) + 2 * k), k0 + static_cast<uint64_t>(2 * k),
                     part == 0 ? C::IDESC_HI : C::IDESC_LO, part > 0 || k > 0, issue);
-      commit(s_full(i));
+      commit(s_full(i, 0));
+    };
+    auto half_scores = [&](int i, int h, int u) {      // 64 columns of it
+      const uint64_t q = dq + static_cast<uint64_t>(i * 2 * (C::QTILE >> 4));
+      const uint64_t k0 = dk + static_cast<uint64_t>((u % ST) * (C::TILE >> 4) + h * (kHalf * D >> 4));
+#pragma unroll
+      for (int part = 0; part < 2; ++part)
+#pragma unroll
+        for (int k = 0; k < D / 32; ++k)
+          mma_f8_ss(tmem + i * 128 + h * kHalf, q + static_cast<uint64_t>(part * (C::QTILE >> 4) + 2 * k), k0 + static_cast<uint64_t>(2 * k),
+                    part == 0 ? C::HALF_HI : C::HALF_LO, part > 0 || k > 0, issue);
+      commit(s_full(i, h));
     };
     while (ok && walk.next(a)) {
       const int n = it.t1 - it.t0, two = it.rows > 128;
@@ -210,7 +223,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
       for (int i = 0; i <= two; ++i) {
         if (!wait(q_full(i), i == 0 ? items_a++ : items_b++)) break;
         tc_fence_after_sync();
-        scores(i, t);
+        if constexpr (TREE) {
+          half_scores(i, 0, t);
+          half_scores(i, 1, t);
+        } else {
+          scores(i, t);
+        }
       }
       if (!ok) break;
       commit(empty(t % ST));
@@ -219,20 +237,31 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
       for (int u = t; ok && u < t + n; ++u) {
         const bool more = u + 1 < t + n;
         const uint64_t v = dv + static_cast<uint64_t>((u & 1) * (C::VTILE >> 4));
+        auto weigh = [&](int i, int h) {      // O += P V of half a slot tile
+          if (!wait(p_full(i, h), (i == 0 ? done_a : done_b) + u - t)) return;
+          tc_fence_after_sync();
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          if (!ok || i > two) break;
+          for (int k = 0; k < kHalf / 16; ++k)
+            mma_f16_ts(tmem + 256 + i * 128, tmem + i * 128 + h * kHalf + k * 8, v + static_cast<uint64_t>((h * 4 + k) * (2048 >> 4)), C::IDESC_O,
+                       u > t || h > 0 || k > 0, issue);
+          commit(o_done(i, h));
+        };
+        if constexpr (TREE) {
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            if (!wait(p_full(i, h), (i == 0 ? done_a : done_b) + u - t)) break;
-            tc_fence_after_sync();
-#pragma unroll
-            for (int k = 0; k < kHalf / 16; ++k)
-              mma_f16_ts(tmem + 256 + i * 128, tmem + i * 128 + h * kHalf + k * 8, v + static_cast<uint64_t>((h * 4 + k) * (2048 >> 4)), C::IDESC_O,
-                         u > t || h > 0 || k > 0, issue);
-            commit(o_done(i, h));
+          for (int part = 0; part < 4; ++part) {
+            const int i = kOrder ? part & 1 : part >> 1, h = kOrder ? part >> 1 : part & 1;
+            if (!ok || i > two) continue;
+            weigh(i, h);
+            if (ok && more) half_scores(i, h, u + 1);
           }
-          if (ok && more) scores(i, u + 1);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            if (!ok || i > two) break;
+            weigh(i, 0);
+            if (ok) weigh(i, 1);
+            if (ok && more) scores(i, u + 1);
+          }
         }
         if (!ok) break;
         commit(vfree(u & 1));
@@ -410,8 +439,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
           slot0 = it.span.tile(it.t0 + (g >> 1)) * kKvTile;
           whole = kv_whole(slot0, p_lo, p_hi, a.window, a.sinks);
           // (S first: a row tile that left items out may be rounds ahead of the others until its products run)
-          ok = kv_wait(s_full(i), (mine + (g >> 1)) & 1) && kv_wait(known(u & 3), (u >> 2) & 1) && (whole || kv_wait(ready(b), (u >> 1) & 1));
+          ok = kv_wait(s_full(i, 0), (mine + (g >> 1)) & 1) && kv_wait(known(u & 3), (u >> 2) & 1) && (whole || kv_wait(ready(b), (u >> 1) & 1));
           ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          tc_fence_after_sync();
+        } else if (TREE) {
+          ok = __all_sync(0xffffffffu, kv_wait(s_full(i, 1), (mine + (g >> 1)) & 1));
           if (!ok) break;
           tc_fence_after_sync();
         }
@@ -506,8 +539,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
             l *= f;
             peak = 0.f;
             if (g > 0) {
-              // (S of the tile is complete, so the products of the tiles before are)
+              // (S of the tile is complete, so the products of the tiles before are; of half a tile, those of the half before it need not be)
               if (h == 1) ok = __all_sync(0xffffffffu, kv_wait(o_done(i, 0), (mine + (g >> 1)) & 1));
+              else if (TREE) ok = __all_sync(0xffffffffu, kv_wait(o_done(i, 1), (mine + (g >> 1) - 1) & 1));
               if (!ok) break;
               tc_fence_after_sync();
 #pragma unroll 1
