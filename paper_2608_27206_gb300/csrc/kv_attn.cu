@@ -28,36 +28,53 @@ pace_status_t make_map(CUtensorMap* m, const pace_kv_cache* c, void* codes) {
   return r == CUDA_SUCCESS ? PACE_OK : PACE_ERR_INVALID_ARG;
 }
 
-// Sequences of at most kFewRows query rows per KV head take the transposed products of kv_decode.cu.
-constexpr int kFewRows = 32;
+// Sequences of at most so many query rows per KV head take the transposed products of kv_decode.cu, trees up to kFewNodes of them: with 17
+// to 32 the two halves of a CTA of kv_prefill.cu are faster (64 trees of 28 rows on 5001-28007 slots 230 us against 424, 8 on
+// 700-9000 30 against 36), below they are not (14 rows: 214 us against 229).
+constexpr int kFewRows = 32, kFewNodes = 16;
+// Trees of few rows go with the others in one launch where that gives the others this many slot tiles more at most (a launch of their own
+// and its join cost 14 us, a slot tile 1.5 us of a CTA).
+constexpr int kAlong = 8 * kPlanCtas;
 
 // Rows of a tile for few-row sequences: 8, 16 or 32, what the largest needs (0: there are none).
-int few_rows(const int32_t* cu_q, int B, int group) {
+int few_rows(const int32_t* cu_q, int B, int group, int limit) {
   int most = 0;
   for (int b = 0; b < B; ++b) {
     const int64_t rows = static_cast<int64_t>(cu_q[b + 1] - cu_q[b]) * group;
-    if (rows <= kFewRows) most = std::max(most, static_cast<int>(rows));
+    if (rows <= limit) most = std::max(most, static_cast<int>(rows));
   }
   return most == 0 ? 0 : most <= 8 ? 8 : most <= 16 ? 16 : 32;
 }
 
 // Rows of the call's largest tile.
-int most_rows(const int32_t* cu_q, int B, int group) {
+int most_rows(const int32_t* cu_q, int B, int group, int limit) {
   for (int b = 0; b < B; ++b)
-    if (static_cast<int64_t>(cu_q[b + 1] - cu_q[b]) * group > kFewRows) return kManyRows;
-  return few_rows(cu_q, B, group);
+    if (static_cast<int64_t>(cu_q[b + 1] - cu_q[b]) * group > limit) return kManyRows;
+  return few_rows(cu_q, B, group, limit);
 }
 
 int64_t slot_tiles(int max_len) { return std::max(1, (max_len + kKvTile - 1) / kKvTile); }
 
+// Most rows of the sequences that kv_decode.cu takes in a call.
+int few_limit(const int32_t* cu_q, int B, int group, int heads, int max_len, bool tree) {
+  if (!tree) return kFewRows;
+  int64_t few = 0, many = 0;
+  for (int b = 0; b < B; ++b) {
+    const int64_t rows = static_cast<int64_t>(cu_q[b + 1] - cu_q[b]) * group;
+    few += rows > 0 && rows <= kFewNodes;
+    many += rows > kFewNodes;
+  }
+  return many > 0 && few * heads * slot_tiles(max_len) <= kAlong ? 0 : kFewNodes;
+}
+
 // The sequences of a form that the next launch takes, from b on (b: the first that it leaves); its row tiles.
-int64_t next_launch(const int32_t* cu_q, int B, int group, bool is_few, int rows, int& b, KvSeqs* s) {
+int64_t next_launch(const int32_t* cu_q, int B, int group, int limit, bool is_few, int rows, int& b, KvSeqs* s) {
   int64_t tiles = 0;
   int nb = 0;
   for (; b < B && nb < kKvMaxB; ++b) {
     const int n = cu_q[b + 1] - cu_q[b];
     const int64_t r = static_cast<int64_t>(n) * group;
-    if (n == 0 || (r <= kFewRows) != is_few) continue;
+    if (n == 0 || (r <= limit) != is_few) continue;
     tiles += (r + rows - 1) / rows;
     if (s != nullptr) {
       s->seq[nb] = b;
@@ -75,17 +92,18 @@ int64_t next_launch(const int32_t* cu_q, int B, int group, bool is_few, int rows
 }
 
 // What the size query and the call refuse alike, and before anything is launched.
-pace_status_t check_attention(const pace_kv_cache* cache, const int32_t* cu_q, int B, int n_q_heads, int max_len) {
+pace_status_t check_attention(const pace_kv_cache* cache, const int32_t* cu_q, int B, int n_q_heads, int max_len, bool tree) {
   PACE_CHECK(check_cache(cache));
   PACE_CHECK(check_prefix(cu_q, B));
   if (n_q_heads < 1 || n_q_heads % cache->n_kv_heads != 0 || n_q_heads / cache->n_kv_heads > kKvMaxGroup) return PACE_ERR_INVALID_ARG;
   if (max_len < 0 || max_len > (1 << 30)) return PACE_ERR_INVALID_ARG;
   const int group = n_q_heads / cache->n_kv_heads;
   if (cu_q[B] > (1 << 30) / group) return PACE_ERR_INVALID_ARG;
+  const int limit = few_limit(cu_q, B, group, cache->n_kv_heads, max_len, tree);
   const int64_t most = INT32_MAX / (cache->n_kv_heads * (slot_tiles(max_len) + kItemCost));      // row tiles of a launch
   for (const bool is_few : {true, false})
     for (int b = 0; b < B;)
-      if (next_launch(cu_q, B, group, is_few, is_few ? few_rows(cu_q, B, group) : kManyRows, b, nullptr) > most) return PACE_ERR_INVALID_ARG;
+      if (next_launch(cu_q, B, group, limit, is_few, is_few ? few_rows(cu_q, B, group, limit) : kManyRows, b, nullptr) > most) return PACE_ERR_INVALID_ARG;
   return PACE_OK;
 }
 
@@ -117,8 +135,9 @@ pace_status_t check_tree(const int32_t* cu_q, int B) {
 }
 
 size_t workspace_size(const pace_kv_cache* cache, const int32_t* cu_q, int B, int n_q_heads, int max_len, bool tree) {
-  if (B <= 0 || check_attention(cache, cu_q, B, n_q_heads, max_len) != PACE_OK || (tree && check_tree(cu_q, B) != PACE_OK)) return 0;
-  return workspace(most_rows(cu_q, B, n_q_heads / cache->n_kv_heads), cache->head_dim, cu_q, B, tree).total;
+  if (B <= 0 || check_attention(cache, cu_q, B, n_q_heads, max_len, tree) != PACE_OK || (tree && check_tree(cu_q, B) != PACE_OK)) return 0;
+  const int group = n_q_heads / cache->n_kv_heads, limit = few_limit(cu_q, B, group, cache->n_kv_heads, max_len, tree);
+  return workspace(most_rows(cu_q, B, group, limit), cache->head_dim, cu_q, B, tree).total;
 }
 
 // Both calls; parents null: the queries follow one another.
@@ -127,7 +146,7 @@ pace_status_t attend(const pace_kv_cache* cache, const void* Q, int64_t q_row_st
                      float scale, int window, int sinks, void* out, float* lse, void* ws, size_t ws_bytes, cudaStream_t stream) {
   if (B < 0) return PACE_ERR_INVALID_ARG;
   if (B == 0) return PACE_OK;
-  PACE_CHECK(check_attention(cache, cu_q, B, n_q_heads, max_len));
+  PACE_CHECK(check_attention(cache, cu_q, B, n_q_heads, max_len, tree));
   if (tree) PACE_CHECK(check_tree(cu_q, B));
   if (cu_q[B] == 0) return PACE_OK;
   if (tree && (parents == nullptr || reinterpret_cast<uintptr_t>(parents) % 4 != 0)) return PACE_ERR_INVALID_ARG;
@@ -137,8 +156,8 @@ pace_status_t attend(const pace_kv_cache* cache, const void* Q, int64_t q_row_st
   if (seq_lens == nullptr || block_table == nullptr || table_stride < 1 || table_stride > INT32_MAX || sinks < 0) return PACE_ERR_INVALID_ARG;
   if (max_len > table_stride * cache->page_size) return PACE_ERR_INVALID_ARG;
   if (!(scale > 0.f) || !std::isfinite(scale)) return PACE_ERR_INVALID_ARG;
-  const int few = few_rows(cu_q, B, group);
-  const Workspace w = workspace(most_rows(cu_q, B, group), D, cu_q, B, tree);
+  const int limit = few_limit(cu_q, B, group, cache->n_kv_heads, max_len, tree), few = few_rows(cu_q, B, group, limit);
+  const Workspace w = workspace(most_rows(cu_q, B, group, limit), D, cu_q, B, tree);
   if (ws == nullptr || reinterpret_cast<uintptr_t>(ws) % 16 != 0 || ws_bytes < w.total) return PACE_ERR_WORKSPACE;
   PACE_CHECK(check_device());
   KvMaps maps;
@@ -177,7 +196,7 @@ pace_status_t attend(const pace_kv_cache* cache, const void* Q, int64_t q_row_st
   for (const bool is_few : {true, false}) {
     const int rows = is_few ? few : kManyRows;
     for (int b = 0; b < B;) {
-      const int64_t tiles = next_launch(cu_q, B, group, is_few, rows, b, &a.s);
+      const int64_t tiles = next_launch(cu_q, B, group, limit, is_few, rows, b, &a.s);
       if (tiles == 0) break;
       const unsigned grid = static_cast<unsigned>(std::min<int64_t>({tiles * cache->n_kv_heads * slot_tiles(max_len), sms, kPlanCtas}));
       if (is_few) PACE_CHECK(launch_kv_decode(maps, a, D, rows, grid, status, stream));

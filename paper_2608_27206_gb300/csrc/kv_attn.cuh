@@ -341,7 +341,8 @@ __device__ __forceinline__ void load_cols(uint32_t addr, uint32_t (&v)[N]) {
   }
 }
 
-// The rings that warp 0 fills: ST places of a K tile, SV of a V tile, `stride` bytes apart.
+// The rings that warp 0 fills: ST places of a K tile, SV of a V tile, `stride` bytes apart.  JOINT: one ring of ST + SV places, K and V of
+// a tile one after the other (`k`, `empty`; two arrivals free a place).
 struct KvRings {
   uint8_t* k;
   uint8_t* v;
@@ -354,7 +355,7 @@ struct KvRings {
 
 // Warp 0 of a CTA: fetches the slot tiles of its share, K and V in boxes of a page, at most 128 rows, each by TMA; the tile's 8 K
 // and 8 V scales by 4-byte copies.
-template <int D, int ST, int SV, typename Walk>
+template <int D, int ST, int SV, bool JOINT = false, typename Walk>
 __device__ __forceinline__ void kv_fetch(const KvMaps& maps, const KvAttnArgs& a, Walk& walk, const KvRings& ring, int* abort,
                                          int* status) {
   using namespace ptx;
@@ -390,8 +391,16 @@ __device__ __forceinline__ void kv_fetch(const KvMaps& maps, const KvAttnArgs& a
         page = 0;      // (the sequence's results mean nothing then; the copy stays inside the cache)
       }
       const int s = t % ST, v = t % SV;
-      bool ok = t < ST || kv_wait(smem_u32(&ring.empty[s]), (t / ST - 1) & 1);
-      if (ring.v_empty != nullptr) ok = ok && (t < SV || kv_wait(smem_u32(&ring.v_empty[v]), (t / SV - 1) & 1));
+      constexpr int PLACES = ST + SV;
+      static_assert(!JOINT || 2 * ST > PLACES, "a tile's barrier is not used again before the tile that had it is done with");
+      bool ok;
+      if constexpr (JOINT) {
+        ok = 2 * t < PLACES || kv_wait(smem_u32(&ring.empty[2 * t % PLACES]), (2 * t / PLACES - 1) & 1);
+        ok = ok && (2 * t + 1 < PLACES || kv_wait(smem_u32(&ring.empty[(2 * t + 1) % PLACES]), ((2 * t + 1) / PLACES - 1) & 1));
+      } else {
+        ok = t < ST || kv_wait(smem_u32(&ring.empty[s]), (t / ST - 1) & 1);
+        if (ring.v_empty != nullptr) ok = ok && (t < SV || kv_wait(smem_u32(&ring.v_empty[v]), (t / SV - 1) & 1));
+      }
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) {
         if (lane == 0) stop(abort, status);
@@ -411,8 +420,10 @@ __device__ __forceinline__ void kv_fetch(const KvMaps& maps, const KvAttnArgs& a
       __syncwarp();
       if (lane < boxes && there) {
         const int y = (it.head << a.c.page_shift) + ((slot0 + lane * box_rows) & ((1 << a.c.page_shift) - 1));
-        tma_load_3d(smem_u32(ring.k + s * ring.stride + lane * box_rows * D), &maps.k, 0, y, page, smem_u32(&ring.full[s]));
-        tma_load_3d(smem_u32(ring.v + v * ring.stride + lane * box_rows * D), &maps.v, 0, y, page, smem_u32(&ring.full[s]));
+        uint8_t* k_to = ring.k + (JOINT ? 2 * t % PLACES : s) * ring.stride;
+        uint8_t* v_to = JOINT ? ring.k + (2 * t + 1) % PLACES * ring.stride : ring.v + v * ring.stride;
+        tma_load_3d(smem_u32(k_to + lane * box_rows * D), &maps.k, 0, y, page, smem_u32(&ring.full[s]));
+        tma_load_3d(smem_u32(v_to + lane * box_rows * D), &maps.v, 0, y, page, smem_u32(&ring.full[s]));
       }
     }
   }

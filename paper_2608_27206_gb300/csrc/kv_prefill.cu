@@ -44,7 +44,6 @@ constexpr int kHalf = 64;          // columns of S at a time
 constexpr float kMost = 32768.f;   // sum of 64 weights at which w moves
 constexpr int kAfter = 6;          // log2 of what that sum is when w has moved, at most (so the largest weight is 2^-1 at least)
 constexpr float kFar = 0x1p22f;    // a row's maximum from which on its scores are taken relative to one of them
-constexpr bool kOrder = true;
 constexpr uint32_t kTmem = 512;    // S of A and B, then O of A and B, 128 columns each
 
 template <int D>
@@ -65,10 +64,11 @@ struct PrefillCfg {
 template <int D>
 struct alignas(16) PrefillCtl {
   static constexpr int ST = PrefillCfg<D>::STAGES, SV = PrefillCfg<D>::VSTAGES;
-  uint64_t full[ST], empty[ST], v_empty[SV], known[4], ready[2], vfree[2], s_full[2][2], p_full[2][2], q_full[2], o_done[2][2];
+  uint64_t full[ST], empty[ST + SV], v_empty[SV], known[4], ready[2], vfree[2], s_full[2][2], p_full[2][2], q_full[2], o_done[2][2], x_full[2], x_read[2];
   float scales[ST][16];
   float4 block[4][8];           // of the last tiles, per block of 16 slots: K scale, log2(V scale), 1 / V scale
   uint32_t nan[2][4];           // slots of which some row sees a NaN value
+  float4 state[2][128];         // of the rows of a pair's halves: m, w, l, far
   int scan[2 * kThreads / 32];
   KvShare share;
   uint32_t tmem;
@@ -80,9 +80,20 @@ __device__ __forceinline__ bool kv_whole(int slot0, int p_all, int p_last, int w
   return slot0 + kKvTile - 1 <= p_all && (window <= 0 || slot0 > p_last - window || slot0 + kKvTile <= sinks);
 }
 
+// Of a tree: whether A and B take every other slot tile of an item that has one row tile.
+constexpr int kPairTiles = 8;
+template <bool TREE>
+__device__ __forceinline__ bool kv_pair(const KvItem& it) { return TREE && it.rows <= 128 && it.t1 - it.t0 >= kPairTiles; }
+
 __device__ __forceinline__ uint32_t f16x2(float lo, float hi) {
   uint32_t r;
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+__device__ __forceinline__ uint32_t bf16x2(uint32_t lo, uint32_t hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(__uint_as_float(hi)), "f"(__uint_as_float(lo)));
   return r;
 }
 
@@ -113,7 +124,7 @@ template <int D, bool TREE>
 __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_constant__ KvMaps maps, const __grid_constant__ KvAttnArgs a,
                                                                  int* status) {
   using C = PrefillCfg<D>;
-  constexpr int ST = C::STAGES;
+  constexpr int ST = C::STAGES, PLACES = ST + C::VSTAGES;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* sK = smem;                              // K tiles, as codes
@@ -131,6 +142,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
   auto p_full = [&](int i, int h) { return smem_u32(&ctl->p_full[i][h]); };
   auto q_full = [&](int i) { return smem_u32(&ctl->q_full[i]); };
   auto o_done = [&](int i, int h) { return smem_u32(&ctl->o_done[i][h]); };
+  auto x_full = [&](int i) { return smem_u32(&ctl->x_full[i]); };
+  auto x_read = [&](int i) { return smem_u32(&ctl->x_read[i]); };
 
   kv_begin<TREE>(a);
   const KvShare share = kv_share<kManyRows, D, TREE>(a, ctl->scan, &ctl->share, status);
@@ -142,10 +155,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
   if (warp == 0 && lane == 0) {
     prefetch_tensormap(&maps.k);
     prefetch_tensormap(&maps.v);
-    for (int s = 0; s < ST; ++s) {
-      mbar_init(full(s), 33);
-      mbar_init(empty(s), 1);
-    }
+    for (int s = 0; s < ST; ++s) mbar_init(full(s), 33);
+    for (int s = 0; s < (TREE ? PLACES : ST); ++s) mbar_init(empty(s), TREE ? 2 : 1);
     for (int s = 0; s < C::VSTAGES; ++s) mbar_init(smem_u32(&ctl->v_empty[s]), 2);
     for (int b = 0; b < 4; ++b) mbar_init(known(b), 1);
     for (int i = 0; i < 2; ++i) {
@@ -157,6 +168,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
         mbar_init(o_done(i, h), 1);
       }
       mbar_init(q_full(i), 4);
+      mbar_init(x_full(i), 4);
+      mbar_init(x_read(i), 4);
     }
     fence_mbar_init();
     ctl->abort = 0;
@@ -173,7 +186,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
   if (warp == 0) {
     KvWalk<kManyRows, TREE> walk;
     walk.begin(share);
-    kv_fetch<D, ST, C::VSTAGES>(maps, a, walk, KvRings{sK, sC, C::TILE, ctl->full, ctl->empty, ctl->v_empty, ctl->scales}, &ctl->abort, status);
+    kv_fetch<D, ST, C::VSTAGES, TREE>(maps, a, walk, KvRings{sK, sC, C::TILE, ctl->full, ctl->empty, ctl->v_empty, ctl->scales}, &ctl->abort, status);
   } else if (warp == 1) {
     // ---- products: P V of a slot tile, half by half as the weights come, then S of the next; A and B in turn ----------
     // The warp stays converged: operands of these instructions are registers of the whole warp, and in one lane's branch each took 80
@@ -194,9 +207,17 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
     auto commit = [&](uint32_t bar) {
       if (issue) mma_commit(bar);
     };
+    auto release = [&](int u) {      // the place of K of slot tile u
+      if constexpr (TREE) {
+        commit(empty(2 * u % PLACES));
+        commit(empty(2 * u % PLACES));
+      } else {
+        commit(empty(u % ST));
+      }
+    };
     auto scores = [&](int i, int u) {      // S of slot tile u
       const uint64_t q = dq + static_cast<uint64_t>(i * 2 * (C::QTILE >> 4));
-      const uint64_t k0 = dk + static_cast<uint64_t>((u % ST) * (C::TILE >> 4));
+      const uint64_t k0 = dk + static_cast<uint64_t>((TREE ? 2 * u % PLACES : u % ST) * (C::TILE >> 4));
 #pragma unroll
       for (int part = 0; part < 2; ++part)
 #pragma unroll
@@ -207,7 +228,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
     };
     auto half_scores = [&](int i, int h, int u) {      // 64 columns of it
       const uint64_t q = dq + static_cast<uint64_t>(i * 2 * (C::QTILE >> 4));
-      const uint64_t k0 = dk + static_cast<uint64_t>((u % ST) * (C::TILE >> 4) + h * (kHalf * D >> 4));
+      const uint64_t k0 = dk + static_cast<uint64_t>((TREE ? 2 * u % PLACES : u % ST) * (C::TILE >> 4) + h * (kHalf * D >> 4));
 #pragma unroll
       for (int part = 0; part < 2; ++part)
 #pragma unroll
@@ -216,8 +237,52 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                     part == 0 ? C::HALF_HI : C::HALF_LO, part > 0 || k > 0, issue);
       commit(s_full(i, h));
     };
+    auto both_scores = [&](int i, int u) {      // whole, for owners who wait for halves
+      scores(i, u);
+      commit(s_full(i, 1));
+    };
+    auto weigh = [&](int i, int h, int u, int round, bool first) {      // O += P V of half a slot tile
+      if (!wait(p_full(i, h), round)) return;
+      tc_fence_after_sync();
+      const uint64_t v = dv + static_cast<uint64_t>((u & 1) * (C::VTILE >> 4));
+#pragma unroll
+      for (int k = 0; k < kHalf / 16; ++k)
+        mma_f16_ts(tmem + 256 + i * 128, tmem + i * 128 + h * kHalf + k * 8, v + static_cast<uint64_t>((h * 4 + k) * (2048 >> 4)), C::IDESC_O,
+                   !first || h > 0 || k > 0, issue);
+      commit(o_done(i, h));
+    };
     while (ok && walk.next(a)) {
       const int n = it.t1 - it.t0, two = it.rows > 128;
+      if (kv_pair<TREE>(it)) {
+        if (!wait(full(t % ST), t / ST) || !wait(q_full(0), items_a++)) break;
+        tc_fence_after_sync();
+        both_scores(0, t);
+        release(t);
+        if (!wait(full((t + 1) % ST), (t + 1) / ST) || !wait(q_full(1), items_b++)) break;
+        tc_fence_after_sync();
+        both_scores(1, t + 1);
+        release(t + 1);
+#pragma unroll 1
+        for (int u = t; ok && u < t + n; ++u) {
+          const bool more = u + 2 < t + n;
+          const int k = u - t, i = k & 1, round = (i == 0 ? done_a : done_b) + (k >> 1);
+          if (!wait(ready(u & 1), u >> 1)) break;
+          weigh(i, 0, u, round, k < 2);
+          if (more && (!ok || !wait(full((u + 2) % ST), (u + 2) / ST))) break;
+          if (more) half_scores(i, 0, u + 2);
+          if (ok) weigh(i, 1, u, round, k < 2);
+          if (!ok) break;
+          commit(vfree(u & 1));
+          if (more) {
+            half_scores(i, 1, u + 2);
+            release(u + 2);
+          }
+        }
+        t += n;
+        done_a += (n + 1) >> 1;
+        done_b += n >> 1;
+        continue;
+      }
       if (!wait(full(t % ST), t / ST)) break;
 #pragma unroll 1
       for (int i = 0; i <= two; ++i) {
@@ -231,42 +296,32 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
         }
       }
       if (!ok) break;
-      commit(empty(t % ST));
+      release(t);
       if ((n > 1 && !wait(full((t + 1) % ST), (t + 1) / ST)) || !wait(ready(t & 1), t >> 1)) break;
 #pragma unroll 1
       for (int u = t; ok && u < t + n; ++u) {
         const bool more = u + 1 < t + n;
-        const uint64_t v = dv + static_cast<uint64_t>((u & 1) * (C::VTILE >> 4));
-        auto weigh = [&](int i, int h) {      // O += P V of half a slot tile
-          if (!wait(p_full(i, h), (i == 0 ? done_a : done_b) + u - t)) return;
-          tc_fence_after_sync();
-#pragma unroll
-          for (int k = 0; k < kHalf / 16; ++k)
-            mma_f16_ts(tmem + 256 + i * 128, tmem + i * 128 + h * kHalf + k * 8, v + static_cast<uint64_t>((h * 4 + k) * (2048 >> 4)), C::IDESC_O,
-                       u > t || h > 0 || k > 0, issue);
-          commit(o_done(i, h));
-        };
         if constexpr (TREE) {
 #pragma unroll
           for (int part = 0; part < 4; ++part) {
-            const int i = kOrder ? part & 1 : part >> 1, h = kOrder ? part >> 1 : part & 1;
+            const int i = part & 1, h = part >> 1;
             if (!ok || i > two) continue;
-            weigh(i, h);
+            weigh(i, h, u, (i == 0 ? done_a : done_b) + u - t, u == t);
             if (ok && more) half_scores(i, h, u + 1);
           }
         } else {
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             if (!ok || i > two) break;
-            weigh(i, 0);
-            if (ok) weigh(i, 1);
+            weigh(i, 0, u, (i == 0 ? done_a : done_b) + u - t, u == t);
+            if (ok) weigh(i, 1, u, (i == 0 ? done_a : done_b) + u - t, u == t);
             if (ok && more) scores(i, u + 1);
           }
         }
         if (!ok) break;
         commit(vfree(u & 1));
         if (more) {
-          commit(empty((u + 1) % ST));
+          release(u + 1);
           if ((u + 2 < t + n && !wait(full((u + 2) % ST), (u + 2) / ST)) || !wait(ready((u + 1) & 1), (u + 1) >> 1)) break;
         }
       }
@@ -308,7 +363,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
         for (int part = warp - 2; part < 4; part += 2) {
           const int row = part * 32 + lane, slot = slot0 + row;      // a slot of the tile
           const bool any = slot <= it.p_last && (a.window <= 0 || slot > it.p_first - a.window || slot < a.sinks);
-          const uint8_t* src = sC + (t % C::VSTAGES) * C::TILE + row * D;
+          const uint8_t* src = (TREE ? sK + (2 * t + 1) % PLACES * C::TILE : sC + (t % C::VSTAGES) * C::TILE) + row * D;
           uint4 u[D / 16];
 #pragma unroll
           for (int e = 0; e < D / 16; ++e) u[e] = *reinterpret_cast<const uint4*>(src + (e ^ (D == 128 ? row & 7 : (row >> 1) & 3)) * 16);
@@ -343,7 +398,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
         __syncwarp();
         if (lane == 0) {
           mbar_arrive(ready(b));
-          mbar_arrive(smem_u32(&ctl->v_empty[t % C::VSTAGES]));
+          mbar_arrive(TREE ? empty((2 * t + 1) % PLACES) : smem_u32(&ctl->v_empty[t % C::VSTAGES]));
         }
       }
     }
@@ -356,18 +411,20 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
     KvWalk<kManyRows, TREE> walk;
     walk.begin(share);
     const KvItem& it = walk.it;
-    int t = 0, mine = 0;      // slot tiles of the CTA, of this row tile
+    int t = 0, mine = 0, joins = 0;      // slot tiles of the CTA, of this row tile; pairs joined
     bool ok = true;
     while (ok && walk.next(a)) {
-      if (i == 1 && it.rows <= 128) {
-        t += it.t1 - it.t0;
+      const int n = it.t1 - it.t0;
+      const bool pair = kv_pair<TREE>(it);
+      if (i == 1 && it.rows <= 128 && !pair) {
+        t += n;
         continue;
       }
-      const int row = i * 128 + me;
+      const int row0 = pair ? 0 : i * 128, row = row0 + me;
       const bool real = row < it.rows;
       auto slot_of = [&](int r) { return it.p0 + static_cast<int>(a.by_group(it.row0 + min(r, it.rows - 1))); };
       int p = slot_of(row);      // of the row (of a tree's node: its position)
-      const int p_lo = TREE ? it.p_all : slot_of(i * 128), p_hi = slot_of(i * 128 + 127);      // of the tile's first and last
+      const int p_lo = TREE ? it.p_all : slot_of(row0), p_hi = slot_of(row0 + 127);      // of the tile's first and last
       int64_t node = 0;
       if constexpr (TREE) {
         node = a.s.q0[it.i] + p - it.p0;
@@ -428,15 +485,15 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
       // and m a score of the row that is the largest so far to within 2^20, so that what w is about is small again.
       bool far = false;
       float m = 0.f;      // (0 of other rows)
-      const int n = it.t1 - it.t0;
+      const int n_mine = pair ? (n + 1 - i) >> 1 : n;
       int slot0 = 0;
       bool whole = true;
 #pragma unroll 1
-      for (int g = 0; g < 2 * n; ++g) {      // half tiles
-        const int h = g & 1, u = t + (g >> 1), b = u & 1;
+      for (int g = 0; g < 2 * n_mine; ++g) {      // half tiles
+        const int h = g & 1, v = pair ? i + (g & ~1) : g >> 1, u = t + v, b = u & 1;
         const uint32_t sX = sS + h * kHalf;
         if (h == 0) {
-          slot0 = it.span.tile(it.t0 + (g >> 1)) * kKvTile;
+          slot0 = it.span.tile(it.t0 + v) * kKvTile;
           whole = kv_whole(slot0, p_lo, p_hi, a.window, a.sinks);
           // (S first: a row tile that left items out may be rounds ahead of the others until its products run)
           ok = kv_wait(s_full(i, 0), (mine + (g >> 1)) & 1) && kv_wait(known(u & 3), (u >> 2) & 1) && (whole || kv_wait(ready(b), (u >> 1) & 1));
@@ -604,15 +661,76 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
       }
       if (!ok) break;
       t += n;
-      mine += n;
+      mine += n_mine;
       // ---- the item's (part of the) output -----------------------------------------------------
       ok = __all_sync(0xffffffffu, kv_wait(o_done(i, 1), (mine - 1) & 1));
       if (!ok) break;
       tc_fence_after_sync();
-      const float inv = l == 0.f ? 0.f : 1.f / l, rel = l == 0.f ? -INFINITY : log2f(l);
       const bool complete = it.t0 == 0 && it.t1 == it.span.n;
       const int64_t slot = (2 * static_cast<int64_t>(blockIdx.x) + (it.t0 == 0 ? 1 : 0)) * kManyRows + row;
       const int64_t at = complete ? kv_out_row(a, it, real ? row : 0) : slot;
+      if (pair) {
+        // A ends the first half of the columns and B the second, each with what the other leaves of them in its q tile (its products have
+        // completed): out = (O f + O' f') / (l f + l' f'), f = 2^(its base less the larger one)
+        constexpr int HALF = D / 2, CHUNKS = HALF / 4;      // columns, and their 16-byte chunks in a row
+        auto left = [&](int whose, int chunk) { return reinterpret_cast<float4*>(sQ + whose * 2 * C::QTILE + me * HALF * 4 + ((chunk ^ (me & (CHUNKS - 1))) * 16)); };
+#pragma unroll 1
+        for (int q = 0; q < HALF / 32; ++q) {
+          uint32_t o[32];
+          load_cols(sO + (1 - i) * HALF + 32 * q, o);
+#pragma unroll
+          for (int e = 0; e < 32; e += 4)
+            *left(i, 8 * q + e / 4) = make_float4(__uint_as_float(o[e]), __uint_as_float(o[e + 1]), __uint_as_float(o[e + 2]), __uint_as_float(o[e + 3]));
+        }
+        ctl->state[i][me] = make_float4(m, w, l, far ? 1.f : 0.f);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(x_full(i));
+        ok = __all_sync(0xffffffffu, kv_wait(x_full(1 - i), joins & 1));
+        if (!ok) break;
+        const float4 its = ctl->state[1 - i][me];
+        const float apart = l == 0.f ? -INFINITY : its.z == 0.f ? INFINITY : (m - its.x) + (w - its.y);      // (one that saw nothing has no say)
+        const bool first = !(apart < 0.f);
+        const float f = first ? 1.f : exp2f(apart), f2 = first ? exp2f(-apart) : 1.f;
+        const float sum = (l == 0.f ? 0.f : l * f) + (its.z == 0.f ? 0.f : its.z * f2);
+        const float by = l == 0.f ? 0.f : f / sum, by2 = its.z == 0.f ? 0.f : f2 / sum;
+#pragma unroll 1
+        for (int q = 0; q < HALF / 32; ++q) {
+          uint32_t o[32];
+          load_cols(sO + i * HALF + 32 * q, o);
+#pragma unroll
+          for (int e = 0; e < 32; e += 4) {
+            const float4 x = *left(1 - i, 8 * q + e / 4);
+            const float y[4] = {x.x, x.y, x.z, x.w};
+            // (a half that saw nothing is zero, whatever its accumulator holds)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              o[e + k] = __float_as_uint((l == 0.f ? 0.f : __uint_as_float(o[e + k]) * by) + (its.z == 0.f ? 0.f : y[k] * by2));
+          }
+          if (real && complete) {
+#pragma unroll
+            for (int e = 0; e < 32; e += 8)
+              *reinterpret_cast<uint4*>(a.out + at * D + i * HALF + 32 * q + e) =
+                  make_uint4(bf16x2(o[e], o[e + 1]), bf16x2(o[e + 2], o[e + 3]), bf16x2(o[e + 4], o[e + 5]), bf16x2(o[e + 6], o[e + 7]));
+          } else if (real) {
+#pragma unroll
+            for (int e = 0; e < 32; e += 4) *reinterpret_cast<uint4*>(a.part + slot * D + i * HALF + 32 * q + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+          }
+        }
+        if (real && i == 0) {
+          const float rel = sum == 0.f ? -INFINITY : log2f(sum), base = first ? w : its.y, top = first ? m : its.x;
+          const bool high = first ? far : its.w != 0.f;
+          if (!complete) a.part_lse[slot] = high ? make_float2(top, base + rel) : make_float2(base, rel);
+          else if (a.lse != nullptr) a.lse[at] = (top + (base + rel)) * 0.69314718055994531f;
+        }
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(x_read(1 - i));
+        ok = __all_sync(0xffffffffu, kv_wait(x_read(i), joins & 1));      // (the next q goes where the other reads)
+        if (!ok) break;
+        ++joins;
+        continue;
+      }
+      const float inv = l == 0.f ? 0.f : 1.f / l, rel = l == 0.f ? -INFINITY : log2f(l);
       // complete rows go out by way of the q tile, which is done with (this warp's rows), so that lanes write side by side
 #pragma unroll 1
       for (int q = 0; q < D / 32; ++q) {
