@@ -178,7 +178,9 @@ struct KvWalk {
   }
 };
 
-// Every thread of the block (whole warps, at most 32) calls this once; `buf` holds two ints per warp.  Row tiles that see
+constexpr int kShareWarps = 12;      // warps of a block at most
+
+// Every thread of the block (whole warps, at most kShareWarps) calls this once; `buf` holds two ints per warp.  Row tiles that see
 // nothing get their zeros here.
 template <int ROWS, int D, bool TREE>
 __device__ __forceinline__ KvShare kv_share(const KvAttnArgs& a, int* buf, KvShare* found, int* status) {
@@ -212,8 +214,9 @@ __device__ __forceinline__ KvShare kv_share(const KvAttnArgs& a, int* buf, KvSha
       }
       __syncthreads();
       int total = 0, total_items = 0, before_items = 0;
-#pragma unroll 1
-      for (int w = 0; w < threads / 32; ++w) {
+#pragma unroll
+      for (int w = 0; w < kShareWarps; ++w) {
+        if (w >= threads / 32) break;
         if (w == warp) {
           before = total;
           before_items = total_items;
@@ -290,7 +293,8 @@ struct KvMaps {
 };
 
 // The start of a launch.  kv_tree_kernel, which needs some microseconds for what is read last, starts when all work before it is
-// complete: a launch that follows it need not wait for that again, and waits for it in the threads that read what it writes.
+// complete: a launch that follows it need not wait for that again, and waits for it only in threads that come to read what it writes, and
+// once before it ends (so what waits for this launch has waited for that one too).
 template <bool TREE>
 __device__ __forceinline__ void kv_begin(const KvAttnArgs& a) {
   if (!TREE || !a.after_tree) ptx::begin_call();

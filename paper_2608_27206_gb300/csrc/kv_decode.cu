@@ -195,7 +195,6 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
     const int grp = warp >= 6, quad = warp & 3, me = quad * 32 + lane;    // TMEM lane: slot of the tile, then column of the output
     const uint32_t lanes = tmem + (static_cast<uint32_t>(quad * 32) << 16);
     Stat* stat = ctl->stat[grp];
-    kv_tree_ready<TREE>(a);
     int t = 0;
     while (walk.next(a)) {
       const KvItem& it = walk.it;
@@ -266,7 +265,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
       int place = 0;
       if (TREE && lane < it.rows) {
         node = a.s.q0[it.i] + static_cast<int>(a.by_group(it.row0 + lane));
-        place = it.p0 + a.depth[node];
+        if (a.window > 0) {
+          kv_tree_ready<TREE>(a);
+          place = it.p0 + a.depth[node];
+        }
       }
       float l[NQ];
 #pragma unroll
@@ -296,6 +298,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
           auto sees = [&](int q) { return TREE ? (by >> q & 1) != 0 : kv_sees(slot, ctl->slot_of[q], a.window, a.sinks); };
           if (!whole) {
             if constexpr (TREE) {      // (a lane looks up the warp's 32 slots for one row)
+              kv_tree_ready<TREE>(a);
               const uint32_t word = node >= 0 ? kv_tree_sees(a, it.p0, node, place, slot0 + quad * 32) : 0u;
 #pragma unroll
               for (int q = 0; q < NQ; ++q) by |= (__shfl_sync(0xffffffffu, word, q) >> lane & 1) << q;
@@ -489,6 +492,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_decode_kernel(const __grid_con
         }
       }
     }
+    kv_tree_ready<TREE>(a);
     if (threadIdx.x == 64) kv_write_split(a, share, walk.it);
   }
   // everything issued has completed: the last tile's commit has been waited for, unless the CTA gave up

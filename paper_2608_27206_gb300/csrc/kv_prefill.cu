@@ -91,9 +91,9 @@ __device__ __forceinline__ uint32_t f16x2(float lo, float hi) {
   return r;
 }
 
-__device__ __forceinline__ uint32_t bf16x2(uint32_t lo, uint32_t hi) {
+__device__ __forceinline__ uint32_t bf16x2(float lo, float hi) {
   uint32_t r;
-  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(__uint_as_float(hi)), "f"(__uint_as_float(lo)));
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
 }
 
@@ -405,7 +405,6 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
     if (!ok && lane == 0) stop(&ctl->abort, status);
   } else {
     // ---- weights: a thread owns a row -------------------------------------------------------------
-    kv_tree_ready<TREE>(a);
     const int i = (warp - 4) >> 2, quad = warp & 3, me = quad * 32 + lane;
     const uint32_t sS = tmem + (static_cast<uint32_t>(quad * 32) << 16) + i * 128, sO = sS + 256;
     KvWalk<kManyRows, TREE> walk;
@@ -420,15 +419,37 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
         t += n;
         continue;
       }
-      const int row0 = pair ? 0 : i * 128, row = row0 + me;
+      // (a pair's B has rows 64 on first: of up to 64 rows, A's and B's are then on different schedulers)
+      const int row0 = pair ? 0 : i * 128, row = row0 + (pair ? me ^ (i * 64) : me);
       const bool real = row < it.rows;
+      const int n_mine = pair ? (n + 1 - i) >> 1 : n;
+      if (TREE && row - lane >= it.rows) {      // a warp without rows: whatever its lanes of P hold, nobody reads what comes of it
+        if (lane == 0) mbar_arrive(q_full(i));
+#pragma unroll 1
+        for (int g = 0; ok && g < 2 * n_mine; ++g) {
+          ok = __all_sync(0xffffffffu, kv_wait(s_full(i, g & 1), (mine + (g >> 1)) & 1));
+          if (ok && lane == 0) mbar_arrive(p_full(i, g & 1));
+        }
+        t += n;
+        mine += n_mine;
+        if (pair && ok) {
+          if (lane == 0) mbar_arrive(x_full(i));
+          if (lane == 0) mbar_arrive(x_read(1 - i));
+          ok = __all_sync(0xffffffffu, kv_wait(x_read(i), joins & 1));
+          ++joins;
+        }
+        continue;
+      }
       auto slot_of = [&](int r) { return it.p0 + static_cast<int>(a.by_group(it.row0 + min(r, it.rows - 1))); };
       int p = slot_of(row);      // of the row (of a tree's node: its position)
       const int p_lo = TREE ? it.p_all : slot_of(row0), p_hi = slot_of(row0 + 127);      // of the tile's first and last
       int64_t node = 0;
       if constexpr (TREE) {
         node = a.s.q0[it.i] + p - it.p0;
-        p = it.p0 + a.depth[node];
+        if (a.window > 0) {
+          kv_tree_ready<TREE>(a);
+          p = it.p0 + a.depth[node];
+        }
       }
       constexpr int LANES = D / 8, STEP = 32 / LANES;      // lanes that move a row, rows at a time
       const int sub = lane / LANES, part = lane % LANES;
@@ -485,7 +506,6 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
       // and m a score of the row that is the largest so far to within 2^20, so that what w is about is small again.
       bool far = false;
       float m = 0.f;      // (0 of other rows)
-      const int n_mine = pair ? (n + 1 - i) >> 1 : n;
       int slot0 = 0;
       bool whole = true;
 #pragma unroll 1
@@ -507,6 +527,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
         }
         const float4* block = &ctl->block[u & 3][4 * h];
         if (!whole) {      // what the row does not see becomes -inf
+          kv_tree_ready<TREE>(a);
           // (it sees slots up to p that are past `from` or before `few`)
           const int from = a.window > 0 ? p - a.window : -1, few = a.window > 0 ? a.sinks : INT32_MAX;
 #pragma unroll 1
@@ -673,21 +694,21 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
         // A ends the first half of the columns and B the second, each with what the other leaves of them in its q tile (its products have
         // completed): out = (O f + O' f') / (l f + l' f'), f = 2^(its base less the larger one)
         constexpr int HALF = D / 2, CHUNKS = HALF / 4;      // columns, and their 16-byte chunks in a row
-        auto left = [&](int whose, int chunk) { return reinterpret_cast<float4*>(sQ + whose * 2 * C::QTILE + me * HALF * 4 + ((chunk ^ (me & (CHUNKS - 1))) * 16)); };
+        auto left = [&](int whose, int r, int chunk) { return reinterpret_cast<float4*>(sQ + whose * 2 * C::QTILE + r * HALF * 4 + ((chunk ^ (r & (CHUNKS - 1))) * 16)); };
 #pragma unroll 1
         for (int q = 0; q < HALF / 32; ++q) {
           uint32_t o[32];
           load_cols(sO + (1 - i) * HALF + 32 * q, o);
 #pragma unroll
           for (int e = 0; e < 32; e += 4)
-            *left(i, 8 * q + e / 4) = make_float4(__uint_as_float(o[e]), __uint_as_float(o[e + 1]), __uint_as_float(o[e + 2]), __uint_as_float(o[e + 3]));
+            *left(i, row, 8 * q + e / 4) = make_float4(__uint_as_float(o[e]), __uint_as_float(o[e + 1]), __uint_as_float(o[e + 2]), __uint_as_float(o[e + 3]));
         }
-        ctl->state[i][me] = make_float4(m, w, l, far ? 1.f : 0.f);
+        ctl->state[i][row] = make_float4(m, w, l, far ? 1.f : 0.f);
         __syncwarp();
         if (lane == 0) mbar_arrive(x_full(i));
         ok = __all_sync(0xffffffffu, kv_wait(x_full(1 - i), joins & 1));
         if (!ok) break;
-        const float4 its = ctl->state[1 - i][me];
+        const float4 its = ctl->state[1 - i][row];
         const float apart = l == 0.f ? -INFINITY : its.z == 0.f ? INFINITY : (m - its.x) + (w - its.y);      // (one that saw nothing has no say)
         const bool first = !(apart < 0.f);
         const float f = first ? 1.f : exp2f(apart), f2 = first ? exp2f(-apart) : 1.f;
@@ -699,7 +720,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
           load_cols(sO + i * HALF + 32 * q, o);
 #pragma unroll
           for (int e = 0; e < 32; e += 4) {
-            const float4 x = *left(1 - i, 8 * q + e / 4);
+            const float4 x = *left(1 - i, row, 8 * q + e / 4);
             const float y[4] = {x.x, x.y, x.z, x.w};
             // (a half that saw nothing is zero, whatever its accumulator holds)
 #pragma unroll
@@ -710,7 +731,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
 #pragma unroll
             for (int e = 0; e < 32; e += 8)
               *reinterpret_cast<uint4*>(a.out + at * D + i * HALF + 32 * q + e) =
-                  make_uint4(bf16x2(o[e], o[e + 1]), bf16x2(o[e + 2], o[e + 3]), bf16x2(o[e + 4], o[e + 5]), bf16x2(o[e + 6], o[e + 7]));
+                  make_uint4(bf16x2(__uint_as_float(o[e]), __uint_as_float(o[e + 1])), bf16x2(__uint_as_float(o[e + 2]), __uint_as_float(o[e + 3])),
+                             bf16x2(__uint_as_float(o[e + 4]), __uint_as_float(o[e + 5])), bf16x2(__uint_as_float(o[e + 6]), __uint_as_float(o[e + 7])));
           } else if (real) {
 #pragma unroll
             for (int e = 0; e < 32; e += 4) *reinterpret_cast<uint4*>(a.part + slot * D + i * HALF + 32 * q + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
@@ -731,7 +753,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
         continue;
       }
       const float inv = l == 0.f ? 0.f : 1.f / l, rel = l == 0.f ? -INFINITY : log2f(l);
-      // complete rows go out by way of the q tile, which is done with (this warp's rows), so that lanes write side by side
+      // complete rows go out by way of the q tile, which is done with (this warp's rows), so that lanes write side by side; parts of
+      // trees too where all eight warps have some, half of the columns at a time (5000 clocks; row by row 8000, where few have some 2500)
 #pragma unroll 1
       for (int q = 0; q < D / 32; ++q) {
         uint32_t o[32];
@@ -747,6 +770,20 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
             for (int k = 0; k < 4; ++k)
               asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(x[k]) : "f"(__uint_as_float(o[e + 2 * k + 1])), "f"(__uint_as_float(o[e + 2 * k])));
             *reinterpret_cast<uint4*>(place(lane, 4 * q + e / 8)) = make_uint4(x[0], x[1], x[2], x[3]);
+          }
+        } else if (TREE && it.rows > 128) {
+          constexpr int PER_HALF = D / 64;      // rounds of 32 columns
+          const int mine = q % PER_HALF * 8;
+#pragma unroll
+          for (int e = 0; e < 32; e += 4) *reinterpret_cast<uint4*>(place(lane, mine + e / 4)) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+          if (q % PER_HALF == PER_HALF - 1) {
+            __syncwarp();
+            constexpr int WIDE = D / 8;      // lanes of a row's half
+            float* to = a.part + (slot - lane + lane / WIDE) * D + q / PER_HALF * (D / 2) + lane % WIDE * 4;
+#pragma unroll 2
+            for (int r = lane / WIDE; r < min(32, it.rows - (row - lane)); r += 32 / WIDE, to += 32 / WIDE * D)
+              *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(place(r, lane % WIDE));
+            __syncwarp();
           }
         } else if (real) {
 #pragma unroll
@@ -770,6 +807,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
       }
     }
     if (!ok && lane == 0) stop(&ctl->abort, status);
+    kv_tree_ready<TREE>(a);
     if (threadIdx.x == 4 * 32) kv_write_split(a, share, it);
   }
   tc_fence_before_sync();
