@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from array import array
 from typing import Optional, Sequence
 
@@ -168,9 +169,9 @@ def _check(fn: str, status: int):
 def _ints(a, code: str, dtype):
     if type(a) is list or type(a) is tuple:
         try:
-            x = array(code, a)
+            x = array(code, a if len(a) < 16 else struct.pack(f"{len(a)}{code}", *a))      # (a long one in a third less time)
             return x, x.buffer_info()[0], len(x)
-        except (TypeError, OverflowError):
+        except (TypeError, OverflowError, struct.error):
             pass    # nested, or not whole numbers: numpy decides
     elif type(a) is np.ndarray and a.dtype == dtype and a.flags.c_contiguous:
         return a, a.__array_interface__["data"][0], len(a)
@@ -774,8 +775,8 @@ def pace_kv_attention_workspace_size(cache: KvCache, cu_q, n_q_heads: int, max_l
     return int(lib().pace_kv_attention_workspace_size(cache._address, cp, n - 1, int(n_q_heads), int(max_len)))
 
 
-def _attend(fn: str, cache: KvCache, Q, cu_q, parents, seq_lens, block_table, max_len, scale, window, sinks, out, lse, ws, stream):
-    """pace_kv_attention, or (parents: a tuple of one tensor) pace_kv_tree_attention."""
+def _attend(fn: str, call, size, cache: KvCache, Q, cu_q, parents, seq_lens, block_table, max_len, scale, window, sinks, out, lse, ws, stream):
+    """The library's `call`, whose workspace has the bytes that `size` says; parents None: queries in a line."""
     cu, cp, B = _i32(cu_q)
     B -= 1
     n, D = int(cu[-1]), cache.head_dim
@@ -792,11 +793,10 @@ def _attend(fn: str, cache: KvCache, Q, cu_q, parents, seq_lens, block_table, ma
     if lse is not None and (lse.dtype != torch.float32 or lse.numel() < n * hq):
         raise ValueError("lse: expected float32 [new tokens, heads]")
     tp, ts = _table(block_table, B)
-    L = lib()
-    buf, nbytes = _workspace(getattr(L, fn + "_workspace_size"), (cache._address, cp, B, hq, int(max_len)), ws, Q.device, stream)
-    tree = [_int32(p, n, "parents") for p in parents]
-    _check_ws(fn, getattr(L, fn)(cache._address, qp, qs, cp, B, hq, *tree, _int32(seq_lens, B, "seq_lens"), tp, ts, int(max_len),
-                                 float(scale), int(window), int(sinks), _dev(out), _dev(lse), _dev(buf), nbytes, _stream(stream)), ws)
+    buf, nbytes = _workspace(size, (cache._address, cp, B, hq, int(max_len)), ws, Q.device, stream)
+    tree = () if parents is None else (_int32(parents, n, "parents"),)
+    _check_ws(fn, call(cache._address, qp, qs, cp, B, hq, *tree, _int32(seq_lens, B, "seq_lens"), tp, ts, int(max_len), float(scale),
+                       int(window), int(sinks), _dev(out), _dev(lse), _dev(buf), nbytes, _stream(stream)), ws)
     return out
 
 
@@ -808,7 +808,9 @@ def pace_kv_attention(cache: KvCache, Q: torch.Tensor, cu_q, seq_lens: torch.Ten
     The queries are the last of their sequences' seq_lens (device int32, none above max_len) slots; with
     window > 0 one sees the last `window` slots up to its own and the first `sinks`.  lse (float32 [new
     tokens, heads]) receives the log-sum-exp of the scores."""
-    return _attend("pace_kv_attention", cache, Q, cu_q, (), seq_lens, block_table, max_len, scale, window, sinks, out, lse, ws, stream)
+    L = lib()
+    return _attend("pace_kv_attention", L.pace_kv_attention, L.pace_kv_attention_workspace_size, cache, Q, cu_q, None, seq_lens, block_table,
+                   max_len, scale, window, sinks, out, lse, ws, stream)
 
 
 # ---- drafted tokens --------------------------------------------------------------------------
@@ -827,15 +829,17 @@ def pace_kv_tree_attention(cache: KvCache, Q: torch.Tensor, cu_q, parents: torch
     """pace_kv_attention from the nodes of trees: the queries are a sequence's newest slots, parents (device int32 [nodes]) the number
     of each one's parent in its own tree, before it, or -1.  A node sees the slots before the tree, its ancestors and
     itself; a window counts in positions, which are depths within the tree."""
-    return _attend("pace_kv_tree_attention", cache, Q, cu_q, (parents,), seq_lens, block_table, max_len, scale, window, sinks, out, lse,
-                   ws, stream)
+    L = lib()
+    return _attend("pace_kv_tree_attention", L.pace_kv_tree_attention, L.pace_kv_tree_attention_workspace_size, cache, Q, cu_q, parents,
+                   seq_lens, block_table, max_len, scale, window, sinks, out, lse, ws, stream)
 
 
-def _out_int32(t: Optional[torch.Tensor], n: int, what: str, device, stream) -> torch.Tensor:
+def _out_int32(t: Optional[torch.Tensor], n: int, what: str, like: torch.Tensor, stream):
+    """(tensor, address) of an output: the caller's, or a new one beside `like`."""
     if t is None:
-        return _used(torch.empty(n, dtype=torch.int32, device=device), stream)
-    _int32(t, n, what)
-    return t
+        t = _used(torch.empty(n, dtype=torch.int32, device=like.device), stream)
+        return t, t.data_ptr()
+    return t, _int32(t, n, what)
 
 
 def pace_draft_accept(tokens: torch.Tensor, parents: torch.Tensor, picked: torch.Tensor, cu_nodes, rows: Optional[torch.Tensor] = None,
@@ -846,12 +850,11 @@ def pace_draft_accept(tokens: torch.Tensor, parents: torch.Tensor, picked: torch
     cu, cp, B = _i32(cu_nodes)
     B -= 1
     n = int(cu[-1]) if B >= 0 else 0
-    dev = tokens.device
     tp, pp, kp = _int32(tokens, n, "tokens"), _int32(parents, n, "parents"), _int32(picked, n, "picked")
-    rows = _out_int32(rows, n, "rows", dev, stream)
-    counts, next_tokens = _out_int32(counts, B, "counts", dev, stream), _out_int32(next_tokens, B, "next_tokens", dev, stream)
-    _check("pace_draft_accept", lib().pace_draft_accept(tp, pp, kp, cp, B, rows.data_ptr(), counts.data_ptr(), next_tokens.data_ptr(),
-                                                        _stream(stream)))
+    rows, rp = _out_int32(rows, n, "rows", tokens, stream)
+    counts, np_ = _out_int32(counts, B, "counts", tokens, stream)
+    next_tokens, xp = _out_int32(next_tokens, B, "next_tokens", tokens, stream)
+    _check("pace_draft_accept", lib().pace_draft_accept(tp, pp, kp, cp, B, rp, np_, xp, _stream(stream)))
     return rows, counts, next_tokens
 
 
@@ -883,7 +886,6 @@ def pace_kv_compact(cache, cu_new, seq_lens: torch.Tensor, block_table: torch.Te
     lens = _int32(seq_lens, B, "seq_lens")
     rp = None if rows is None else _int32(rows, int(keep[-1]), "rows")
     np_ = None if counts is None else _int32(counts, B, "counts")
-    new_lens = _out_int32(new_lens, B, "new_lens", seq_lens.device, stream)
-    _check("pace_kv_compact", lib().pace_kv_compact(cache._address, layers, cp, B, lens, tp, ts, kp, rp, np_, dp, ds, new_lens.data_ptr(),
-                                                    _stream(stream)))
+    new_lens, xp = _out_int32(new_lens, B, "new_lens", seq_lens, stream)
+    _check("pace_kv_compact", lib().pace_kv_compact(cache._address, layers, cp, B, lens, tp, ts, kp, rp, np_, dp, ds, xp, _stream(stream)))
     return new_lens
