@@ -100,7 +100,7 @@ pace_status_t check_attention(const pace_kv_cache* cache, const int32_t* cu_q, i
   const int group = n_q_heads / cache->n_kv_heads;
   if (cu_q[B] > (1 << 30) / group) return PACE_ERR_INVALID_ARG;
   const int limit = few_limit(cu_q, B, group, cache->n_kv_heads, max_len, tree);
-  const int64_t most = INT32_MAX / (cache->n_kv_heads * (slot_tiles(max_len) + kItemCost));      // row tiles of a launch
+  const int64_t most = INT32_MAX / (cache->n_kv_heads * (slot_tiles(max_len) + (tree ? kTreeCost : kItemCost)));      // row tiles of a launch
   for (const bool is_few : {true, false})
     for (int b = 0; b < B;)
       if (next_launch(cu_q, B, group, limit, is_few, is_few ? few_rows(cu_q, B, group, limit) : kManyRows, b, nullptr) > most) return PACE_ERR_INVALID_ARG;

@@ -24,7 +24,8 @@ namespace pace {
 constexpr int kKvTile = 128;      // slots of one tile
 constexpr float kNone = -0x1p127f;   // a row's maximum before its first slot, below any score (and finite: x - kNone is never NaN)
 constexpr int kManyRows = 256;    // rows of a tile of the form for many
-constexpr int kItemCost = 3;      // slot tiles that the queries and the output of a (row tile, head) are worth
+constexpr int kItemCost = 3;      // slot tiles that the queries and the output of a (row tile, head) are worth,
+constexpr int kTreeCost = 5;      // of trees of many rows
 constexpr int kPlanCtas = 152;    // CTAs of a launch at most: an SM each (the size queries need no device)
 
 // The launch's sequences, those without queries left out.
@@ -228,7 +229,8 @@ __device__ __forceinline__ KvShare kv_share(const KvAttnArgs& a, int* buf, KvSha
       const int c = blockIdx.x;
       if (c >= s.ctas) return s;      // nothing to do (the whole block)
       // (few tiles: one each, however dear the rest is; unless items are so few that a CTA need not have parts of two)
-      s.cost = total >= kItemCost * s.ctas || (total > s.ctas && total >= 4 * kItemCost * total_items) ? kItemCost : 0;
+      constexpr int COST = TREE && ROWS == kManyRows ? kTreeCost : kItemCost;
+      s.cost = total >= COST * s.ctas || (total > s.ctas && total >= 4 * COST * total_items) ? COST : 0;
       total += s.cost * total_items;
       before += sum - mine + s.cost * (before_items + num - items);
       mine += s.cost * items;

@@ -643,27 +643,28 @@ __global__ void __launch_bounds__(256) kv_attn_combine(const __grid_constant__ K
   join_rows<D, ROWS, PARTS, SPLIT>(a, tile_rows, blockIdx.x, sp, blockIdx.y * (8 / SPLIT) * ROWS);
 }
 
-// The same where a few items have many parts and many rows each (a tree on one long sequence: 4 items of 182 rows in 38 parts): every block
-// lists the rows of all split items and takes its share of them, a row at a time, with eight warps.
-template <int D>
+// The same for nodes of trees, where few items may have many parts and many rows each (on one long sequence: 4 items of 182 rows in 38
+// parts): every block lists the rows of all split items and takes its share of them, 8 / SPLIT at a time with SPLIT warps each.
+template <int D, int SPLIT>
 __global__ void __launch_bounds__(256) kv_attn_combine_list(const __grid_constant__ KvAttnArgs a, int tile_rows, int ctas) {
   static_assert(kPlanCtas <= 256, "a thread per CTA of the launch");
-  __shared__ int s_end[8][32], s_warp[8];      // rows up to each CTA's item, within its warp; of each warp
+  constexpr int TAKE = 8 / SPLIT;
+  __shared__ int s_end[8][32], s_warp[8];      // takes of rows up to each CTA's item, within its warp; of each warp
   launch_dependents();
   grid_dependency_wait();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int rows = 0;
+  int takes = 0;
   if (static_cast<int>(threadIdx.x) < ctas) {
     const int4 raw = __ldcg(reinterpret_cast<const int4*>(a.split + threadIdx.x));
-    if (raw.w > 0) rows = min(a.s.nq[raw.x] * a.group - raw.y * tile_rows, tile_rows);
+    if (raw.w > 0) takes = (min(a.s.nq[raw.x] * a.group - raw.y * tile_rows, tile_rows) + TAKE - 1) / TAKE;
   }
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int x = __shfl_up_sync(0xffffffffu, rows, o);
-    if (lane >= o) rows += x;
+    const int x = __shfl_up_sync(0xffffffffu, takes, o);
+    if (lane >= o) takes += x;
   }
-  s_end[warp][lane] = rows;
-  if (lane == 31) s_warp[warp] = rows;
+  s_end[warp][lane] = takes;
+  if (lane == 31) s_warp[warp] = takes;
   __syncthreads();
   int total = 0;
 #pragma unroll
@@ -672,11 +673,11 @@ __global__ void __launch_bounds__(256) kv_attn_combine_list(const __grid_constan
   for (int task = blockIdx.x; task < total; task += gridDim.x) {
     int w = 0, left = task;
     while (left >= s_warp[w]) left -= s_warp[w++];
-    const uint32_t after = __ballot_sync(0xffffffffu, s_end[w][lane] > left);      // the first whose rows reach it
+    const uint32_t after = __ballot_sync(0xffffffffu, s_end[w][lane] > left);      // the first whose takes reach it
     const int k = __ffs(after) - 1, c = 32 * w + k;
     const int4 raw = __ldcg(reinterpret_cast<const int4*>(a.split + c));
-    join_rows<D, 1, 8, 8>(a, tile_rows, c, KvSplit{raw.x, raw.y, raw.z, raw.w}, left - (k > 0 ? s_end[w][k - 1] : 0));
-    __syncthreads();      // (the joined sums' places are used again)
+    join_rows<D, 1, 8, SPLIT>(a, tile_rows, c, KvSplit{raw.x, raw.y, raw.z, raw.w}, (left - (k > 0 ? s_end[w][k - 1] : 0)) * TAKE);
+    if (SPLIT > 1) __syncthreads();      // (the joined sums' places are used again)
   }
 }
 
@@ -714,10 +715,12 @@ pace_status_t launch_kv_decode(const KvMaps& maps, const KvAttnArgs& a, int D, i
 }
 
 pace_status_t launch_kv_combine(const KvAttnArgs& a, int D, int rows, unsigned grid, int64_t items, cudaStream_t stream) {
-  // Nodes of trees, eight parts or more to an item: rows one by one on every SM.
-  if (a.family != nullptr && rows == kManyRows && grid >= 8 * items)
-    return launch_dependent(D == 128 ? kv_attn_combine_list<128> : kv_attn_combine_list<64>, static_cast<unsigned>(std::min<int64_t>(items * rows, kPlanCtas * 6)),
-                            256, 0, 1, stream, a, rows, static_cast<int>(grid));
+  // (eight parts or more to an item: rows one by one)
+  if (a.family != nullptr && rows == kManyRows) {
+    const bool one = grid >= 8 * items;
+    auto* kernel = D == 128 ? (one ? kv_attn_combine_list<128, 8> : kv_attn_combine_list<128, 1>) : (one ? kv_attn_combine_list<64, 8> : kv_attn_combine_list<64, 1>);
+    return launch_dependent(kernel, static_cast<unsigned>(std::min<int64_t>(items * rows, kPlanCtas * 6)), 256, 0, 1, stream, a, rows, static_cast<int>(grid));
+  }
   if (rows == kManyRows)
     return launch_dependent(D == 128 ? kv_attn_combine<128, 4, 4, 1> : kv_attn_combine<64, 4, 4, 1>, dim3(grid, static_cast<unsigned>(rows / 32)),
                             256, 0, 1, stream, a, rows);

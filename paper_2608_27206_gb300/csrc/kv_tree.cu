@@ -2,8 +2,9 @@
 //
 // kv_tree_kernel: of every node its depth and, as bits over the tree's slots, which of them it sees: its ancestors and itself, as far
 // as the window around its position lets it.  The attention kernels read a word of bits where they would compare slots.  A thread goes
-// up from a node twice, for its depth and for its bits; parents lie in shared memory.  All latency: a tree of 26 nodes takes 3 us, most of
-// it the launch.
+// up from a node twice, for its depth and for its bits, in shared memory and run by run: nodes whose parent is the one before them follow
+// each other in slots and positions, so that a line of drafts is one step and a tree takes as many as it branches on the way.  All latency: a
+// tree of 26 nodes takes 3 us, most of it the launch; the attention starts beside it.
 //
 // draft_accept_kernel: a warp walks a tree.  A child comes after its parent, so one pass over the nodes in order finds the path: of each
 // 32 nodes, those that agree with what was picked after their parent are known at once, and a ballot finds the first child of the node
@@ -26,35 +27,69 @@ struct TreeArgs {
 constexpr int kTreeThreads = 256;
 
 __global__ void __launch_bounds__(kTreeThreads) kv_tree_kernel(const __grid_constant__ TreeArgs a, int* status) {
-  __shared__ int16_t up[PACE_TREE_MAX];
+  constexpr int WORDS = PACE_TREE_MAX / 32;
+  __shared__ int16_t up[PACE_TREE_MAX], head[PACE_TREE_MAX];      // parents; where the run of a node begins
+  __shared__ uint32_t begins[WORDS];                              // nodes that begin one
   ptx::begin_call();
-  const int b = blockIdx.x, at = a.cu[b], n = a.cu[b + 1] - at;
+  const int b = blockIdx.x, at = a.cu[b], n = a.cu[b + 1] - at, lane = threadIdx.x & 31;
   const int base = min(max(a.lens[a.b0 + b], 0), a.max_len) - n;
-  for (int t = threadIdx.x; t < n; t += kTreeThreads) {
-    int p = a.t.parents[at + t];
+  for (int t0 = threadIdx.x - lane; t0 < n; t0 += kTreeThreads) {
+    const int t = t0 + lane;
+    int p = t < n ? a.t.parents[at + t] : -1;
     if (p < -1 || p >= t) {
       record_error(status, PACE_ERR_INVALID_ARG, K_KV_TREE);
       p = -1;
     }
     up[t] = static_cast<int16_t>(p);
+    const uint32_t bits = __ballot_sync(0xffffffffu, p != t - 1 || t == 0);
+    if (lane == 0) begins[t0 / 32] = bits;
+  }
+  __syncthreads();
+  for (int t = threadIdx.x; t < n; t += kTreeThreads) {
+    int w = t / 32;
+    uint32_t bits = begins[w] & (0xFFFFFFFFu >> (31 - t % 32));
+    while (bits == 0) bits = begins[--w];      // (node 0 begins one)
+    head[t] = static_cast<int16_t>(32 * w + 31 - __clz(bits));
   }
   __syncthreads();
   for (int t = threadIdx.x; t < n; t += kTreeThreads) {
     int depth = 0;
-    for (int p = up[t]; p >= 0; p = up[p]) ++depth;
+    for (int x = t;;) {
+      depth += x - head[x];
+      x = up[head[x]];
+      if (x < 0) break;
+      ++depth;
+    }
     a.t.depth[at + t] = depth;
-    // ancestors come in falling order, and so do the words of their slots
+    // runs come in falling order, and so do the words of their slots
     uint32_t* row = a.t.family + static_cast<int64_t>(at + t) * a.t.words;
-    int k = a.t.words - 1, place = base + depth;
+    int k = a.t.words - 1;
     uint32_t bits = 0;
-    for (int p = t, far = 0; p >= 0; p = up[p], ++far, --place) {
-      if (base + p < 0 || (a.window > 0 && far >= a.window && place >= a.sinks)) continue;
-      const int word = ((base + p) >> 5) - (base >> 5);
-      for (; k > word; --k) {
-        row[k] = bits;
-        bits = 0;
+    auto see = [&](int from, int to) {      // slots from .. to - 1
+      from = max(from, 0);
+      if (from >= to) return;
+      for (int word = ((to - 1) >> 5) - (base >> 5), low = (from >> 5) - (base >> 5); word >= low; --word) {
+        for (; k > word; --k) {
+          row[k] = bits;
+          bits = 0;
+        }
+        const int slot0 = 32 * (word + (base >> 5));
+        bits |= below(to - slot0) & ~below(from - slot0);
       }
-      bits |= 1u << ((base + p) & 31);
+    };
+    int place = base + depth, far = 0;      // position of x, generations from t
+    for (int x = t; x >= 0;) {
+      const int h = head[x], first = base + h, end = base + x + 1;      // the run's slots, positions up to `place`
+      if (a.window > 0) {
+        const int near = max(end - max(a.window - far, 0), first), sink = min(max(end - 1 - place + a.sinks, first), near);
+        see(near, end);
+        see(first, sink);
+      } else {
+        see(first, end);
+      }
+      far += x - h + 1;
+      place -= x - h + 1;
+      x = up[h];
     }
     for (; k >= 0; --k) {
       row[k] = bits;
