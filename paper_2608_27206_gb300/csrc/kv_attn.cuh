@@ -25,7 +25,7 @@ constexpr int kKvTile = 128;      // slots of one tile
 constexpr float kNone = -0x1p127f;   // a row's maximum before its first slot, below any score (and finite: x - kNone is never NaN)
 constexpr int kManyRows = 256;    // rows of a tile of the form for many
 constexpr int kItemCost = 3;      // slot tiles that the queries and the output of a (row tile, head) are worth,
-constexpr int kTreeCost = 5;      // of trees of many rows
+constexpr int kTreeCost = 5;      // of trees of many rows (40 of 182 rows on 5001-28007 slots 241 us with 3, 237 with 5 and 7; 8 of 21 rows on 700-9000 25, 25, 28)
 constexpr int kPlanCtas = 152;    // CTAs of a launch at most: an SM each (the size queries need no device)
 
 // The launch's sequences, those without queries left out.

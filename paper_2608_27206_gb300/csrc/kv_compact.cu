@@ -10,7 +10,12 @@
 // written blocks of all sequences form a line, block by block and in it layer by layer, of which every CTA takes an equal
 // share, as the lengths and counts on the device have it.  In place, blocks are written in order: what block i overwrites are
 // sources of blocks up to i, which have been read, since r_i >= i.  So a warp goes over a sequence's blocks of one head by itself, with the rows of
-// the next blocks on their way (reading ahead takes nothing away: only earlier blocks have been written), and needs no other order.
+// the next blocks on their way (reading ahead takes nothing away: only earlier blocks have been written), and needs no other order; where there are
+// many blocks a CTA takes sixteen at a time.
+//
+// Measured, 28 layers of 4 heads of 128: 4260 of 10589 tokens to other pages 44.5 us, 5.5 TB/s (a plain copy of as many bytes 41; 64 when
+// every block had its CTA, 56 with as many instructions for the largest code and the ratio as that took: 600 of a warp per block and head, 460
+// now, of which one in two issue slots is used), in place 75 us; the accepted tokens of 64 trees 14 us either way, which is latency.
 #include <cuda_fp16.h>
 
 #include <algorithm>

@@ -644,7 +644,8 @@ __global__ void __launch_bounds__(256) kv_attn_combine(const __grid_constant__ K
 }
 
 // The same for nodes of trees, where few items may have many parts and many rows each (on one long sequence: 4 items of 182 rows in 38
-// parts): every block lists the rows of all split items and takes its share of them, 8 / SPLIT at a time with SPLIT warps each.
+// parts): every block lists the rows of all split items and takes its share of them, 8 / SPLIT at a time with SPLIT warps each.  (That
+// sequence 25 us all told instead of 45; 8 trees of 21 rows 25 instead of 31.)
 template <int D, int SPLIT>
 __global__ void __launch_bounds__(256) kv_attn_combine_list(const __grid_constant__ KvAttnArgs a, int tile_rows, int ctas) {
   static_assert(kPlanCtas <= 256, "a thread per CTA of the launch");

@@ -25,6 +25,17 @@
 // S in TMEM.  Measured: a prompt of 10825 tokens, 28 + 4 heads of 128: 815-830 us, 1.01-1.03 PFLOP/s; 517 tokens at the end of 11342:
 // 102 us.  Tried and slower, when these were 790-815 and 97: S by halves of 64 columns (A is read twice as often: 844 us), two threads per
 // row on four warps per scheduler (908), a warp of MMAs per row tile (872), a single row tile with S ahead (1013; the short call 89).
+//
+// Nodes of trees (TREE) have few rows to an item, so that a slot tile is bound by the chain alone; what differs for them:
+//   S of the next slot tile is formed half by half, each as soon as P of that half has been used up (q crosses shared memory twice as often,
+//   but a half's owners find the next one ready: 40 trees of 182 rows on 5001-28007 slots 257 us with S whole, 238 by halves);
+//   of an item of one row tile and kPairTiles slot tiles or more, A and B take every other slot tile and join at the end (64 such trees
+//   of 63 rows 278 us with B idle, 224); K and V tiles then share one ring, as S runs two tiles ahead;
+//   parts of full tiles go out by way of shared memory, and warps without rows only keep step.
+// Measured: those 40 trees 236 us, 845 TFLOP/s and 2.4 TB/s; 64 of 63 rows 224 us, 4.0 TB/s.  In the former a slot tile takes 3600 clocks, 2600 of
+// them shared memory's (S by halves 1540, P V 510, V's conversion and the fetch 640), the rest hand-overs from P to products to S; tensor pipe
+// 52 % active.  One item alone costs 20000 clocks besides its tiles: the plan 4000, q 4500-7000, its first tile 1500 more, its output 2500-6000.
+// Tried: A's two halves before B's (250 us instead of 238), a pair's halves in step instead of in turn (275 instead of 235).
 // Roles of a CTA (one per SM): warp 0 fetches, warp 1 issues the MMAs, warps 2-3 turn V into f16 (they also see to NaN that must
 // not reach rows that do not look at it), warps 4-7 and 8-11 own the rows of A and B.
 #include <cuda_bf16.h>
@@ -43,7 +54,8 @@ constexpr int kThreads = 384;
 constexpr int kHalf = 64;          // columns of S at a time
 constexpr float kMost = 32768.f;   // sum of 64 weights at which w moves
 constexpr int kAfter = 6;          // log2 of what that sum is when w has moved, at most (so the largest weight is 2^-1 at least)
-constexpr float kFar = 0x1p22f;    // a row's maximum from which on its scores are taken relative to one of them
+constexpr float kFar = 0x1p22f;    // a row's maximum from which on its scores are taken relative to one of them; of trees, whose halves and parts are
+constexpr float kTreeFar = 0x1p12f;      // more often joined where one is past it and the other not: a score rounded there is 2^-12 off, at 2^22 a quarter
 constexpr uint32_t kTmem = 512;    // S of A and B, then O of A and B, 128 columns each
 
 template <int D>
@@ -80,7 +92,8 @@ __device__ __forceinline__ bool kv_whole(int slot0, int p_all, int p_last, int w
   return slot0 + kKvTile - 1 <= p_all && (window <= 0 || slot0 > p_last - window || slot0 + kKvTile <= sinks);
 }
 
-// Of a tree: whether A and B take every other slot tile of an item that has one row tile.
+// Of a tree: whether A and B take every other slot tile of an item that has one row tile.  (Joining them costs what two or three slot tiles
+// take: with 4 for 8, 32 trees of 128 rows on 700-9000 slots 112 us instead of 108; with 16, 64 of dim 64 110 instead of 105.)
 constexpr int kPairTiles = 8;
 template <bool TREE>
 __device__ __forceinline__ bool kv_pair(const KvItem& it) { return TREE && it.rows <= 128 && it.t1 - it.t0 >= kPairTiles; }
@@ -410,6 +423,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
     KvWalk<kManyRows, TREE> walk;
     walk.begin(share);
     const KvItem& it = walk.it;
+    constexpr float FAR = TREE ? kTreeFar : kFar;
     int t = 0, mine = 0, joins = 0;      // slot tiles of the CTA, of this row tile; pairs joined
     bool ok = true;
     while (ok && walk.next(a)) {
@@ -500,7 +514,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
         if (lane == 0) mbar_arrive(q_full(i));
       }
       float w = kNone, l = 0.f, peak = 0.f;      // peak: the largest sum of 64 weights under w
-      // A maximum below kFar is a whole number, and so are the logarithms of the scales: x + (log2(vs) - w) has one rounding, of
+      // A maximum below FAR is a whole number, and so are the logarithms of the scales: x + (log2(vs) - w) has one rounding, of
       // a small result.  Beyond it log2(vs) - w would lose bits, scores that are equal come out different, and weights under a w that
       // is their maximum pass 1 by any factor.  There (`far`) S of the half tile is first turned into x - m, x rounded like any score
       // and m a score of the row that is the largest so far to within 2^20, so that what w is about is small again.
@@ -557,7 +571,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
             load_cols(sX + 16 * (e0 & 3), y);
             const float mul = fmaxf(block[e0 & 3].x * c, 1e-37f);
             if (e0 == 4 && mine) {
-              const float to = top > least + 0x1p20f ? top : least;
+              const float to = top > least + FAR / 4 ? top : least;
               back = m - to;
               m = to;
             }
@@ -575,7 +589,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
         uint32_t words[32];
         bool over = g == 0 || back != 0.f;      // the row's w has to move
         float sum = INFINITY;                   // (by how much: not known)
-        // Two rounds at most: a move leaves a sum of 64 weights of at most 2^0.5 each.  (Below kFar the largest weight's exponent is
+        // Two rounds at most: a move leaves a sum of 64 weights of at most 2^0.5 each.  (Below FAR the largest weight's exponent is
         // exact to 2^-1; of a far row x - m is at most 0 where m has just moved, else below 2^20.)
         int rounds = 4;
 #pragma unroll 1
@@ -591,8 +605,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
             // further from the next)
             peak = over ? sum : peak;
             float now = peak >= static_cast<float>(2 << kAfter) ? w + static_cast<float>(static_cast<int>(__float_as_uint(peak) >> 23) - 126 - kAfter) : w;
-            bool find = over && !(sum < INFINITY && fabsf(now) < kFar);
-            if (!over && !(fabsf(now) < kFar)) now = w;
+            bool find = over && !(sum < INFINITY && fabsf(now) < FAR);
+            if (!over && !(fabsf(now) < FAR)) now = w;
 #pragma unroll 1
             while (__any_sync(0xffffffffu, find)) {
               float top = kNone;
@@ -606,7 +620,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
                 for (int e = 0; e < 16; ++e) top = fmaxf(top, fmaf(__uint_as_float(y[e]), mul, k.y));
               }
               if (find) now = ceilf(top);
-              find = find && !far && top > kNone && !(fabsf(top) < kFar);
+              find = find && !far && top > kNone && !(fabsf(top) < FAR);
               if (!__any_sync(0xffffffffu, find)) break;
               level(find, -INFINITY);      // (once: these are far now)
               far = far || find;

@@ -865,6 +865,8 @@ class KvLayers:
         self.caches = list(caches)
         if any(not isinstance(c, KvCache) for c in self.caches):
             raise ValueError("expected caches")
+        if len({c.view.k for c in self.caches}) < len(self.caches):
+            raise ValueError("a layer more than once")
         self.views = (KvCacheView * max(len(self.caches), 1))(*[c.view for c in self.caches])
         self._address = ctypes.addressof(self.views)
 

@@ -341,3 +341,10 @@ def test_zeros_under_a_large_scale_join_a_small_one(pace, away):  # noqa: F811
         pool.s[n][pages[2]] = 2.0 ** 110
     _upload(pool)
     case.check(case.call())
+
+
+def test_a_layer_is_listed_once(pace):  # noqa: F811
+    caches = [Pool(pace, 49, [20], 1, 64, 16).cache for _ in range(2)]
+    pace.KvLayers(caches)
+    with pytest.raises(ValueError):
+        pace.KvLayers([caches[0], caches[1], caches[0]])

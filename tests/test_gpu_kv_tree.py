@@ -6,7 +6,8 @@ import pytest
 import torch
 
 from oracle import pace_oracle as O
-from test_gpu_kv import Pool, _cu, _f64, _tokens, _upload, pace  # noqa: F401
+from test_gpu_kv import BF16, Pool, _cu, _f64, _tokens, _upload, pace  # noqa: F401
+from test_gpu_kv_range import _pattern, _set_keys
 
 pytestmark = pytest.mark.gpu
 
@@ -309,3 +310,27 @@ def test_accept_replayed(pace):  # noqa: F811
         g.replay()
         for a, b in zip(outs, pace.pace_draft_accept(tokens, parents, picked, cu)):
             assert torch.equal(a, b)
+
+
+# Scores in base 2 of up to +-mantissa 2^log2_size, exact (see the range tests): below, at and above where a row's are taken relative to one
+@pytest.mark.parametrize("log2_size,mantissa", [(11, 1.9), (12, 1.0), (13, 1.0), (14, 1.3), (21, 1.9), (22, 1.0), (23, 1.0), (26, 1.7320508), (80, 1.3), (110, 1.1)])
+@pytest.mark.parametrize("shape", ["rise", "fall", "saw"])
+@pytest.mark.parametrize("count,hq,hkv,dim", [(90, 14, 2, 128), (50, 8, 8, 64), (3, 14, 2, 128), (2, 8, 8, 64)])
+def test_scores_of_any_size(pace, shape, log2_size, mantissa, count, hq, hkv, dim):  # noqa: F811
+    length = 1300
+    pool = Pool(pace, 42, [length], hkv, dim, 64, spread=8)
+    j = np.arange(length)
+    curve = {"rise": j / length * 2 - 1, "fall": 1 - j / length * 2, "saw": (j % 170) / 170 * (0.2 + 0.8 * j / length)}[shape]
+    u = _pattern(hkv, dim)
+    of_scale, of_q = log2_size // 2 - 8, log2_size // 4
+    _set_keys(pool, u, curve * 256, log2_size - 8 - of_scale - of_q)
+    _upload(pool)
+    steep = np.resize([1.0, -1.0, 0.125, 0.5, -0.25], count * hq).reshape(count, hq, 1)
+    Q = torch.from_numpy(steep * 2.0 ** of_q * np.repeat(u, hq // hkv, axis=0)[None]).to(BF16).cuda()
+    scale = float(np.float32(mantissa * math.log(2) * 2.0 ** of_scale / dim))
+    parents = tree("random", count)
+    out = pace.pace_kv_tree_attention(pool.cache, Q, [0, count], _ids(parents), pool.lens, pool.table, length, scale=scale)
+    r = O.kv_attention(_f64(Q), pool.read("k", 0), pool.read("v", 0), O.kv_tree_visible(length, parents), scale)
+    err = np.abs(_f64(out) - r["out"])
+    tol = 2.0 ** -8 * np.abs(r["out"]) + 2.0 ** -8 * r["abs_out"] + 2.0 ** -17 * r["peak"][..., None]
+    assert np.all(err <= tol), (float((err - tol).max()), float(err.max()))
