@@ -533,6 +533,29 @@ def kv_attention(Q: np.ndarray, K: np.ndarray, V: np.ndarray, visible: np.ndarra
     return dict(out=out, lse=lse, abs_out=absout, abs_score=score, peak=peak)
 
 
+def kv_attention_dense(Q: np.ndarray, K: np.ndarray, V: np.ndarray, visible: np.ndarray, scale: float) -> Dict[str, np.ndarray]:
+    """kv_attention with whole matrices, for long sequences: the same results.  Hidden slots of K and V must be finite."""
+    n, hq, d = Q.shape
+    g = hq // K.shape[1]
+    out, absout = np.zeros((n, hq, d)), np.zeros((n, hq, d))
+    lse, score, peak = np.full((n, hq), -np.inf), np.zeros((n, hq)), np.zeros((n, hq))
+    some = visible.any(axis=1)
+    for h in range(K.shape[1]):
+        k, v = K[:, h], V[:, h]
+        top_v = np.abs(v).max(axis=1)
+        for head in range(h * g, h * g + g):
+            s = np.where(visible, scale * (Q[:, head] @ k.T), -np.inf)
+            m = np.where(some, s.max(axis=1), 0.0)
+            w = np.exp(s - m[:, None])
+            total = w.sum(axis=1)
+            lse[some, head] = (m + np.log(np.where(some, total, 1.0)))[some]
+            w /= np.where(some, total, 1.0)[:, None]
+            out[:, head], absout[:, head] = w @ v, w @ np.abs(v)
+            score[:, head] = np.where(visible, scale * (np.abs(Q[:, head]) @ np.abs(k).T), 0.0).max(axis=1)
+            peak[:, head] = np.sqrt(visible.sum(axis=1)) * (w * top_v).max(axis=1)
+    return dict(out=out, lse=lse, abs_out=absout, abs_score=score, peak=peak)
+
+
 def tree_family(parents: Sequence[int]) -> List[List[int]]:
     """Of every node itself and its ancestors, ascending; parents come before their children, -1 is none."""
     family: List[List[int]] = []

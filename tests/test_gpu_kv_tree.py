@@ -56,7 +56,7 @@ def check_tree(P, pool, Q, parents, window=0, sinks=0, **kw):
         see = O.kv_tree_visible(pool.host_lens[b], up, window, sinks)
         hidden = ~see.any(0)
         k[hidden] = v[hidden] = 0
-        r = O.kv_attention(q[cu[b]:cu[b + 1]], k, v, see, D ** -0.5)
+        r = O.kv_attention_dense(q[cu[b]:cu[b + 1]], k, v, see, D ** -0.5)
         score = 2.0 ** -23 * (D + 8) * r["abs_score"] + 2.0 ** -20
         got = _f64(out[cu[b]:cu[b + 1]])
         tol = 2.0 ** -8 * np.abs(r["out"]) + (2.0 ** -8 + 2 * score[..., None]) * r["abs_out"] + 2.0 ** -17 * r["peak"][..., None]
@@ -151,7 +151,7 @@ def test_nodes_before_the_first_slot(pace, n):  # noqa: F811
         base = length - n
         k, v = pool.read("k", b), pool.read("v", b)
         see = O.kv_tree_visible(length, parents[b])
-        r = O.kv_attention(_f64(Q[b * n:(b + 1) * n]), k, v, see, 64 ** -0.5)
+        r = O.kv_attention_dense(_f64(Q[b * n:(b + 1) * n]), k, v, see, 64 ** -0.5)
         np.testing.assert_allclose(_f64(out[b * n:(b + 1) * n]), r["out"], rtol=0, atol=2.0 ** -6 * max(1.0, np.abs(r["out"]).max()))
         assert base >= 0 or not r["out"][:-base].any()
 
@@ -330,7 +330,7 @@ def test_scores_of_any_size(pace, shape, log2_size, mantissa, count, hq, hkv, di
     scale = float(np.float32(mantissa * math.log(2) * 2.0 ** of_scale / dim))
     parents = tree("random", count)
     out = pace.pace_kv_tree_attention(pool.cache, Q, [0, count], _ids(parents), pool.lens, pool.table, length, scale=scale)
-    r = O.kv_attention(_f64(Q), pool.read("k", 0), pool.read("v", 0), O.kv_tree_visible(length, parents), scale)
+    r = O.kv_attention_dense(_f64(Q), pool.read("k", 0), pool.read("v", 0), O.kv_tree_visible(length, parents), scale)
     err = np.abs(_f64(out) - r["out"])
     tol = 2.0 ** -8 * np.abs(r["out"]) + 2.0 ** -8 * r["abs_out"] + 2.0 ** -17 * r["peak"][..., None]
     assert np.all(err <= tol), (float((err - tol).max()), float(err.max()))

@@ -38,7 +38,7 @@ def check_some(P, pool, Q, parents, which, **kw):
         see = O.kv_tree_visible(pool.host_lens[b], parents[b], window, sinks)
         hidden = ~see.any(0)
         k[hidden] = v[hidden] = 0
-        r = O.kv_attention(_f64(Q[cu[b]:cu[b + 1]]), k, v, see, D ** -0.5)
+        r = O.kv_attention_dense(_f64(Q[cu[b]:cu[b + 1]]), k, v, see, D ** -0.5)
         score = 2.0 ** -23 * (D + 8) * r["abs_score"] + 2.0 ** -20      # (the bounds of check_tree)
         tol = 2.0 ** -8 * np.abs(r["out"]) + (2.0 ** -8 + 2 * score[..., None]) * r["abs_out"] + 2.0 ** -17 * r["peak"][..., None]
         assert np.all(np.abs(_f64(out[cu[b]:cu[b + 1]]) - r["out"]) <= tol), b
@@ -80,7 +80,7 @@ def test_rows_that_see_one_half_or_nothing(pace, dim):  # noqa: F811
         see = O.kv_tree_visible(lens[b], parents[b], 8, 1400)
         hidden = ~see.any(0)
         k[hidden] = v[hidden] = 0
-        r = O.kv_attention(_f64(Q[cu[b]:cu[b + 1]]), k, v, see, dim ** -0.5)
+        r = O.kv_attention_dense(_f64(Q[cu[b]:cu[b + 1]]), k, v, see, dim ** -0.5)
         none = ~see.any(1)
         got = out[cu[b]:cu[b + 1]]
         assert not got[none].any() and torch.isneginf(lse[cu[b]:cu[b + 1]][none]).all() and none.any() == (lens[b] < 40)
@@ -134,7 +134,7 @@ def test_scores_of_any_size(pace, shape, log2_size, mantissa, dim):  # noqa: F81
     parents = tree("random", count)
     lse = torch.empty(count, hq, device="cuda")
     out = pace.pace_kv_tree_attention(pool.cache, Q, [0, count], _ids(parents), pool.lens, pool.table, length, scale=scale, lse=lse)
-    r = O.kv_attention(_f64(Q), pool.read("k", 0), pool.read("v", 0), O.kv_tree_visible(length, parents), scale)
+    r = O.kv_attention_dense(_f64(Q), pool.read("k", 0), pool.read("v", 0), O.kv_tree_visible(length, parents), scale)
     # (as check_exact_scores of the range tests: one rounding to bf16, weights of 8 bits twice over, what is far below off by 2^-18; lse five roundings)
     err = np.abs(_f64(out) - r["out"])
     tol = 2.0 ** -8 * np.abs(r["out"]) + 2.0 ** -8 * r["abs_out"] + 2.0 ** -17 * r["peak"][..., None]

@@ -29,6 +29,17 @@ def test_visibility_of_a_tree():
     assert not O.kv_tree_visible(2, [-1, 0, 1])[0].any()      # a node before the first slot
 
 
+@pytest.mark.parametrize("scale", [0.2, 1e4])
+def test_attention_by_matrices_is_attention_row_by_row(scale):
+    rng = np.random.default_rng(3)
+    Q, K, V = rng.normal(size=(9, 6, 16)), rng.normal(size=(40, 2, 16)), rng.normal(size=(40, 2, 16))
+    see = O.kv_tree_visible(40, [-1, 0, 0, 1, 2, -1, 5, 3, 1], window=11, sinks=3)
+    see[4] = False
+    a, b = O.kv_attention(Q, K, V, see, scale), O.kv_attention_dense(Q, K, V, see, scale)
+    for n in a:
+        np.testing.assert_allclose(b[n], a[n], rtol=1e-11, atol=1e-300)
+
+
 def test_walk():
     tokens, parents = [5, 7, 8, 7, 9, 9], [-1, 0, 0, 0, 2, 2]
     assert O.draft_accept(tokens, parents, [8, 0, 9, 0, 1, 1]) == [0, 2, 4]
