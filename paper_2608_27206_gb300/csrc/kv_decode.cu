@@ -644,12 +644,12 @@ __global__ void __launch_bounds__(256) kv_attn_combine(const __grid_constant__ K
 }
 
 // The same for nodes of trees, where few items may have many parts and many rows each (on one long sequence: 4 items of 182 rows in 38
-// parts): every block lists the rows of all split items and takes its share of them, 8 / SPLIT at a time with SPLIT warps each.  (That
+// parts): every block lists the rows of all split items and takes its share of them, 8 / SPLIT times ROWS at a time, ROWS with SPLIT warps.  (That
 // sequence 25 us all told instead of 45; 8 trees of 21 rows 25 instead of 31.)
-template <int D, int SPLIT>
+template <int D, int ROWS, int PARTS, int SPLIT>
 __global__ void __launch_bounds__(256) kv_attn_combine_list(const __grid_constant__ KvAttnArgs a, int tile_rows, int ctas) {
   static_assert(kPlanCtas <= 256, "a thread per CTA of the launch");
-  constexpr int TAKE = 8 / SPLIT;
+  constexpr int TAKE = 8 / SPLIT * ROWS;
   __shared__ int s_end[8][32], s_warp[8];      // takes of rows up to each CTA's item, within its warp; of each warp
   launch_dependents();
   grid_dependency_wait();
@@ -677,10 +677,13 @@ __global__ void __launch_bounds__(256) kv_attn_combine_list(const __grid_constan
     const uint32_t after = __ballot_sync(0xffffffffu, s_end[w][lane] > left);      // the first whose takes reach it
     const int k = __ffs(after) - 1, c = 32 * w + k;
     const int4 raw = __ldcg(reinterpret_cast<const int4*>(a.split + c));
-    join_rows<D, 1, 8, SPLIT>(a, tile_rows, c, KvSplit{raw.x, raw.y, raw.z, raw.w}, (left - (k > 0 ? s_end[w][k - 1] : 0)) * TAKE);
+    join_rows<D, ROWS, PARTS, SPLIT>(a, tile_rows, c, KvSplit{raw.x, raw.y, raw.z, raw.w}, (left - (k > 0 ? s_end[w][k - 1] : 0)) * TAKE);
     if (SPLIT > 1) __syncthreads();      // (the joined sums' places are used again)
   }
 }
+
+// Rows of a call that are joined one to a warp, at most (7168 of 5 parts 36.7 us that way and 36.2 by fours, 16384 50.8 and 49.0; 2016 26.6 and 29.5).
+constexpr int kSingly = 6144;
 
 template <int D, int NQ, bool TREE>
 pace_status_t run_decode(const KvMaps& maps, const KvAttnArgs& a, unsigned grid, int* status, cudaStream_t stream) {
@@ -716,10 +719,14 @@ pace_status_t launch_kv_decode(const KvMaps& maps, const KvAttnArgs& a, int D, i
 }
 
 pace_status_t launch_kv_combine(const KvAttnArgs& a, int D, int rows, unsigned grid, int64_t items, cudaStream_t stream) {
-  // (eight parts or more to an item: rows one by one)
   if (a.family != nullptr && rows == kManyRows) {
-    const bool one = grid >= 8 * items;
-    auto* kernel = D == 128 ? (one ? kv_attn_combine_list<128, 8> : kv_attn_combine_list<128, 1>) : (one ? kv_attn_combine_list<64, 8> : kv_attn_combine_list<64, 1>);
+    int64_t all = 0;      // rows
+    for (int i = 0; i < a.s.nb; ++i) all += a.s.nq[i];
+    all *= a.q_heads;
+    // eight parts or more to an item: a row by eight warps; else by one, or (many rows) four of them
+    auto* kernel = grid >= 8 * items ? (D == 128 ? kv_attn_combine_list<128, 1, 8, 8> : kv_attn_combine_list<64, 1, 8, 8>)
+                   : all <= kSingly  ? (D == 128 ? kv_attn_combine_list<128, 1, 8, 1> : kv_attn_combine_list<64, 1, 8, 1>)
+                                     : (D == 128 ? kv_attn_combine_list<128, 4, 4, 1> : kv_attn_combine_list<64, 4, 4, 1>);
     return launch_dependent(kernel, static_cast<unsigned>(std::min<int64_t>(items * rows, kPlanCtas * 6)), 256, 0, 1, stream, a, rows, static_cast<int>(grid));
   }
   if (rows == kManyRows)
