@@ -698,7 +698,7 @@ PACE_API pace_status_t pace_draft_accept(const int32_t* tokens, const int32_t* p
  * or whose page number is out of range.  A page number of dst_table out of range records it, and that block is not
  * stored.  A count out of range, or a sequence shorter than n_b, records it; nothing of that sequence moves, and its new length is its length.
  *
- *  layers       host    [n_layers] caches alike in everything but their addresses (any number, none twice)
+ *  layers       host    [n_layers] caches alike in everything but their addresses (one at least, none twice)
  *  cu_new       host    int32 [B+1] prefix of the newest tokens per sequence that are looked at (0 allowed)
  *  seq_lens     device  int32 [B], those tokens included
  *  block_table  device  int32 [B][table_stride] as for pace_kv_append; entries of pages that hold no token to be read are not read

@@ -385,8 +385,8 @@ extern "C" pace_status_t pace_kv_compact(const pace_kv_cache* layers, int n_laye
                                          const int32_t* block_table, int64_t table_stride, const int32_t* cu_rows, const int32_t* rows,
                                          const int32_t* counts, const int32_t* dst_table, int64_t dst_stride, int32_t* new_lens,
                                          pace_stream_t stream) {
-  if (B < 0 || n_layers < 0) return PACE_ERR_INVALID_ARG;
-  if (B == 0 || n_layers == 0) return PACE_OK;
+  if (B < 0 || n_layers < 1) return PACE_ERR_INVALID_ARG;
+  if (B == 0) return PACE_OK;
   if (layers == nullptr) return PACE_ERR_INVALID_ARG;
   for (int l = 0; l < n_layers; ++l) {
     PACE_CHECK(check_cache(layers + l));

@@ -706,8 +706,10 @@ namespace {
 
 template <int D, bool TREE>
 pace_status_t run_rows(const KvMaps& maps, const KvAttnArgs& a, int rows, unsigned grid, int* status, cudaStream_t stream) {
-  return rows == 8 ? run_decode<D, 8, TREE>(maps, a, grid, status, stream) : rows == 16 ? run_decode<D, 16, TREE>(maps, a, grid, status, stream)
-                                                                                    : run_decode<D, 32, TREE>(maps, a, grid, status, stream);
+  if (rows == 8) return run_decode<D, 8, TREE>(maps, a, grid, status, stream);
+  if constexpr (!TREE)      // (trees have 16 at most)
+    if (rows == 32) return run_decode<D, 32, TREE>(maps, a, grid, status, stream);
+  return run_decode<D, 16, TREE>(maps, a, grid, status, stream);
 }
 
 }  // namespace

@@ -517,7 +517,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
       // A maximum below FAR is a whole number, and so are the logarithms of the scales: x + (log2(vs) - w) has one rounding, of
       // a small result.  Beyond it log2(vs) - w would lose bits, scores that are equal come out different, and weights under a w that
       // is their maximum pass 1 by any factor.  There (`far`) S of the half tile is first turned into x - m, x rounded like any score
-      // and m a score of the row that is the largest so far to within 2^20, so that what w is about is small again.
+      // and m a score of the row that is the largest so far to within FAR / 4, so that what w is about is small again.
       bool far = false;
       float m = 0.f;      // (0 of other rows)
       int slot0 = 0;
@@ -590,7 +590,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prefill_kernel(const __grid_co
         bool over = g == 0 || back != 0.f;      // the row's w has to move
         float sum = INFINITY;                   // (by how much: not known)
         // Two rounds at most: a move leaves a sum of 64 weights of at most 2^0.5 each.  (Below FAR the largest weight's exponent is
-        // exact to 2^-1; of a far row x - m is at most 0 where m has just moved, else below 2^20.)
+        // exact to 2^-1; of a far row x - m is at most 0 where m has just moved, else below FAR / 4.)
         int rounds = 4;
 #pragma unroll 1
         while (true) {

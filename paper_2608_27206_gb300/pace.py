@@ -863,11 +863,11 @@ class KvLayers:
 
     def __init__(self, caches: Sequence[KvCache]):
         self.caches = list(caches)
-        if any(not isinstance(c, KvCache) for c in self.caches):
+        if not self.caches or any(not isinstance(c, KvCache) for c in self.caches):
             raise ValueError("expected caches")
         if len({c.view.k for c in self.caches}) < len(self.caches):
             raise ValueError("a layer more than once")
-        self.views = (KvCacheView * max(len(self.caches), 1))(*[c.view for c in self.caches])
+        self.views = (KvCacheView * len(self.caches))(*[c.view for c in self.caches])
         self._address = ctypes.addressof(self.views)
 
 

@@ -348,3 +348,30 @@ def test_a_layer_is_listed_once(pace):  # noqa: F811
     pace.KvLayers(caches)
     with pytest.raises(ValueError):
         pace.KvLayers([caches[0], caches[1], caches[0]])
+
+
+@pytest.mark.parametrize("away", [False, True])
+def test_scales_that_are_no_powers_of_two(pace, away):  # noqa: F811
+    """Of another program's cache: 3/2 of a power, under which a code's product has six significant bits at most and is rounded once."""
+    case = Case(pace, 50, (130, 77), (100, 77), (40, 30), 2, 64, 32, away=away)
+    for n in "kv":
+        case.pools[0].s[n][::2] *= 1.5
+    _upload(case.pools[0])
+    case.check(case.call())
+
+
+def test_the_largest_values(pace):  # noqa: F811
+    """The largest bf16 is stored as 256 under 2^120, past what 32 bits hold: it stays what it is."""
+    pool = Pool(pace, 51, [40], 2, 64, 16, poison=False)
+    x = torch.full((40, 2, 64), 3.3895e38, dtype=torch.bfloat16, device="cuda")
+    x[::2] = -x[::2] * 0.5
+    pace.pace_kv_append(pool.cache, x, x, [0, 40], pool.lens, pool.table)
+    was = pool.now("k")
+    kept = [1, 3, 4, 21, 39]
+    lens = pace.pace_kv_compact(pool.cache, [0, 40], pool.lens, pool.table, cu_rows=[0, 5], rows=_ids(kept))
+    codes, scales = pool.now("k")
+    page = pool.pages[0]
+    assert lens.tolist() == [5] and (scales[page[0]] == 2.0 ** 120).all()
+    for i, j in enumerate(kept):
+        assert np.array_equal(codes[page[0], :, i], was[0][page[j // 16], :, j % 16])
+    assert pace.pace_device_status(clear=True) == (0, 0)
