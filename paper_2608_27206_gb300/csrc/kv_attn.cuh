@@ -25,7 +25,7 @@ constexpr int kKvTile = 128;      // slots of one tile
 constexpr float kNone = -0x1p127f;   // a row's maximum before its first slot, below any score (and finite: x - kNone is never NaN)
 constexpr int kManyRows = 256;    // rows of a tile of the form for many
 constexpr int kItemCost = 3;      // slot tiles that the queries and the output of a (row tile, head) are worth,
-constexpr int kTreeCost = 5;      // of trees of many rows (40 of 182 rows on 5001-28007 slots 241 us with 3, 237 with 5 and 7; 8 of 21 rows on 700-9000 25, 25, 28)
+constexpr int kTreeCost = 6;      // of trees of many rows (with 5, 6, 7: 16 ragged ones of dim 64 24.0, 24.9, 26.2 us; 32 of 128 rows on 700-9000 slots 103, 101, 96)
 constexpr int kPlanCtas = 152;    // CTAs of a launch at most: an SM each (the size queries need no device)
 
 // The launch's sequences, those without queries left out.
@@ -230,7 +230,10 @@ __device__ __forceinline__ KvShare kv_share(const KvAttnArgs& a, int* buf, KvSha
       if (c >= s.ctas) return s;      // nothing to do (the whole block)
       // (few tiles: one each, however dear the rest is; unless items are so few that a CTA need not have parts of two)
       constexpr int COST = TREE && ROWS == kManyRows ? kTreeCost : kItemCost;
-      s.cost = total >= COST * s.ctas || (total > s.ctas && total >= 4 * COST * total_items) ? COST : 0;
+      // (Trees: as soon as a CTA has more than one.  A batch of one long tree and seven short ones, 636 tiles of 52 items, took 68 us where
+      // several short items came to one CTA, and takes 33.)
+      if (TREE && ROWS == kManyRows) s.cost = total > s.ctas ? COST : 0;
+      else s.cost = total >= COST * s.ctas || (total > s.ctas && total >= 4 * COST * total_items) ? COST : 0;
       total += s.cost * total_items;
       before += sum - mine + s.cost * (before_items + num - items);
       mine += s.cost * items;
