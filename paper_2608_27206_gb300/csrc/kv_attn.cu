@@ -33,9 +33,10 @@ pace_status_t make_map(CUtensorMap* m, const pace_kv_cache* c, void* codes) {
 // 700-9000 31 against 36), below they are not (8 of 14 rows 22 us against 30).
 constexpr int kFewRows = 32, kFewNodes = 16;
 // Trees of few rows go with the others in one launch where that gives the others this many slot tiles more at most, were all of them as
-// long as max_len (a launch of their own and its join cost 14 us, a slot tile 1 us more of a CTA than there: 16 ragged trees of dim 64
-// 42 us in two launches, 28 in one).
-constexpr int kAlong = 16 * kPlanCtas;
+// long as max_len: a launch of their own and its join cost 14 to 20 us, of a long row tile of one to eight rows a slot tile 0.3 us more of a CTA than
+// there (64 single nodes on 5001-28007 slots 150 us, 21 rows each 208).  Mean of 699 ragged batches of both kinds 27.3 us with 16 for 64 here,
+// 25.4 with 48, 24.8 without a limit.
+constexpr int kAlong = 64 * kPlanCtas;
 
 // Rows of a tile for few-row sequences: 8, 16 or 32, what the largest needs (0: there are none).
 int few_rows(const int32_t* cu_q, int B, int group, int limit) {
