@@ -29,8 +29,8 @@ pace_status_t make_map(CUtensorMap* m, const pace_kv_cache* c, void* codes) {
 }
 
 // Sequences of at most so many query rows per KV head take the transposed products of kv_decode.cu, trees up to kFewNodes of them: with 17
-// to 32 the two halves of a CTA of kv_prefill.cu are faster (64 trees of 28 rows on 5001-28007 slots 212 us against 424, 8 on
-// 700-9000 31 against 36), below they are not (8 of 14 rows 22 us against 30).
+// to 32 the two halves of a CTA of kv_prefill.cu are faster (64 trees of 28 rows on 5001-28007 slots 211 us against 424, 8 on
+// 700-9000 25 against 36), below they are not (8 of 14 rows 22 us against 30 then).
 constexpr int kFewRows = 32, kFewNodes = 16;
 // Trees of few rows go with the others in one launch where that gives the others this many slot tiles more at most, were all of them as
 // long as max_len: a launch of their own and its join cost 14 to 20 us, of a long row tile of one to eight rows a slot tile 0.3 us more of a CTA than

@@ -30,9 +30,9 @@
 //   S of the next slot tile is formed half by half, each as soon as P of that half has been used up (q crosses shared memory twice as often,
 //   but a half's owners find the next one ready: 40 trees of 182 rows on 5001-28007 slots 257 us with S whole, 238 by halves);
 //   of an item of one row tile and kPairTiles slot tiles or more, A and B take every other slot tile and join at the end (64 such trees
-//   of 63 rows 278 us with B idle, 224); K and V tiles then share one ring, as S runs two tiles ahead;
+//   of 63 rows 278 us with B idle, 220); K and V tiles then share one ring, as S runs two tiles ahead;
 //   parts of full tiles go out by way of shared memory, and warps without rows only keep step.
-// Measured: those 40 trees 236 us, 845 TFLOP/s and 2.4 TB/s; 64 of 63 rows 224 us, 4.0 TB/s.  In the former a slot tile takes 3600 clocks, 2600 of
+// Measured: those 40 trees 233 us, 855 TFLOP/s and 2.4 TB/s; 64 of 63 rows 220 us, 4.0 TB/s.  In the former a slot tile takes 3600 clocks, 2600 of
 // them shared memory's (S by halves 1540, P V 510, V's conversion and the fetch 640), the rest hand-overs from P to products to S; tensor pipe
 // 52 % active.  One item alone costs 20000 clocks besides its tiles: the plan 4000, q 4500-7000, its first tile 1500 more, its output 2500-6000.
 // Tried: A's two halves before B's (250 us instead of 238), a pair's halves in step instead of in turn (275 instead of 235).
