@@ -182,14 +182,14 @@ pace_status_t attend(const pace_kv_cache* cache, const void* Q, int64_t q_row_st
   a.group = group;
   a.by_group = fast_div(static_cast<uint32_t>(group));
   a.window = window < max_len ? window : 0;      // (one of max_len leaves nothing out; smaller ones keep slot - window within 32 bits)
-  a.sinks = sinks;
+  a.sinks = std::min(sinks, max_len);      // (no position reaches max_len; sums with it stay within 32 bits)
   a.max_len = max_len;
   int* status = device_status_word();
   int sms = 0;
   PACE_CHECK(sm_count(&sms));
   if (tree) {
     KvTree t{parents, reinterpret_cast<int32_t*>(static_cast<uint8_t*>(ws) + w.depth), reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(ws) + w.family), w.words};
-    PACE_CHECK(launch_kv_tree(t, cu_q, B, seq_lens, max_len, a.window, sinks, status, stream));
+    PACE_CHECK(launch_kv_tree(t, cu_q, B, seq_lens, max_len, a.window, a.sinks, status, stream));
     a.depth = t.depth;
     a.family = t.family;
     a.words = t.words;
