@@ -656,7 +656,7 @@ PACE_API size_t pace_kv_tree_attention_workspace_size(const pace_kv_cache* cache
  *  n_b at most PACE_TREE_MAX.  Everything else, formats, limits and errors, as for pace_kv_attention; a page none of whose slots any node
  *  sees may be anything.  A sequence shorter than its nodes has its first ones before slot 0: nobody sees those, and a node that sees
  *  nothing gives out = 0 and lse = -inf.  Weights are held as there, to 8 bits for at most 16 query rows per KV head and to 11 for more (where
- *  such trees come together, and few of the former, for all); a launch takes row tiles * n_kv_heads * (tiles of 128 slots in max_len + 5) < 2^31.
+ *  such trees come together, and few of the former, for all); a launch takes row tiles * n_kv_heads * (tiles of 128 slots in max_len + 6) < 2^31.
  */
 PACE_API pace_status_t pace_kv_tree_attention(const pace_kv_cache* cache, const void* Q, int64_t q_row_stride, const int32_t* cu_q,
                                               int B, int n_q_heads, const int32_t* parents, const int32_t* seq_lens,

@@ -24,7 +24,7 @@ namespace pace {
 constexpr int kKvTile = 128;      // slots of one tile
 constexpr float kNone = -0x1p127f;   // a row's maximum before its first slot, below any score (and finite: x - kNone is never NaN)
 constexpr int kManyRows = 256;    // rows of a tile of the form for many
-constexpr int kItemCost = 3;      // slot tiles that the queries and the output of a (row tile, head) are worth,
+constexpr int kItemCost = 3;      // slot tiles that the queries and the output of a (row tile, head) are worth (pace.h states both: the size of a launch),
 constexpr int kTreeCost = 6;      // of trees of many rows (with 5, 6, 7: 16 ragged ones of dim 64 24.0, 24.9, 26.2 us; 32 of 128 rows on 700-9000 slots 103, 101, 96)
 constexpr int kPlanCtas = 152;    // CTAs of a launch at most: an SM each (the size queries need no device)
 
