@@ -12,8 +12,9 @@ calls of a serving loop:
 
 Everything is allocated once, and what a step needs is on the device, lengths included, so a step
 can be captured in a CUDA graph and replayed while the sequences grow.  The host counts along: a call
-or a replay that would take a sequence past max_len raises before it issues anything.  What the
-kernels report (numbers out of range, values that are not finite) shows in check().
+or a replay that would take a sequence past max_len raises before it issues anything, and one that
+raises for another reason takes its tokens back.  What the kernels report (numbers out of range,
+values that are not finite) shows in check().
 
     python -m paper_2608_27206_gb300.serve
 
@@ -23,6 +24,7 @@ and times decode steps, and steps of drafted trees where --nodes is given.
 from __future__ import annotations
 
 import argparse
+import contextlib
 import time
 from typing import Optional, Sequence
 
@@ -38,8 +40,9 @@ class CapturedStep(torch.cuda.CUDAGraph):
     layer: "ServeLayer"
 
     def replay(self) -> None:
-        self.layer._take_one()
+        self.layer._require_one()
         super().replay()
+        self.layer._steps += 1
 
 
 class ServeLayer:
@@ -82,18 +85,31 @@ class ServeLayer:
                 (not self._loose or max(a + b for a, b in zip(self._lengths(), new)) > self.max_len):
             raise ValueError(f"{what} past max_len ({self.max_len})")
 
-    def _take(self, cu_new: Sequence[int], what: str) -> None:
-        """Counts new tokens (a prefix over the sequences), and raises if they do not fit."""
+    @contextlib.contextmanager
+    def _taking(self, cu_new: Sequence[int], what: str):
+        """Counts new tokens (a prefix over the sequences) for the calls inside: raises if they do not fit, and counts them no more if a call
+        raises (what it may have stored lies behind the sequences' ends then)."""
         new = [int(b) - int(a) for a, b in zip(cu_new, cu_new[1:])]
         if len(new) != self.B or min(new) < 0:
             raise ValueError(f"cu_new: expected a prefix of {self.B} numbers of tokens")
         self._require(new, what)
+        more = torch.tensor(new, dtype=torch.int32, device=self.lens.device)
+        self.lens += more
+        try:
+            yield
+        except BaseException:
+            self.lens -= more
+            raise
         self._of_prompts = [a + b for a, b in zip(self._of_prompts, new)]
-        self.lens += torch.tensor(new, dtype=torch.int32, device=self.lens.device)
 
-    def _take_one(self) -> None:
+    def _require_one(self) -> None:
         self._require([1] * self.B, "a step")
-        self._steps += 1
+
+    def _require_heads(self, Q: torch.Tensor) -> None:
+        """Raises unless the attention takes as many heads as Q has: before the keys beside it are stored."""
+        heads, of = self.cache.n_kv_heads, Q.shape[1] if Q.dim() == 3 else 0
+        if of < 1 or of % heads or of // heads > 64:
+            raise ValueError(f"Q: expected [rows, heads, D], heads a multiple of {heads}")
 
     def reset(self) -> None:
         """Empties the sequences."""
@@ -111,36 +127,49 @@ class ServeLayer:
                rows: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Appends cu_new[b + 1] - cu_new[b] tokens to every sequence b (0: none) and attends from each of them: a whole prompt, a
         chunk of one or a chat's next turn.  rows picks the tokens out of K, V, Q and positions.  bf16 [cu_new[-1], heads, D]."""
-        self._take(cu_new, "a prompt")
-        q = P.pace_kv_append(self.cache, K, V, cu_new, self.lens, self.table, rows=rows, rope=self.rope, positions=positions,
-                             sections=self.sections, q=Q)
-        return P.pace_kv_attention(self.cache, q, cu_new, self.lens, self.table, self.max_len, window=self.window, sinks=self.sinks)
+        self._require_heads(Q)
+        with self._taking(cu_new, "a prompt"):
+            q = P.pace_kv_append(self.cache, K, V, cu_new, self.lens, self.table, rows=rows, rope=self.rope, positions=positions,
+                                 sections=self.sections, q=Q)
+            return P.pace_kv_attention(self.cache, q, cu_new, self.lens, self.table, self.max_len, window=self.window, sinks=self.sinks)
 
     def step(self, K: torch.Tensor, V: torch.Tensor, Q: torch.Tensor, positions: torch.Tensor) -> torch.Tensor:
         """One token for every sequence: row b of K, V, Q and of the position ids.  The result is overwritten by the next step."""
-        self._take_one()
-        return self._step(K, V, Q, positions)
+        self._require_one()
+        out = self._step(K, V, Q, positions)
+        self._steps += 1
+        return out
 
     def _step(self, K: torch.Tensor, V: torch.Tensor, Q: torch.Tensor, positions: torch.Tensor) -> torch.Tensor:
+        if Q.dim() != 3 or Q.shape[1] != self.n_q_heads:      # (self.q has room for fewer)
+            raise ValueError(f"Q: expected [{self.B}, {self.n_q_heads}, D]")
         self.lens += 1
-        P.pace_kv_append(self.cache, K, V, self.one, self.lens, self.table, rope=self.rope, positions=positions,
-                         sections=self.sections, q=Q, q_out=self.q)
-        return P.pace_kv_attention(self.cache, self.q, self.one, self.lens, self.table, self.max_len, window=self.window,
-                                   sinks=self.sinks, out=self.out, ws=self.ws)
+        try:
+            P.pace_kv_append(self.cache, K, V, self.one, self.lens, self.table, rope=self.rope, positions=positions,
+                             sections=self.sections, q=Q, q_out=self.q)
+            return P.pace_kv_attention(self.cache, self.q, self.one, self.lens, self.table, self.max_len, window=self.window,
+                                       sinks=self.sinks, out=self.out, ws=self.ws)
+        except BaseException:
+            self.lens -= 1
+            raise
 
     def draft(self, K: torch.Tensor, V: torch.Tensor, Q: torch.Tensor, parents: torch.Tensor, cu_nodes: Sequence[int],
               positions: torch.Tensor) -> torch.Tensor:
         """Appends cu_nodes[b + 1] - cu_nodes[b] drafted tokens to every sequence b, the nodes of a tree (parents, device int32: the
         number of each one's parent in its tree, before it, or -1; node 0 is the token that the model picked last), and attends from each:
-        bf16 [nodes, heads, D].  positions are the ids of the sequence's end and the nodes' depths.  accept() is to follow."""
+        bf16 [nodes, heads, D].  positions are the ids of the sequence's end and the nodes' depths.  accept() is to follow, and
+        reads parents again."""
         if max(int(b) - int(a) for a, b in zip(cu_nodes, cu_nodes[1:])) > P.TREE_MAX:
             raise ValueError(f"a tree of more than {P.TREE_MAX} nodes")
-        self._take(cu_nodes, "a tree")
+        self._require_heads(Q)
+        P._int32(parents, int(cu_nodes[-1]), "parents")      # (raises before anything is stored)
+        with self._taking(cu_nodes, "a tree"):
+            q = P.pace_kv_append(self.cache, K, V, cu_nodes, self.lens, self.table, rope=self.rope, positions=positions,
+                                 sections=self.sections, q=Q)
+            out = P.pace_kv_tree_attention(self.cache, q, cu_nodes, parents, self.lens, self.table, self.max_len, window=self.window,
+                                           sinks=self.sinks)
         self._tree = list(cu_nodes), parents
-        q = P.pace_kv_append(self.cache, K, V, cu_nodes, self.lens, self.table, rope=self.rope, positions=positions,
-                             sections=self.sections, q=Q)
-        return P.pace_kv_tree_attention(self.cache, q, cu_nodes, parents, self.lens, self.table, self.max_len, window=self.window,
-                                        sinks=self.sinks)
+        return out
 
     def accept(self, tokens: torch.Tensor, picked: torch.Tensor):
         """Of the drafted tokens (device int32, as are those picked after each node) keeps the path that the picked ones agree with.
