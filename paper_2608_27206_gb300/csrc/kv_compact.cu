@@ -28,7 +28,7 @@ namespace {
 
 constexpr int kMoveThreads = 256, kMoveCtas = 4;      // to other pages: threads of a CTA, CTAs of an SM
 constexpr int kSlideThreads = 128;                    // in place, a warp per head's K or V
-constexpr int kSlideBlocks = 4;                       // ... whose blocks are looked up so many at a time
+constexpr int kSlideBlocks = 4;                       // ... with so many blocks of a sequence at most
 constexpr int kWideWarps = 16;                        // in place, a CTA per head's K or V
 constexpr int kMaxLayers = 64;                        // of one launch
 
@@ -290,7 +290,7 @@ __global__ void __launch_bounds__(kMoveThreads, kMoveCtas) kv_move_kernel(const 
   }
 }
 
-// In place, few blocks of a sequence: a warp per head's K or V.
+// In place, kSlideBlocks blocks of a sequence at most (the call's lists have room for no more): a warp per head's K or V.
 template <int D>
 __global__ void __launch_bounds__(kSlideThreads) kv_slide_kernel(const __grid_constant__ CompactArgs a, int* status) {
   constexpr int WARPS = kSlideThreads / 32;
@@ -301,31 +301,25 @@ __global__ void __launch_bounds__(kSlideThreads) kv_slide_kernel(const __grid_co
   const Kept k = kept_of(a, b);
   if (blockIdx.y == 0 && tid == 0) put_length(a, b, k, status);
   if (k.count <= 0) return;
-  const int task = blockIdx.y * WARPS + (tid >> 5), layer = static_cast<int>(a.by_tasks(task));
-  const bool mine = layer < a.layers;
-  const HeadOf h = head_of(a, mine ? layer : 0, mine ? task - layer * 2 * a.heads : 0);
   const int64_t first = k.base / kKvBlock, last = (static_cast<int64_t>(k.base) + k.count - 1) / kKvBlock;
-#pragma unroll 1
-  for (int64_t block0 = first; block0 <= last; block0 += kSlideBlocks) {
-    const int n = static_cast<int>(min(last - block0 + 1, static_cast<int64_t>(kSlideBlocks)));
-    for (int i = tid; i < n * kKvBlock; i += kSlideThreads) {
-      const int64_t block = block0 + i / kKvBlock;
-      const int page = target_of(a, b, block, status, i % kKvBlock == 0);
-      s_from[i / kKvBlock][i % kKvBlock] = source_of(a, b, k, block0 * kKvBlock + i, page, D, status);
-      if (i % kKvBlock == 0) s_page[i / kKvBlock] = page;
-    }
-    __syncthreads();
-    if (mine) {
-      Rows<D> r[2];
-      get_rows<D>(a, h, s_from[0], r[0]);
+  const int n = static_cast<int>(last - first) + 1;
+  for (int i = tid; i < n * kKvBlock; i += kSlideThreads) {
+    const int64_t block = first + i / kKvBlock;
+    const int page = target_of(a, b, block, status, i % kKvBlock == 0);
+    s_from[i / kKvBlock][i % kKvBlock] = source_of(a, b, k, first * kKvBlock + i, page, D, status);
+    if (i % kKvBlock == 0) s_page[i / kKvBlock] = page;
+  }
+  __syncthreads();
+  const int task = blockIdx.y * WARPS + (tid >> 5), layer = static_cast<int>(a.by_tasks(task));
+  if (layer >= a.layers) return;
+  const HeadOf h = head_of(a, layer, task - layer * 2 * a.heads);
+  Rows<D> r[2];
+  get_rows<D>(a, h, s_from[0], r[0]);
 #pragma unroll
-      for (int j = 0; j < kSlideBlocks; ++j) {
-        if (j >= n) break;
-        if (j + 1 < n) get_rows<D>(a, h, s_from[j + 1], r[(j + 1) & 1]);
-        if (s_page[j] >= 0) put_rows<D>(a, h, r[j & 1], place_of(a, s_page[j], (block0 + j) * kKvBlock, D), slots_of(k, block0 + j), status);
-      }
-    }
-    __syncthreads();      // (the rows' sources have been used)
+  for (int j = 0; j < kSlideBlocks; ++j) {
+    if (j >= n) break;
+    if (j + 1 < n) get_rows<D>(a, h, s_from[j + 1], r[(j + 1) & 1]);
+    if (s_page[j] >= 0) put_rows<D>(a, h, r[j & 1], place_of(a, s_page[j], (first + j) * kKvBlock, D), slots_of(k, first + j), status);
   }
 }
 
@@ -448,7 +442,7 @@ extern "C" pace_status_t pace_kv_compact(const pace_kv_cache* layers, int n_laye
       }
       if (in_place) {
         // A warp by itself moves a block in a microsecond, a round of a CTA takes little more: few blocks of many sequences go by warps, which
-        // waste none, more than kSlideBlocks by CTAs.
+        // waste none, where a list may reach more than kSlideBlocks (wherever in a block its first token lands) by CTAs.
         int most = 0;
         for (int i = 0; i < a.nb; ++i) most = std::max(most, a.cu_rows[i + 1] - a.cu_rows[i]);
         const unsigned tasks = static_cast<unsigned>(a.layers * 2 * a.heads), warps = kSlideThreads / 32, nb = static_cast<unsigned>(a.nb);
