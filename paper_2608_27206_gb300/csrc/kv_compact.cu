@@ -364,12 +364,6 @@ __global__ void __launch_bounds__(32 * kWideWarps, CTAS) kv_slide_wide_kernel(co
   }
 }
 
-// Whether [p, p + np) and [q, q + nq), in int32, have a part in common.
-bool overlap(const int32_t* p, int64_t np, const int32_t* q, int64_t nq) {
-  const auto a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
-  return np > 0 && nq > 0 && a < b + 4 * static_cast<uintptr_t>(nq) && b < a + 4 * static_cast<uintptr_t>(np);
-}
-
 }  // namespace
 }  // namespace pace
 

@@ -700,10 +700,6 @@ pace_status_t run_decode(const KvMaps& maps, const KvAttnArgs& a, unsigned grid,
   return launch_dependent(kv_decode_kernel<D, NQ, TREE>, grid, kThreads, smem, 1, stream, maps, a, status);
 }
 
-}  // namespace
-
-namespace {
-
 template <int D, bool TREE>
 pace_status_t run_rows(const KvMaps& maps, const KvAttnArgs& a, int rows, unsigned grid, int* status, cudaStream_t stream) {
   if (rows == 8) return run_decode<D, 8, TREE>(maps, a, grid, status, stream);

@@ -154,12 +154,6 @@ __global__ void __launch_bounds__(32 * kAcceptWarps) draft_accept_kernel(const _
   }
 }
 
-// Whether [p, p + np) and [q, q + nq), in int32, have a part in common.
-bool overlap(const int32_t* p, int64_t np, const int32_t* q, int64_t nq) {
-  const auto a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
-  return np > 0 && nq > 0 && a < b + 4 * static_cast<uintptr_t>(nq) && b < a + 4 * static_cast<uintptr_t>(np);
-}
-
 }  // namespace
 
 pace_status_t launch_kv_tree(const KvTree& t, const int32_t* cu_q, int B, const int32_t* lens, int max_len, int window, int sinks, int* status,

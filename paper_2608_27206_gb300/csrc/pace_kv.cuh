@@ -52,6 +52,12 @@ inline pace_status_t check_prefix(const int32_t* cu, int B) {
   return cu[B] <= (1 << 30) ? PACE_OK : PACE_ERR_INVALID_ARG;
 }
 
+// Whether [p, p + np) and [q, q + nq), in int32, have a part in common.
+inline bool overlap(const int32_t* p, int64_t np, const int32_t* q, int64_t nq) {
+  const auto a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+  return np > 0 && nq > 0 && a < b + 4 * static_cast<uintptr_t>(nq) && b < a + 4 * static_cast<uintptr_t>(np);
+}
+
 // Rows `stride` elements apart of `heads` heads of D bf16: 16-byte aligned, no overlap.
 inline bool rows_ok(const void* p, int64_t stride, int heads, int D) {
   return p != nullptr && reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 8 == 0 &&
