@@ -173,7 +173,8 @@ class ServeLayer:
 
     def accept(self, tokens: torch.Tensor, picked: torch.Tensor):
         """Of the drafted tokens (device int32, as are those picked after each node) keeps the path that the picked ones agree with.
-        Returns its rows, their number per sequence and the token to go on with, as pace_draft_accept does."""
+        Returns its rows, their number per sequence and the token to go on with, as pace_draft_accept does.  (The rejected ones leave
+        the cache, and no scale stands for them any more; what a large one has cost tokens of the same 16 slots when it was appended stays lost.)"""
         if self._tree is None:
             raise ValueError("nothing has been drafted")
         cu, parents = self._tree
